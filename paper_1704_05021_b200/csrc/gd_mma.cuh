@@ -1,0 +1,228 @@
+// Tensor-core products on sm_100a: tiled copies into swizzled shared memory, tcgen05.mma with accumulators in tensor
+// memory, and the epilogue the linear layer's kernels share.
+//
+// The products are D[i, j] = sum_k A(i, k) B(j, k) with 16-bit operands.  Shared memory holds a block of 64 k in rows of 128
+// bytes under the 128-byte swizzle (the hardware XORs address bits 4..6 with bits 7..9), in one of two forms:
+//   K-major   rows are i (or j), 64 consecutive k in a row: one copy box {64 k, rows}
+//   MN-major  rows are k, 64 consecutive i (or j) in a row: boxes {64 i, 64 k} of 8 KB, one per 64 i
+// so an operand is read as it lies in memory, transposed or not.
+#pragma once
+
+#include <cuda.h>      // CUtensorMap (types only: the encoder is asked from the runtime)
+
+#include "gd_train.cuh"
+
+namespace gd {
+
+constexpr uint32_t kBlockK = 64;
+
+// ---------------------------------------------------------------- clusters
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t peer_address(uint32_t smem_address, uint32_t rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_address), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float4 peer_load4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 peer_load2(uint32_t a) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+  return v;
+}
+
+// ---------------------------------------------------------------- copies and products
+__device__ __forceinline__ void tile_load(void* dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* b) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
+               "l"(map), "r"(x), "r"(y), "r"(smem_u32(b))
+               : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
+// Shared-memory descriptor of an operand block (128-byte swizzle; bit 46: the sm_100 form).  The stride between groups of 8 rows
+// is 1024 bytes in both forms; `lead` is the distance between boxes of 64 i (MN-major; not used K-major).
+__device__ __forceinline__ uint64_t operand_desc(uint32_t smem_address, uint32_t lead) {
+  return (uint64_t)((smem_address & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// Instruction descriptor: fp32 accumulators, both operands bf16 or both fp16.
+__host__ __device__ constexpr uint32_t mma_desc(uint32_t m, uint32_t n, bool bf16, bool a_mn, bool b_mn) {
+  return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (a_mn ? 1u : 0u) << 15 | (b_mn ? 1u : 0u) << 16 | (n >> 3) << 17 | (m >> 4) << 24;
+}
+template <int CTAS>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+  if constexpr (CTAS == 1)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(desc), "r"((uint32_t)add)
+                 : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(desc), "r"((uint32_t)add)
+                 : "memory");
+}
+// b receives one arrive when all products issued so far by this thread have been done.
+__device__ __forceinline__ void mma_commit(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+template <int CTAS>
+__device__ __forceinline__ void tmem_alloc(uint32_t* dst, uint32_t columns) {
+  if constexpr (CTAS == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+template <int CTAS>
+__device__ __forceinline__ void tmem_free(uint32_t address, uint32_t columns) {
+  if constexpr (CTAS == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns) : "memory");
+  else
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns) : "memory");
+}
+// Eight columns of the warp's 32 accumulator lanes: r[c] of lane l is D[l, c].  tmem_ready() before the registers are used.
+__device__ __forceinline__ void tmem_load8(uint32_t address, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+               : "r"(address)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ready() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// ---------------------------------------------------------------- activations and epilogue
+// x Phi(x) and x / (1 + exp(-x)), and their slopes
+__device__ __forceinline__ float gelu(float x) { return 0.5f * x * (1.f + erff(x * 0.70710678118654752f)); }
+__device__ __forceinline__ float gelu_slope(float x) {
+  return 0.5f * (1.f + erff(x * 0.70710678118654752f)) + x * __expf(-0.5f * x * x) * 0.39894228040143268f;
+}
+__device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + __expf(-x)); }
+__device__ __forceinline__ float silu_slope(float x) {
+  const float s = __fdividef(1.f, 1.f + __expf(-x));
+  return s * (1.f + x * (1.f - s));
+}
+__device__ __forceinline__ float activate(float z, int act) {
+  switch (act) {
+    case GD_ACT_RELU: return z < 0.f ? 0.f : z;      // (a NaN stays one)
+    case GD_ACT_GELU: return gelu(z);
+    case GD_ACT_SILU: return silu(z);
+    default: return z;
+  }
+}
+
+// What happens to a product on its way out: out[r, c] = act(D + bias[c]) + add[r, c], and pre[r, c] = D + bias[c].
+struct Epilogue {
+  void* out;
+  const void* bias;
+  const void* add;
+  void* pre;
+  uint64_t ld_out, ld_add, ld_pre;
+  uint32_t rows, cols;
+  int32_t dtype;        // of pre (16 bits)
+  int32_t out_dtype, bias_dtype, add_dtype;
+  int32_t activation;
+  uint32_t vectors;     // every buffer above takes 16-byte accesses at columns that are multiples of 8
+};
+
+__device__ __forceinline__ float load_as(const void* p, uint64_t i, int dt) {
+  if (dt == GD_DTYPE_FP32) return static_cast<const float*>(p)[i];
+  return dt == GD_DTYPE_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_as(void* p, uint64_t i, int dt, float x) {
+  if (dt == GD_DTYPE_FP32) static_cast<float*>(p)[i] = x;
+  else if (dt == GD_DTYPE_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
+  else static_cast<__half*>(p)[i] = __float2half_rn(x);
+}
+__device__ __forceinline__ void load8_as(const void* p, uint64_t i, int dt, float (&x)[8]) {
+  if (dt == GD_DTYPE_FP32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+    const float4 a = q[0], b = q[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    return;
+  }
+  const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = dt == GD_DTYPE_BF16 ? unpack2<GD_DTYPE_BF16>(w[j]) : unpack2<GD_DTYPE_FP16>(w[j]);
+    x[2 * j] = f.x, x[2 * j + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void store8_as(void* p, uint64_t i, int dt, const float (&x)[8]) {
+  if (dt == GD_DTYPE_FP32) {
+    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
+    q[0] = make_float4(x[0], x[1], x[2], x[3]);
+    q[1] = make_float4(x[4], x[5], x[6], x[7]);
+    return;
+  }
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w[j] = dt == GD_DTYPE_BF16 ? pack2<GD_DTYPE_BF16>(x[2 * j], x[2 * j + 1]) : pack2<GD_DTYPE_FP16>(x[2 * j], x[2 * j + 1]);
+  *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Eight neighbours of one output row, c a multiple of 8.
+__device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t c, float (&v)[8]) {
+  if (r >= e.rows || c >= e.cols) return;
+  if (e.vectors && c + 8 <= e.cols) {
+    if (e.bias) {
+      float b[8];
+      load8_as(e.bias, c, e.bias_dtype, b);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += b[j];
+    }
+    if (e.pre) store8_as(e.pre, (uint64_t)r * e.ld_pre + c, e.dtype, v);
+    if (e.activation != GD_ACT_NONE) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = activate(v[j], e.activation);
+    }
+    if (e.add) {
+      float b[8];
+      load8_as(e.add, (uint64_t)r * e.ld_add + c, e.add_dtype, b);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += b[j];
+    }
+    store8_as(e.out, (uint64_t)r * e.ld_out + c, e.out_dtype, v);
+    return;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < 8; ++j) {
+    if (c + j >= e.cols) break;
+    float z = v[j];
+    if (e.bias) z += load_as(e.bias, c + j, e.bias_dtype);
+    if (e.pre) store_as(e.pre, (uint64_t)r * e.ld_pre + c + j, e.dtype, z);
+    z = activate(z, e.activation);
+    if (e.add) z += load_as(e.add, (uint64_t)r * e.ld_add + c + j, e.add_dtype);
+    store_as(e.out, (uint64_t)r * e.ld_out + c + j, e.out_dtype, z);
+  }
+}
+
+// ---------------------------------------------------------------- host side
+// A 16-bit matrix whose rows are contiguous, as one operand: `extent` values of i (or j) and `depth` of k.
+struct Operand {
+  const void* p;
+  uint64_t ld;
+  bool mn_major;       // rows of the matrix are k
+};
+struct Product {
+  Operand a, b;        // of the output's rows and of its columns
+  uint32_t depth;      // extent of k
+  bool bf16;
+  Epilogue ep;
+  int* status;
+};
+bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_t depth, uint32_t box_extent, bool bf16);
+cudaError_t launch_product(const Product& p, cudaStream_t stream);
+
+}  // namespace gd

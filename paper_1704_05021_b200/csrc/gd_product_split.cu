@@ -1,0 +1,291 @@
+// The product for outputs of few tiles: one tile of 128 x BN per CTA, the
+// contraction split over a cluster of 1 .. 8 CTAs.
+//
+// What bounds these calls is not arithmetic but how many SMs take part and how many bytes each keeps in flight: one row through a
+// 4096 x 4096 layer is 33 MB of weights and next to no products.  So the longer side of the output lies on the tile's
+// 128 accumulator lanes and the shorter one on its BN columns (the output is then written transposed, which costs nothing: the lanes of
+// a warp are neighbours in memory), BN shrinks with the shorter side, and where there are fewer tiles than SMs the CTAs of
+// a cluster take a part of k each.  They put their partial tiles into shared memory and every one sums, in rank order, the slice of
+// rows it then finishes and stores: no workspace, no atomics, the same bits every time.  Two CTAs share an SM, so one's
+// copies run under the other's epilogue.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "gd_mma.cuh"
+
+namespace gd {
+
+namespace {
+
+constexpr uint32_t kThreadsSplit = 256;
+constexpr uint32_t kTileA = 128 * kBlockK * 2;      // bytes of A's block
+
+template <bool B_MN, int BN>
+struct SplitShape {
+  static constexpr uint32_t kTileB = (B_MN && BN < 64 ? 64 : BN) * kBlockK * 2;
+  static constexpr uint32_t kStage = kTileA + kTileB;
+  static constexpr uint32_t kStages = BN == 128 ? 3 : 4;
+  static constexpr uint32_t kPitchLanes = 132;      // partial tile, one row per column of D (output written transposed)
+  static constexpr uint32_t kPitchCols = BN + 4;    // partial tile, one row per lane of D
+  static constexpr uint32_t kBytes = kStages * kStage + 1024;      // + alignment of the blocks
+  static_assert(kStages * kStage >= 128 * kPitchCols * 4 && kStages * kStage >= BN * kPitchLanes * 4, "the partial tile takes the blocks' place");
+};
+
+struct SplitArgs {
+  CUtensorMap a, b;
+  Epilogue ep;
+  int* status;
+  uint32_t blocks_k, tiles_i, desc;
+  uint32_t transposed;     // D's lanes are the output's columns
+};
+
+template <bool A_MN, bool B_MN, int BN, int SPLITS>
+__global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const __grid_constant__ SplitArgs g) {
+  using S = SplitShape<B_MN, BN>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t full[S::kStages], empty[S::kStages], done;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  constexpr uint32_t kColumns = BN < 32 ? 32 : BN;
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
+  const uint32_t rank = SPLITS > 1 ? cluster_rank() : 0u, tile = blockIdx.x / SPLITS;
+  const uint32_t i0 = tile % g.tiles_i * 128u, j0 = tile / g.tiles_i * BN;
+  const uint32_t k0 = g.blocks_k * rank / SPLITS, k1 = g.blocks_k * (rank + 1) / SPLITS;     // (blocks_k < 2^26: no overflow)
+  if (tid == 0) {
+    for (uint32_t s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1u), mbar_init(&empty[s], 1u);
+    mbar_init(&done, 1u);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (g.blocks_k) prefetch_map(&g.a), prefetch_map(&g.b);
+  }
+  if (warp == 1) tmem_alloc<1>(&s_tmem, kColumns);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  const volatile int* abort = &s_abort;
+  pdl_wait();
+  pdl_trigger();
+
+  if (tid == 0) {                                    // copies
+    uint32_t issued = 0;
+    bool ok = true;
+    for (uint32_t k = k0; k < k1; ++k, ++issued) {
+      const uint32_t s = issued % S::kStages;
+      if (issued >= S::kStages && !mbar_wait(&empty[s], (issued / S::kStages + 1u) & 1u, abort)) { ok = false; break; }
+      unsigned char* at = smem + s * S::kStage;
+      mbar_arrive_expect_tx(&full[s], S::kStage);
+      if constexpr (A_MN) {
+        tile_load(at, &g.a, (int32_t)i0, (int32_t)(k * kBlockK), &full[s]);
+        tile_load(at + 8192, &g.a, (int32_t)i0 + 64, (int32_t)(k * kBlockK), &full[s]);
+      } else {
+        tile_load(at, &g.a, (int32_t)(k * kBlockK), (int32_t)i0, &full[s]);
+      }
+      if constexpr (B_MN) {
+#pragma unroll
+        for (uint32_t c = 0; c < S::kTileB / 8192u; ++c)
+          tile_load(at + kTileA + c * 8192u, &g.b, (int32_t)(j0 + c * 64u), (int32_t)(k * kBlockK), &full[s]);
+      } else {
+        tile_load(at + kTileA, &g.b, (int32_t)(k * kBlockK), (int32_t)j0, &full[s]);
+      }
+    }
+    if (!ok) {                                       // a wait ran out: let the copies in flight land before the CTA may end
+      s_abort = 1;
+      const int none = 0;
+      for (uint32_t n = issued > S::kStages ? issued - S::kStages : 0u; n < issued; ++n)
+        (void)mbar_wait(&full[n % S::kStages], (n / S::kStages) & 1u, &none);
+    }
+  } else if (tid == 32) {                            // products
+    bool ok = true;
+    uint32_t n = 0;
+    for (uint32_t k = k0; k < k1; ++k, ++n) {
+      const uint32_t s = n % S::kStages;
+      if (!mbar_wait(&full[s], (n / S::kStages) & 1u, abort)) { ok = false; break; }
+      fence_after();
+      const uint32_t at = smem_u32(smem + s * S::kStage);
+#pragma unroll
+      for (uint32_t q = 0; q < kBlockK / 16; ++q) {
+        const uint64_t a = operand_desc(at + q * (A_MN ? 2048u : 32u), 8192u);
+        const uint64_t b = operand_desc(at + kTileA + q * (B_MN ? 2048u : 32u), 8192u);
+        mma<1>(tmem, a, b, g.desc, n | q);
+      }
+      mma_commit(&empty[s]);
+    }
+    if (ok) mma_commit(&done); else s_abort = 1;
+  }
+  __syncwarp();
+  const bool any = k1 > k0;
+  const bool good = !any || mbar_wait(&done, 0u, abort);
+  if (!good) {
+    s_abort = 1;
+    if (lane == 0) atomicExch(g.status, GD_ERR_DEVICE_TIMEOUT);
+  }
+  __syncthreads();                                   // (the producer has seen its copies land)
+  fence_after();
+
+  // the partial tile, from tensor memory to shared memory: warps w and w + 4 take the lanes of quarter w, half of the columns each
+  float* part = reinterpret_cast<float*>(smem);
+  {
+    constexpr uint32_t kHalf = BN / 2;
+    const uint32_t c0 = (warp >> 2) * kHalf, i = (warp & 3u) * 32u + lane;
+    float v[kHalf];
+    if (any) {
+#pragma unroll
+      for (uint32_t c = 0; c < kHalf; c += 8) tmem_load8(tmem + ((warp & 3u) * 32u << 16) + c0 + c, v + c);
+      tmem_ready();
+    } else {
+#pragma unroll
+      for (uint32_t c = 0; c < kHalf; ++c) v[c] = 0.f;
+    }
+    if (g.transposed) {
+#pragma unroll
+      for (uint32_t c = 0; c < kHalf; ++c) part[(c0 + c) * S::kPitchLanes + i] = v[c];
+    } else {
+#pragma unroll
+      for (uint32_t c = 0; c < kHalf; c += 4)
+        *reinterpret_cast<float4*>(part + i * S::kPitchCols + c0 + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+    }
+  }
+  if constexpr (SPLITS > 1) {
+    cluster_arrive();
+    cluster_wait();
+  } else {
+    __syncthreads();
+  }
+  // this CTA's rows of the output tile
+  const uint32_t rows = (g.transposed ? BN : 128u) / SPLITS, vecs = (g.transposed ? 128u : BN) / 8u;
+  const uint32_t pitch = g.transposed ? S::kPitchLanes : S::kPitchCols;
+  const uint32_t out_r = (g.transposed ? j0 : i0) + rank * rows, out_c = g.transposed ? i0 : j0;
+  for (uint32_t t = tid; t < rows * vecs; t += kThreadsSplit) {
+    const uint32_t r = t / vecs, c = t % vecs * 8u;
+    const float* at = part + (rank * rows + r) * pitch + c;
+    float v[8];
+    if constexpr (SPLITS > 1) {
+      const uint32_t address = smem_u32(at);
+#pragma unroll
+      for (uint32_t q = 0; q < SPLITS; ++q) {
+        const uint32_t peer = peer_address(address, q);
+        const float4 x = peer_load4(peer), y = peer_load4(peer + 16);
+        const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = q == 0 ? w[j] : v[j] + w[j];
+      }
+    } else {
+      const float4 x = *reinterpret_cast<const float4*>(at), y = *reinterpret_cast<const float4*>(at + 4);
+      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+    }
+    finish8(g.ep, out_r + r, out_c + c, v);
+  }
+  fence_before();
+  if constexpr (SPLITS > 1) {
+    cluster_arrive();                                // the others may still be reading this CTA's partial tile
+    cluster_wait();
+  } else {
+    __syncthreads();
+  }
+  fence_after();
+  if (warp == 1) tmem_free<1>(tmem, kColumns);
+}
+
+template <bool A_MN, bool B_MN, int BN, int SPLITS>
+cudaError_t launch_shape(const SplitArgs& g, uint32_t tiles, cudaStream_t stream) {
+  constexpr uint32_t bytes = SplitShape<B_MN, BN>::kBytes;
+  auto kernel = product_split_kernel<A_MN, B_MN, BN, SPLITS>;
+  static PerDeviceInt ready;
+  int dev;
+  if (!ready.get(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
+    ready.set(dev, 1);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(tiles * SPLITS);
+  cfg.blockDim = dim3(kThreadsSplit);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = SPLITS;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = SPLITS > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, g);
+}
+template <bool A_MN, bool B_MN, int BN>
+cudaError_t launch_splits(uint32_t splits, const SplitArgs& g, uint32_t tiles, cudaStream_t stream) {
+  switch (splits) {
+    case 1: return launch_shape<A_MN, B_MN, BN, 1>(g, tiles, stream);
+    case 2: return launch_shape<A_MN, B_MN, BN, 2>(g, tiles, stream);
+    case 4: return launch_shape<A_MN, B_MN, BN, 4>(g, tiles, stream);
+    default: return launch_shape<A_MN, B_MN, BN, 8>(g, tiles, stream);
+  }
+}
+template <bool A_MN, bool B_MN>
+cudaError_t launch_bn(uint32_t bn, uint32_t splits, const SplitArgs& g, uint32_t tiles, cudaStream_t stream) {
+  switch (bn) {
+    case 16: return launch_splits<A_MN, B_MN, 16>(splits, g, tiles, stream);
+    case 32: return launch_splits<A_MN, B_MN, 32>(splits, g, tiles, stream);
+    case 64: return launch_splits<A_MN, B_MN, 64>(splits, g, tiles, stream);
+    default: return launch_splits<A_MN, B_MN, 128>(splits, g, tiles, stream);
+  }
+}
+
+struct Choice {
+  bool transposed;
+  uint32_t bn, splits;
+};
+// The tile shape and split with the smallest estimated time, in cycles of an SM: the k blocks a CTA works through, each taking the
+// longer of its products (2 BN cycles) and its copies (64 bytes per cycle), times the waves, plus what a CTA costs by itself.
+Choice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn) {
+  const uint32_t sms = (uint32_t)sm_count();
+  Choice best{false, 128, 1};
+  double best_cost = 1e300;
+  for (int t = 0; t < 2; ++t) {
+    const uint32_t ei = t ? cols : rows, ej = t ? rows : cols;
+    const bool j_mn = t ? a_mn : b_mn;
+    for (uint32_t bn = 16; bn <= 128; bn *= 2) {
+      const double tile_b = (j_mn && bn < 64 ? 64 : bn) * 128.0;
+      const double block = std::max(2.0 * bn, (kTileA + tile_b) / 64.0);
+      const double tiles = std::ceil(ei / 128.0) * std::ceil(ej / (double)bn);
+      for (uint32_t splits = 1; splits <= 8; splits *= 2) {
+        if (splits > 1 && blocks_k < 2 * splits) break;
+        const double ctas = tiles * splits;
+        const double waves = std::ceil(ctas / sms);
+        const double cost = waves * (std::ceil(blocks_k / (double)splits) * block + 8.0 * bn + 600.0) + (splits > 1 ? 800.0 + 100.0 * splits : 0.0);
+        if (cost < best_cost) best_cost = cost, best = Choice{t != 0, bn, splits};
+      }
+    }
+  }
+  return best;
+}
+
+}  // namespace
+
+cudaError_t launch_product_split(const Product& p, cudaStream_t stream) {
+  const uint32_t blocks_k = (p.depth + kBlockK - 1) / kBlockK;
+  const Choice c = choose(p.ep.rows, p.ep.cols, blocks_k, p.a.mn_major, p.b.mn_major);
+  const Operand& oi = c.transposed ? p.b : p.a;
+  const Operand& oj = c.transposed ? p.a : p.b;
+  const uint32_t ei = c.transposed ? p.ep.cols : p.ep.rows, ej = c.transposed ? p.ep.rows : p.ep.cols;
+  SplitArgs g;
+  std::memset(&g, 0, sizeof(g));
+  if (p.depth && (!encode_operand(&g.a, oi, ei, p.depth, oi.mn_major ? 64 : 128, p.bf16) ||
+                  !encode_operand(&g.b, oj, ej, p.depth, oj.mn_major ? 64 : c.bn, p.bf16)))
+    return cudaErrorInvalidValue;
+  g.ep = p.ep;
+  g.status = p.status;
+  g.blocks_k = blocks_k;
+  g.tiles_i = (ei + 127) / 128;
+  g.desc = mma_desc(128, c.bn, p.bf16, oi.mn_major, oj.mn_major);
+  g.transposed = c.transposed;
+  const uint64_t tiles = (uint64_t)g.tiles_i * ((ej + c.bn - 1) / c.bn);
+  if (tiles * c.splits > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+  if (oi.mn_major) return oj.mn_major ? launch_bn<true, true>(c.bn, c.splits, g, (uint32_t)tiles, stream) : launch_bn<true, false>(c.bn, c.splits, g, (uint32_t)tiles, stream);
+  return oj.mn_major ? launch_bn<false, true>(c.bn, c.splits, g, (uint32_t)tiles, stream) : launch_bn<false, false>(c.bn, c.splits, g, (uint32_t)tiles, stream);
+}
+
+}  // namespace gd
