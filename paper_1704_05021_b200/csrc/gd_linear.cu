@@ -1,13 +1,24 @@
 // The linear layer (gd_linear_forward, gd_linear_backward): argument checks, the layout of ragged operands, the activation's
 // slope with the bias gradient, and the products (gd_product_split.cu, gd_product_large.cu).
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 #include "gd_mma.cuh"
 
 namespace gd {
 
+double cost_product_split(const Product& p);       // estimated cycles
 cudaError_t launch_product_split(const Product& p, cudaStream_t stream);
+cudaError_t launch_product_pair(const Product& p, cudaStream_t stream);
+
+namespace {
+// Estimated cycles of the pairs' kernel: 512 per k block of a 256 x 256 tile and what a tile costs besides, times the waves.
+double cost_product_pair(const Product& p) {
+  const double tiles = std::ceil(p.ep.rows / 256.0) * std::ceil(p.ep.cols / 256.0), blocks_k = std::ceil(p.depth / (double)kBlockK);
+  return std::ceil(tiles / (sm_count() / 2)) * std::max(512.0 * blocks_k, 4000.0) + 6000.0;
+}
+}  // namespace
 
 // Tiled-copy map of an operand.  The encoder is the driver's; it is asked for through the runtime, so that the library does not link
 // against libcuda and loads on a machine without a GPU.
@@ -33,7 +44,8 @@ bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_
 cudaError_t launch_product(const Product& p, cudaStream_t stream) {
   if (p.ep.rows == 0 || p.ep.cols == 0) return cudaSuccess;
   ProfileScope ps(stream, PT_LINEAR);
-  const cudaError_t e = launch_product_split(p, stream);
+  const bool pair = p.depth && cost_product_pair(p) < cost_product_split(p);
+  const cudaError_t e = pair ? launch_product_pair(p, stream) : launch_product_split(p, stream);
   if (e == cudaSuccess) note_launches(1);
   return e;
 }

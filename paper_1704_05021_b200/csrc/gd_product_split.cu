@@ -18,7 +18,7 @@ namespace gd {
 
 namespace {
 
-constexpr uint32_t kThreadsSplit = 256;
+constexpr uint32_t kSumWarps = 8, kThreadsSplit = (kSumWarps + 2) * 32;      // + one warp that asks for copies, one that issues products
 constexpr uint32_t kTileA = 128 * kBlockK * 2;      // bytes of A's block
 
 template <bool B_MN, int BN>
@@ -37,6 +37,7 @@ struct SplitArgs {
   Epilogue ep;
   int* status;
   uint32_t blocks_k, tiles_i, desc;
+  uint32_t chain;          // k blocks the tensor cores sum before the sum is joined to the others in fp32 registers
   uint32_t transposed;     // D's lanes are the output's columns
 };
 
@@ -44,23 +45,23 @@ template <bool A_MN, bool B_MN, int BN, int SPLITS>
 __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const __grid_constant__ SplitArgs g) {
   using S = SplitShape<B_MN, BN>;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t full[S::kStages], empty[S::kStages], done;
+  __shared__ uint64_t full[S::kStages], empty[S::kStages], sum_full[2], sum_empty[2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  constexpr uint32_t kColumns = BN < 32 ? 32 : BN;
+  constexpr uint32_t kColumns = BN < 32 ? 32 : 2 * BN;      // two accumulators
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
   const uint32_t rank = SPLITS > 1 ? cluster_rank() : 0u, tile = blockIdx.x / SPLITS;
   const uint32_t i0 = tile % g.tiles_i * 128u, j0 = tile / g.tiles_i * BN;
   const uint32_t k0 = g.blocks_k * rank / SPLITS, k1 = g.blocks_k * (rank + 1) / SPLITS;     // (blocks_k < 2^26: no overflow)
   if (tid == 0) {
     for (uint32_t s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1u), mbar_init(&empty[s], 1u);
-    mbar_init(&done, 1u);
+    for (uint32_t s = 0; s < 2; ++s) mbar_init(&sum_full[s], 1u), mbar_init(&sum_empty[s], kSumWarps);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (g.blocks_k) prefetch_map(&g.a), prefetch_map(&g.b);
   }
-  if (warp == 1) tmem_alloc<1>(&s_tmem, kColumns);
+  if (warp == kSumWarps) tmem_alloc<1>(&s_tmem, kColumns);
   fence_before();
   __syncthreads();
   fence_after();
@@ -69,76 +70,90 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
   pdl_wait();
   pdl_trigger();
 
-  if (tid == 0) {                                    // copies
-    uint32_t issued = 0;
-    bool ok = true;
-    for (uint32_t k = k0; k < k1; ++k, ++issued) {
-      const uint32_t s = issued % S::kStages;
-      if (issued >= S::kStages && !mbar_wait(&empty[s], (issued / S::kStages + 1u) & 1u, abort)) { ok = false; break; }
-      unsigned char* at = smem + s * S::kStage;
-      mbar_arrive_expect_tx(&full[s], S::kStage);
-      if constexpr (A_MN) {
-        tile_load(at, &g.a, (int32_t)i0, (int32_t)(k * kBlockK), &full[s]);
-        tile_load(at + 8192, &g.a, (int32_t)i0 + 64, (int32_t)(k * kBlockK), &full[s]);
-      } else {
-        tile_load(at, &g.a, (int32_t)(k * kBlockK), (int32_t)i0, &full[s]);
-      }
-      if constexpr (B_MN) {
-#pragma unroll
-        for (uint32_t c = 0; c < S::kTileB / 8192u; ++c)
-          tile_load(at + kTileA + c * 8192u, &g.b, (int32_t)(j0 + c * 64u), (int32_t)(k * kBlockK), &full[s]);
-      } else {
-        tile_load(at + kTileA, &g.b, (int32_t)(k * kBlockK), (int32_t)j0, &full[s]);
-      }
-    }
-    if (!ok) {                                       // a wait ran out: let the copies in flight land before the CTA may end
-      s_abort = 1;
-      const int none = 0;
-      for (uint32_t n = issued > S::kStages ? issued - S::kStages : 0u; n < issued; ++n)
-        (void)mbar_wait(&full[n % S::kStages], (n / S::kStages) & 1u, &none);
-    }
-  } else if (tid == 32) {                            // products
-    bool ok = true;
-    uint32_t n = 0;
-    for (uint32_t k = k0; k < k1; ++k, ++n) {
-      const uint32_t s = n % S::kStages;
-      if (!mbar_wait(&full[s], (n / S::kStages) & 1u, abort)) { ok = false; break; }
-      fence_after();
-      const uint32_t at = smem_u32(smem + s * S::kStage);
-#pragma unroll
-      for (uint32_t q = 0; q < kBlockK / 16; ++q) {
-        const uint64_t a = operand_desc(at + q * (A_MN ? 2048u : 32u), 8192u);
-        const uint64_t b = operand_desc(at + kTileA + q * (B_MN ? 2048u : 32u), 8192u);
-        mma<1>(tmem, a, b, g.desc, n | q);
-      }
-      mma_commit(&empty[s]);
-    }
-    if (ok) mma_commit(&done); else s_abort = 1;
-  }
-  __syncwarp();
-  const bool any = k1 > k0;
-  const bool good = !any || mbar_wait(&done, 0u, abort);
-  if (!good) {
-    s_abort = 1;
-    if (lane == 0) atomicExch(g.status, GD_ERR_DEVICE_TIMEOUT);
-  }
-  __syncthreads();                                   // (the producer has seen its copies land)
-  fence_after();
-
-  // the partial tile, from tensor memory to shared memory: warps w and w + 4 take the lanes of quarter w, half of the columns each
   float* part = reinterpret_cast<float*>(smem);
-  {
-    constexpr uint32_t kHalf = BN / 2;
-    const uint32_t c0 = (warp >> 2) * kHalf, i = (warp & 3u) * 32u + lane;
-    float v[kHalf];
-    if (any) {
+  constexpr uint32_t kHalf = BN / 2;
+  float v[kHalf];
+  bool good = true;
+  if (warp == kSumWarps) {                           // copies
+    if (lane == 0) {
+      uint32_t issued = 0;
+      for (uint32_t k = k0; k < k1; ++k, ++issued) {
+        const uint32_t s = issued % S::kStages;
+        if (issued >= S::kStages && !mbar_wait(&empty[s], (issued / S::kStages + 1u) & 1u, abort)) { good = false; break; }
+        unsigned char* at = smem + s * S::kStage;
+        mbar_arrive_expect_tx(&full[s], S::kStage);
+        if constexpr (A_MN) {
+          tile_load(at, &g.a, (int32_t)i0, (int32_t)(k * kBlockK), &full[s]);
+          tile_load(at + 8192, &g.a, (int32_t)i0 + 64, (int32_t)(k * kBlockK), &full[s]);
+        } else {
+          tile_load(at, &g.a, (int32_t)(k * kBlockK), (int32_t)i0, &full[s]);
+        }
+        if constexpr (B_MN) {
 #pragma unroll
-      for (uint32_t c = 0; c < kHalf; c += 8) tmem_load8(tmem + ((warp & 3u) * 32u << 16) + c0 + c, v + c);
-      tmem_ready();
-    } else {
-#pragma unroll
-      for (uint32_t c = 0; c < kHalf; ++c) v[c] = 0.f;
+          for (uint32_t c = 0; c < S::kTileB / 8192u; ++c)
+            tile_load(at + kTileA + c * 8192u, &g.b, (int32_t)(j0 + c * 64u), (int32_t)(k * kBlockK), &full[s]);
+        } else {
+          tile_load(at + kTileA, &g.b, (int32_t)(k * kBlockK), (int32_t)j0, &full[s]);
+        }
+      }
+      if (!good) {                                   // a wait ran out: let the copies in flight land before the CTA may end
+        s_abort = 1;
+        const int none = 0;
+        for (uint32_t n = issued > S::kStages ? issued - S::kStages : 0u; n < issued; ++n)
+          (void)mbar_wait(&full[n % S::kStages], (n / S::kStages) & 1u, &none);
+      }
     }
+  } else if (warp == kSumWarps + 1) {                // products
+    if (lane == 0) {
+      uint32_t n = 0, chain = 0;
+      for (uint32_t k = k0; good && k < k1; ++chain) {
+        const uint32_t end = min(k + g.chain, k1), buf = chain & 1u, sum = tmem + buf * BN;
+        if (chain >= 2 && !mbar_wait(&sum_empty[buf], (chain / 2 + 1u) & 1u, abort)) { good = false; break; }
+        fence_after();
+        for (const uint32_t first = k; k < end; ++k, ++n) {
+          const uint32_t s = n % S::kStages;
+          if (!mbar_wait(&full[s], (n / S::kStages) & 1u, abort)) { good = false; break; }
+          fence_after();
+          const uint32_t at = smem_u32(smem + s * S::kStage);
+#pragma unroll
+          for (uint32_t q = 0; q < kBlockK / 16; ++q) {
+            const uint64_t a = operand_desc(at + q * (A_MN ? 2048u : 32u), 8192u);
+            const uint64_t b = operand_desc(at + kTileA + q * (B_MN ? 2048u : 32u), 8192u);
+            mma<1>(sum, a, b, g.desc, (k - first) | q);
+          }
+          mma_commit(&empty[s]);
+        }
+        if (good) mma_commit(&sum_full[buf]);
+      }
+      if (!good) s_abort = 1;
+    }
+  } else {
+    // the chains' sums, joined in registers: warps w and w + 4 take the lanes of quarter w, half of the columns each
+    const uint32_t quarter = warp & 3u, c0 = (warp >> 2) * kHalf, i = quarter * 32u + lane;
+#pragma unroll
+    for (uint32_t c = 0; c < kHalf; ++c) v[c] = 0.f;
+    uint32_t chain = 0;
+    for (uint32_t k = k0; k < k1; k += g.chain, ++chain) {
+      const uint32_t buf = chain & 1u;
+      if (!mbar_wait(&sum_full[buf], (chain / 2) & 1u, abort)) { good = false; break; }
+      fence_after();
+#pragma unroll
+      for (uint32_t c = 0; c < kHalf; c += 8) {
+        float t[8];
+        tmem_load8(tmem + (quarter * 32u << 16) + buf * BN + c0 + c, t);
+        tmem_ready();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[c + j] += t[j];
+      }
+      fence_before();
+      if (lane == 0) mbar_arrive(&sum_empty[buf]);
+    }
+    if (!good) s_abort = 1;
+  }
+  if (!good && lane == 0) atomicExch(g.status, GD_ERR_DEVICE_TIMEOUT);
+  __syncthreads();                                   // every product is done and every copy has landed: the blocks' place is free
+  if (warp < kSumWarps) {
+    const uint32_t c0 = (warp >> 2) * kHalf, i = (warp & 3u) * 32u + lane;
     if (g.transposed) {
 #pragma unroll
       for (uint32_t c = 0; c < kHalf; ++c) part[(c0 + c) * S::kPitchLanes + i] = v[c];
@@ -178,15 +193,13 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
     }
     finish8(g.ep, out_r + r, out_c + c, v);
   }
-  fence_before();
   if constexpr (SPLITS > 1) {
     cluster_arrive();                                // the others may still be reading this CTA's partial tile
     cluster_wait();
   } else {
     __syncthreads();
   }
-  fence_after();
-  if (warp == 1) tmem_free<1>(tmem, kColumns);
+  if (warp == kSumWarps) tmem_free<1>(tmem, kColumns);
 }
 
 template <bool A_MN, bool B_MN, int BN, int SPLITS>
@@ -237,13 +250,13 @@ cudaError_t launch_bn(uint32_t bn, uint32_t splits, const SplitArgs& g, uint32_t
 struct Choice {
   bool transposed;
   uint32_t bn, splits;
+  double cost;
 };
 // The tile shape and split with the smallest estimated time, in cycles of an SM: the k blocks a CTA works through, each taking the
 // longer of its products (2 BN cycles) and its copies (64 bytes per cycle), times the waves, plus what a CTA costs by itself.
 Choice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn) {
   const uint32_t sms = (uint32_t)sm_count();
-  Choice best{false, 128, 1};
-  double best_cost = 1e300;
+  Choice best{false, 128, 1, 1e300};
   for (int t = 0; t < 2; ++t) {
     const uint32_t ei = t ? cols : rows, ej = t ? rows : cols;
     const bool j_mn = t ? a_mn : b_mn;
@@ -256,7 +269,7 @@ Choice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b
         const double ctas = tiles * splits;
         const double waves = std::ceil(ctas / sms);
         const double cost = waves * (std::ceil(blocks_k / (double)splits) * block + 8.0 * bn + 600.0) + (splits > 1 ? 800.0 + 100.0 * splits : 0.0);
-        if (cost < best_cost) best_cost = cost, best = Choice{t != 0, bn, splits};
+        if (cost < best.cost) best = Choice{t != 0, bn, splits, cost};
       }
     }
   }
@@ -264,6 +277,10 @@ Choice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b
 }
 
 }  // namespace
+
+double cost_product_split(const Product& p) {
+  return choose(p.ep.rows, p.ep.cols, (p.depth + kBlockK - 1) / kBlockK, p.a.mn_major, p.b.mn_major).cost;
+}
 
 cudaError_t launch_product_split(const Product& p, cudaStream_t stream) {
   const uint32_t blocks_k = (p.depth + kBlockK - 1) / kBlockK;
@@ -279,6 +296,7 @@ cudaError_t launch_product_split(const Product& p, cudaStream_t stream) {
   g.ep = p.ep;
   g.status = p.status;
   g.blocks_k = blocks_k;
+  g.chain = chain_blocks(p);
   g.tiles_i = (ei + 127) / 128;
   g.desc = mma_desc(128, c.bn, p.bf16, oi.mn_major, oj.mn_major);
   g.transposed = c.transposed;
