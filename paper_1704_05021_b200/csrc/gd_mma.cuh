@@ -99,13 +99,43 @@ __device__ __forceinline__ void tmem_load8(uint32_t address, float* r) {
                : "r"(address)
                : "memory");
 }
+// Thirty-two columns, one instruction.
+__device__ __forceinline__ void tmem_load32(uint32_t address, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+      "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]),
+        "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]),
+        "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(address)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_ready() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---------------------------------------------------------------- activations and epilogue
-// x Phi(x) and x / (1 + exp(-x)), and their slopes
-__device__ __forceinline__ float gelu(float x) { return 0.5f * x * (1.f + erff(x * 0.70710678118654752f)); }
+// x Phi(x) and x / (1 + exp(-x)), and their slopes.  Phi by formula 7.1.26 of Abramowitz and Stegun (erf to 1.5e-7, one
+// exponential that is also the density's): a third of the instructions of erff, which a tile's 65536 values pay for.
+__device__ __forceinline__ float normal_cdf(float x, float* gauss) {
+  const float a = fabsf(x) * 0.70710678118654752f;
+  const float t = __fdividef(1.f, fmaf(0.3275911f, a, 1.f));
+  const float e = __expf(-a * a);
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float tail = 0.5f * p * t * e;
+  *gauss = e;
+  return x < 0.f ? tail : 1.f - tail;
+}
+__device__ __forceinline__ float gelu(float x) {
+  float e;
+  return x * normal_cdf(x, &e);
+}
 __device__ __forceinline__ float gelu_slope(float x) {
-  return 0.5f * (1.f + erff(x * 0.70710678118654752f)) + x * __expf(-0.5f * x * x) * 0.39894228040143268f;
+  float e;
+  const float phi = normal_cdf(x, &e);
+  return fmaf(x * 0.39894228040143268f, e, phi);
 }
 __device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + __expf(-x)); }
 __device__ __forceinline__ float silu_slope(float x) {
@@ -144,6 +174,14 @@ __device__ __forceinline__ void store_as(void* p, uint64_t i, int dt, float x) {
   else if (dt == GD_DTYPE_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
   else static_cast<__half*>(p)[i] = __float2half_rn(x);
 }
+__device__ __forceinline__ void widen8(const uint4& q, int dt, float (&x)[8]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = dt == GD_DTYPE_BF16 ? unpack2<GD_DTYPE_BF16>(w[j]) : unpack2<GD_DTYPE_FP16>(w[j]);
+    x[2 * j] = f.x, x[2 * j + 1] = f.y;
+  }
+}
 __device__ __forceinline__ void load8_as(const void* p, uint64_t i, int dt, float (&x)[8]) {
   if (dt == GD_DTYPE_FP32) {
     const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
@@ -151,13 +189,7 @@ __device__ __forceinline__ void load8_as(const void* p, uint64_t i, int dt, floa
     x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     return;
   }
-  const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
-  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float2 f = dt == GD_DTYPE_BF16 ? unpack2<GD_DTYPE_BF16>(w[j]) : unpack2<GD_DTYPE_FP16>(w[j]);
-    x[2 * j] = f.x, x[2 * j + 1] = f.y;
-  }
+  widen8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i), dt, x);
 }
 __device__ __forceinline__ void store8_as(void* p, uint64_t i, int dt, const float (&x)[8]) {
   if (dt == GD_DTYPE_FP32) {
@@ -172,6 +204,18 @@ __device__ __forceinline__ void store8_as(void* p, uint64_t i, int dt, const flo
     w[j] = dt == GD_DTYPE_BF16 ? pack2<GD_DTYPE_BF16>(x[2 * j], x[2 * j + 1]) : pack2<GD_DTYPE_FP16>(x[2 * j], x[2 * j + 1]);
   *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+  if (act == GD_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];
+  } else if (act == GD_ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = gelu(v[j]);
+  } else if (act == GD_ACT_SILU) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = silu(v[j]);
+  }
+}
 // Eight neighbours of one output row, c a multiple of 8.
 __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t c, float (&v)[8]) {
   if (r >= e.rows || c >= e.cols) return;
@@ -183,10 +227,7 @@ __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t 
       for (int j = 0; j < 8; ++j) v[j] += b[j];
     }
     if (e.pre) store8_as(e.pre, (uint64_t)r * e.ld_pre + c, e.dtype, v);
-    if (e.activation != GD_ACT_NONE) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = activate(v[j], e.activation);
-    }
+    activate8(v, e.activation);
     if (e.add) {
       float b[8];
       load8_as(e.add, (uint64_t)r * e.ld_add + c, e.add_dtype, b);

@@ -19,11 +19,10 @@ namespace {
 
 constexpr uint32_t kPairWarps = 8;                            // that finish tiles
 constexpr uint32_t kPairThreads = (kPairWarps + 2) * 32;
-constexpr uint32_t kPairStages = 5;
+constexpr uint32_t kPairStages = 6;
 constexpr uint32_t kHalfBlock = 128 * kBlockK * 2;            // one CTA's half of a block of A or of B
 constexpr uint32_t kPairStage = 2 * kHalfBlock;
-constexpr uint32_t kPiecePitch = 36;                          // floats between rows of a piece: a multiple of 4 that spreads over the banks
-constexpr uint32_t kPieceBytes = 32 * kPiecePitch * 4;
+constexpr uint32_t kPieceBytes = 32 * 32 * 4;
 constexpr uint32_t kPairBytes = kPairStages * kPairStage + kPairWarps * kPieceBytes + 1024;
 constexpr uint32_t kGroup = 8;
 
@@ -156,20 +155,63 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       uint32_t tr, tc;
       tile_place(t, g.tiles_r, g.tiles_c, &tr, &tc);
       const uint32_t r0 = tr * 256u + rank * 128u + quarter * 32u, c0 = tc * 256u + half;
-      // a piece of 32 x 32: each lane puts its row into shared memory, then the warp works along the rows
+      // A piece of 32 x 32: each lane puts its row into shared memory, then the warp works along the rows.  A row's 16-byte chunks are
+      // XORed with the row's number, so that neither the lanes' rows nor the rows' neighbours meet in a bank.
       const auto put = [&](const float* w) {
         __syncwarp();
 #pragma unroll
-        for (uint32_t c = 0; c < 32; c += 4) *reinterpret_cast<float4*>(piece + lane * kPiecePitch + c) = make_float4(w[c], w[c + 1], w[c + 2], w[c + 3]);
+        for (uint32_t c = 0; c < 8; ++c)
+          *reinterpret_cast<float4*>(piece + lane * 32u + (c ^ (lane & 7u)) * 4u) = make_float4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
         __syncwarp();
       };
+      const auto get8 = [&](uint32_t r, float (&o)[8]) {   // the lane's eight columns of row r
+        const uint32_t c = (lane & 3u) * 2u;
+        const float4 x = *reinterpret_cast<const float4*>(piece + r * 32u + (c ^ (r & 7u)) * 4u), y = *reinterpret_cast<const float4*>(piece + r * 32u + ((c + 1u) ^ (r & 7u)) * 4u);
+        o[0] = x.x, o[1] = x.y, o[2] = x.z, o[3] = x.w, o[4] = y.x, o[5] = y.y, o[6] = y.z, o[7] = y.w;
+      };
+      // what the epilogue reads is asked for before the sum is there: a lane's eight columns of the bias, its rows of the residual
+      const bool fast = g.ep.vectors && r0 + 32 <= g.ep.rows && c0 + 128 <= g.ep.cols, add16 = g.ep.add && g.ep.add_dtype != GD_DTYPE_FP32;
+      const uint32_t lr = lane >> 2, lc = (lane & 3u) * 8u;
+      float bias[8];
+      uint4 add[4];
+      const auto fetch = [&](uint32_t q) {
+        if (!fast) return;
+        if (g.ep.bias) load8_as(g.ep.bias, c0 + 32 * q + lc, g.ep.bias_dtype, bias);
+        if (add16) {
+#pragma unroll
+          for (uint32_t u = 0; u < 4; ++u)
+            add[u] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(g.ep.add) + (uint64_t)(r0 + u * 8 + lr) * g.ep.ld_add + c0 + 32 * q + lc);
+        }
+      };
       const auto finish = [&](uint32_t q) {
+        const uint32_t c = c0 + 32 * q + lc;
+        if (!fast) {
 #pragma unroll 1
+          for (uint32_t u = 0; u < 4; ++u) {
+            float o[8];
+            get8(u * 8 + lr, o);
+            finish8(g.ep, r0 + u * 8 + lr, c, o);
+          }
+          return;
+        }
+#pragma unroll
         for (uint32_t u = 0; u < 4; ++u) {
-          const uint32_t r = u * 8 + (lane >> 2), c = (lane & 3u) * 8u;
-          const float4 x = *reinterpret_cast<const float4*>(piece + r * kPiecePitch + c), y = *reinterpret_cast<const float4*>(piece + r * kPiecePitch + c + 4);
-          float o[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-          finish8(g.ep, r0 + r, c0 + 32 * q + c, o);
+          const uint64_t r = r0 + u * 8 + lr;
+          float o[8];
+          get8(u * 8 + lr, o);
+          if (g.ep.bias) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] += bias[j];
+          }
+          if (g.ep.pre) store8_as(g.ep.pre, r * g.ep.ld_pre + c, g.ep.dtype, o);
+          activate8(o, g.ep.activation);
+          if (g.ep.add) {
+            float w[8];
+            if (add16) widen8(add[u], g.ep.add_dtype, w); else load8_as(g.ep.add, r * g.ep.ld_add + c, GD_DTYPE_FP32, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] += w[j];
+          }
+          store8_as(g.ep.out, r * g.ep.ld_out + c, g.ep.out_dtype, o);
         }
       };
       const auto release = [&](uint32_t buf) {       // this warp has read its part of the sum
@@ -200,19 +242,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
         if (!good) break;
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q) {
+          fetch(q);
           put(v + 32 * q);
           finish(q);
         }
       } else {
         const uint32_t buf = chain & 1u;
+        fetch(0);
         if (!mbar_wait(&sum_full[buf], (chain / 2) & 1u, abort)) { good = false; break; }
         fence_after();
         ++chain;
 #pragma unroll 1
         for (uint32_t q = 0; q < 4; ++q) {
+          if (q) fetch(q);
           float v[32];
-#pragma unroll
-          for (uint32_t c = 0; c < 32; c += 8) tmem_load8(from + buf * 256u + 32 * q + c, v + c);
+          tmem_load32(from + buf * 256u + 32 * q, v);
           tmem_ready();
           if (q == 3) release(buf);
           put(v);

@@ -92,26 +92,48 @@ def _dtype_of(dtype: torch.dtype) -> int:
     return _DTYPES[dtype]
 
 
-def _matrix(t: torch.Tensor, name: str, rows: int, cols: int, dtype, device) -> int:
+# The checks below run on every call and cost more than the launch if done naively: one comparison each for the common case (a
+# contiguous tensor of the right type, shape and device), everything else in the functions that explain.
+
+def _matrix(t: torch.Tensor, name: str, rows: int, cols: int, dtype, index: int) -> int:
     """Checks a [rows, cols] tensor whose rows are contiguous and returns its leading dimension."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{name}: expected {dtype} [{rows}, {cols}] on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != index:
+        raise ValueError(f"{name}: expected {dtype} [{rows}, {cols}] on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.is_contiguous():
+        return cols
     ld, step = t.stride()
     if (step != 1 and cols > 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{name}: the elements of a row must be neighbours and rows must not overlap (strides {ld}, {step})")
     return ld if rows > 1 else cols
 
 
-def _vector(t: torch.Tensor, name: str, n: int, dtypes, device) -> None:
-    if t.dtype not in dtypes or t.device != device or t.dim() != 1 or t.numel() != n or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: expected {n} contiguous {' or '.join(map(str, dtypes))} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+def _vector(t: torch.Tensor, name: str, n: int, dtypes, index: int) -> None:
+    if t.dtype not in dtypes or t.shape != (n,) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} contiguous {' or '.join(map(str, dtypes))} on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
 
 
-def _cuda(device) -> torch.device:
+def _scalar(t: Optional[torch.Tensor], name: str, index: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.numel() != 1 or t.dtype is not torch.float32 or t.get_device() != index:
+        raise ValueError(f"{name} is one float32 on cuda:{index}")
+    return t.data_ptr()
+
+
+def _cuda_index(device) -> int:
     device = torch.device(device)
     if device.type != "cuda":
         raise RuntimeError("a CUDA device is needed: the library has no CPU path")
-    return torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
+    return torch.cuda.current_device() if device.index is None else device.index
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # the current stream's handle without a Stream object around it
+
+
+def _stream(stream, index: int):
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(index)
+    return B._stream_handle(stream)
 
 
 class LinearSession:
@@ -128,46 +150,56 @@ class LinearSession:
             raise ValueError("LinearSession takes bfloat16 or float16")
         if activation not in _ACTIVATIONS or w_layout not in _LAYOUTS:
             raise ValueError(f"activation is one of {sorted(_ACTIVATIONS)}, w_layout one of {sorted(_LAYOUTS)}")
-        self.device = _cuda(device)
+        self._index = index = _cuda_index(device)
+        self.device = torch.device("cuda", index)
         self.n_in, self.n_out, self.max_rows, self.dtype, self.activation, self.w_layout = int(n_in), int(n_out), int(max_rows), dtype, activation, w_layout
         self.w_shape = (self.n_in, self.n_out) if w_layout == "in_out" else (self.n_out, self.n_in)
+        self._lib = load_library()
         size = C.c_size_t(0)
-        B._check(load_library().gd_linear_workspace_bytes(self.max_rows, self.n_out, self.n_in, int(any_layout), C.byref(size)), "gd_linear_workspace_bytes")
+        B._check(self._lib.gd_linear_workspace_bytes(self.max_rows, self.n_out, self.n_in, int(any_layout), C.byref(size)), "gd_linear_workspace_bytes")
         self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
         self.workspace[:256].zero_()
-        code = _DTYPES[dtype]
         self._forward, self._backward = _LinearForwardArgs(), _LinearBackwardArgs()
         for a in (self._forward, self._backward):
-            a.n, a.k, a.dtype = self.n_out, self.n_in, code
+            a.n, a.k, a.dtype = self.n_out, self.n_in, _DTYPES[dtype]
             a.activation, a.w_layout = _ACTIVATIONS[activation], _LAYOUTS[w_layout]
             a.workspace, a.workspace_bytes = self.workspace.data_ptr(), size.value
+        self._forward_ref, self._backward_ref = C.byref(self._forward), C.byref(self._backward)
 
     def _rows(self, t: torch.Tensor) -> int:
-        if t.dim() != 2 or t.shape[0] > self.max_rows:
+        m = t.shape[0] if t.dim() == 2 else -1
+        if not 0 <= m <= self.max_rows:
             raise ValueError(f"at most {self.max_rows} rows of a matrix, got {list(t.shape)}")
-        return t.shape[0]
+        return m
 
     def forward(self, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """act(x W + bias) + residual, into `out` (float32, or the session's type; made here if None) and, if `pre` is given, x W + bias."""
-        m, n, k, dt, dev, a = self._rows(x), self.n_out, self.n_in, self.dtype, self.device, self._forward
+        m, n, dt, index, a = self._rows(x), self.n_out, self.dtype, self._index, self._forward
         if out is None:
-            out = torch.empty(m, n, dtype=dt, device=dev)
+            out = torch.empty(m, n, dtype=dt, device=self.device)
+        out_dt = out.dtype if out.dtype is torch.float32 else dt
         a.m = m
-        a.x, a.ldx = x.data_ptr(), _matrix(x, "x", m, k, dt, dev)
-        a.w, a.ldw = w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, dev)
-        a.y, a.ldy = out.data_ptr(), _matrix(out, "out", m, n, torch.float32 if out.dtype == torch.float32 else dt, dev)
-        a.y_dtype = _DTYPES[out.dtype]
-        a.bias = None
-        if bias is not None:
-            _vector(bias, "bias", n, (torch.float32, dt), dev)
+        a.ldx = _matrix(x, "x", m, self.n_in, dt, index)
+        a.ldw = _matrix(w, "w", *self.w_shape, dt, index)
+        a.ldy = _matrix(out, "out", m, n, out_dt, index)
+        a.x, a.w, a.y, a.y_dtype = x.data_ptr(), w.data_ptr(), out.data_ptr(), _DTYPES[out_dt]
+        if bias is None:
+            a.bias = None
+        else:
+            _vector(bias, "bias", n, (torch.float32, dt), index)
             a.bias, a.bias_dtype = bias.data_ptr(), _DTYPES[bias.dtype]
-        a.residual = a.pre = None
-        if residual is not None:
-            a.residual, a.ld_residual = residual.data_ptr(), _matrix(residual, "residual", m, n, dt, dev)
-        if pre is not None:
-            a.pre, a.ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, dev)
-        B._check(load_library().gd_linear_forward(C.byref(a), B._stream_handle(stream)), "gd_linear_forward")
+        if residual is None:
+            a.residual = None
+        else:
+            a.residual, a.ld_residual = residual.data_ptr(), _matrix(residual, "residual", m, n, dt, index)
+        if pre is None:
+            a.pre = None
+        else:
+            a.pre, a.ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, index)
+        code = self._lib.gd_linear_forward(self._forward_ref, _stream(stream, index))
+        if code:
+            raise B.GdError(code, "gd_linear_forward")
         return out
 
     def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor], pre: Optional[torch.Tensor] = None,
@@ -177,34 +209,43 @@ class LinearSession:
 
         dw has w's shape, in float32 or the session's type; db is float32.  accumulate adds to dw (float32) and db.
         """
-        m, n, k, dt, dev, a = self._rows(dy), self.n_out, self.n_in, self.dtype, self.device, self._backward
+        m, n, k, dt, index, a = self._rows(dy), self.n_out, self.n_in, self.dtype, self._index, self._backward
         if self.activation != "none" and pre is None:
             raise ValueError("backward needs the pre-activation that forward wrote")
         a.m, a.flags = m, GD_LINEAR_ACCUMULATE if accumulate else 0
-        a.dy, a.ld_dy = dy.data_ptr(), _matrix(dy, "dy", m, n, dt, dev)
-        a.pre = a.x = a.w = a.dx = a.dw = a.db = None
-        a.dw_dtype = GD_DTYPE_FP32
-        if pre is not None:
-            a.pre, a.ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, dev)
-        if dx is not None:
+        a.dy, a.ld_dy = dy.data_ptr(), _matrix(dy, "dy", m, n, dt, index)
+        if pre is None:
+            a.pre = None
+        else:
+            a.pre, a.ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, index)
+        if dx is None:
+            a.w = a.dx = None
+        else:
             if w is None:
                 raise ValueError("dx needs w")
-            a.w, a.ldw = w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, dev)
-            a.dx, a.ld_dx = dx.data_ptr(), _matrix(dx, "dx", m, k, dt, dev)
-        if dw is not None:
+            a.w, a.ldw = w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, index)
+            a.dx, a.ld_dx = dx.data_ptr(), _matrix(dx, "dx", m, k, dt, index)
+        if dw is None:
+            a.x = a.dw = None
+            a.dw_dtype = GD_DTYPE_FP32
+        else:
             if x is None:
                 raise ValueError("dw needs x")
-            a.x, a.ldx = x.data_ptr(), _matrix(x, "x", m, k, dt, dev)
-            a.dw, a.ld_dw = dw.data_ptr(), _matrix(dw, "dw", *self.w_shape, torch.float32 if dw.dtype == torch.float32 else dt, dev)
-            a.dw_dtype = _DTYPES[dw.dtype]
-        if db is not None:
-            _vector(db, "db", n, (torch.float32,), dev)
+            dw_dt = dw.dtype if dw.dtype is torch.float32 else dt
+            a.x, a.ldx = x.data_ptr(), _matrix(x, "x", m, k, dt, index)
+            a.dw, a.ld_dw, a.dw_dtype = dw.data_ptr(), _matrix(dw, "dw", *self.w_shape, dw_dt, index), _DTYPES[dw_dt]
+        if db is None:
+            a.db = None
+        else:
+            _vector(db, "db", n, (torch.float32,), index)
             a.db = db.data_ptr()
-        B._check(load_library().gd_linear_backward(C.byref(a), B._stream_handle(stream)), "gd_linear_backward")
+        code = self._lib.gd_linear_backward(self._backward_ref, _stream(stream, index))
+        if code:
+            raise B.GdError(code, "gd_linear_backward")
 
     def status(self, stream=None) -> int:
         """GD_OK, or GD_ERR_DEVICE_TIMEOUT if a device-side wait of any call so far gave up (waits for the stream)."""
-        return load_library().gd_linear_status(self.workspace.data_ptr(), B._stream_handle(stream))
+        return self._lib.gd_linear_status(self.workspace.data_ptr(), _stream(stream, self._index))
 
 
 def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
@@ -215,25 +256,24 @@ def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, loss: Optional[to
     grad_scale_dev.  Rows whose target is ignore_index have loss and gradient 0."""
     if logits.dim() != 2:
         raise ValueError(f"logits: expected a matrix, got {list(logits.shape)}")
-    dev = _cuda(logits.device)
+    index = logits.get_device()
+    if index < 0:
+        raise RuntimeError("a CUDA device is needed: the library has no CPU path")
     rows, classes = logits.shape
-    a = _CrossEntropyArgs()
-    a.rows, a.classes, a.dtype = rows, classes, _dtype_of(logits.dtype)
-    a.logits, a.ld_logits = logits.data_ptr(), _matrix(logits, "logits", rows, classes, logits.dtype, dev)
-    _vector(targets, "targets", rows, (torch.int64, torch.int32), dev)
-    a.targets, a.target_bits, a.ignore_index = targets.data_ptr(), 64 if targets.dtype == torch.int64 else 32, ignore_index
-    a.grad_scale = grad_scale
-    if grad_scale_dev is not None:
-        if grad_scale_dev.numel() != 1 or grad_scale_dev.dtype != torch.float32 or grad_scale_dev.device != dev:
-            raise ValueError("grad_scale_dev is one float32 on the logits' device")
-        a.grad_scale_dev = grad_scale_dev.data_ptr()
-    for name, t in (("loss", loss), ("lse", lse)):
-        if t is not None:
-            _vector(t, name, rows, (torch.float32,), dev)
-            setattr(a, name, t.data_ptr())
-    if grad is not None:
-        a.grad, a.ld_grad = grad.data_ptr(), _matrix(grad, "grad", rows, classes, logits.dtype, dev)
-    B._check(load_library().gd_cross_entropy(C.byref(a), B._stream_handle(stream)), "gd_cross_entropy")
+    dtype = logits.dtype
+    ld = _matrix(logits, "logits", rows, classes, dtype, index)
+    _vector(targets, "targets", rows, (torch.int64, torch.int32), index)
+    if loss is not None:
+        _vector(loss, "loss", rows, (torch.float32,), index)
+    if lse is not None:
+        _vector(lse, "lse", rows, (torch.float32,), index)
+    a = _CrossEntropyArgs(rows, classes, _dtype_of(dtype), 64 if targets.dtype is torch.int64 else 32, logits.data_ptr(), ld, targets.data_ptr(),
+                          ignore_index, grad_scale, 0, _scalar(grad_scale_dev, "grad_scale_dev", index), None if loss is None else loss.data_ptr(),
+                          None if lse is None else lse.data_ptr(), None if grad is None else grad.data_ptr(),
+                          0 if grad is None else _matrix(grad, "grad", rows, classes, dtype, index))
+    code = load_library().gd_cross_entropy(C.byref(a), _stream(stream, index))
+    if code:
+        raise B.GdError(code, "gd_cross_entropy")
 
 
 class AdamWSession:
@@ -254,7 +294,8 @@ class AdamWSession:
             raise ValueError("AdamWSession needs at least one tensor")
         if (m is None) != (v is None) or (m_scale is None) != (v_scale is None) or (m is None and m_scale is not None):
             raise ValueError("give both moments, and the scales of both or of neither")
-        dev = _cuda(self.params[0].device)
+        self._index = _cuda_index(self.params[0].device)
+        dev = self.params[0].device
         sizes = [p.numel() for p in self.params]
         if m is not None:
             state_bits = 32 if m_scale is None else 8
@@ -311,9 +352,7 @@ class AdamWSession:
         a = self._args
         a.step, a.lr, a.beta1, a.beta2, a.eps = step, lr, beta1, beta2, eps
         a.grad_scale, a.seed = grad_scale, seed & 0xFFFFFFFF
-        a.grad_scale_dev = None
-        if grad_scale_dev is not None:
-            if grad_scale_dev.numel() != 1 or grad_scale_dev.dtype != torch.float32 or grad_scale_dev.device != self._device:
-                raise ValueError("grad_scale_dev is one float32 on the tensors' device")
-            a.grad_scale_dev = grad_scale_dev.data_ptr()
-        B._check(load_library().gd_adamw_step(C.byref(a), B._stream_handle(stream)), "gd_adamw_step")
+        a.grad_scale_dev = _scalar(grad_scale_dev, "grad_scale_dev", self._index)
+        code = load_library().gd_adamw_step(C.byref(a), _stream(stream, self._index))
+        if code:
+            raise B.GdError(code, "gd_adamw_step")
