@@ -4,7 +4,7 @@
 // 8 bits.  One launch takes up to kMaxTensors tensors, whose table travels as the kernel argument (no device copy, no
 // allocation); a CTA takes one chunk of kChunk consecutive elements of one tensor.  A warp works on blocks of 128 elements, four
 // per lane in one 16-byte access, because 128 is also the unit that shares a scale in the 8-bit moments: its largest
-// magnitude is one warp reduction, and nothing but the warp has to agree on it.  kBlocks of them are in flight per warp.
+// magnitude is one warp reduction, and nothing but the warp has to agree on it.
 // A tensor whose buffers do not all start on a vector boundary (pieces of a flat vector do not), and a tensor's last,
 // partial block, go element by element, lane-contiguous, with the same arithmetic.
 #include <cmath>
@@ -14,9 +14,9 @@
 namespace gd {
 namespace {
 
-constexpr int kBlocks = 2;                        // blocks of 128 elements a warp has in flight
-constexpr uint32_t kAdamThreads = 256;
-constexpr uint32_t kChunk = kAdamThreads / 32 * kBlocks * 128;
+constexpr uint32_t kAdamThreads = 256, kStride = kAdamThreads / 32 * 128;
+template <int BITS>
+constexpr uint32_t kChunk = (BITS == 8 ? 8 : 2) * kStride;   // elements a CTA takes: blocks a warp works through x its warps' stride
 
 struct TensorEntry {
   void* param;
@@ -85,12 +85,24 @@ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-// fp8 (e4m3) of a magnitude y < 256, rounded up or down by 16 random bits.  In units of the last bit kept, times 2^20, a normal
-// number is its own bits less the exponent's bias; below 2^-6 the step is fixed, which adding 2^-6 turns into the same form.
-__device__ __forceinline__ uint32_t encode_fp8(float y, uint32_t random16) {
-  const uint32_t units = y >= 0x1p-6f ? __float_as_uint(y) - (120u << 23) : __float_as_uint(__fadd_rn(y, 0x1p-6f)) - (121u << 23);
-  const uint32_t code = (units + (random16 << 4)) >> 20;
-  return (__float_as_uint(y) & 0x7F800000u) == 0x7F800000u ? 127u : min(code, 127u);
+// fp8 (e4m3) of a magnitude y < 256, rounded up or down by 16 random bits.  In units of 2^-20 of the last bit kept a normal number
+// is its own bits (exponent and mantissa run on); below 2^-6 the step is fixed, and y / 2 + 2^-7 has the bits that continue the
+// normal numbers' downwards - it is also the larger of the two exactly there, so one maximum picks the case.  The code's seven bits
+// come out in the top byte, 0xC0 too high; four of them are put right together by pack_codes().
+__device__ __forceinline__ uint32_t encode_fp8(float y, uint32_t random_bits_8_to_23) {
+  return (__float_as_uint(fmaxf(y, fmaf(y, 0.5f, 0x1p-7f))) << 4) + random_bits_8_to_23;
+}
+// (top byte - 0xC0) of each: a code is below 0x80, so that is the sixth bit turned over and the seventh cleared
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&x)[4]) {
+  return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410);
+}
+__device__ __forceinline__ uint32_t pack_codes(const uint32_t (&x)[4]) { return (top_bytes(x) ^ 0x40404040u) & 0x7F7F7F7Fu; }
+// what is not finite becomes NaN
+__device__ __forceinline__ uint32_t nan_codes(uint32_t codes, const float (&x)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (!(fabsf(x[j]) < INFINITY)) codes |= 0x7Fu << (8 * j);
+  return codes;
 }
 __device__ __forceinline__ float2 decode_fp8x2(uint32_t two) {
   uint32_t h;
@@ -98,9 +110,20 @@ __device__ __forceinline__ float2 decode_fp8x2(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// The scale of a block from the bits of its largest magnitude, and its reciprocal: powers of two, so both products are exact.
-__device__ __forceinline__ void block_scale(uint32_t top_bits, float* scale, float* inverse) {
-  const int e = max((int)(top_bits >> 23) - 7, 1);
+// The largest magnitude of a warp's values (NaN if there is one).
+__device__ __forceinline__ float largest(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return r;
+}
+__device__ __forceinline__ float warp_largest(float x) {
+  float r;
+  asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+// The scale of a block from its largest magnitude, and its reciprocal: powers of two, so both products are exact.
+__device__ __forceinline__ void block_scale(float top, float* scale, float* inverse) {
+  const int e = max((int)(__float_as_uint(top) >> 23) - 7, 1);
   *scale = __uint_as_float((uint32_t)e << 23);
   *inverse = __uint_as_float((uint32_t)(254 - e) << 23);
 }
@@ -115,6 +138,168 @@ __device__ __forceinline__ void update(float& p, float g, float& m, float& v, fl
   p = __fsub_rn(__fmul_rn(p, decay), __fmul_rn(__fdiv_rn(m, d), s.step_size));
 }
 
+// What a lane holds of a block: four elements.
+template <int BITS>
+struct Block {
+  float p[4], g[4], m[4], v[4];
+  uint32_t mc, vc;              // the 8-bit moments as they lie in memory, and their scales
+  float ms, vs;
+};
+
+template <int PT, int GT>
+__device__ __forceinline__ void load_block(Block<32>& b, const TensorEntry& t, uint64_t at, uint32_t lane) {
+  load4<PT>(t.param, at + 4 * lane, b.p);
+  load4<GT>(t.grad, at + 4 * lane, b.g);
+  load4<GD_DTYPE_FP32>(t.m, at + 4 * lane, b.m);
+  load4<GD_DTYPE_FP32>(t.v, at + 4 * lane, b.v);
+}
+// A block on its way through shared memory: parameters, gradients, codes of m and of v, the two scales.
+constexpr int kStages = 4;
+constexpr uint32_t kStageBytes = 512 + 512 + 128 + 128 + 16;
+template <uint32_t BYTES>
+__device__ __forceinline__ void ask(void* dst, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(BYTES) : "memory");
+}
+template <int PT, int GT>
+__device__ __forceinline__ void ask_block(unsigned char* stage, const TensorEntry& t, uint64_t at, uint32_t lane) {
+  constexpr uint32_t pb = PT == GD_DTYPE_FP32 ? 16 : 8, gb = GT == GD_DTYPE_FP32 ? 16 : 8;
+  const uint64_t e = at / 4 + lane;
+  ask<pb>(stage + pb * lane, static_cast<const unsigned char*>(t.param) + e * pb);
+  ask<gb>(stage + 512 + gb * lane, static_cast<const unsigned char*>(t.grad) + e * gb);
+  ask<4>(stage + 1024 + 4 * lane, static_cast<const unsigned char*>(t.m) + e * 4);
+  ask<4>(stage + 1152 + 4 * lane, static_cast<const unsigned char*>(t.v) + e * 4);
+  if (lane < 2) ask<4>(stage + 1280 + 4 * lane, (lane ? t.v_scale : t.m_scale) + (at >> 7));
+}
+template <int DT>
+__device__ __forceinline__ void take4(const unsigned char* p, uint32_t lane, float (&x)[4]) {
+  if constexpr (DT == GD_DTYPE_FP32) {
+    const float4 q = reinterpret_cast<const float4*>(p)[lane];
+    x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
+  } else {
+    const uint2 q = reinterpret_cast<const uint2*>(p)[lane];
+    const float2 a = unpack2<DT>(q.x), b = unpack2<DT>(q.y);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+  }
+}
+template <int PT, int GT>
+__device__ __forceinline__ void take_block(Block<8>& b, const unsigned char* stage, uint32_t lane) {
+  take4<PT>(stage, lane, b.p);
+  take4<GT>(stage + 512, lane, b.g);
+  b.mc = reinterpret_cast<const uint32_t*>(stage + 1024)[lane];
+  b.vc = reinterpret_cast<const uint32_t*>(stage + 1152)[lane];
+  b.ms = reinterpret_cast<const float*>(stage + 1280)[0];
+  b.vs = reinterpret_cast<const float*>(stage + 1280)[1];
+}
+// Element by element: element j of a lane is at + lane + 32 j.  What lies past the end is held as zeros.
+template <int PT, int GT, int BITS>
+__device__ __forceinline__ void load_ragged(Block<BITS>& b, const TensorEntry& t, uint64_t at, uint32_t lane) {
+  b.mc = b.vc = 0u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint64_t e = at + lane + 32 * j;
+    const bool in = e < t.n;
+    b.p[j] = in ? load1<PT>(t.param, e) : 0.f;
+    b.g[j] = in ? load1<GT>(t.grad, e) : 0.f;
+    if constexpr (BITS == 32) {
+      b.m[j] = in ? static_cast<const float*>(t.m)[e] : 0.f;
+      b.v[j] = in ? static_cast<const float*>(t.v)[e] : 0.f;
+    } else if (in) {
+      b.mc |= (uint32_t)static_cast<const uint8_t*>(t.m)[e] << (8 * j);
+      b.vc |= (uint32_t)static_cast<const uint8_t*>(t.v)[e] << (8 * j);
+    }
+  }
+  if constexpr (BITS == 8) {
+    b.ms = t.m_scale[at >> 7];
+    b.vs = t.v_scale[at >> 7];
+  }
+}
+
+// The update of a block; with 8-bit moments also their new codes (mc, vc) and scales (ms, vs).
+template <bool RAGGED, int BITS>
+__device__ __forceinline__ void update_block(Block<BITS>& b, const AdamScalars& s, float scale, float decay, uint32_t random_base, uint64_t at, uint64_t n,
+                                             uint32_t lane) {
+  float root[4];
+  if constexpr (BITS == 8) {
+    const float2 m01 = decode_fp8x2(b.mc & 0xFFFFu), m23 = decode_fp8x2(b.mc >> 16);
+    const float2 v01 = decode_fp8x2(b.vc & 0xFFFFu), v23 = decode_fp8x2(b.vc >> 16);
+    b.m[0] = __fmul_rn(m01.x, b.ms), b.m[1] = __fmul_rn(m01.y, b.ms), b.m[2] = __fmul_rn(m23.x, b.ms), b.m[3] = __fmul_rn(m23.y, b.ms);
+    const float r[4] = {__fmul_rn(v01.x, b.vs), __fmul_rn(v01.y, b.vs), __fmul_rn(v23.x, b.vs), __fmul_rn(v23.y, b.vs)};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b.v[j] = __fmul_rn(r[j], r[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) update(b.p[j], b.g[j], b.m[j], b.v[j], root[j], s, scale, decay);
+  if constexpr (BITS == 8) {
+    if constexpr (RAGGED) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (at + lane + 32 * j >= n) b.m[j] = root[j] = 0.f;
+    }
+    const float m_top = warp_largest(largest(largest(b.m[0], b.m[1]), largest(b.m[2], b.m[3])));
+    const float v_top = warp_largest(largest(largest(root[0], root[1]), largest(root[2], root[3])));
+    float m_inverse, v_inverse;
+    block_scale(m_top, &b.ms, &m_inverse);
+    block_scale(v_top, &b.vs, &v_inverse);
+    uint32_t cm[4], cv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t e = (uint32_t)at + (RAGGED ? lane + 32 * j : 4 * lane + j);
+      const uint32_t h = mix32(e * 0x9E3779B9u + random_base);
+      cm[j] = encode_fp8(__fmul_rn(fabsf(b.m[j]), m_inverse), __byte_perm(h, 0u, 0x4324));
+      float y = __fmul_rn(root[j], v_inverse);
+      if (root[j] > 0.f) y = fmaxf(y, 0x1p-9f);          // at least the smallest positive code, whose step this is
+      cv[j] = encode_fp8(y, __byte_perm(h, 0u, 0x4104));
+    }
+    const uint32_t signs[4] = {__float_as_uint(b.m[0]), __float_as_uint(b.m[1]), __float_as_uint(b.m[2]), __float_as_uint(b.m[3])};
+    b.mc = pack_codes(cm);
+    b.vc = pack_codes(cv);
+    if (!(m_top < INFINITY && v_top < INFINITY)) {       // the same for the whole warp
+      b.mc = nan_codes(b.mc, b.m);
+      b.vc = nan_codes(b.vc, root);
+    }
+    b.mc |= top_bytes(signs) & 0x80808080u;
+  }
+}
+
+template <int PT, int BITS>
+__device__ __forceinline__ void store_block(const Block<BITS>& b, const TensorEntry& t, int copy_dtype, uint64_t at, uint32_t lane) {
+  store4<PT>(t.param, at + 4 * lane, b.p);
+  if (t.copy) {
+    if (copy_dtype == GD_DTYPE_BF16) store4<GD_DTYPE_BF16>(t.copy, at + 4 * lane, b.p);
+    else if (copy_dtype == GD_DTYPE_FP16) store4<GD_DTYPE_FP16>(t.copy, at + 4 * lane, b.p);
+    else store4<GD_DTYPE_FP32>(t.copy, at + 4 * lane, b.p);
+  }
+  if constexpr (BITS == 32) {
+    store4<GD_DTYPE_FP32>(t.m, at + 4 * lane, b.m);
+    store4<GD_DTYPE_FP32>(t.v, at + 4 * lane, b.v);
+  } else {
+    __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.m) + at + 4 * lane), b.mc);
+    __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + at + 4 * lane), b.vc);
+  }
+}
+template <int PT, int BITS>
+__device__ __forceinline__ void store_ragged(const Block<BITS>& b, const TensorEntry& t, int copy_dtype, uint64_t at, uint32_t lane) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint64_t e = at + lane + 32 * j;
+    if (e >= t.n) continue;
+    store1<PT>(t.param, e, b.p[j]);
+    if (t.copy) {
+      if (copy_dtype == GD_DTYPE_BF16) store1<GD_DTYPE_BF16>(t.copy, e, b.p[j]);
+      else if (copy_dtype == GD_DTYPE_FP16) store1<GD_DTYPE_FP16>(t.copy, e, b.p[j]);
+      else store1<GD_DTYPE_FP32>(t.copy, e, b.p[j]);
+    }
+    if constexpr (BITS == 32) {
+      static_cast<float*>(t.m)[e] = b.m[j];
+      static_cast<float*>(t.v)[e] = b.v[j];
+    } else {
+      static_cast<uint8_t*>(t.m)[e] = (uint8_t)(b.mc >> (8 * j));
+      static_cast<uint8_t*>(t.v)[e] = (uint8_t)(b.vc >> (8 * j));
+    }
+  }
+}
+
 template <int PT, int GT, int BITS, uint32_t CAP>
 __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamTable<CAP> table) {
   const AdamScalars& s = table.s;
@@ -124,148 +309,72 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     const uint32_t mid = (lo + hi) >> 1;
     if (table.t[mid].chunk0 <= blockIdx.x) lo = mid; else hi = mid;
   }
-  const TensorEntry& t = table.t[lo];
-  const uint32_t lane = lane_id();
-  const uint64_t first = (uint64_t)(blockIdx.x - t.chunk0) * kChunk + (threadIdx.x >> 5) * (kBlocks * 128u);
-  const uint64_t n = t.n;
-  if (first >= n) return;
+  const TensorEntry t = table.t[lo];
+  const uint32_t lane = lane_id(), random_base = s.seed + t.index * 0x85EBCA77u;
+  uint64_t at = (uint64_t)(blockIdx.x - t.chunk0) * kChunk<BITS> + (threadIdx.x >> 5) * 128u;
+  const uint64_t end = min(t.n, (uint64_t)(blockIdx.x - t.chunk0 + 1) * kChunk<BITS>);
   pdl_wait();
   pdl_trigger();
   const float scale = s.grad_scale_dev ? __fmul_rn(s.grad_scale, *s.grad_scale_dev) : s.grad_scale;
-  const bool vec = t.vectors && first + kBlocks * 128u <= n;
-
-  float p[kBlocks][4], g[kBlocks][4], m[kBlocks][4], v[kBlocks][4];
-  uint32_t mc[kBlocks], vc[kBlocks];
-  float ms[kBlocks], vs[kBlocks];
+  Block<BITS> b;
+  if constexpr (BITS == 8) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    if (t.vectors && at + 128u <= end) {
+      unsigned char* ring = smem + (threadIdx.x >> 5) * (kStages * kStageBytes);
+      uint64_t ask = at;
 #pragma unroll
-  for (int b = 0; b < kBlocks; ++b) {
-    const uint64_t at = first + b * 128u;
-    if (vec) {
-      load4<PT>(t.param, at + 4 * lane, p[b]);
-      load4<GT>(t.grad, at + 4 * lane, g[b]);
-      if constexpr (BITS == 32) {
-        load4<GD_DTYPE_FP32>(t.m, at + 4 * lane, m[b]);
-        load4<GD_DTYPE_FP32>(t.v, at + 4 * lane, v[b]);
-      } else {
-        mc[b] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.m) + at + 4 * lane));
-        vc[b] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.v) + at + 4 * lane));
-        ms[b] = t.m_scale[at >> 7];
-        vs[b] = t.v_scale[at >> 7];
+      for (int i = 0; i < kStages - 1; ++i, ask += kStride) {
+        if (ask + 128u <= end) ask_block<PT, GT>(ring + i * kStageBytes, t, ask, lane);
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
-    } else {
-      mc[b] = vc[b] = 0u;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint64_t e = at + lane + 32 * j;
-        const bool in = e < n;
-        p[b][j] = in ? load1<PT>(t.param, e) : 0.f;
-        g[b][j] = in ? load1<GT>(t.grad, e) : 0.f;
-        if constexpr (BITS == 32) {
-          m[b][j] = in ? static_cast<const float*>(t.m)[e] : 0.f;
-          v[b][j] = in ? static_cast<const float*>(t.v)[e] : 0.f;
-        } else if (in) {
-          mc[b] |= (uint32_t)static_cast<const uint8_t*>(t.m)[e] << (8 * j);
-          vc[b] |= (uint32_t)static_cast<const uint8_t*>(t.v)[e] << (8 * j);
-        }
+      for (uint32_t i = 0; at + 128u <= end; ++i, at += kStride, ask += kStride) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();                      // everybody's part of this block has landed, and the block before it has been read
+        if (ask + 128u <= end) ask_block<PT, GT>(ring + (i + kStages - 1) % kStages * kStageBytes, t, ask, lane);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        take_block<PT, GT>(b, ring + i % kStages * kStageBytes, lane);
+        update_block<false, BITS>(b, s, scale, t.decay, random_base, at, t.n, lane);
+        if (lane == 0) t.m_scale[at >> 7] = b.ms, t.v_scale[at >> 7] = b.vs;
+        store_block<PT, BITS>(b, t, s.copy_dtype, at, lane);
       }
-      if constexpr (BITS == 8) {
-        ms[b] = at < n ? t.m_scale[at >> 7] : 0.f;
-        vs[b] = at < n ? t.v_scale[at >> 7] : 0.f;
+    }
+  } else {
+    Block<BITS> next;
+    if (t.vectors && at + 128u <= end) {
+      load_block<PT, GT>(b, t, at, lane);
+      while (true) {
+        const uint64_t after = at + kStride;
+        const bool more = after + 128u <= end;
+        if (more) load_block<PT, GT>(next, t, after, lane);        // under way while this block is worked on
+        update_block<false, BITS>(b, s, scale, t.decay, random_base, at, t.n, lane);
+        store_block<PT, BITS>(b, t, s.copy_dtype, at, lane);
+        at = after;
+        if (!more) break;
+        b = next;
       }
     }
   }
-#pragma unroll
-  for (int b = 0; b < kBlocks; ++b) {
-    const uint64_t at = first + b * 128u;
-    if (at >= n) break;
-    float root[4];
+  for (; at < end; at += kStride) {
+    load_ragged<PT, GT, BITS>(b, t, at, lane);
+    update_block<true, BITS>(b, s, scale, t.decay, random_base, at, t.n, lane);
     if constexpr (BITS == 8) {
-      const float2 m01 = decode_fp8x2(mc[b] & 0xFFFFu), m23 = decode_fp8x2(mc[b] >> 16);
-      const float2 v01 = decode_fp8x2(vc[b] & 0xFFFFu), v23 = decode_fp8x2(vc[b] >> 16);
-      m[b][0] = __fmul_rn(m01.x, ms[b]), m[b][1] = __fmul_rn(m01.y, ms[b]), m[b][2] = __fmul_rn(m23.x, ms[b]), m[b][3] = __fmul_rn(m23.y, ms[b]);
-      const float r[4] = {__fmul_rn(v01.x, vs[b]), __fmul_rn(v01.y, vs[b]), __fmul_rn(v23.x, vs[b]), __fmul_rn(v23.y, vs[b])};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[b][j] = __fmul_rn(r[j], r[j]);
+      if (lane == 0) t.m_scale[at >> 7] = b.ms, t.v_scale[at >> 7] = b.vs;
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) update(p[b][j], g[b][j], m[b][j], v[b][j], root[j], s, scale, t.decay);
-    if constexpr (BITS == 8) {
-      uint32_t m_top = 0u, v_top = 0u;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool in = vec || at + lane + 32 * j < n;      // (elements past the end hold zeros, but eps = 0 would make them NaN in p only)
-        m_top = max(m_top, in ? __float_as_uint(m[b][j]) & 0x7FFFFFFFu : 0u);
-        v_top = max(v_top, in ? __float_as_uint(root[j]) & 0x7FFFFFFFu : 0u);
-      }
-      m_top = __reduce_max_sync(0xFFFFFFFFu, m_top);
-      v_top = __reduce_max_sync(0xFFFFFFFFu, v_top);
-      float m_scale, m_inverse, v_scale, v_inverse;
-      block_scale(m_top, &m_scale, &m_inverse);
-      block_scale(v_top, &v_scale, &v_inverse);
-      mc[b] = vc[b] = 0u;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t e = (uint32_t)at + (vec ? 4 * lane + j : lane + 32 * j);
-        const uint32_t h = mix32(e * 0x9E3779B9u + s.seed + t.index * 0x85EBCA77u);
-        const uint32_t sign = __float_as_uint(m[b][j]) >> 31 << 7;
-        const uint32_t cm = encode_fp8(__fmul_rn(fabsf(m[b][j]), m_inverse), h >> 16) | sign;
-        uint32_t cv = encode_fp8(__fmul_rn(fabsf(root[j]), v_inverse), h & 0xFFFFu);
-        if (root[j] > 0.f && cv == 0u) cv = 1u;
-        cv |= __float_as_uint(root[j]) >> 31 << 7;
-        mc[b] |= cm << (8 * j);
-        vc[b] |= cv << (8 * j);
-      }
-      if (lane == 0) {
-        t.m_scale[at >> 7] = m_scale;
-        t.v_scale[at >> 7] = v_scale;
-      }
-    }
-    if (vec) {
-      store4<PT>(t.param, at + 4 * lane, p[b]);
-      if (t.copy) {
-        if (s.copy_dtype == GD_DTYPE_BF16) store4<GD_DTYPE_BF16>(t.copy, at + 4 * lane, p[b]);
-        else if (s.copy_dtype == GD_DTYPE_FP16) store4<GD_DTYPE_FP16>(t.copy, at + 4 * lane, p[b]);
-        else store4<GD_DTYPE_FP32>(t.copy, at + 4 * lane, p[b]);
-      }
-      if constexpr (BITS == 32) {
-        store4<GD_DTYPE_FP32>(t.m, at + 4 * lane, m[b]);
-        store4<GD_DTYPE_FP32>(t.v, at + 4 * lane, v[b]);
-      } else {
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.m) + at + 4 * lane), mc[b]);
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + at + 4 * lane), vc[b]);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint64_t e = at + lane + 32 * j;
-        if (e >= n) continue;
-        store1<PT>(t.param, e, p[b][j]);
-        if (t.copy) {
-          if (s.copy_dtype == GD_DTYPE_BF16) store1<GD_DTYPE_BF16>(t.copy, e, p[b][j]);
-          else if (s.copy_dtype == GD_DTYPE_FP16) store1<GD_DTYPE_FP16>(t.copy, e, p[b][j]);
-          else store1<GD_DTYPE_FP32>(t.copy, e, p[b][j]);
-        }
-        if constexpr (BITS == 32) {
-          static_cast<float*>(t.m)[e] = m[b][j];
-          static_cast<float*>(t.v)[e] = v[b][j];
-        } else {
-          static_cast<uint8_t*>(t.m)[e] = (uint8_t)(mc[b] >> (8 * j));
-          static_cast<uint8_t*>(t.v)[e] = (uint8_t)(vc[b] >> (8 * j));
-        }
-      }
-    }
+    store_ragged<PT, BITS>(b, t, s.copy_dtype, at, lane);
   }
 }
 
 template <int PT, int GT, int BITS>
 cudaError_t launch_cap(const AdamTable<kMaxTensors>& full, uint32_t chunks, cudaStream_t stream) {
+  constexpr size_t smem = BITS == 8 ? kAdamThreads / 32 * kStages * kStageBytes : 0;
+  static_assert(smem <= 48 * 1024, "without asking for more shared memory");
   if (full.s.n_tensors <= kFewTensors) {
     AdamTable<kFewTensors> few;
     few.s = full.s;
     for (uint32_t i = 0; i < full.s.n_tensors; ++i) few.t[i] = full.t[i];
-    return launch_dependent(adamw_kernel<PT, GT, BITS, kFewTensors>, dim3(chunks), dim3(kAdamThreads), 0, stream, few);
+    return launch_dependent(adamw_kernel<PT, GT, BITS, kFewTensors>, dim3(chunks), dim3(kAdamThreads), smem, stream, few);
   }
-  return launch_dependent(adamw_kernel<PT, GT, BITS, kMaxTensors>, dim3(chunks), dim3(kAdamThreads), 0, stream, full);
+  return launch_dependent(adamw_kernel<PT, GT, BITS, kMaxTensors>, dim3(chunks), dim3(kAdamThreads), smem, stream, full);
 }
 template <int PT, int GT>
 cudaError_t launch_bits(int bits, const AdamTable<kMaxTensors>& table, uint32_t chunks, cudaStream_t stream) {
@@ -328,6 +437,7 @@ extern "C" int gd_adamw_step(const gd_adamw_args* a, void* stream) {
   s.seed = a->seed;
   s.copy_dtype = a->copy_dtype;
   s.n_tensors = 0;
+  const uint64_t chunk = eight ? kChunk<8> : kChunk<32>;
   uint64_t chunks = 0;
   auto flush = [&]() -> int {
     if (s.n_tensors == 0) return GD_OK;
@@ -339,7 +449,7 @@ extern "C" int gd_adamw_step(const gd_adamw_args* a, void* stream) {
   for (uint32_t i = 0; i < a->n_tensors; ++i) {
     const gd_adamw_tensor& t = a->tensors[i];
     if (t.n == 0) continue;
-    const uint64_t need = (t.n + kChunk - 1) / kChunk;
+    const uint64_t need = (t.n + chunk - 1) / chunk;
     if (s.n_tensors == kMaxTensors || chunks + need > 0x7FFFFFFFull) {
       const int rc = flush();
       if (rc != GD_OK) return rc;

@@ -17,6 +17,7 @@ constexpr float kNegInf = -INFINITY;
 constexpr uint32_t kRowThreads = 256;
 constexpr uint32_t kShortClasses = 1024;       // 32 lanes x 32 registers
 constexpr uint32_t kSliceBytes = 40u << 10;    // a slice this long leaves room for five CTAs on an SM: one's loads run under another's sums and stores
+constexpr uint32_t kParts = 4;                 // bulk copies a slice arrives by: the maximum is taken of one while the others are under way
 constexpr uint32_t kMaxStage = 200u << 10;     // shared memory a CTA may ask for its slice
 
 struct XentArgs {
@@ -102,55 +103,59 @@ __global__ void __launch_bounds__(kRowThreads) xent_row_kernel(const __grid_cons
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ float s_warp[kRowThreads / 32][2];
   __shared__ float2 s_pair;
-  T* held = reinterpret_cast<T*>(smem);
+  __shared__ uint64_t s_full[kParts];
   const uint32_t tid = threadIdx.x, rank = cluster > 1 ? cluster_rank() : 0u;
   const uint64_t row = blockIdx.x / cluster;
   const uint32_t c0 = min(rank * slice, a.classes), c1 = min(c0 + slice, a.classes), len = c1 - c0;
   const T* x = static_cast<const T*>(a.logits) + row * a.ld_logits + c0;
   T* out = a.grad ? static_cast<T*>(a.grad) + row * a.ld_grad + c0 : nullptr;
+  if (tid == 0) {
+    for (uint32_t p = 0; p < kParts; ++p) mbar_init(&s_full[p], 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
   pdl_wait();
   pdl_trigger();
   const int64_t target = target_of(a, row);
   const float scale = a.grad_scale_dev ? a.grad_scale * *a.grad_scale_dev : a.grad_scale;
   const float target_logit = target >= 0 ? Elem<DT>::get(static_cast<const T*>(a.logits)[row * a.ld_logits + target]) : 0.f;
 
-  // [0, head) and [body, len) element by element, [head, body) in pieces; a piece starts at an element whose address is a multiple of 16
-  const uint32_t shift = (uint32_t)((uintptr_t)x & 15u) / sizeof(T);
+  // [0, head) and [body, len) element by element, [head, body) in pieces of 16 bytes whose addresses are multiples of 16
   const bool pieces = !out || ((uintptr_t)out & 15u) == ((uintptr_t)x & 15u);
-  const uint32_t head = pieces ? min((V - shift) % V, len) : 0u;
+  const uint32_t head = pieces ? min((V - (uint32_t)((uintptr_t)x & 15u) / (uint32_t)sizeof(T)) % V, len) : 0u;
   const uint32_t n_vec = pieces ? (len - head) / V : 0u, body = pieces ? head + n_vec * V : 0u;
-  const uint32_t rest = pieces ? head + (len - body) : len;       // elements outside the pieces
-  // shared memory holds the first vectors (all of the slice, usually); elements outside the pieces are read again
-  const uint32_t kept = min(n_vec, stage / V);
-  uint4* held_vec = reinterpret_cast<uint4*>(held);
+  const uint32_t rest = pieces ? head + (len - body) : len;       // elements outside the pieces: read from memory each time
+  // shared memory holds the first `kept` pieces (all of them, usually), brought by bulk copies in kParts parts
+  const uint32_t kept = min(n_vec, stage / V), part = ((kept + kParts - 1) / kParts + 7u) & ~7u;
+  const uint4* held_vec = reinterpret_cast<const uint4*>(smem);
   const uint4* x_vec = reinterpret_cast<const uint4*>(x + head);
+  if (tid == 0) {
+    for (uint32_t p = 0; p < kParts; ++p) {
+      const uint32_t v0 = min(p * part, kept), v1 = min(v0 + part, kept);
+      mbar_arrive_expect_tx(&s_full[p], (v1 - v0) * 16u);
+      if (v1 > v0) bulk_load(smem + v0 * 16u, x_vec + v0, (v1 - v0) * 16u, &s_full[p]);
+    }
+  }
+  bool landed = true;
 
   float m = kNegInf;                             // (a NaN is passed over here and turns up in the sum)
-  {
-    constexpr int U = 4;                         // pieces in flight per thread
-    uint32_t i = tid;
-    for (; i + (U - 1) * kRowThreads < n_vec; i += U * kRowThreads) {
-      uint4 q[U];
+  for (uint32_t i = kept + tid; i < n_vec; i += kRowThreads) {
+    float f[V];
+    Vec<DT>::get(__ldcs(x_vec + i), f);
 #pragma unroll
-      for (int u = 0; u < U; ++u) q[u] = __ldcs(x_vec + i + u * kRowThreads);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i + u * kRowThreads < kept) held_vec[i + u * kRowThreads] = q[u];
-        float f[V];
-        Vec<DT>::get(q[u], f);
-#pragma unroll
-        for (uint32_t j = 0; j < V; ++j) m = fmaxf(m, f[j]);
-      }
-    }
-    for (; i < n_vec; i += kRowThreads) {
-      const uint4 q = __ldcs(x_vec + i);
-      if (i < kept) held_vec[i] = q;
+    for (uint32_t j = 0; j < V; ++j) m = fmaxf(m, f[j]);
+  }
+  for (uint32_t e = tid; e < rest; e += kRowThreads) m = fmaxf(m, Elem<DT>::get(x[e < head ? e : body + (e - head)]));
+  const int never = 0;
+  for (uint32_t p = 0; p < kParts; ++p) {
+    landed = landed && mbar_wait(&s_full[p], 0u, &never);
+    const uint32_t v1 = min((p + 1) * part, kept);
+    for (uint32_t i = p * part + tid; i < v1; i += kRowThreads) {
       float f[V];
-      Vec<DT>::get(q, f);
+      Vec<DT>::get(held_vec[i], f);
 #pragma unroll
       for (uint32_t j = 0; j < V; ++j) m = fmaxf(m, f[j]);
     }
-    for (uint32_t e = tid; e < rest; e += kRowThreads) m = fmaxf(m, Elem<DT>::get(x[e < head ? e : body + (e - head)]));
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
@@ -159,7 +164,7 @@ __global__ void __launch_bounds__(kRowThreads) xent_row_kernel(const __grid_cons
 #pragma unroll
   for (uint32_t w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, s_warp[w][0]);
 
-  float s = 0.f;
+  float s = landed ? 0.f : NAN;                  // (a copy that never came: the row's results say so)
   const float base = m == kNegInf ? 0.f : m;     // (nothing but masked classes here: every term is exp(-inf) = 0, or a NaN)
   for (uint32_t i = tid; i < n_vec; i += kRowThreads) {
     const uint4 q = i < kept ? held_vec[i] : __ldcs(x_vec + i);
