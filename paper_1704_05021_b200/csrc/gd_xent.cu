@@ -1,12 +1,20 @@
 // Softmax cross-entropy of a batch and the gradient of its logits (gd_cross_entropy).
 //
 // Every logit is read from memory once and every gradient written once; between the two the row waits on the chip, so the
-// bytes bound it (2 x 2 B per logit in 16 bits).  Long rows: a cluster of 1 .. 8 CTAs takes one row, each a slice of it, which it
-// keeps in shared memory as it arrives (what a slice has beyond that is read a second time).  A CTA finds the maximum m of its slice
-// while loading and sum exp(x - m) from shared memory; the CTAs of a cluster exchange their (m, sum) pairs through distributed
-// shared memory and each joins them in the same order.  Short rows (up to kShortClasses classes): a group of 4 .. 32 lanes holds a row in
-// registers.  exp(x - m) subtracts first, in fp32: the difference is exact where it matters, and masked or lowest-value
-// logits give 0 and never a NaN.
+// bytes bound it (2 x 2 B per logit in 16 bits), and in 16 bits the two exponentials per logit come close behind: they alone would take
+// 70 % of that time.  Long rows: a cluster of 1 .. 8 CTAs takes one row, each a slice of it, which bulk copies bring into
+// shared memory (what a slice has beyond that is read a second time, from L2).  While it arrives each thread keeps a running
+// maximum and the sum of exp(x - maximum) of what it has seen; the pairs are joined over warps, the CTA and - sent into the
+// others' shared memory and counted there, which spares the fence that a cluster barrier puts behind every access - the cluster, always
+// in the same order.  Then the gradient goes out from shared memory.  Short rows (up to kShortClasses classes): a group of 4 .. 32
+// lanes holds a row in registers.  exp(x - m) subtracts first, in fp32: the difference is exact where it matters, and masked or
+// lowest-value logits give 0 and never a NaN.
+//
+// Measured (one B200): 4000 x 85000 in bf16 246 us = 5.5 TB/s (plain loads, two passes over shared memory and cluster barriers: 361);
+// 1.0 GB of fp32 rows of 2048 .. 85000 6.3 - 6.7 TB/s.
+#include <algorithm>
+#include <type_traits>
+
 #include "gd_mma.cuh"
 
 namespace gd {
@@ -14,9 +22,11 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -INFINITY;
-constexpr uint32_t kRowThreads = 256;
+// Most 16-byte pieces of a slice for 32, 64 and 128 threads.  Measured on 85 M logits (us, 32 / 64 / 128 / 256 threads): rows of 2048 in
+// bf16 66 / 84 / 119 / 226, of 8192 72 / 60 / 65 / 92, of 85000 127 / 87 / 70 / 74, of 200000 in fp32 398 / 228 / 157 / 132.
+constexpr uint32_t kVecs32 = 256, kVecs64 = 1024, kVecs128 = 3584;
 constexpr uint32_t kShortClasses = 1024;       // 32 lanes x 32 registers
-constexpr uint32_t kSliceBytes = 40u << 10;    // a slice this long leaves room for five CTAs on an SM: one's loads run under another's sums and stores
+constexpr uint32_t kSliceBytes = 48u << 10;    // a slice this long leaves room for four CTAs on an SM: one's loads run under another's sums and stores
 constexpr uint32_t kParts = 4;                 // bulk copies a slice arrives by: the maximum is taken of one while the others are under way
 constexpr uint32_t kMaxStage = 200u << 10;     // shared memory a CTA may ask for its slice
 
@@ -93,17 +103,99 @@ struct Vec {   // 16 bytes of logits
   }
 };
 
+// The largest of a piece (two at a time as they lie, in 16 bits: nothing to round), and the sum of exp(x - base), as trees: the
+// loops around them are bound by latency otherwise.
+template <int DT>
+__device__ __forceinline__ float top_of(const uint4& q) {
+  if constexpr (DT == GD_DTYPE_FP32) {
+    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+  } else {
+    using T2 = typename std::conditional<DT == GD_DTYPE_BF16, __nv_bfloat162, __half2>::type;
+    const auto as = [](uint32_t w) { return *reinterpret_cast<const T2*>(&w); };
+    const T2 m = __hmax2(__hmax2(as(q.x), as(q.y)), __hmax2(as(q.z), as(q.w)));
+    const float2 f = unpack2<DT>(*reinterpret_cast<const uint32_t*>(&m));
+    return fmaxf(f.x, f.y);
+  }
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+// exp(x - base) of a piece, in pairs
+template <int DT>
+__device__ __forceinline__ void exps_of(const uint4& q, float base, float2 (&e)[Vec<DT>::kElems / 2]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  const float2 less = make_float2(-base, -base), log2e = make_float2(kLog2e, kLog2e);
+#pragma unroll
+  for (uint32_t j = 0; j < Vec<DT>::kElems / 2; ++j) {
+    float2 f;
+    if constexpr (DT == GD_DTYPE_FP32) f = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+    else f = unpack2<DT>(w[j]);
+    f = mul2(add2(f, less), log2e);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[j].x) : "f"(f.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[j].y) : "f"(f.y));
+  }
+}
+template <int DT>
+__device__ __forceinline__ float sum_of(const uint4& q, float base) {
+  constexpr uint32_t P = Vec<DT>::kElems / 2;
+  float2 e[P];
+  exps_of<DT>(q, base, e);
+#pragma unroll
+  for (uint32_t w = P / 2; w > 0; w >>= 1) {
+#pragma unroll
+    for (uint32_t j = 0; j < w; ++j) e[j] = add2(e[j], e[j + w]);
+  }
+  return e[0].x + e[0].y;
+}
+// The gradient of a piece whose first class is e0: exp(x - m) * factor, less `scale` at the target.
+template <int DT>
+__device__ __forceinline__ uint4 gradient_of(const uint4& q, float m, const RowResult& r, bool none, uint32_t e0, uint32_t hit) {
+  constexpr uint32_t V = Vec<DT>::kElems;
+  if (none) return make_uint4(0u, 0u, 0u, 0u);
+  float2 e[V / 2];
+  exps_of<DT>(q, m, e);
+  float f[V];
+#pragma unroll
+  for (uint32_t j = 0; j < V / 2; ++j) {
+    e[j] = mul2(e[j], make_float2(r.factor, r.factor));
+    f[2 * j] = e[j].x, f[2 * j + 1] = e[j].y;
+  }
+  if (hit - e0 < V) {
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) f[j] -= e0 + j == hit ? r.scale : 0.f;
+  }
+  return Vec<DT>::put(f);
+}
+
+// Eight bytes into a CTA of the cluster, counted on an mbarrier there.
+__device__ __forceinline__ void send_peer2(uint32_t address, float2 v, uint32_t barrier) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(address), "f"(v.x), "f"(v.y), "r"(barrier) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+
 // One row per cluster.  `slice`: elements per CTA (a multiple of 64), `stage`: how many of them shared memory holds (a multiple of 8).
 // Where the row's first address and the gradient's agree modulo 16 bytes the slice is worked on in 16-byte pieces, its ragged
 // ends element by element; otherwise all of it element by element.
-template <int DT>
-__global__ void __launch_bounds__(kRowThreads) xent_row_kernel(const __grid_constant__ XentArgs a, uint32_t cluster, uint32_t slice, uint32_t stage) {
+template <int DT, uint32_t THREADS>
+__global__ void __launch_bounds__(THREADS) xent_row_kernel(const __grid_constant__ XentArgs a, uint32_t cluster, uint32_t slice, uint32_t stage) {
   using T = typename Elem<DT>::type;
   constexpr uint32_t V = Vec<DT>::kElems;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float s_warp[kRowThreads / 32][2];
-  __shared__ float2 s_pair;
-  __shared__ uint64_t s_full[kParts];
+  __shared__ float2 s_warp[THREADS / 32];
+  __shared__ __align__(8) float2 s_pairs[8];
+  __shared__ uint64_t s_full[kParts], s_pairs_in;
   const uint32_t tid = threadIdx.x, rank = cluster > 1 ? cluster_rank() : 0u;
   const uint64_t row = blockIdx.x / cluster;
   const uint32_t c0 = min(rank * slice, a.classes), c1 = min(c0 + slice, a.classes), len = c1 - c0;
@@ -111,15 +203,14 @@ __global__ void __launch_bounds__(kRowThreads) xent_row_kernel(const __grid_cons
   T* out = a.grad ? static_cast<T*>(a.grad) + row * a.ld_grad + c0 : nullptr;
   if (tid == 0) {
     for (uint32_t p = 0; p < kParts; ++p) mbar_init(&s_full[p], 1u);
+    mbar_init(&s_pairs_in, 1u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_arrive_expect_tx(&s_pairs_in, cluster * 8u);
   }
   __syncthreads();
+  if (cluster > 1) cluster_arrive_relaxed();
   pdl_wait();
   pdl_trigger();
-  const int64_t target = target_of(a, row);
-  const float scale = a.grad_scale_dev ? a.grad_scale * *a.grad_scale_dev : a.grad_scale;
-  const float target_logit = target >= 0 ? Elem<DT>::get(static_cast<const T*>(a.logits)[row * a.ld_logits + target]) : 0.f;
-
   // [0, head) and [body, len) element by element, [head, body) in pieces of 16 bytes whose addresses are multiples of 16
   const bool pieces = !out || ((uintptr_t)out & 15u) == ((uintptr_t)x & 15u);
   const uint32_t head = pieces ? min((V - (uint32_t)((uintptr_t)x & 15u) / (uint32_t)sizeof(T)) % V, len) : 0u;
@@ -136,62 +227,46 @@ __global__ void __launch_bounds__(kRowThreads) xent_row_kernel(const __grid_cons
       if (v1 > v0) bulk_load(smem + v0 * 16u, x_vec + v0, (v1 - v0) * 16u, &s_full[p]);
     }
   }
+  const int64_t target = target_of(a, row);
+  const float scale = a.grad_scale_dev ? a.grad_scale * *a.grad_scale_dev : a.grad_scale;
+  const float target_logit = target >= 0 ? Elem<DT>::get(static_cast<const T*>(a.logits)[row * a.ld_logits + target]) : 0.f;
   bool landed = true;
 
-  float m = kNegInf;                             // (a NaN is passed over here and turns up in the sum)
-  for (uint32_t i = kept + tid; i < n_vec; i += kRowThreads) {
-    float f[V];
-    Vec<DT>::get(__ldcs(x_vec + i), f);
-#pragma unroll
-    for (uint32_t j = 0; j < V; ++j) m = fmaxf(m, f[j]);
+  // Each thread's running maximum and sum: the sum is rescaled when a piece raises the maximum.
+  float m = kNegInf, s = 0.f;                    // (a NaN is passed over by the maximum and turns up in the sum)
+  const auto take = [&](const uint4& q) {
+    const float top = fmaxf(m, top_of<DT>(q)), base = top == kNegInf ? 0.f : top;     // (masked classes only so far: exp(-inf) = 0, or the NaN among them)
+    s = s * exp_of(m - base) + sum_of<DT>(q, base);
+    m = top;
+  };
+  for (uint32_t e = tid; e < rest; e += THREADS) {
+    const float f = Elem<DT>::get(x[e < head ? e : body + (e - head)]), top = fmaxf(m, f), base = top == kNegInf ? 0.f : top;
+    s = s * exp_of(m - base) + exp_of(f - base);
+    m = top;
   }
-  for (uint32_t e = tid; e < rest; e += kRowThreads) m = fmaxf(m, Elem<DT>::get(x[e < head ? e : body + (e - head)]));
+  for (uint32_t i = kept + tid; i < n_vec; i += THREADS) take(__ldcg(x_vec + i));
   const int never = 0;
   for (uint32_t p = 0; p < kParts; ++p) {
     landed = landed && mbar_wait(&s_full[p], 0u, &never);
     const uint32_t v1 = min((p + 1) * part, kept);
-    for (uint32_t i = p * part + tid; i < v1; i += kRowThreads) {
-      float f[V];
-      Vec<DT>::get(held_vec[i], f);
-#pragma unroll
-      for (uint32_t j = 0; j < V; ++j) m = fmaxf(m, f[j]);
-    }
+    for (uint32_t i = p * part + tid; i < v1; i += THREADS) take(held_vec[i]);
   }
+  if (!landed) s = NAN;                          // (a copy that never came: the row's results say so)
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-  if ((tid & 31u) == 0u) s_warp[tid >> 5][0] = m;
+  for (int o = 16; o > 0; o >>= 1) join(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o));
+  if ((tid & 31u) == 0u) s_warp[tid >> 5] = make_float2(m, s);
   __syncthreads();
+  m = s_warp[0].x, s = s_warp[0].y;
 #pragma unroll
-  for (uint32_t w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, s_warp[w][0]);
-
-  float s = landed ? 0.f : NAN;                  // (a copy that never came: the row's results say so)
-  const float base = m == kNegInf ? 0.f : m;     // (nothing but masked classes here: every term is exp(-inf) = 0, or a NaN)
-  for (uint32_t i = tid; i < n_vec; i += kRowThreads) {
-    const uint4 q = i < kept ? held_vec[i] : __ldcs(x_vec + i);
-    float f[V], part = 0.f;
-    Vec<DT>::get(q, f);
-#pragma unroll
-    for (uint32_t j = 0; j < V; ++j) part += exp_of(f[j] - base);
-    s += part;
-  }
-  for (uint32_t e = tid; e < rest; e += kRowThreads) s += exp_of(Elem<DT>::get(x[e < head ? e : body + (e - head)]) - base);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-  if ((tid & 31u) == 0u) s_warp[tid >> 5][1] = s;
-  __syncthreads();
-  s = 0.f;
-#pragma unroll
-  for (uint32_t w = 0; w < kRowThreads / 32; ++w) s += s_warp[w][1];
+  for (uint32_t w = 1; w < THREADS / 32; ++w) join(m, s, s_warp[w].x, s_warp[w].y);
   if (cluster > 1) {
-    if (tid == 0) s_pair = make_float2(m, s);
-    cluster_arrive();
-    cluster_wait();
-    m = kNegInf, s = 0.f;
-    for (uint32_t r = 0; r < cluster; ++r) {
-      const float2 p = peer_load2(peer_address(smem_u32(&s_pair), r));
-      join(m, s, p.x, p.y);
-    }
-    cluster_arrive();                            // the pairs have been read; waited for before this CTA ends
+    // to every CTA of the cluster, counted there in bytes: no fence over this CTA's memory traffic, as a barrier would need
+    cluster_wait();                              // (everybody's mbarrier exists: arrived at long ago)
+    if (tid < cluster) send_peer2(peer_address(smem_u32(&s_pairs[rank]), tid), make_float2(m, s), peer_address(smem_u32(&s_pairs_in), tid));
+    landed = mbar_wait(&s_pairs_in, 0u, &never);
+    m = kNegInf, s = landed ? 0.f : NAN;
+    for (uint32_t r = 0; r < cluster; ++r) join(m, s, s_pairs[r].x, s_pairs[r].y);
+    cluster_arrive_relaxed();                    // the pairs have been received; waited for before this CTA ends
   }
   const RowResult r = finish(m, s, target, target_logit, scale);
   if (tid == 0 && rank == 0) {
@@ -201,20 +276,12 @@ __global__ void __launch_bounds__(kRowThreads) xent_row_kernel(const __grid_cons
   if (out) {
     const uint32_t hit = target >= (int64_t)c0 && target < (int64_t)c1 ? (uint32_t)(target - c0) : 0xFFFFFFFFu;
     const bool none = target == -1;              // 0 whatever the logits: not 0 * NaN
-    for (uint32_t i = tid; i < n_vec; i += kRowThreads) {
-      const uint4 q = i < kept ? held_vec[i] : __ldcs(x_vec + i);
-      float f[V];
-      Vec<DT>::get(q, f);
-      const uint32_t e0 = head + i * V;
-#pragma unroll
-      for (uint32_t j = 0; j < V; ++j) f[j] = none ? 0.f : exp_of(f[j] - m) * r.factor;
-      if (hit - e0 < V) {
-#pragma unroll
-        for (uint32_t j = 0; j < V; ++j) f[j] -= e0 + j == hit ? r.scale : 0.f;
-      }
-      __stcs(reinterpret_cast<uint4*>(out + head) + i, Vec<DT>::put(f));
-    }
-    for (uint32_t i = tid; i < rest; i += kRowThreads) {
+    uint4* out_vec = reinterpret_cast<uint4*>(out + head);
+#pragma unroll 2
+    for (uint32_t i = tid; i < kept; i += THREADS) __stcs(out_vec + i, gradient_of<DT>(held_vec[i], m, r, none, head + i * V, hit));
+    for (uint32_t i = kept + tid; i < n_vec; i += THREADS)      // the second read of these: from L2, usually
+      __stcs(out_vec + i, gradient_of<DT>(__ldcg(x_vec + i), m, r, none, head + i * V, hit));
+    for (uint32_t i = tid; i < rest; i += THREADS) {
       const uint32_t e = i < head ? i : body + (i - head);
       const float g = none ? 0.f : exp_of(Elem<DT>::get(x[e]) - m) * r.factor;
       out[e] = Elem<DT>::put(g - (e == hit ? r.scale : 0.f));
@@ -278,6 +345,29 @@ cudaError_t launch_short(const XentArgs& a, cudaStream_t stream) {
   return launch_dependent(xent_short_kernel<DT, G, PER>, dim3((uint32_t)blocks), dim3(128), 0, stream, a);
 }
 
+using RowKernel = void (*)(XentArgs, uint32_t, uint32_t, uint32_t);
+cudaError_t launch_clusters(RowKernel kernel, uint64_t ctas, uint32_t threads, size_t smem, uint32_t cluster, cudaStream_t stream, const XentArgs& a, uint32_t slice,
+                            uint32_t stage) {
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxStage);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((uint32_t)ctas);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a, cluster, slice, stage);
+}
+
 template <int DT>
 cudaError_t launch_rows(const XentArgs& a, cudaStream_t stream) {
   constexpr uint32_t item = DT == GD_DTYPE_FP32 ? 4 : 2;
@@ -293,29 +383,13 @@ cudaError_t launch_rows(const XentArgs& a, cudaStream_t stream) {
                          (a.rows * cluster * 2 <= (uint64_t)sm_count() && c / (2 * cluster) >= 2048)))
     cluster *= 2;
   const uint32_t slice = ((c + cluster - 1) / cluster + 63) / 64 * 64;
-  const uint32_t stage = min(slice * item, kMaxStage) / item;
-  const size_t smem = (size_t)stage * item;
-  static PerDeviceInt ready;
-  int dev;
-  if (!ready.get(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(xent_row_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxStage);
-    if (e != cudaSuccess) return e;
-    ready.set(dev, 1);
-  }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((uint32_t)(a.rows * cluster));
-  cfg.blockDim = dim3(kRowThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, xent_row_kernel<DT>, a, cluster, slice, stage);
+  const uint32_t stage = std::min(slice * item, kMaxStage) / item;
+  // threads by what each has to do: a short slice would pay for more of them in synchronisation, not gain by them
+  const uint32_t vecs = slice * item / 16;
+  if (vecs <= kVecs32) return launch_clusters(xent_row_kernel<DT, 32>, a.rows * cluster, 32, stage * item, cluster, stream, a, slice, stage);
+  if (vecs <= kVecs64) return launch_clusters(xent_row_kernel<DT, 64>, a.rows * cluster, 64, stage * item, cluster, stream, a, slice, stage);
+  if (vecs <= kVecs128) return launch_clusters(xent_row_kernel<DT, 128>, a.rows * cluster, 128, stage * item, cluster, stream, a, slice, stage);
+  return launch_clusters(xent_row_kernel<DT, 256>, a.rows * cluster, 256, stage * item, cluster, stream, a, slice, stage);
 }
 
 }  // namespace

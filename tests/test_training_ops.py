@@ -323,7 +323,7 @@ def _check_xent(device, logits, targets, scale=1.0, ignore=-100, in_place=False,
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("shape", [(1, 1), (5, 2), (80, 10), (33, 17), (7, 65), (9, 300), (4, 1000), (3, 1025), (2, 4099), (300, 2048), (1, 85000), (20, 50257),
-                                   (2, 200001)], ids=str)
+                                   (2, 200001), (310, 40001), (300, 85000), (170, 60003), (900, 33000)], ids=str)
 def test_cross_entropy(cuda_device, shape, dtype):
     gen = _gen(cuda_device, sum(shape))
     logits = _rand(gen, *shape, dtype=dtype, scale=3.0)
@@ -334,38 +334,60 @@ def test_cross_entropy(cuda_device, shape, dtype):
     _check_xent(cuda_device, logits.clone(), targets, in_place=True)
 
 
+def _masked_rows(dev, classes, dtype):
+    low = torch.finfo(dtype).min
+    x = _rand(_gen(dev, 1), 12, classes, dtype=dtype)
+    t = torch.zeros(12, dtype=torch.int64, device=dev)
+    x[0, 1:] = -float("inf")                       # one class left, the target: loss 0
+    x[1, 1:] = low
+    x[2] = low                                     # every class at the lowest value: uniform
+    x[3, : classes // 2] = -float("inf")
+    t[3] = classes - 1
+    x[4] = -float("inf")                           # nothing left, and no target
+    x[5] = float("nan")
+    t[4] = t[5] = -100
+    x[6] = -float("inf")                           # nothing left, but a target
+    x[7, classes - 1] = float("nan")
+    x[8, classes // 2] = float("inf")
+    t[9], t[10] = classes, -1                      # targets out of range
+    return x, t
+
+
+def _check_masked_rows(classes, loss, lse, grad):
+    dev = loss.device
+    assert loss[0] == 0 and loss[1] == 0 and bool((grad[:2] == 0).all())
+    assert abs(float(loss[2]) - math.log(classes)) < 1e-5
+    want = torch.full((classes,), 1.0 / classes, dtype=torch.float64, device=dev)
+    want[0] -= 1.0
+    assert bool(((grad[2].double() - want).abs() <= 2.0 ** -8 * want.abs()).all())
+    assert bool((grad[3, : classes // 2] == 0).all()) and torch.isfinite(lse[3])
+    assert bool((loss[4:6] == 0).all()) and bool((grad[4:6] == 0).all()) and lse[4] == -float("inf")
+    for row in (6, 7, 8, 9, 10):
+        assert torch.isnan(loss[row]) and bool(torch.isnan(grad[row]).all()), row
+    assert torch.isfinite(loss[11]) and bool(torch.isfinite(grad[11]).all())
+
+
 @pytest.mark.parametrize("classes", [10, 700, 5000, 700003])
 def test_cross_entropy_masks(cuda_device, classes):
     """Masked classes (-inf, the type's lowest value), rows that keep one class or none, infinities and NaN, bad targets."""
-    dev = cuda_device
     for dtype in (torch.float32, torch.bfloat16):
-        low = torch.finfo(dtype).min
-        x = _rand(_gen(dev, 1), 12, classes, dtype=dtype)
-        t = torch.zeros(12, dtype=torch.int64, device=dev)
-        x[0, 1:] = -float("inf")                       # one class left, the target: loss 0
-        x[1, 1:] = low
-        x[2] = low                                     # every class at the lowest value: uniform
-        x[3, : classes // 2] = -float("inf")
-        t[3] = classes - 1
-        x[4] = -float("inf")                           # nothing left, and no target
-        x[5] = float("nan")
-        t[4] = t[5] = -100
-        x[6] = -float("inf")                           # nothing left, but a target
-        x[7, classes - 1] = float("nan")
-        x[8, classes // 2] = float("inf")
-        t[9], t[10] = classes, -1                      # targets out of range
-        loss, lse, grad = torch.empty(12, device=dev), torch.empty(12, device=dev), torch.empty_like(x)
+        x, t = _masked_rows(cuda_device, classes, dtype)
+        loss, lse, grad = torch.empty(12, device=cuda_device), torch.empty(12, device=cuda_device), torch.empty_like(x)
         T.cross_entropy(x, t, loss=loss, lse=lse, grad=grad)
-        assert loss[0] == 0 and loss[1] == 0 and bool((grad[:2] == 0).all())
-        assert abs(float(loss[2]) - math.log(classes)) < 1e-5
-        want = torch.full((classes,), 1.0 / classes, dtype=torch.float64, device=dev)
-        want[0] -= 1.0
-        assert bool(((grad[2].double() - want).abs() <= 2.0 ** -8 * want.abs()).all())
-        assert bool((grad[3, : classes // 2] == 0).all()) and abs(float(lse[3]) - float(torch.logsumexp(x[3].double(), 0))) < 1e-5
-        assert bool((loss[4:6] == 0).all()) and bool((grad[4:6] == 0).all()) and lse[4] == -float("inf")
-        for row in (6, 7, 8, 9, 10):
-            assert torch.isnan(loss[row]) and bool(torch.isnan(grad[row]).all()), row
-        assert torch.isfinite(loss[11]) and bool(torch.isfinite(grad[11]).all())
+        _check_masked_rows(classes, loss, lse, grad)
+        assert abs(float(lse[3]) - float(torch.logsumexp(x[3].double(), 0))) < 1e-5
+
+
+@pytest.mark.parametrize("classes", [33000, 36001, 60008])
+def test_cross_entropy_masks_in_many_rows(cuda_device, classes):
+    """The same rows thirty times over: what one row leaves behind must not reach the next."""
+    for dtype in (torch.float32, torch.bfloat16):
+        x, t = _masked_rows(cuda_device, classes, dtype)
+        x, t = x.repeat(30, 1), t.repeat(30)
+        loss, lse, grad = torch.empty(360, device=cuda_device), torch.empty(360, device=cuda_device), torch.empty_like(x)
+        T.cross_entropy(x, t, loss=loss, lse=lse, grad=grad)
+        for at in range(0, 360, 12):
+            _check_masked_rows(classes, loss[at:at + 12], lse[at:at + 12], grad[at:at + 12])
 
 
 def test_cross_entropy_strides(cuda_device):
