@@ -22,7 +22,7 @@ double cost_product_pair(const Product& p) {
 
 // Tiled-copy map of an operand.  The encoder is the driver's; it is asked for through the runtime, so that the library does not link
 // against libcuda and loads on a machine without a GPU.
-bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_t depth, uint32_t box_extent, bool bf16) {
+bool encode_tile(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t width, uint64_t height, uint32_t box_width, uint32_t box_height, int dtype) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   static std::atomic<void*> found{nullptr};
@@ -33,12 +33,20 @@ bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_
       return false;
     found.store(f, std::memory_order_release);
   }
-  const cuuint64_t dims[2] = {o.mn_major ? extent : depth, o.mn_major ? depth : extent};
-  const cuuint64_t strides[1] = {o.ld * 2};
-  const cuuint32_t box[2] = {64, box_extent}, steps[2] = {1, 1};
-  return reinterpret_cast<Encode>(f)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(o.p), dims, strides,
-                                     box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[2] = {width, height}, strides[1] = {row_bytes};
+  const cuuint32_t box[2] = {box_width, box_height}, steps[2] = {1, 1};
+  const CUtensorMapDataType type = dtype == GD_DTYPE_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == GD_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                            : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return reinterpret_cast<Encode>(f)(map, type, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_t depth, uint32_t box_extent, bool bf16) {
+  return encode_tile(map, o.p, o.ld * 2, o.mn_major ? extent : depth, o.mn_major ? depth : extent, 64, box_extent, bf16 ? GD_DTYPE_BF16 : GD_DTYPE_FP16);
+}
+bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, int dtype) {
+  const uint64_t item = dtype == GD_DTYPE_FP32 ? 4 : 2;
+  return encode_tile(map, p, (ep.rows > 1 ? ld : (ep.cols + 7) / 8 * 8) * item, ep.cols, ep.rows, (uint32_t)(128 / item), 32, dtype);
 }
 
 cudaError_t launch_product(const Product& p, cudaStream_t stream) {

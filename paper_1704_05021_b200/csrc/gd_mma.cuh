@@ -216,6 +216,13 @@ __device__ __forceinline__ void activate8(float (&v)[8], int act) {
     for (int j = 0; j < 8; ++j) v[j] = silu(v[j]);
   }
 }
+// One element of the output, z = D + bias given.
+__device__ __forceinline__ void finish1(const Epilogue& e, uint32_t r, uint32_t c, float z) {
+  if (e.pre) store_as(e.pre, (uint64_t)r * e.ld_pre + c, e.dtype, z);
+  z = activate(z, e.activation);
+  if (e.add) z += load_as(e.add, (uint64_t)r * e.ld_add + c, e.add_dtype);
+  store_as(e.out, (uint64_t)r * e.ld_out + c, e.out_dtype, z);
+}
 // Eight neighbours of one output row, c a multiple of 8.
 __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t c, float (&v)[8]) {
   if (r >= e.rows || c >= e.cols) return;
@@ -240,12 +247,7 @@ __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t 
 #pragma unroll
   for (uint32_t j = 0; j < 8; ++j) {
     if (c + j >= e.cols) break;
-    float z = v[j];
-    if (e.bias) z += load_as(e.bias, c + j, e.bias_dtype);
-    if (e.pre) store_as(e.pre, (uint64_t)r * e.ld_pre + c + j, e.dtype, z);
-    z = activate(z, e.activation);
-    if (e.add) z += load_as(e.add, (uint64_t)r * e.ld_add + c + j, e.add_dtype);
-    store_as(e.out, (uint64_t)r * e.ld_out + c + j, e.out_dtype, z);
+    finish1(e, r, c + j, e.bias ? v[j] + load_as(e.bias, c + j, e.bias_dtype) : v[j]);
   }
 }
 
@@ -270,6 +272,7 @@ struct Product {
 constexpr uint32_t kChainBlocks = 512 / kBlockK;
 inline uint32_t chain_blocks(const Product& p) { return p.ep.out_dtype == GD_DTYPE_FP32 ? kChainBlocks : 0x7FFFFFFFu; }
 bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_t depth, uint32_t box_extent, bool bf16);
+bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, int dtype);     // 32 rows x 128 bytes of a result
 cudaError_t launch_product(const Product& p, cudaStream_t stream);
 
 }  // namespace gd

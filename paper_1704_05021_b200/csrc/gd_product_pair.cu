@@ -1,12 +1,13 @@
 // The product for outputs of many tiles: pairs of CTAs on 256 x 256 tiles, one persistent pair per two SMs.
 //
-// Bound by the tensor cores, if they are fed.  A 128 x 256 x 64 block takes an SM 512 cycles; the pair's instruction
-// (cta_group::2) lets each SM bring only its own half of A and of B, 32 KB, so an SM draws 64 bytes per cycle from L2 where a tile of
-// its own of that size would draw 96, and 128 x 128 tiles 128.  Ten warps: one thread asks for the copies (kStages blocks deep),
-// one thread of the leading CTA issues the products for both, eight warps take finished sums out of tensor memory into registers, 128
-// columns of 32 lanes each, hand the tensor memory back at once and finish the tile while the next one is summed into the other
-// half of it: 2 x 256 columns, all there are.  On its way out a piece of 32 x 32 passes through shared memory so that a warp's
-// accesses to bias, residual and results run along rows, 64 bytes of 8 rows each.
+// Bound by the tensor cores, if they are fed, and by the power the GPU may draw.  A 128 x 256 x 64 block takes an SM 512 cycles; the
+// pair's instruction (cta_group::2) lets each SM bring only its own half of A and of B, 32 KB, so an SM draws 64 bytes per cycle
+// from L2 where a tile of its own of that size would draw 96, and 128 x 128 tiles 128.  Ten warps: one thread asks for the copies
+// (kPairStages blocks deep), one thread of the leading CTA issues the products for both, eight warps take finished sums out of tensor
+// memory, 128 columns of 32 lanes each, and finish the tile while the next one is summed into the other half of it: 2 x 256
+// columns, all there are.  A lane holds a row, so results leave through shared memory: a piece of 32 rows x 128 bytes per warp, two of
+// them in turn, stored by the copy engine, which cuts what lies outside the matrix and takes any row pitch that is a multiple of 16 bytes; the
+// residual comes in the same way, into the piece the result is then written over.  Other pitches: element by element, a row at a time.
 //
 // Tiles are taken in groups of kGroup tile rows, column by column, so that what the pairs read at one time stays in L2.
 #include <algorithm>
@@ -19,15 +20,16 @@ namespace {
 
 constexpr uint32_t kPairWarps = 8;                            // that finish tiles
 constexpr uint32_t kPairThreads = (kPairWarps + 2) * 32;
-constexpr uint32_t kPairStages = 6;
+constexpr uint32_t kPairStages = 5;
 constexpr uint32_t kHalfBlock = 128 * kBlockK * 2;            // one CTA's half of a block of A or of B
 constexpr uint32_t kPairStage = 2 * kHalfBlock;
-constexpr uint32_t kPieceBytes = 32 * 32 * 4;
-constexpr uint32_t kPairBytes = kPairStages * kPairStage + kPairWarps * kPieceBytes + 1024;
+constexpr uint32_t kPieceBytes = 32 * 128;                  // rows x bytes of a piece
+constexpr uint32_t kPairBytes = kPairStages * kPairStage + kPairWarps * 2 * kPieceBytes + 1024;
 constexpr uint32_t kGroup = 8;
 
 struct PairArgs {
   CUtensorMap a, b;
+  CUtensorMap out, pre, add;      // pieces of the results and of the residual (TILED)
   Epilogue ep;
   int* status;
   uint32_t blocks_k, chain, desc;
@@ -47,6 +49,14 @@ __device__ __forceinline__ void mbar_arrive_peer(uint32_t address) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
 }
 
+__device__ __forceinline__ void tile_store(const CUtensorMap* map, const void* src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(smem_u32(src)) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <int LEFT>
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }   // all but LEFT have left shared memory
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // first row and column tile of the t-th tile: groups of kGroup tile rows, within a group column by column
 __device__ __forceinline__ void tile_place(uint32_t t, uint32_t tiles_r, uint32_t tiles_c, uint32_t* r, uint32_t* c) {
   const uint32_t in_group = kGroup * tiles_c, group = t / in_group, rest = t % in_group;
@@ -56,10 +66,11 @@ __device__ __forceinline__ void tile_place(uint32_t t, uint32_t tiles_r, uint32_
 }
 
 // CHAINED: a tile's sum is made of several (fp32 results), joined in registers; otherwise it goes from tensor memory straight out.
-template <bool A_MN, bool B_MN, bool CHAINED>
+// TILED: results and residual go through the copy engine.  WIDE: the results are fp32.
+template <bool A_MN, bool B_MN, bool CHAINED, bool TILED, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) product_pair_kernel(const __grid_constant__ PairArgs g) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t full[kPairStages], empty[kPairStages], sum_full[2], sum_empty[2];
+  __shared__ uint64_t full[kPairStages], empty[kPairStages], sum_full[2], sum_empty[2], add_full[kPairWarps][2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -69,6 +80,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
   if (tid == 0) {
     for (uint32_t s = 0; s < kPairStages; ++s) mbar_init(&full[s], 1u), mbar_init(&empty[s], 1u);
     for (uint32_t s = 0; s < 2; ++s) mbar_init(&sum_full[s], 1u), mbar_init(&sum_empty[s], 2 * kPairWarps);   // (the leader's: both CTAs' warps)
+    for (uint32_t w = 0; w < kPairWarps; ++w) mbar_init(&add_full[w][0], 1u), mbar_init(&add_full[w][1], 1u);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (g.blocks_k) prefetch_map(&g.a), prefetch_map(&g.b);
@@ -148,78 +160,130 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
     }
   } else {
     // warps w and w + 4 take the lanes of quarter w, 128 of the 256 columns each
+    constexpr uint32_t W = TILED && !WIDE ? 64 : 32, kPieces = 128 / W, kChunk = WIDE ? 4 : 8;     // columns of a piece, of 16 bytes of it
     const uint32_t quarter = warp & 3u, half = (warp >> 2) * 128u;
-    float* piece = reinterpret_cast<float*>(smem + kPairStages * kPairStage) + warp * (kPieceBytes / 4);
-    uint32_t chain = 0;
+    unsigned char* pieces = smem + kPairStages * kPairStage + warp * 2 * kPieceBytes;
+    const Epilogue& ep = g.ep;
+    uint32_t chain = 0, add_phase = 0;
     for (uint32_t t = pair; good && t < tiles; t += pairs) {
       uint32_t tr, tc;
       tile_place(t, g.tiles_r, g.tiles_c, &tr, &tc);
       const uint32_t r0 = tr * 256u + rank * 128u + quarter * 32u, c0 = tc * 256u + half;
-      // A piece of 32 x 32: each lane puts its row into shared memory, then the warp works along the rows.  A row's 16-byte chunks are
-      // XORed with the row's number, so that neither the lanes' rows nor the rows' neighbours meet in a bank.
-      const auto put = [&](const float* w) {
-        __syncwarp();
-#pragma unroll
-        for (uint32_t c = 0; c < 8; ++c)
-          *reinterpret_cast<float4*>(piece + lane * 32u + (c ^ (lane & 7u)) * 4u) = make_float4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
-        __syncwarp();
-      };
-      const auto get8 = [&](uint32_t r, float (&o)[8]) {   // the lane's eight columns of row r
-        const uint32_t c = (lane & 3u) * 2u;
-        const float4 x = *reinterpret_cast<const float4*>(piece + r * 32u + (c ^ (r & 7u)) * 4u), y = *reinterpret_cast<const float4*>(piece + r * 32u + ((c + 1u) ^ (r & 7u)) * 4u);
-        o[0] = x.x, o[1] = x.y, o[2] = x.z, o[3] = x.w, o[4] = y.x, o[5] = y.y, o[6] = y.z, o[7] = y.w;
-      };
-      // what the epilogue reads is asked for before the sum is there: a lane's eight columns of the bias, its rows of the residual
-      const bool fast = g.ep.vectors && r0 + 32 <= g.ep.rows && c0 + 128 <= g.ep.cols, add16 = g.ep.add && g.ep.add_dtype != GD_DTYPE_FP32;
-      const uint32_t lr = lane >> 2, lc = (lane & 3u) * 8u;
-      float bias[8];
-      uint4 add[4];
-      const auto fetch = [&](uint32_t q) {
-        if (!fast) return;
-        if (g.ep.bias) load8_as(g.ep.bias, c0 + 32 * q + lc, g.ep.bias_dtype, bias);
-        if (add16) {
-#pragma unroll
-          for (uint32_t u = 0; u < 4; ++u)
-            add[u] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(g.ep.add) + (uint64_t)(r0 + u * 8 + lr) * g.ep.ld_add + c0 + 32 * q + lc);
-        }
-      };
-      const auto finish = [&](uint32_t q) {
-        const uint32_t c = c0 + 32 * q + lc;
-        if (!fast) {
-#pragma unroll 1
-          for (uint32_t u = 0; u < 4; ++u) {
-            float o[8];
-            get8(u * 8 + lr, o);
-            finish8(g.ep, r0 + u * 8 + lr, c, o);
-          }
-          return;
-        }
-#pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) {
-          const uint64_t r = r0 + u * 8 + lr;
-          float o[8];
-          get8(u * 8 + lr, o);
-          if (g.ep.bias) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] += bias[j];
-          }
-          if (g.ep.pre) store8_as(g.ep.pre, r * g.ep.ld_pre + c, g.ep.dtype, o);
-          activate8(o, g.ep.activation);
-          if (g.ep.add) {
-            float w[8];
-            if (add16) widen8(add[u], g.ep.add_dtype, w); else load8_as(g.ep.add, r * g.ep.ld_add + c, GD_DTYPE_FP32, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] += w[j];
-          }
-          store8_as(g.ep.out, r * g.ep.ld_out + c, g.ep.out_dtype, o);
-        }
-      };
+      const uint32_t from = tmem + (quarter * 32u << 16) + half;
       const auto release = [&](uint32_t buf) {       // this warp has read its part of the sum
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_peer(peer_address(smem_u32(&sum_empty[buf]), 0));
       };
-      const uint32_t from = tmem + (quarter * 32u << 16) + half;
+      // Lane l holds the bias of columns 4 l .. 4 l + 3; asked for before the sum is there.
+      float bias[4] = {0.f, 0.f, 0.f, 0.f};
+      if (TILED && ep.bias) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+          if (c0 + 4 * lane + i < ep.cols) bias[i] = load_as(ep.bias, c0 + 4 * lane + i, ep.bias_dtype);
+      }
+      // The residual of piece p, into the buffer whose place the result takes (buffer 0 alone where z also needs one).
+      const auto ask_add = [&](uint32_t p) {
+        const uint32_t at = ep.pre ? 0u : p & 1u;
+        mbar_arrive_expect_tx(&add_full[warp][at], kPieceBytes);
+        tile_load(pieces + at * kPieceBytes, &g.add, (int32_t)(c0 + p * W), (int32_t)r0, &add_full[warp][at]);
+      };
+      // v: the lane's row of piece p
+      const auto finish = [&](uint32_t p, float* v) {
+        const uint32_t c = c0 + p * W;
+        if constexpr (TILED) {
+          const bool inside = r0 < ep.rows && c < ep.cols;
+          const uint32_t at = ep.pre ? 0u : p & 1u;
+          unsigned char* mine = pieces + at * kPieceBytes + lane * 128u;
+          unsigned char* z = pieces + kPieceBytes + lane * 128u;
+          if (!ep.add || ep.pre) {                   // (with a residual the buffer was free before its copy was asked for)
+            if (lane == 0) { if (ep.pre) stores_read<0>(); else stores_read<1>(); }
+            __syncwarp();
+          }
+          if (ep.bias) {
+#pragma unroll
+            for (uint32_t j = 0; j < W; ++j) v[j] += __shfl_sync(0xFFFFFFFFu, bias[j & 3u], (p * W + j) >> 2);
+          }
+          if constexpr (!WIDE) {
+            if (ep.pre) {
+#pragma unroll
+              for (uint32_t j = 0; j < 8; ++j) {
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = v[8 * j + i];
+                store8_as(z + (j ^ (lane & 7u)) * 16u, 0, ep.dtype, o);
+              }
+              fence_async();
+              __syncwarp();
+              if (lane == 0 && inside) tile_store(&g.pre, pieces + kPieceBytes, (int32_t)c, (int32_t)r0);
+            }
+          }
+          if (ep.add) {
+            good = mbar_wait(&add_full[warp][at], add_phase >> at & 1u, abort) && good;
+            add_phase ^= 1u << at;
+          }
+#pragma unroll
+          for (uint32_t j = 0; j < 8; ++j) {
+            unsigned char* chunk = mine + (j ^ (lane & 7u)) * 16u;
+            if constexpr (WIDE) {
+              float o[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+              if (ep.activation != GD_ACT_NONE) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = activate(o[i], ep.activation);
+              }
+              if (ep.add) {
+                const float4 w = *reinterpret_cast<const float4*>(chunk);
+                o[0] += w.x, o[1] += w.y, o[2] += w.z, o[3] += w.w;
+              }
+              *reinterpret_cast<float4*>(chunk) = make_float4(o[0], o[1], o[2], o[3]);
+            } else {
+              float o[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] = v[8 * j + i];
+              activate8(o, ep.activation);
+              if (ep.add) {
+                float w[8];
+                load8_as(chunk, 0, ep.dtype, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] += w[i];
+              }
+              store8_as(chunk, 0, ep.dtype, o);
+            }
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (inside) tile_store(&g.out, pieces + at * kPieceBytes, (int32_t)c, (int32_t)r0);
+            if (ep.add && p + 1 < kPieces) {
+              if (ep.pre) stores_read<0>(); else stores_read<1>();
+              ask_add(p + 1);
+            }
+          }
+        } else {
+          // any pitch: a row of the piece at a time, one column per lane
+          float* piece = reinterpret_cast<float*>(pieces);
+          __syncwarp();
+#pragma unroll
+          for (uint32_t j = 0; j < 8; ++j)
+            *reinterpret_cast<float4*>(piece + lane * 32u + (j ^ (lane & 7u)) * 4u) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          __syncwarp();
+          const bool in = c + lane < ep.cols;
+          const float bias = in && ep.bias ? load_as(ep.bias, c + lane, ep.bias_dtype) : 0.f;
+          if (in) {
+#pragma unroll 4
+            for (uint32_t r = 0; r < 32; ++r) {
+              if (r0 + r >= ep.rows) break;
+              finish1(ep, r0 + r, c + lane, piece[r * 32u + ((lane >> 2) ^ (r & 7u)) * 4u + (lane & 3u)] + bias);
+            }
+          }
+        }
+      };
+      if constexpr (TILED) {
+        if (ep.add && lane == 0) {                   // the first piece's residual is under way while the sum is still being made
+          stores_read<0>();
+          ask_add(0);
+        }
+      }
       if constexpr (CHAINED) {
         float v[128];
 #pragma unroll
@@ -239,29 +303,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           }
           release(buf);
         }
-        if (!good) break;
+        if (good) {
 #pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          fetch(q);
-          put(v + 32 * q);
-          finish(q);
+          for (uint32_t p = 0; p < kPieces; ++p) finish(p, v + p * W);
         }
       } else {
         const uint32_t buf = chain & 1u;
-        fetch(0);
-        if (!mbar_wait(&sum_full[buf], (chain / 2) & 1u, abort)) { good = false; break; }
-        fence_after();
+        good = mbar_wait(&sum_full[buf], (chain / 2) & 1u, abort);
         ++chain;
+        if (good) {
+          fence_after();
 #pragma unroll 1
-        for (uint32_t q = 0; q < 4; ++q) {
-          if (q) fetch(q);
-          float v[32];
-          tmem_load32(from + buf * 256u + 32 * q, v);
-          tmem_ready();
-          if (q == 3) release(buf);
-          put(v);
-          finish(q);
+          for (uint32_t p = 0; p < kPieces; ++p) {
+            float v[W];
+#pragma unroll
+            for (uint32_t c = 0; c < W; c += 32) tmem_load32(from + buf * 256u + p * W + c, v + c);
+            tmem_ready();
+            if (p + 1 == kPieces) release(buf);
+            finish(p, v);
+          }
         }
+      }
+    }
+    if constexpr (TILED) {
+      if (lane == 0) {
+        // (a residual asked for by a tile whose sum never came still has to land)
+        const int none = 0;
+        if (!good && ep.add) (void)mbar_wait(&add_full[warp][0], add_phase & 1u, &none, 1000000ull);
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
       }
     }
     if (!good) s_abort = 1;
@@ -274,9 +343,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
   if (warp == kPairWarps) tmem_free<2>(tmem, 512);
 }
 
-template <bool A_MN, bool B_MN, bool CHAINED>
+template <bool A_MN, bool B_MN, bool CHAINED, bool TILED, bool WIDE>
 cudaError_t launch_pair(const PairArgs& g, cudaStream_t stream) {
-  auto kernel = product_pair_kernel<A_MN, B_MN, CHAINED>;
+  auto kernel = product_pair_kernel<A_MN, B_MN, CHAINED, TILED, WIDE>;
   static PerDeviceInt ready;
   int dev;
   if (!ready.get(&dev)) {
@@ -288,8 +357,13 @@ cudaError_t launch_pair(const PairArgs& g, cudaStream_t stream) {
   return launch_dependent(kernel, dim3(2 * pairs), dim3(kPairThreads), kPairBytes, stream, g);
 }
 template <bool A_MN, bool B_MN>
-cudaError_t launch_majors(const PairArgs& g, cudaStream_t stream) {
-  return g.chain < g.blocks_k ? launch_pair<A_MN, B_MN, true>(g, stream) : launch_pair<A_MN, B_MN, false>(g, stream);
+cudaError_t launch_majors(const PairArgs& g, bool tiled, cudaStream_t stream) {
+  const bool chained = g.chain < g.blocks_k;            // (fp32 results only)
+  if (g.ep.out_dtype == GD_DTYPE_FP32) {
+    if (tiled) return chained ? launch_pair<A_MN, B_MN, true, true, true>(g, stream) : launch_pair<A_MN, B_MN, false, true, true>(g, stream);
+    return chained ? launch_pair<A_MN, B_MN, true, false, true>(g, stream) : launch_pair<A_MN, B_MN, false, false, true>(g, stream);
+  }
+  return tiled ? launch_pair<A_MN, B_MN, false, true, false>(g, stream) : launch_pair<A_MN, B_MN, false, false, false>(g, stream);
 }
 
 }  // namespace
@@ -307,8 +381,15 @@ cudaError_t launch_product_pair(const Product& p, cudaStream_t stream) {
   g.desc = mma_desc(256, 256, p.bf16, p.a.mn_major, p.b.mn_major);
   g.tiles_r = (p.ep.rows + 255) / 256;
   g.tiles_c = (p.ep.cols + 255) / 256;
-  if (p.a.mn_major) return p.b.mn_major ? launch_majors<true, true>(g, stream) : cudaErrorInvalidValue;   // (no call has A alone transposed)
-  return p.b.mn_major ? launch_majors<false, true>(g, stream) : launch_majors<false, false>(g, stream);
+  // Results and residual as pieces of 32 rows x 128 bytes, where every row starts at a multiple of 16 bytes; a residual of another type
+  // than the results, or z next to fp32 results, does not fit a piece.
+  const bool wide = g.ep.out_dtype == GD_DTYPE_FP32;
+  const bool tiled = g.ep.vectors && !(wide && g.ep.pre) && (!g.ep.add || g.ep.add_dtype == g.ep.out_dtype);
+  if (tiled && (!encode_piece(&g.out, g.ep.out, g.ep.ld_out, g.ep, g.ep.out_dtype) || (g.ep.pre && !encode_piece(&g.pre, g.ep.pre, g.ep.ld_pre, g.ep, g.ep.dtype)) ||
+                (g.ep.add && !encode_piece(&g.add, g.ep.add, g.ep.ld_add, g.ep, g.ep.add_dtype))))
+    return cudaErrorInvalidValue;
+  if (p.a.mn_major) return p.b.mn_major ? launch_majors<true, true>(g, tiled, stream) : cudaErrorInvalidValue;   // (no call has A alone transposed)
+  return p.b.mn_major ? launch_majors<false, true>(g, tiled, stream) : launch_majors<false, false>(g, tiled, stream);
 }
 
 }  // namespace gd
