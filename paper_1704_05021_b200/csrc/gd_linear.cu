@@ -63,121 +63,188 @@ namespace {
 constexpr uint32_t kStatusBytes = 256;
 
 // ---------------------------------------------------------------- ragged operands
-// A matrix of 16-bit elements whose rows are no multiple of 16 bytes (or start anywhere), laid out with rows of ld_dst elements, a
-// multiple of 8; the columns between are zeros.  A thread makes 16 bytes of the result: bound by the bytes, read and written once.
-__global__ void __launch_bounds__(256) pack_kernel(const uint16_t* __restrict__ src, uint64_t ld, uint32_t rows, uint32_t cols, uint4* __restrict__ dst,
-                                                   uint32_t vecs) {
-  pdl_wait();
-  pdl_trigger();
-  const uint64_t total = (uint64_t)rows * vecs;
-  for (uint64_t t = (uint64_t)blockIdx.x * 256u + threadIdx.x; t < total; t += (uint64_t)gridDim.x * 256u) {
-    const uint32_t r = (uint32_t)(t / vecs), c = (uint32_t)(t % vecs) * 8u;
-    const uint16_t* s = src + r * ld + c;
-    uint32_t w[4];
-    if (c + 8 <= cols && ((uintptr_t)s & 3u) == 0) {
+// A matrix of 16-bit elements whose rows are no multiple of 16 bytes (or start anywhere), laid out with rows of 8 `vecs` elements; the
+// columns between are zeros.  A thread makes 16 bytes of the result: bound by the bytes, read and written once.
+struct Pack {
+  const uint16_t* src;
+  uint4* dst;
+  uint64_t ld;
+  uint32_t rows, cols, vecs;
+};
+struct Packs {
+  Pack p[2];
+  uint32_t count;
+};
+__device__ __forceinline__ void pack_rows(const Packs& all, uint64_t first, uint64_t step) {
+  for (uint32_t i = 0; i < all.count; ++i) {
+    const Pack& k = all.p[i];
+    const uint64_t total = (uint64_t)k.rows * k.vecs;
+    for (uint64_t t = first; t < total; t += step) {
+      const uint32_t r = (uint32_t)(t / k.vecs), c = (uint32_t)(t % k.vecs) * 8u;
+      const uint16_t* s = k.src + r * k.ld + c;
+      uint32_t w[4];
+      if (c + 8 <= k.cols && ((uintptr_t)s & 3u) == 0) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = reinterpret_cast<const uint32_t*>(s)[j];
-    } else {
+        for (int j = 0; j < 4; ++j) w[j] = reinterpret_cast<const uint32_t*>(s)[j];
+      } else {
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        const uint32_t a = c + 2 * j < cols ? s[2 * j] : 0u, b = c + 2 * j + 1 < cols ? s[2 * j + 1] : 0u;
-        w[j] = a | b << 16;
+        for (uint32_t j = 0; j < 4; ++j) {
+          const uint32_t a = c + 2 * j < k.cols ? s[2 * j] : 0u, b = c + 2 * j + 1 < k.cols ? s[2 * j + 1] : 0u;
+          w[j] = a | b << 16;
+        }
       }
+      k.dst[t] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    dst[t] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
-cudaError_t launch_pack(const void* src, uint64_t ld, uint64_t rows, uint64_t cols, void* dst, cudaStream_t stream) {
+constexpr uint32_t kPackThreads = 256;
+__global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constant__ Packs all) {
+  pdl_wait();
+  pdl_trigger();
+  pack_rows(all, (uint64_t)blockIdx.x * kPackThreads + threadIdx.x, (uint64_t)gridDim.x * kPackThreads);
+}
+uint32_t pack_ctas(const Packs& all, uint32_t threads) {
+  uint64_t most = 0;
+  for (uint32_t i = 0; i < all.count; ++i) most = std::max(most, ((uint64_t)all.p[i].rows * all.p[i].vecs + threads - 1) / threads);
+  return (uint32_t)std::min<uint64_t>(most, (uint64_t)sm_count() * 4096 / threads);
+}
+cudaError_t launch_pack(const Packs& all, cudaStream_t stream) {
+  if (all.count == 0) return cudaSuccess;
   ProfileScope ps(stream, PT_LINEAR_PACK);
-  const uint64_t vecs = (cols + 7) / 8, blocks = (rows * vecs + 255) / 256;
-  const cudaError_t e = launch_dependent(pack_kernel, dim3((uint32_t)std::min<uint64_t>(blocks, (uint64_t)sm_count() * 16)), dim3(256), 0, stream,
-                                         static_cast<const uint16_t*>(src), ld, (uint32_t)rows, (uint32_t)cols, static_cast<uint4*>(dst), (uint32_t)vecs);
+  const cudaError_t e = launch_dependent(pack_kernel, dim3(pack_ctas(all, kPackThreads)), dim3(kPackThreads), 0, stream, all);
   if (e == cudaSuccess) note_launches(1);
   return e;
 }
 
 // ---------------------------------------------------------------- dz and db
-// dz = dy * act'(pre), rounded to the operands' type, and the sums of its columns before that rounding, in one pass over dy and pre.
-// A cluster of kSlopeCtas CTAs takes 64 columns, each a share of the rows; a thread takes 8 neighbouring columns of every 32nd
-// row.  The threads' sums meet in shared memory and the CTAs' through distributed shared memory, always in the same order: no atomics,
-// no second launch.  Bound by the bytes (dy and pre read, dz written).
-constexpr uint32_t kSlopeCtas = 8, kSlopeRows = 32;
+// dz = dy * act'(pre), rounded to the operands' type, and the sums of its columns before that rounding, in one pass over dy and pre;
+// ragged operands of the products that follow are laid out by the same launch, in CTAs of their own.
+// A cluster of kSlopeCtas CTAs takes `width` columns (64, or 32 where 64 would leave SMs without a CTA), each CTA a share of the rows; a
+// thread takes 8 neighbouring columns of every so many rows.  The threads' sums meet by shuffles and in shared memory, the CTAs' are sent
+// to the first of the cluster and counted there, always in the same order: no atomics, no second launch.  Bound by the bytes (dy and
+// pre read, dz written) where there are many columns, by the 25 instructions an entry of GELU or SiLU takes where there are few.
+constexpr uint32_t kSlopeCtas = 8, kSlopeThreads = 512, kSlopeWarps = kSlopeThreads / 32, kAhead = 2;
 struct SlopeArgs {
   const void* dy;
   const void* pre;
   void* dz;            // NULL: only the sums are wanted
   float* db;           // NULL: only dz is wanted
   uint64_t ld_dy, ld_pre, ld_dz;
-  uint32_t rows, cols;
+  uint32_t rows, cols, width, ctas;      // ctas: those that take columns; the others lay out `packs`
   int32_t activation;
   uint32_t accumulate, vectors;
+  Packs packs;
 };
 template <int DT>
-__global__ void __launch_bounds__(256) slope_kernel(const __grid_constant__ SlopeArgs a) {
-  __shared__ float s_sum[kSlopeRows][64 + 1];
-  __shared__ __align__(16) float s_total[64];
+__global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_constant__ SlopeArgs a) {
+  __shared__ float s_sum[kSlopeWarps][64];
+  __shared__ __align__(8) float s_all[kSlopeCtas][64];
+  __shared__ uint64_t s_in;
+  __shared__ int s_never;
+  const uint32_t rank = cluster_rank(), tid = threadIdx.x, lane = tid & 31u, groups = a.width / 8u;      // groups: threads side by side in a row
+  const bool pack = blockIdx.x >= a.ctas;
+  if (tid == 0) {
+    s_never = 0;
+    mbar_init(&s_in, 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (rank == 0) mbar_arrive_expect_tx(&s_in, kSlopeCtas * a.width * 4u);
+  }
+  __syncthreads();
+  cluster_arrive_relaxed();
   pdl_wait();
   pdl_trigger();
-  const uint32_t rank = cluster_rank(), tid = threadIdx.x, c = blockIdx.x / kSlopeCtas * 64u + (tid & 7u) * 8u;
+  if (pack) {
+    pack_rows(a.packs, (uint64_t)(blockIdx.x - a.ctas) * kSlopeThreads + tid, (uint64_t)(gridDim.x - a.ctas) * kSlopeThreads);
+    cluster_wait();
+    cluster_arrive_relaxed();
+    cluster_wait();
+    return;
+  }
+  const uint32_t col0 = blockIdx.x / kSlopeCtas * a.width, c = col0 + tid % groups * 8u, step = kSlopeThreads / groups;
   const uint32_t per = (a.rows + kSlopeCtas - 1) / kSlopeCtas, r0 = min(rank * per, a.rows), r1 = min(r0 + per, a.rows);
   const bool whole = a.vectors && c + 8 <= a.cols;
   float sum[8] = {};
   if (c < a.cols) {
-#pragma unroll 2
-    for (uint32_t r = r0 + (tid >> 3); r < r1; r += kSlopeRows) {
+    for (uint32_t first = r0 + tid / groups; first < r1; first += kAhead * step) {
+      uint4 gq[kAhead], zq[kAhead];
       float g[8], z[8];
       if (whole) {
-        load8_as(a.dy, r * a.ld_dy + c, DT, g);
-        if (a.activation != GD_ACT_NONE) load8_as(a.pre, r * a.ld_pre + c, DT, z);
-      } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-          const bool in = c + j < a.cols;
-          g[j] = in ? load_as(a.dy, r * a.ld_dy + c + j, DT) : 0.f;
-          z[j] = in && a.activation != GD_ACT_NONE ? load_as(a.pre, r * a.ld_pre + c + j, DT) : 0.f;
+        for (uint32_t u = 0; u < kAhead; ++u) {      // these rows' loads are under way together
+          const uint64_t r = first + u * step;
+          if (r >= r1) break;
+          gq[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.dy) + r * a.ld_dy + c));
+          if (a.activation != GD_ACT_NONE) zq[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.pre) + r * a.ld_pre + c));
         }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (a.activation == GD_ACT_RELU) g[j] = z[j] > 0.f ? g[j] : 0.f * g[j];
-        else if (a.activation == GD_ACT_GELU) g[j] *= gelu_slope(z[j]);
-        else if (a.activation == GD_ACT_SILU) g[j] *= silu_slope(z[j]);
-        sum[j] += g[j];
-      }
-      // (dz's own rows are padded to a multiple of 8 with zeros, which the ragged case above made)
-      if (a.dz) store8_as(a.dz, r * a.ld_dz + c, DT, g);
-    }
-  }
-  if (!a.db) return;
+      for (uint32_t u = 0; u < kAhead; ++u) {
+        const uint64_t r = first + u * step;
+        if (r >= r1) break;
+        if (whole) {
+          widen8(gq[u], DT, g);
+          if (a.activation != GD_ACT_NONE) widen8(zq[u], DT, z);
+        } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) s_sum[tid >> 3][(tid & 7u) * 8u + j] = sum[j];
-  __syncthreads();
-  if (tid < 64) {
-    float t = 0.f;
-#pragma unroll 8
-    for (uint32_t r = 0; r < kSlopeRows; ++r) t += s_sum[r][tid];
-    s_total[tid] = t;
-  }
-  cluster_arrive();
-  cluster_wait();
-  const uint32_t col = blockIdx.x / kSlopeCtas * 64u + tid * 2u;
-  if (rank == 0 && tid < 32) {
-    float2 t = make_float2(0.f, 0.f);
-    for (uint32_t q = 0; q < kSlopeCtas; ++q) {
-      const float2 x = peer_load2(peer_address(smem_u32(s_total + 2 * tid), q));
-      t.x += x.x, t.y += x.y;
+          for (uint32_t j = 0; j < 8; ++j) {
+            const bool in = c + j < a.cols;
+            g[j] = in ? load_as(a.dy, r * a.ld_dy + c + j, DT) : 0.f;
+            z[j] = in && a.activation != GD_ACT_NONE ? load_as(a.pre, r * a.ld_pre + c + j, DT) : 0.f;
+          }
+        }
+        if (a.activation == GD_ACT_RELU) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) g[j] = z[j] > 0.f ? g[j] : 0.f * g[j];
+        } else if (a.activation == GD_ACT_GELU) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) g[j] *= gelu_slope(z[j]);
+        } else if (a.activation == GD_ACT_SILU) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) g[j] *= silu_slope(z[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += g[j];
+        // (dz's own rows are padded to a multiple of 8 with zeros, which the ragged case above made)
+        if (a.dz) store8_as(a.dz, r * a.ld_dz + c, DT, g);
+      }
     }
-    if (col < a.cols) a.db[col] = a.accumulate ? a.db[col] + t.x : t.x;
-    if (col + 1 < a.cols) a.db[col + 1] = a.accumulate ? a.db[col + 1] + t.y : t.y;
   }
-  cluster_arrive();
+  if (a.db) {
+    for (uint32_t o = groups; o < 32u; o *= 2) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += __shfl_xor_sync(0xFFFFFFFFu, sum[j], o);
+    }
+    if (lane < groups) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s_sum[tid >> 5][lane * 8u + j] = sum[j];
+    }
+    __syncthreads();
+    cluster_wait();                                  // (the first CTA's mbarrier exists)
+    if (tid < a.width / 2) {
+      float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+      for (uint32_t w = 0; w < kSlopeWarps; ++w) t.x += s_sum[w][2 * tid], t.y += s_sum[w][2 * tid + 1];
+      send_peer2(peer_address(smem_u32(&s_all[rank][2 * tid]), 0), t, peer_address(smem_u32(&s_in), 0));
+    }
+    if (rank == 0 && tid < a.width) {
+      float t = mbar_wait(&s_in, 0u, &s_never) ? 0.f : NAN;
+      for (uint32_t q = 0; q < kSlopeCtas; ++q) t += s_all[q][tid];
+      const uint32_t col = col0 + tid;
+      if (col < a.cols) a.db[col] = a.accumulate ? a.db[col] + t : t;
+    }
+  } else {
+    cluster_wait();
+  }
+  cluster_arrive_relaxed();                          // (nobody leaves while something may still be on its way to it)
   cluster_wait();
 }
-cudaError_t launch_slope(const SlopeArgs& a, int dtype, cudaStream_t stream) {
+cudaError_t launch_slope(SlopeArgs& a, int dtype, cudaStream_t stream) {
   ProfileScope ps(stream, PT_LINEAR_SLOPE);
+  a.width = (a.cols + 63) / 64 * kSlopeCtas < 2u * sm_count() ? 32 : 64;
+  a.ctas = (a.cols + a.width - 1) / a.width * kSlopeCtas;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((a.cols + 63) / 64 * kSlopeCtas);
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3(a.ctas + (pack_ctas(a.packs, kSlopeThreads) + kSlopeCtas - 1) / kSlopeCtas * kSlopeCtas);
+  cfg.blockDim = dim3(kSlopeThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -210,14 +277,14 @@ struct Workspace {
 // A leading dimension for one row is never used: a ragged one would only cause a copy.
 uint64_t row_step(uint64_t ld, uint64_t rows, uint64_t cols) { return rows > 1 ? ld : up(cols, 8); }
 
-// `p` as an operand the tiled copies can read, laid out in the workspace if need be.
-int operand(const void* p, uint64_t ld, uint64_t rows, uint64_t cols, Workspace& ws, cudaStream_t stream, Operand* o) {
+// `p` as an operand the tiled copies can read, added to what has to be laid out in the workspace if need be.
+int operand(const void* p, uint64_t ld, uint64_t rows, uint64_t cols, Workspace& ws, Packs* packs, Operand* o) {
   o->p = p;
   o->ld = row_step(ld, rows, cols);
   if (rows == 0 || cols == 0 || tiles_as_it_is(p, o->ld)) return GD_OK;
   void* q = ws.take(rows, cols);
   if (!q) return GD_ERR_WORKSPACE;
-  if (launch_pack(p, ld, rows, cols, q, stream) != cudaSuccess) return GD_ERR_CUDA;
+  packs->p[packs->count++] = Pack{static_cast<const uint16_t*>(p), static_cast<uint4*>(q), ld, (uint32_t)rows, (uint32_t)cols, (uint32_t)((cols + 7) / 8)};
   o->p = q;
   o->ld = up(cols, 8);
   return GD_OK;
@@ -247,15 +314,11 @@ int forward(const gd_linear_forward_args* a, cudaStream_t stream) {
   if (a->residual == a->y && (a->y_dtype != a->dtype || (a->m > 1 && a->ldy != a->ld_residual))) return GD_ERR_INVALID_ARG;
   if (check_workspace(a->workspace, a->workspace_bytes) != GD_OK) return GD_ERR_WORKSPACE;
   Workspace ws{(unsigned char*)a->workspace, kStatusBytes, a->workspace_bytes};
-  // (all sizes are known before anything is enqueued: a workspace that is too small is found here)
-  {
-    Workspace probe = ws;
-    if (a->k && !tiles_as_it_is(a->x, row_step(a->ldx, a->m, a->k)) && !probe.take(a->m, a->k)) return GD_ERR_WORKSPACE;
-    if (a->k && !tiles_as_it_is(a->w, row_step(a->ldw, w_rows, w_cols)) && !probe.take(w_rows, w_cols)) return GD_ERR_WORKSPACE;
-  }
+  Packs packs;
+  packs.count = 0;
   Product p;
   std::memset(&p, 0, sizeof(p));
-  if ((rc = operand(a->x, a->ldx, a->m, a->k, ws, stream, &p.a)) != GD_OK || (rc = operand(a->w, a->ldw, w_rows, w_cols, ws, stream, &p.b)) != GD_OK) return rc;
+  if ((rc = operand(a->x, a->ldx, a->m, a->k, ws, &packs, &p.a)) != GD_OK || (rc = operand(a->w, a->ldw, w_rows, w_cols, ws, &packs, &p.b)) != GD_OK) return rc;
   p.b.mn_major = in_out;
   p.depth = (uint32_t)a->k;
   p.bf16 = a->dtype == GD_DTYPE_BF16;
@@ -270,7 +333,7 @@ int forward(const gd_linear_forward_args* a, cudaStream_t stream) {
   const bool one = a->m == 1;
   e.vectors = vector_rows(e.out, one ? 8 : e.ld_out, e.out_dtype) && vector_rows(e.bias, 8, GD_DTYPE_FP32) && vector_rows(e.add, one ? 8 : e.ld_add, e.add_dtype) &&
               vector_rows(e.pre, one ? 8 : e.ld_pre, e.dtype);
-  return launch_product(p, stream) == cudaSuccess ? GD_OK : GD_ERR_CUDA;
+  return launch_pack(packs, stream) == cudaSuccess && launch_product(p, stream) == cudaSuccess ? GD_OK : GD_ERR_CUDA;
 }
 
 int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
@@ -301,11 +364,9 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     dz.p = s.dz, dz.ld = s.ld_dz;
   }
   Operand w{}, x{};
-  {
-    Workspace probe = ws;
-    if (has_dx && n && !tiles_as_it_is(a->w, row_step(a->ldw, w_rows, w_cols)) && !probe.take(w_rows, w_cols)) return GD_ERR_WORKSPACE;
-    if (has_dw && m && !tiles_as_it_is(a->x, row_step(a->ldx, m, k)) && !probe.take(m, k)) return GD_ERR_WORKSPACE;
-  }
+  s.packs.count = 0;
+  if (has_dx && n && (rc = operand(a->w, a->ldw, w_rows, w_cols, ws, &s.packs, &w)) != GD_OK) return rc;
+  if (has_dw && m && (rc = operand(a->x, a->ldx, m, k, ws, &s.packs, &x)) != GD_OK) return rc;
   if (make || has_db) {
     s.dy = a->dy, s.ld_dy = a->ld_dy;
     s.pre = a->pre, s.ld_pre = a->ld_pre;
@@ -315,6 +376,8 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     s.accumulate = add;
     s.vectors = vector_rows(a->dy, row_step(a->ld_dy, m, n), a->dtype) && (!slope || vector_rows(a->pre, row_step(a->ld_pre, m, n), a->dtype));
     if (launch_slope(s, a->dtype, stream) != cudaSuccess) return GD_ERR_CUDA;
+  } else if (launch_pack(s.packs, stream) != cudaSuccess) {
+    return GD_ERR_CUDA;
   }
   Product p;
   std::memset(&p, 0, sizeof(p));
@@ -322,7 +385,6 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
   p.status = (int*)a->workspace;
   p.ep.dtype = a->dtype;
   if (has_dx) {                       // dx = dz W^T: contraction over n
-    if (n && (rc = operand(a->w, a->ldw, w_rows, w_cols, ws, stream, &w)) != GD_OK) return rc;
     p.a = dz, p.a.mn_major = false;
     p.b = w, p.b.mn_major = !in_out;
     p.depth = (uint32_t)n;
@@ -332,7 +394,6 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     if (launch_product(p, stream) != cudaSuccess) return GD_ERR_CUDA;
   }
   if (has_dw) {                       // dw = x^T dz, or its transpose: contraction over m
-    if (m && (rc = operand(a->x, a->ldx, m, k, ws, stream, &x)) != GD_OK) return rc;
     p.a = in_out ? x : dz, p.b = in_out ? dz : x;
     p.a.mn_major = p.b.mn_major = true;
     p.depth = (uint32_t)m;

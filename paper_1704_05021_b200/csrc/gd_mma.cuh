@@ -23,6 +23,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   return r;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }   // publishes nothing
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_address(uint32_t smem_address, uint32_t rank) {
   uint32_t a;
@@ -34,10 +35,20 @@ __device__ __forceinline__ float4 peer_load4(uint32_t a) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
 }
+__device__ __forceinline__ float peer_load1(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
 __device__ __forceinline__ float2 peer_load2(uint32_t a) {
   float2 v;
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
   return v;
+}
+
+// Eight bytes into a CTA of the cluster, counted on an mbarrier there.
+__device__ __forceinline__ void send_peer2(uint32_t address, float2 v, uint32_t barrier) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(address), "f"(v.x), "f"(v.y), "r"(barrier) : "memory");
 }
 
 // ---------------------------------------------------------------- copies and products
@@ -216,12 +227,35 @@ __device__ __forceinline__ void activate8(float (&v)[8], int act) {
     for (int j = 0; j < 8; ++j) v[j] = silu(v[j]);
   }
 }
-// One element of the output, z = D + bias given.
-__device__ __forceinline__ void finish1(const Epilogue& e, uint32_t r, uint32_t c, float z) {
-  if (e.pre) store_as(e.pre, (uint64_t)r * e.ld_pre + c, e.dtype, z);
-  z = activate(z, e.activation);
-  if (e.add) z += load_as(e.add, (uint64_t)r * e.ld_add + c, e.add_dtype);
-  store_as(e.out, (uint64_t)r * e.ld_out + c, e.out_dtype, z);
+// Up to eight elements of one output column, from row r on, z = D + bias given.
+__device__ __forceinline__ void finish_column(const Epilogue& e, uint32_t r, uint32_t c, float (&z)[8], uint32_t most = 8) {
+  const uint32_t rows = min(e.rows - min(r, e.rows), most);
+  const uint64_t at = (uint64_t)r * e.ld_out + c;
+  if (e.pre) {
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u)
+      if (u < rows) store_as(e.pre, (uint64_t)(r + u) * e.ld_pre + c, e.dtype, z[u]);
+  }
+  activate8(z, e.activation);
+  if (e.add) {
+    float w[8];
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u) w[u] = u < rows ? load_as(e.add, (uint64_t)(r + u) * e.ld_add + c, e.add_dtype) : 0.f;
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u) z[u] += w[u];
+  }
+  if (e.out_dtype == GD_DTYPE_FP32) {
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u)
+      if (u < rows) static_cast<float*>(e.out)[at + u * e.ld_out] = z[u];
+  } else {
+    const bool bf16 = e.out_dtype == GD_DTYPE_BF16;
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u) {
+      const uint32_t w = bf16 ? pack2<GD_DTYPE_BF16>(z[u], 0.f) : pack2<GD_DTYPE_FP16>(z[u], 0.f);
+      if (u < rows) static_cast<uint16_t*>(e.out)[at + u * e.ld_out] = (uint16_t)w;
+    }
+  }
 }
 // Eight neighbours of one output row, c a multiple of 8.
 __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t c, float (&v)[8]) {
@@ -247,7 +281,11 @@ __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t 
 #pragma unroll
   for (uint32_t j = 0; j < 8; ++j) {
     if (c + j >= e.cols) break;
-    finish1(e, r, c + j, e.bias ? v[j] + load_as(e.bias, c + j, e.bias_dtype) : v[j]);
+    float z = e.bias ? v[j] + load_as(e.bias, c + j, e.bias_dtype) : v[j];
+    if (e.pre) store_as(e.pre, (uint64_t)r * e.ld_pre + c + j, e.dtype, z);
+    z = activate(z, e.activation);
+    if (e.add) z += load_as(e.add, (uint64_t)r * e.ld_add + c + j, e.add_dtype);
+    store_as(e.out, (uint64_t)r * e.ld_out + c + j, e.out_dtype, z);
   }
 }
 

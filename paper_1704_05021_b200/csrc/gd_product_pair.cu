@@ -269,12 +269,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           __syncwarp();
           const bool in = c + lane < ep.cols;
           const float bias = in && ep.bias ? load_as(ep.bias, c + lane, ep.bias_dtype) : 0.f;
-          if (in) {
-#pragma unroll 4
-            for (uint32_t r = 0; r < 32; ++r) {
-              if (r0 + r >= ep.rows) break;
-              finish1(ep, r0 + r, c + lane, piece[r * 32u + ((lane >> 2) ^ (r & 7u)) * 4u + (lane & 3u)] + bias);
-            }
+#pragma unroll 1
+          for (uint32_t r = 0; r < 32; r += 8) {     // (eight rows' values first: a store may not be passed by the loads behind it)
+            float o[8];
+#pragma unroll
+            for (uint32_t u = 0; u < 8; ++u) o[u] = piece[(r + u) * 32u + ((lane >> 2) ^ u) * 4u + (lane & 3u)] + bias;
+            if (in) finish_column(ep, r0 + r, c + lane, o);
           }
         }
       };

@@ -173,25 +173,53 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
   const uint32_t rows = (g.transposed ? BN : 128u) / SPLITS, vecs = (g.transposed ? 128u : BN) / 8u;
   const uint32_t pitch = g.transposed ? S::kPitchLanes : S::kPitchCols;
   const uint32_t out_r = (g.transposed ? j0 : i0) + rank * rows, out_c = g.transposed ? i0 : j0;
-  for (uint32_t t = tid; t < rows * vecs; t += kThreadsSplit) {
-    const uint32_t r = t / vecs, c = t % vecs * 8u;
-    const float* at = part + (rank * rows + r) * pitch + c;
-    float v[8];
-    if constexpr (SPLITS > 1) {
-      const uint32_t address = smem_u32(at);
+  if (g.ep.vectors) {
+    for (uint32_t t = tid; t < rows * vecs; t += kThreadsSplit) {
+      const uint32_t r = t / vecs, c = t % vecs * 8u;
+      const float* at = part + (rank * rows + r) * pitch + c;
+      float v[8];
+      if constexpr (SPLITS > 1) {
+        const uint32_t address = smem_u32(at);
 #pragma unroll
-      for (uint32_t q = 0; q < SPLITS; ++q) {
-        const uint32_t peer = peer_address(address, q);
-        const float4 x = peer_load4(peer), y = peer_load4(peer + 16);
-        const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        for (uint32_t q = 0; q < SPLITS; ++q) {
+          const uint32_t peer = peer_address(address, q);
+          const float4 x = peer_load4(peer), y = peer_load4(peer + 16);
+          const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = q == 0 ? w[j] : v[j] + w[j];
+          for (int j = 0; j < 8; ++j) v[j] = q == 0 ? w[j] : v[j] + w[j];
+        }
+      } else {
+        const float4 x = *reinterpret_cast<const float4*>(at), y = *reinterpret_cast<const float4*>(at + 4);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
       }
-    } else {
-      const float4 x = *reinterpret_cast<const float4*>(at), y = *reinterpret_cast<const float4*>(at + 4);
-      v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+      finish8(g.ep, out_r + r, out_c + c, v);
     }
-    finish8(g.ep, out_r + r, out_c + c, v);
+  } else {
+    // rows that start anywhere: a column per thread, up to eight rows of it at a time
+    const uint32_t cols = vecs * 8u, group = rows < 8u ? rows : 8u;
+    for (uint32_t t = tid; t < rows / group * cols; t += kThreadsSplit) {
+      const uint32_t r = t / cols * group, c = t % cols;
+      const float* at = part + (rank * rows + r) * pitch + c;
+      if (out_c + c >= g.ep.cols || out_r + r >= g.ep.rows) continue;
+      const float bias = g.ep.bias ? load_as(g.ep.bias, out_c + c, g.ep.bias_dtype) : 0.f;
+      float v[8];
+#pragma unroll
+      for (uint32_t u = 0; u < 8; ++u) {
+        if (u >= group) continue;
+        if constexpr (SPLITS > 1) {
+          const uint32_t address = smem_u32(at + u * pitch);
+#pragma unroll
+          for (uint32_t q = 0; q < SPLITS; ++q) {
+            const float w = peer_load1(peer_address(address, q));
+            v[u] = q == 0 ? w : v[u] + w;
+          }
+        } else {
+          v[u] = at[u * pitch];
+        }
+        v[u] += bias;
+      }
+      finish_column(g.ep, out_r + r, out_c + c, v, group);
+    }
   }
   if constexpr (SPLITS > 1) {
     cluster_arrive();                                // the others may still be reading this CTA's partial tile

@@ -179,12 +179,6 @@ __device__ __forceinline__ uint4 gradient_of(const uint4& q, float m, const RowR
   return Vec<DT>::put(f);
 }
 
-// Eight bytes into a CTA of the cluster, counted on an mbarrier there.
-__device__ __forceinline__ void send_peer2(uint32_t address, float2 v, uint32_t barrier) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(address), "f"(v.x), "f"(v.y), "r"(barrier) : "memory");
-}
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-
 // One row per cluster.  `slice`: elements per CTA (a multiple of 64), `stage`: how many of them shared memory holds (a multiple of 8).
 // Where the row's first address and the gradient's agree modulo 16 bytes the slice is worked on in 16-byte pieces, its ragged
 // ends element by element; otherwise all of it element by element.
