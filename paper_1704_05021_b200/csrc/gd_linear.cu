@@ -13,10 +13,12 @@ cudaError_t launch_product_split(const Product& p, cudaStream_t stream);
 cudaError_t launch_product_pair(const Product& p, cudaStream_t stream);
 
 namespace {
-// Estimated cycles of the pairs' kernel: 512 per k block of a 256 x 256 tile and what a tile costs besides, times the waves.
+// Estimated cycles of the pairs' kernel: 600 per k block of a 256 x 256 tile (of 512 that the products take), not less than an epilogue
+// takes, times the waves, and the first copies, the last epilogue and the launch.  Measured against it: 256 x 256 x 8192 80000 cycles
+// (89400), 4096 x 4096 x 4096 201000 (166000, at lower clocks), 512 x 2048 x 2048 31000 (31800).
 double cost_product_pair(const Product& p) {
   const double tiles = std::ceil(p.ep.rows / 256.0) * std::ceil(p.ep.cols / 256.0), blocks_k = std::ceil(p.depth / (double)kBlockK);
-  return std::ceil(tiles / (sm_count() / 2)) * std::max(512.0 * blocks_k, 4000.0) + 6000.0;
+  return 12600.0 + std::ceil(tiles / (sm_count() / 2)) * std::max(600.0 * blocks_k, 9000.0);
 }
 }  // namespace
 

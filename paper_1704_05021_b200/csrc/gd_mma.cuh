@@ -51,6 +51,14 @@ __device__ __forceinline__ void send_peer2(uint32_t address, float2 v, uint32_t 
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(address), "f"(v.x), "f"(v.y), "r"(barrier) : "memory");
 }
 
+// True in one thread of the (converged) warp.  The instructions that ask for copies and products take their operands from registers of
+// the whole warp; behind a branch on this the compiler knows that one thread is left and issues them directly.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0u;
+}
+
 // ---------------------------------------------------------------- copies and products
 __device__ __forceinline__ void tile_load(void* dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* b) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),

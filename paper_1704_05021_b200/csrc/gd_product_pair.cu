@@ -97,7 +97,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
   pdl_trigger();
 
   if (warp == kPairWarps) {                          // copies: each CTA its halves, all counted on the leader's barrier
-    if (lane == 0) {
+    if (elect_one()) {
       uint32_t n = 0;
       for (uint32_t t = pair; good && t < tiles; t += pairs) {
         uint32_t tr, tc;
@@ -133,7 +133,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       }
     }
   } else if (warp == kPairWarps + 1) {               // products, issued by the leader for both
-    if (lane == 0 && rank == 0) {
+    if (rank == 0 && elect_one()) {
       uint32_t n = 0, chain = 0;
       for (uint32_t t = pair; good && t < tiles; t += pairs) {
         for (uint32_t k = 0; good && k < g.blocks_k; ++chain) {
@@ -335,7 +335,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
     }
     if (!good) s_abort = 1;
   }
-  if (!good && lane == 0) atomicExch(g.status, GD_ERR_DEVICE_TIMEOUT);
+  if (!good) atomicExch(g.status, GD_ERR_DEVICE_TIMEOUT);
   __syncwarp();
   fence_before();
   cluster_arrive();                                  // neither CTA leaves while the other's products read its memory or its warps signal
