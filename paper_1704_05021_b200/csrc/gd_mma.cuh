@@ -193,14 +193,24 @@ __device__ __forceinline__ void store_as(void* p, uint64_t i, int dt, float x) {
   else if (dt == GD_DTYPE_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
   else static_cast<__half*>(p)[i] = __float2half_rn(x);
 }
-__device__ __forceinline__ void widen8(const uint4& q, int dt, float (&x)[8]) {
+// (one branch for all eight, not one per pair: the code between branches is what the instruction caches see)
+template <int DT>
+__device__ __forceinline__ void widen8_t(const uint4& q, float (&x)[8]) {
   const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 f = dt == GD_DTYPE_BF16 ? unpack2<GD_DTYPE_BF16>(w[j]) : unpack2<GD_DTYPE_FP16>(w[j]);
+    const float2 f = unpack2<DT>(w[j]);
     x[2 * j] = f.x, x[2 * j + 1] = f.y;
   }
 }
+__device__ __forceinline__ void widen8(const uint4& q, int dt, float (&x)[8]) {
+  if (dt == GD_DTYPE_BF16) widen8_t<GD_DTYPE_BF16>(q, x); else widen8_t<GD_DTYPE_FP16>(q, x);
+}
+template <int DT>
+__device__ __forceinline__ uint4 narrow8_t(const float* x) {
+  return make_uint4(pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3]), pack2<DT>(x[4], x[5]), pack2<DT>(x[6], x[7]));
+}
+__device__ __forceinline__ uint4 narrow8(const float* x, int dt) { return dt == GD_DTYPE_BF16 ? narrow8_t<GD_DTYPE_BF16>(x) : narrow8_t<GD_DTYPE_FP16>(x); }
 __device__ __forceinline__ void load8_as(const void* p, uint64_t i, int dt, float (&x)[8]) {
   if (dt == GD_DTYPE_FP32) {
     const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
@@ -217,22 +227,19 @@ __device__ __forceinline__ void store8_as(void* p, uint64_t i, int dt, const flo
     q[1] = make_float4(x[4], x[5], x[6], x[7]);
     return;
   }
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    w[j] = dt == GD_DTYPE_BF16 ? pack2<GD_DTYPE_BF16>(x[2 * j], x[2 * j + 1]) : pack2<GD_DTYPE_FP16>(x[2 * j], x[2 * j + 1]);
-  *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+  *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = narrow8(x, dt);
 }
-__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+template <int N>
+__device__ __forceinline__ void activate_all(float* v, int act) {
   if (act == GD_ACT_RELU) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];
+    for (int j = 0; j < N; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];
   } else if (act == GD_ACT_GELU) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = gelu(v[j]);
+    for (int j = 0; j < N; ++j) v[j] = gelu(v[j]);
   } else if (act == GD_ACT_SILU) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = silu(v[j]);
+    for (int j = 0; j < N; ++j) v[j] = silu(v[j]);
   }
 }
 // Up to eight elements of one output column, from row r on, z = D + bias given.
@@ -244,7 +251,7 @@ __device__ __forceinline__ void finish_column(const Epilogue& e, uint32_t r, uin
     for (uint32_t u = 0; u < 8; ++u)
       if (u < rows) store_as(e.pre, (uint64_t)(r + u) * e.ld_pre + c, e.dtype, z[u]);
   }
-  activate8(z, e.activation);
+  activate_all<8>(z, e.activation);
   if (e.add) {
     float w[8];
 #pragma unroll
@@ -276,7 +283,7 @@ __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t 
       for (int j = 0; j < 8; ++j) v[j] += b[j];
     }
     if (e.pre) store8_as(e.pre, (uint64_t)r * e.ld_pre + c, e.dtype, v);
-    activate8(v, e.activation);
+    activate_all<8>(v, e.activation);
     if (e.add) {
       float b[8];
       load8_as(e.add, (uint64_t)r * e.ld_add + c, e.add_dtype, b);

@@ -160,7 +160,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
     }
   } else {
     // warps w and w + 4 take the lanes of quarter w, 128 of the 256 columns each
-    constexpr uint32_t W = TILED && !WIDE ? 64 : 32, kPieces = 128 / W, kChunk = WIDE ? 4 : 8;     // columns of a piece, of 16 bytes of it
+    constexpr uint32_t W = TILED && !WIDE ? 64 : 32, kPieces = 128 / W;     // columns of a piece
     const uint32_t quarter = warp & 3u, half = (warp >> 2) * 128u;
     unsigned char* pieces = smem + kPairStages * kPairStage + warp * 2 * kPieceBytes;
     const Epilogue& ep = g.ep;
@@ -207,48 +207,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           if constexpr (!WIDE) {
             if (ep.pre) {
 #pragma unroll
-              for (uint32_t j = 0; j < 8; ++j) {
-                float o[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = v[8 * j + i];
-                store8_as(z + (j ^ (lane & 7u)) * 16u, 0, ep.dtype, o);
-              }
+              for (uint32_t j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(z + (j ^ (lane & 7u)) * 16u) = narrow8(v + 8 * j, ep.dtype);
               fence_async();
               __syncwarp();
               if (lane == 0 && inside) tile_store(&g.pre, pieces + kPieceBytes, (int32_t)c, (int32_t)r0);
             }
           }
+          activate_all<W>(v, ep.activation);
           if (ep.add) {
             good = mbar_wait(&add_full[warp][at], add_phase >> at & 1u, abort) && good;
             add_phase ^= 1u << at;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+              const uint4 q = *reinterpret_cast<const uint4*>(mine + (j ^ (lane & 7u)) * 16u);
+              if constexpr (WIDE) {
+                v[4 * j] += __uint_as_float(q.x), v[4 * j + 1] += __uint_as_float(q.y);
+                v[4 * j + 2] += __uint_as_float(q.z), v[4 * j + 3] += __uint_as_float(q.w);
+              } else {
+                float w[8];
+                widen8(q, ep.dtype, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * j + i] += w[i];
+              }
+            }
           }
 #pragma unroll
           for (uint32_t j = 0; j < 8; ++j) {
-            unsigned char* chunk = mine + (j ^ (lane & 7u)) * 16u;
-            if constexpr (WIDE) {
-              float o[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-              if (ep.activation != GD_ACT_NONE) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = activate(o[i], ep.activation);
-              }
-              if (ep.add) {
-                const float4 w = *reinterpret_cast<const float4*>(chunk);
-                o[0] += w.x, o[1] += w.y, o[2] += w.z, o[3] += w.w;
-              }
-              *reinterpret_cast<float4*>(chunk) = make_float4(o[0], o[1], o[2], o[3]);
-            } else {
-              float o[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] = v[8 * j + i];
-              activate8(o, ep.activation);
-              if (ep.add) {
-                float w[8];
-                load8_as(chunk, 0, ep.dtype, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] += w[i];
-              }
-              store8_as(chunk, 0, ep.dtype, o);
-            }
+            uint4* chunk = reinterpret_cast<uint4*>(mine + (j ^ (lane & 7u)) * 16u);
+            if constexpr (WIDE)
+              *chunk = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+            else
+              *chunk = narrow8(v + 8 * j, ep.dtype);
           }
           fence_async();
           __syncwarp();
