@@ -8,8 +8,8 @@
 
 namespace gd {
 
-double cost_product_split(const Product& p);       // estimated cycles
-cudaError_t launch_product_split(const Product& p, cudaStream_t stream);
+SplitChoice choose_product_split(const Product& p);
+cudaError_t launch_product_split(const Product& p, const SplitChoice& c, cudaStream_t stream);
 cudaError_t launch_product_pair(const Product& p, cudaStream_t stream);
 
 namespace {
@@ -54,8 +54,9 @@ bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& 
 cudaError_t launch_product(const Product& p, cudaStream_t stream) {
   if (p.ep.rows == 0 || p.ep.cols == 0) return cudaSuccess;
   ProfileScope ps(stream, PT_LINEAR);
-  const bool pair = p.depth && cost_product_pair(p) < cost_product_split(p);
-  const cudaError_t e = pair ? launch_product_pair(p, stream) : launch_product_split(p, stream);
+  const SplitChoice split = choose_product_split(p);
+  const bool pair = p.depth && cost_product_pair(p) < split.cost;
+  const cudaError_t e = pair ? launch_product_pair(p, stream) : launch_product_split(p, split, stream);
   if (e == cudaSuccess) note_launches(1);
   return e;
 }

@@ -325,6 +325,11 @@ struct Product {
 constexpr uint32_t kChainBlocks = 512 / kBlockK;
 inline uint32_t chain_blocks(const Product& p) { return p.ep.out_dtype == GD_DTYPE_FP32 ? kChainBlocks : 0x7FFFFFFFu; }
 bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_t depth, uint32_t box_extent, bool bf16);
+struct SplitChoice {       // of the split kernel's tile
+  bool transposed;         // D's lanes are the output's columns
+  uint32_t bn, splits;
+  double cost;             // estimated cycles
+};
 bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, int dtype);     // 32 rows x 128 bytes of a result
 cudaError_t launch_product(const Product& p, cudaStream_t stream);
 

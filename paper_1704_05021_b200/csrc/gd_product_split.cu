@@ -279,20 +279,15 @@ cudaError_t launch_bn(uint32_t bn, uint32_t splits, const SplitArgs& g, uint32_t
   }
 }
 
-struct Choice {
-  bool transposed;
-  uint32_t bn, splits;
-  double cost;
-};
 uint32_t tile_bytes(uint32_t bn, bool j_mn) { return kTileA + (j_mn && bn < 64 ? 64 : bn) * kBlockK * 2; }
 // The tile shape and split with the smallest estimated time, in cycles of an SM.  A block takes the longer of its products (2 BN cycles)
 // and its copies (72 bytes per cycle) for as many CTAs as share the SM; a CTA costs its start, its first block's latency and its
 // epilogue besides, a split the exchange of the partial tiles.  The constants are a least-squares fit of the logarithms of 500 measured times
 // (20 shapes, all tiles and splits; within 15 % in the middle); the choice it makes is the fastest or within 10 % of it on all but
 // one of the shapes (10 outputs' gradient of 80 x 4096: 5.7 against 4.7 us).
-Choice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn) {
+SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn) {
   const uint32_t sms = (uint32_t)sm_count();
-  Choice best{false, 128, 1, 1e300};
+  SplitChoice best{false, 128, 1, 1e300};
   for (int t = 0; t < 2; ++t) {
     const uint32_t ei = t ? cols : rows, ej = t ? rows : cols;
     const bool j_mn = t ? a_mn : b_mn;
@@ -305,7 +300,7 @@ Choice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b
         const double block = share * std::max(2.0 * bn, bytes / 72.0);
         const double exchange = splits == 1 ? 0.0 : splits == 2 ? 2200.0 : splits == 4 ? 3750.0 : 7400.0;
         const double cost = 2600.0 + std::ceil(ctas / (share * sms)) * (blocks * block + share * 33.0 * bn + 3750.0 + exchange);
-        if (cost < best.cost) best = Choice{t != 0, bn, splits, cost};
+        if (cost < best.cost) best = SplitChoice{t != 0, bn, splits, cost};
       }
     }
   }
@@ -314,13 +309,12 @@ Choice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b
 
 }  // namespace
 
-double cost_product_split(const Product& p) {
-  return choose(p.ep.rows, p.ep.cols, (p.depth + kBlockK - 1) / kBlockK, p.a.mn_major, p.b.mn_major).cost;
+SplitChoice choose_product_split(const Product& p) {
+  return choose(p.ep.rows, p.ep.cols, (p.depth + kBlockK - 1) / kBlockK, p.a.mn_major, p.b.mn_major);
 }
 
-cudaError_t launch_product_split(const Product& p, cudaStream_t stream) {
+cudaError_t launch_product_split(const Product& p, const SplitChoice& c, cudaStream_t stream) {
   const uint32_t blocks_k = (p.depth + kBlockK - 1) / kBlockK;
-  const Choice c = choose(p.ep.rows, p.ep.cols, blocks_k, p.a.mn_major, p.b.mn_major);
   const Operand& oi = c.transposed ? p.b : p.a;
   const Operand& oj = c.transposed ? p.a : p.b;
   const uint32_t ei = c.transposed ? p.ep.cols : p.ep.rows, ej = c.transposed ? p.ep.rows : p.ep.cols;

@@ -9,6 +9,7 @@ stream, or the one passed as `stream`.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional, Sequence, Union
 
 import torch
@@ -66,6 +67,12 @@ class _AdamwArgs(C.Structure):
                 ("grad_scale", C.c_float), ("reserved", C.c_int32), ("grad_scale_dev", C.c_void_p)]
 
 
+# The parts of the first three that change from call to call, written in one go (setting ctypes fields one by one costs more than the launch):
+# m .. y_dtype .. ld_pre of the first, m .. db of the second, all of the third.
+_FORWARD_FIELDS, _BACKWARD_FIELDS, _LOSS_FIELDS = struct.Struct("<3Q6i11Q"), struct.Struct("<3Q4iIi13Q"), struct.Struct("<2Q2i3Qqfi5Q")
+assert _FORWARD_FIELDS.size == _LinearForwardArgs.workspace.offset and _BACKWARD_FIELDS.size == _LinearBackwardArgs.workspace.offset
+assert _LOSS_FIELDS.size == C.sizeof(_CrossEntropyArgs)
+
 _lib = None
 
 
@@ -74,11 +81,11 @@ def load_library():
     global _lib
     if _lib is None:
         lib = B.load_library()
-        lib.gd_linear_forward.argtypes = [C.POINTER(_LinearForwardArgs), C.c_void_p]
-        lib.gd_linear_backward.argtypes = [C.POINTER(_LinearBackwardArgs), C.c_void_p]
+        lib.gd_linear_forward.argtypes = [C.c_void_p, C.c_void_p]         # (the address of the arguments, or byref of a structure)
+        lib.gd_linear_backward.argtypes = [C.c_void_p, C.c_void_p]
         lib.gd_linear_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.c_int, C.POINTER(C.c_size_t)]
         lib.gd_linear_status.argtypes = [C.c_void_p, C.c_void_p]
-        lib.gd_cross_entropy.argtypes = [C.POINTER(_CrossEntropyArgs), C.c_void_p]
+        lib.gd_cross_entropy.argtypes = [C.c_void_p, C.c_void_p]
         lib.gd_adamw_step.argtypes = [C.POINTER(_AdamwArgs), C.c_void_p]
         for name in EXPORTS:
             getattr(lib, name).restype = C.c_int
@@ -112,9 +119,9 @@ def _vector(t: torch.Tensor, name: str, n: int, dtypes, index: int) -> None:
         raise ValueError(f"{name}: expected {n} contiguous {' or '.join(map(str, dtypes))} on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
 
 
-def _scalar(t: Optional[torch.Tensor], name: str, index: int) -> Optional[int]:
+def _scalar(t: Optional[torch.Tensor], name: str, index: int) -> int:
     if t is None:
-        return None
+        return 0
     if t.numel() != 1 or t.dtype is not torch.float32 or t.get_device() != index:
         raise ValueError(f"{name} is one float32 on cuda:{index}")
     return t.data_ptr()
@@ -161,10 +168,9 @@ class LinearSession:
         self.workspace[:256].zero_()
         self._forward, self._backward = _LinearForwardArgs(), _LinearBackwardArgs()
         for a in (self._forward, self._backward):
-            a.n, a.k, a.dtype = self.n_out, self.n_in, _DTYPES[dtype]
-            a.activation, a.w_layout = _ACTIVATIONS[activation], _LAYOUTS[w_layout]
             a.workspace, a.workspace_bytes = self.workspace.data_ptr(), size.value
-        self._forward_ref, self._backward_ref = C.byref(self._forward), C.byref(self._backward)
+        self._forward_at, self._backward_at = C.addressof(self._forward), C.addressof(self._backward)
+        self._codes = (self.n_out, self.n_in, _DTYPES[dtype], _ACTIVATIONS[activation], _LAYOUTS[w_layout])
 
     def _rows(self, t: torch.Tensor) -> int:
         m = t.shape[0] if t.dim() == 2 else -1
@@ -175,29 +181,22 @@ class LinearSession:
     def forward(self, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """act(x W + bias) + residual, into `out` (float32, or the session's type; made here if None) and, if `pre` is given, x W + bias."""
-        m, n, dt, index, a = self._rows(x), self.n_out, self.dtype, self._index, self._forward
+        m, n, dt, index = self._rows(x), self.n_out, self.dtype, self._index
         if out is None:
             out = torch.empty(m, n, dtype=dt, device=self.device)
         out_dt = out.dtype if out.dtype is torch.float32 else dt
-        a.m = m
-        a.ldx = _matrix(x, "x", m, self.n_in, dt, index)
-        a.ldw = _matrix(w, "w", *self.w_shape, dt, index)
-        a.ldy = _matrix(out, "out", m, n, out_dt, index)
-        a.x, a.w, a.y, a.y_dtype = x.data_ptr(), w.data_ptr(), out.data_ptr(), _DTYPES[out_dt]
-        if bias is None:
-            a.bias = None
-        else:
+        bias_at = bias_code = residual_at = ld_residual = pre_at = ld_pre = 0
+        if bias is not None:
             _vector(bias, "bias", n, (torch.float32, dt), index)
-            a.bias, a.bias_dtype = bias.data_ptr(), _DTYPES[bias.dtype]
-        if residual is None:
-            a.residual = None
-        else:
-            a.residual, a.ld_residual = residual.data_ptr(), _matrix(residual, "residual", m, n, dt, index)
-        if pre is None:
-            a.pre = None
-        else:
-            a.pre, a.ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, index)
-        code = self._lib.gd_linear_forward(self._forward_ref, _stream(stream, index))
+            bias_at, bias_code = bias.data_ptr(), _DTYPES[bias.dtype]
+        if residual is not None:
+            residual_at, ld_residual = residual.data_ptr(), _matrix(residual, "residual", m, n, dt, index)
+        if pre is not None:
+            pre_at, ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, index)
+        _FORWARD_FIELDS.pack_into(self._forward, 0, m, *self._codes, bias_code, _DTYPES[out_dt], 0,
+                                  x.data_ptr(), _matrix(x, "x", m, self.n_in, dt, index), w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, index), bias_at,
+                                  residual_at, ld_residual, out.data_ptr(), _matrix(out, "out", m, n, out_dt, index), pre_at, ld_pre)
+        code = self._lib.gd_linear_forward(self._forward_at, _stream(stream, index))
         if code:
             raise B.GdError(code, "gd_linear_forward")
         return out
@@ -209,37 +208,29 @@ class LinearSession:
 
         dw has w's shape, in float32 or the session's type; db is float32.  accumulate adds to dw (float32) and db.
         """
-        m, n, k, dt, index, a = self._rows(dy), self.n_out, self.n_in, self.dtype, self._index, self._backward
+        m, n, k, dt, index = self._rows(dy), self.n_out, self.n_in, self.dtype, self._index
         if self.activation != "none" and pre is None:
             raise ValueError("backward needs the pre-activation that forward wrote")
-        a.m, a.flags = m, GD_LINEAR_ACCUMULATE if accumulate else 0
-        a.dy, a.ld_dy = dy.data_ptr(), _matrix(dy, "dy", m, n, dt, index)
-        if pre is None:
-            a.pre = None
-        else:
-            a.pre, a.ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, index)
-        if dx is None:
-            a.w = a.dx = None
-        else:
+        pre_at = ld_pre = x_at = ldx = w_at = ldw = dx_at = ld_dx = dw_at = ld_dw = db_at = dw_code = 0
+        if pre is not None:
+            pre_at, ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, index)
+        if dx is not None:
             if w is None:
                 raise ValueError("dx needs w")
-            a.w, a.ldw = w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, index)
-            a.dx, a.ld_dx = dx.data_ptr(), _matrix(dx, "dx", m, k, dt, index)
-        if dw is None:
-            a.x = a.dw = None
-            a.dw_dtype = GD_DTYPE_FP32
-        else:
+            w_at, ldw = w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, index)
+            dx_at, ld_dx = dx.data_ptr(), _matrix(dx, "dx", m, k, dt, index)
+        if dw is not None:
             if x is None:
                 raise ValueError("dw needs x")
             dw_dt = dw.dtype if dw.dtype is torch.float32 else dt
-            a.x, a.ldx = x.data_ptr(), _matrix(x, "x", m, k, dt, index)
-            a.dw, a.ld_dw, a.dw_dtype = dw.data_ptr(), _matrix(dw, "dw", *self.w_shape, dw_dt, index), _DTYPES[dw_dt]
-        if db is None:
-            a.db = None
-        else:
+            x_at, ldx = x.data_ptr(), _matrix(x, "x", m, k, dt, index)
+            dw_at, ld_dw, dw_code = dw.data_ptr(), _matrix(dw, "dw", *self.w_shape, dw_dt, index), _DTYPES[dw_dt]
+        if db is not None:
             _vector(db, "db", n, (torch.float32,), index)
-            a.db = db.data_ptr()
-        code = self._lib.gd_linear_backward(self._backward_ref, _stream(stream, index))
+            db_at = db.data_ptr()
+        _BACKWARD_FIELDS.pack_into(self._backward, 0, m, *self._codes, dw_code, GD_LINEAR_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
+                                   _matrix(dy, "dy", m, n, dt, index), pre_at, ld_pre, x_at, ldx, w_at, ldw, dx_at, ld_dx, dw_at, ld_dw, db_at)
+        code = self._lib.gd_linear_backward(self._backward_at, _stream(stream, index))
         if code:
             raise B.GdError(code, "gd_linear_backward")
 
@@ -267,11 +258,11 @@ def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, loss: Optional[to
         _vector(loss, "loss", rows, (torch.float32,), index)
     if lse is not None:
         _vector(lse, "lse", rows, (torch.float32,), index)
-    a = _CrossEntropyArgs(rows, classes, _dtype_of(dtype), 64 if targets.dtype is torch.int64 else 32, logits.data_ptr(), ld, targets.data_ptr(),
-                          ignore_index, grad_scale, 0, _scalar(grad_scale_dev, "grad_scale_dev", index), None if loss is None else loss.data_ptr(),
-                          None if lse is None else lse.data_ptr(), None if grad is None else grad.data_ptr(),
-                          0 if grad is None else _matrix(grad, "grad", rows, classes, dtype, index))
-    code = load_library().gd_cross_entropy(C.byref(a), _stream(stream, index))
+    args = _LOSS_FIELDS.pack(rows, classes, _dtype_of(dtype), 64 if targets.dtype is torch.int64 else 32, logits.data_ptr(), ld, targets.data_ptr(),
+                             ignore_index, grad_scale, 0, _scalar(grad_scale_dev, "grad_scale_dev", index), 0 if loss is None else loss.data_ptr(),
+                             0 if lse is None else lse.data_ptr(), 0 if grad is None else grad.data_ptr(),
+                             0 if grad is None else _matrix(grad, "grad", rows, classes, dtype, index))
+    code = load_library().gd_cross_entropy(args, _stream(stream, index))
     if code:
         raise B.GdError(code, "gd_cross_entropy")
 
