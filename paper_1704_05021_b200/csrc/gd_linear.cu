@@ -10,15 +10,16 @@ namespace gd {
 
 SplitChoice choose_product_split(const Product& p);
 cudaError_t launch_product_split(const Product& p, const SplitChoice& c, cudaStream_t stream);
-cudaError_t launch_product_pair(const Product& p, cudaStream_t stream);
+cudaError_t launch_product_pair(const Product& p, uint32_t bn, cudaStream_t stream);
 
 namespace {
-// Estimated cycles of the pairs' kernel: 600 per k block of a 256 x 256 tile (of 512 that the products take), not less than an epilogue
-// takes, times the waves, and the first copies, the last epilogue and the launch.  Measured against it: 256 x 256 x 8192 80000 cycles
-// (89400), 4096 x 4096 x 4096 201000 (166000, at lower clocks), 512 x 2048 x 2048 31000 (31800).
-double cost_product_pair(const Product& p) {
-  const double tiles = std::ceil(p.ep.rows / 256.0) * std::ceil(p.ep.cols / 256.0), blocks_k = std::ceil(p.depth / (double)kBlockK);
-  return 12600.0 + std::ceil(tiles / (sm_count() / 2)) * std::max(600.0 * blocks_k, 9000.0);
+// Estimated cycles of the pairs' kernel with tiles of 256 x bn: 600 (440) per k block of which the products take 512 (256), not less than an
+// epilogue takes, times the waves, and the first copies, the last epilogue and the launch.  Narrow tiles pay where wide ones leave
+// pairs without work: weights of 1500 x 1000 over 4000 rows 28.9 against 35.2 us (split kernel 33.4); 8192 x 4096 x 4096 262 against 175.
+double cost_product_pair(const Product& p, uint32_t bn) {
+  const double tiles = std::ceil(p.ep.rows / 256.0) * std::ceil(p.ep.cols / (double)bn), blocks_k = std::ceil(p.depth / (double)kBlockK);
+  const double waves = std::ceil(tiles / (sm_count() / 2));
+  return bn == 256 ? 12600.0 + waves * std::max(600.0 * blocks_k, 9000.0) : 10500.0 + waves * std::max(440.0 * blocks_k, 6000.0);
 }
 }  // namespace
 
@@ -55,8 +56,9 @@ cudaError_t launch_product(const Product& p, cudaStream_t stream) {
   if (p.ep.rows == 0 || p.ep.cols == 0) return cudaSuccess;
   ProfileScope ps(stream, PT_LINEAR);
   const SplitChoice split = choose_product_split(p);
-  const bool pair = p.depth && cost_product_pair(p) < split.cost;
-  const cudaError_t e = pair ? launch_product_pair(p, stream) : launch_product_split(p, split, stream);
+  const double wide = cost_product_pair(p, 256), narrow = cost_product_pair(p, 128);
+  const bool pair = p.depth && std::min(wide, narrow) < split.cost;
+  const cudaError_t e = pair ? launch_product_pair(p, wide <= narrow ? 256 : 128, stream) : launch_product_split(p, split, stream);
   if (e == cudaSuccess) note_launches(1);
   return e;
 }
@@ -82,6 +84,7 @@ __device__ __forceinline__ void pack_rows(const Packs& all, uint64_t first, uint
   for (uint32_t i = 0; i < all.count; ++i) {
     const Pack& k = all.p[i];
     const uint64_t total = (uint64_t)k.rows * k.vecs;
+#pragma unroll 4
     for (uint64_t t = first; t < total; t += step) {
       const uint32_t r = (uint32_t)(t / k.vecs), c = (uint32_t)(t % k.vecs) * 8u;
       const uint16_t* s = k.src + r * k.ld + c;
@@ -109,7 +112,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constan
 uint32_t pack_ctas(const Packs& all, uint32_t threads) {
   uint64_t most = 0;
   for (uint32_t i = 0; i < all.count; ++i) most = std::max(most, ((uint64_t)all.p[i].rows * all.p[i].vecs + threads - 1) / threads);
-  return (uint32_t)std::min<uint64_t>(most, (uint64_t)sm_count() * 4096 / threads);
+  return (uint32_t)std::min<uint64_t>(most, (uint64_t)sm_count() * 2048 / threads);
 }
 cudaError_t launch_pack(const Packs& all, cudaStream_t stream) {
   if (all.count == 0) return cudaSuccess;

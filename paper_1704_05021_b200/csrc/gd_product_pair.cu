@@ -20,11 +20,15 @@ namespace {
 
 constexpr uint32_t kPairWarps = 8;                            // that finish tiles
 constexpr uint32_t kPairThreads = (kPairWarps + 2) * 32;
-constexpr uint32_t kPairStages = 5;
-constexpr uint32_t kHalfBlock = 128 * kBlockK * 2;            // one CTA's half of a block of A or of B
-constexpr uint32_t kPairStage = 2 * kHalfBlock;
+constexpr uint32_t kHalfA = 128 * kBlockK * 2;                // one CTA's half of a block of A
 constexpr uint32_t kPieceBytes = 32 * 128;                  // rows x bytes of a piece
-constexpr uint32_t kPairBytes = kPairStages * kPairStage + kPairWarps * 2 * kPieceBytes + 1024;
+template <int BN>
+struct PairShape {
+  static constexpr uint32_t kHalfB = BN / 2 * kBlockK * 2;
+  static constexpr uint32_t kStage = kHalfA + kHalfB;
+  static constexpr uint32_t kStages = BN == 256 ? 5 : 6;
+  static constexpr uint32_t kBytes = kStages * kStage + kPairWarps * 2 * kPieceBytes + 1024;
+};
 constexpr uint32_t kGroup = 8;
 
 struct PairArgs {
@@ -67,8 +71,9 @@ __device__ __forceinline__ void tile_place(uint32_t t, uint32_t tiles_r, uint32_
 
 // CHAINED: a tile's sum is made of several (fp32 results), joined in registers; otherwise it goes from tensor memory straight out.
 // TILED: results and residual go through the copy engine.  WIDE: the results are fp32.
-template <bool A_MN, bool B_MN, bool CHAINED, bool TILED, bool WIDE>
+template <int BN, bool A_MN, bool B_MN, bool CHAINED, bool TILED, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) product_pair_kernel(const __grid_constant__ PairArgs g) {
+  constexpr uint32_t kPairStages = PairShape<BN>::kStages, kPairStage = PairShape<BN>::kStage, kHalf = BN / 2;     // kHalf: columns a warp finishes
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t full[kPairStages], empty[kPairStages], sum_full[2], sum_empty[2], add_full[kPairWarps][2];
   __shared__ uint32_t s_tmem;
@@ -85,7 +90,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (g.blocks_k) prefetch_map(&g.a), prefetch_map(&g.b);
   }
-  if (warp == kPairWarps) tmem_alloc<2>(&s_tmem, 512);
+  if (warp == kPairWarps) tmem_alloc<2>(&s_tmem, 2 * BN);
   fence_before();
   cluster_arrive();                                  // both CTAs' barriers exist before either signals the other's
   cluster_wait();
@@ -102,7 +107,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       for (uint32_t t = pair; good && t < tiles; t += pairs) {
         uint32_t tr, tc;
         tile_place(t, g.tiles_r, g.tiles_c, &tr, &tc);
-        const int32_t i0 = (int32_t)(tr * 256u + rank * 128u), j0 = (int32_t)(tc * 256u + rank * 128u);
+        const int32_t i0 = (int32_t)(tr * 256u + rank * 128u), j0 = (int32_t)(tc * BN + rank * kHalf);
         for (uint32_t k = 0; k < g.blocks_k; ++k, ++n) {
           const uint32_t s = n % kPairStages;
           if (n >= kPairStages && !mbar_wait(&empty[s], (n / kPairStages + 1u) & 1u, abort)) { good = false; break; }
@@ -117,10 +122,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
             tile_load_pair(at, &g.a, kc, i0, bar);
           }
           if constexpr (B_MN) {
-            tile_load_pair(at + kHalfBlock, &g.b, j0, kc, bar);
-            tile_load_pair(at + kHalfBlock + 8192, &g.b, j0 + 64, kc, bar);
+            tile_load_pair(at + kHalfA, &g.b, j0, kc, bar);
+            if constexpr (BN == 256) tile_load_pair(at + kHalfA + 8192, &g.b, j0 + 64, kc, bar);
           } else {
-            tile_load_pair(at + kHalfBlock, &g.b, kc, j0, bar);
+            tile_load_pair(at + kHalfA, &g.b, kc, j0, bar);
           }
         }
       }
@@ -137,7 +142,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       uint32_t n = 0, chain = 0;
       for (uint32_t t = pair; good && t < tiles; t += pairs) {
         for (uint32_t k = 0; good && k < g.blocks_k; ++chain) {
-          const uint32_t end = min(k + g.chain, g.blocks_k), buf = chain & 1u, sum = tmem + buf * 256u;
+          const uint32_t end = min(k + g.chain, g.blocks_k), buf = chain & 1u, sum = tmem + buf * BN;
           if (chain >= 2 && !mbar_wait(&sum_empty[buf], (chain / 2 + 1u) & 1u, abort)) { good = false; break; }
           fence_after();
           for (const uint32_t first = k; k < end; ++k, ++n) {
@@ -148,7 +153,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
 #pragma unroll
             for (uint32_t q = 0; q < kBlockK / 16; ++q) {
               const uint64_t a = operand_desc(at + q * (A_MN ? 2048u : 32u), 8192u);
-              const uint64_t b = operand_desc(at + kHalfBlock + q * (B_MN ? 2048u : 32u), 8192u);
+              const uint64_t b = operand_desc(at + kHalfA + q * (B_MN ? 2048u : 32u), 8192u);
               mma<2>(sum, a, b, g.desc, (k - first) | q);
             }
             mma_commit_pair(&empty[s]);
@@ -159,16 +164,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       if (!good) s_abort = 1;
     }
   } else {
-    // warps w and w + 4 take the lanes of quarter w, 128 of the 256 columns each
-    constexpr uint32_t W = TILED && !WIDE ? 64 : 32, kPieces = 128 / W;     // columns of a piece
-    const uint32_t quarter = warp & 3u, half = (warp >> 2) * 128u;
+    // warps w and w + 4 take the lanes of quarter w, half of the columns each
+    constexpr uint32_t W = TILED && !WIDE ? 64 : 32, kPieces = kHalf / W;     // columns of a piece
+    const uint32_t quarter = warp & 3u, half = (warp >> 2) * kHalf;
     unsigned char* pieces = smem + kPairStages * kPairStage + warp * 2 * kPieceBytes;
     const Epilogue& ep = g.ep;
     uint32_t chain = 0, add_phase = 0;
     for (uint32_t t = pair; good && t < tiles; t += pairs) {
       uint32_t tr, tc;
       tile_place(t, g.tiles_r, g.tiles_c, &tr, &tc);
-      const uint32_t r0 = tr * 256u + rank * 128u + quarter * 32u, c0 = tc * 256u + half;
+      const uint32_t r0 = tr * 256u + rank * 128u + quarter * 32u, c0 = tc * BN + half;
       const uint32_t from = tmem + (quarter * 32u << 16) + half;
       const auto release = [&](uint32_t buf) {       // this warp has read its part of the sum
         fence_before();
@@ -180,7 +185,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       if (TILED && ep.bias) {
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
-          if (c0 + 4 * lane + i < ep.cols) bias[i] = load_as(ep.bias, c0 + 4 * lane + i, ep.bias_dtype);
+          if (4 * lane < kHalf && c0 + 4 * lane + i < ep.cols) bias[i] = load_as(ep.bias, c0 + 4 * lane + i, ep.bias_dtype);
       }
       // The residual of piece p, into the buffer whose place the result takes (buffer 0 alone where z also needs one).
       const auto ask_add = [&](uint32_t p) {
@@ -274,18 +279,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
         }
       }
       if constexpr (CHAINED) {
-        float v[128];
+        float v[kHalf];
 #pragma unroll
-        for (uint32_t c = 0; c < 128; ++c) v[c] = 0.f;
+        for (uint32_t c = 0; c < kHalf; ++c) v[c] = 0.f;
         for (uint32_t k = 0; k < g.blocks_k; k += g.chain, ++chain) {
           const uint32_t buf = chain & 1u;
           if (!mbar_wait(&sum_full[buf], (chain / 2) & 1u, abort)) { good = false; break; }
           fence_after();
 #pragma unroll
-          for (uint32_t c = 0; c < 128; c += 16) {
+          for (uint32_t c = 0; c < kHalf; c += 16) {
             float w[16];
-            tmem_load8(from + buf * 256u + c, w);
-            tmem_load8(from + buf * 256u + c + 8, w + 8);
+            tmem_load8(from + buf * BN + c, w);
+            tmem_load8(from + buf * BN + c + 8, w + 8);
             tmem_ready();
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[c + j] += w[j];
@@ -306,7 +311,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           for (uint32_t p = 0; p < kPieces; ++p) {
             float v[W];
 #pragma unroll
-            for (uint32_t c = 0; c < W; c += 32) tmem_load32(from + buf * 256u + p * W + c, v + c);
+            for (uint32_t c = 0; c < W; c += 32) tmem_load32(from + buf * BN + p * W + c, v + c);
             tmem_ready();
             if (p + 1 == kPieces) release(buf);
             finish(p, v);
@@ -329,47 +334,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
   fence_before();
   cluster_arrive();                                  // neither CTA leaves while the other's products read its memory or its warps signal
   cluster_wait();
-  if (warp == kPairWarps) tmem_free<2>(tmem, 512);
+  if (warp == kPairWarps) tmem_free<2>(tmem, 2 * BN);
 }
 
-template <bool A_MN, bool B_MN, bool CHAINED, bool TILED, bool WIDE>
+template <int BN, bool A_MN, bool B_MN, bool CHAINED, bool TILED, bool WIDE>
 cudaError_t launch_pair(const PairArgs& g, cudaStream_t stream) {
-  auto kernel = product_pair_kernel<A_MN, B_MN, CHAINED, TILED, WIDE>;
+  auto kernel = product_pair_kernel<BN, A_MN, B_MN, CHAINED, TILED, WIDE>;
   static PerDeviceInt ready;
   int dev;
   if (!ready.get(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPairBytes);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairShape<BN>::kBytes);
     if (e != cudaSuccess) return e;
     ready.set(dev, 1);
   }
   const uint32_t pairs = std::min<uint64_t>((uint64_t)g.tiles_r * g.tiles_c, (uint64_t)sm_count() / 2);
-  return launch_dependent(kernel, dim3(2 * pairs), dim3(kPairThreads), kPairBytes, stream, g);
+  return launch_dependent(kernel, dim3(2 * pairs), dim3(kPairThreads), PairShape<BN>::kBytes, stream, g);
 }
-template <bool A_MN, bool B_MN>
+template <int BN, bool A_MN, bool B_MN>
 cudaError_t launch_majors(const PairArgs& g, bool tiled, cudaStream_t stream) {
   const bool chained = g.chain < g.blocks_k;            // (fp32 results only)
   if (g.ep.out_dtype == GD_DTYPE_FP32) {
-    if (tiled) return chained ? launch_pair<A_MN, B_MN, true, true, true>(g, stream) : launch_pair<A_MN, B_MN, false, true, true>(g, stream);
-    return chained ? launch_pair<A_MN, B_MN, true, false, true>(g, stream) : launch_pair<A_MN, B_MN, false, false, true>(g, stream);
+    if (tiled) return chained ? launch_pair<BN, A_MN, B_MN, true, true, true>(g, stream) : launch_pair<BN, A_MN, B_MN, false, true, true>(g, stream);
+    return chained ? launch_pair<BN, A_MN, B_MN, true, false, true>(g, stream) : launch_pair<BN, A_MN, B_MN, false, false, true>(g, stream);
   }
-  return tiled ? launch_pair<A_MN, B_MN, false, true, false>(g, stream) : launch_pair<A_MN, B_MN, false, false, false>(g, stream);
+  return tiled ? launch_pair<BN, A_MN, B_MN, false, true, false>(g, stream) : launch_pair<BN, A_MN, B_MN, false, false, false>(g, stream);
+}
+template <int BN>
+cudaError_t launch_bn(const Product& p, const PairArgs& g, bool tiled, cudaStream_t stream) {
+  if (p.a.mn_major) return p.b.mn_major ? launch_majors<BN, true, true>(g, tiled, stream) : cudaErrorInvalidValue;   // (no call has A alone transposed)
+  return p.b.mn_major ? launch_majors<BN, false, true>(g, tiled, stream) : launch_majors<BN, false, false>(g, tiled, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_product_pair(const Product& p, cudaStream_t stream) {
+cudaError_t launch_product_pair(const Product& p, uint32_t bn, cudaStream_t stream) {
   PairArgs g;
   std::memset(&g, 0, sizeof(g));
   if (!encode_operand(&g.a, p.a, p.ep.rows, p.depth, p.a.mn_major ? 64 : 128, p.bf16) ||
-      !encode_operand(&g.b, p.b, p.ep.cols, p.depth, p.b.mn_major ? 64 : 128, p.bf16))
+      !encode_operand(&g.b, p.b, p.ep.cols, p.depth, p.b.mn_major ? 64 : bn / 2, p.bf16))
     return cudaErrorInvalidValue;
   g.ep = p.ep;
   g.status = p.status;
   g.blocks_k = (p.depth + kBlockK - 1) / kBlockK;
   g.chain = chain_blocks(p);
-  g.desc = mma_desc(256, 256, p.bf16, p.a.mn_major, p.b.mn_major);
+  g.desc = mma_desc(256, bn, p.bf16, p.a.mn_major, p.b.mn_major);
   g.tiles_r = (p.ep.rows + 255) / 256;
-  g.tiles_c = (p.ep.cols + 255) / 256;
+  g.tiles_c = (p.ep.cols + bn - 1) / bn;
   // Results and residual as pieces of 32 rows x 128 bytes, where every row starts at a multiple of 16 bytes; a residual of another type
   // than the results, or z next to fp32 results, does not fit a piece.
   const bool wide = g.ep.out_dtype == GD_DTYPE_FP32;
@@ -377,8 +387,7 @@ cudaError_t launch_product_pair(const Product& p, cudaStream_t stream) {
   if (tiled && (!encode_piece(&g.out, g.ep.out, g.ep.ld_out, g.ep, g.ep.out_dtype) || (g.ep.pre && !encode_piece(&g.pre, g.ep.pre, g.ep.ld_pre, g.ep, g.ep.dtype)) ||
                 (g.ep.add && !encode_piece(&g.add, g.ep.add, g.ep.ld_add, g.ep, g.ep.add_dtype))))
     return cudaErrorInvalidValue;
-  if (p.a.mn_major) return p.b.mn_major ? launch_majors<true, true>(g, tiled, stream) : cudaErrorInvalidValue;   // (no call has A alone transposed)
-  return p.b.mn_major ? launch_majors<false, true>(g, tiled, stream) : launch_majors<false, false>(g, tiled, stream);
+  return bn == 256 ? launch_bn<256>(p, g, tiled, stream) : launch_bn<128>(p, g, tiled, stream);
 }
 
 }  // namespace gd
