@@ -86,10 +86,14 @@ __device__ __forceinline__ void pack_rows(const Packs& all, uint64_t first, uint
     const uint64_t total = (uint64_t)k.rows * k.vecs;
 #pragma unroll 4
     for (uint64_t t = first; t < total; t += step) {
-      const uint32_t r = (uint32_t)(t / k.vecs), c = (uint32_t)(t % k.vecs) * 8u;
+      // (64-bit division only where 32 bits do not hold the position)
+      const uint32_t r = total >> 32 ? (uint32_t)(t / k.vecs) : (uint32_t)t / k.vecs, c = ((uint32_t)t - r * k.vecs) * 8u;
       const uint16_t* s = k.src + r * k.ld + c;
       uint32_t w[4];
-      if (c + 8 <= k.cols && ((uintptr_t)s & 3u) == 0) {
+      if (c + 8 <= k.cols && ((uintptr_t)s & 7u) == 0) {
+        const uint2 lo = __ldcs(reinterpret_cast<const uint2*>(s)), hi = __ldcs(reinterpret_cast<const uint2*>(s) + 1);
+        w[0] = lo.x, w[1] = lo.y, w[2] = hi.x, w[3] = hi.y;
+      } else if (c + 8 <= k.cols && ((uintptr_t)s & 3u) == 0) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = reinterpret_cast<const uint32_t*>(s)[j];
       } else {
@@ -112,7 +116,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constan
 uint32_t pack_ctas(const Packs& all, uint32_t threads) {
   uint64_t most = 0;
   for (uint32_t i = 0; i < all.count; ++i) most = std::max(most, ((uint64_t)all.p[i].rows * all.p[i].vecs + threads - 1) / threads);
-  return (uint32_t)std::min<uint64_t>(most, (uint64_t)sm_count() * 2048 / threads);
+  return (uint32_t)std::min<uint64_t>(most, (uint64_t)sm_count() * 1024 / threads);
 }
 cudaError_t launch_pack(const Packs& all, cudaStream_t stream) {
   if (all.count == 0) return cudaSuccess;
@@ -125,7 +129,7 @@ cudaError_t launch_pack(const Packs& all, cudaStream_t stream) {
 // ---------------------------------------------------------------- dz and db
 // dz = dy * act'(pre), rounded to the operands' type, and the sums of its columns before that rounding, in one pass over dy and pre;
 // ragged operands of the products that follow are laid out by the same launch, in CTAs of their own.
-// A cluster of kSlopeCtas CTAs takes `width` columns (64, or 32 where 64 would leave SMs without a CTA), each CTA a share of the rows; a
+// A cluster of 1 .. 8 CTAs takes `width` columns (64, or 32 where 64 would leave SMs without a CTA), each CTA a share of the rows; a
 // thread takes 8 neighbouring columns of every so many rows.  The threads' sums meet by shuffles and in shared memory, the CTAs' are sent
 // to the first of the cluster and counted there, always in the same order: no atomics, no second launch.  Bound by the bytes (dy and
 // pre read, dz written) where there are many columns, by the 25 instructions an entry of GELU or SiLU takes where there are few.
@@ -136,7 +140,7 @@ struct SlopeArgs {
   void* dz;            // NULL: only the sums are wanted
   float* db;           // NULL: only dz is wanted
   uint64_t ld_dy, ld_pre, ld_dz;
-  uint32_t rows, cols, width, ctas;      // ctas: those that take columns; the others lay out `packs`
+  uint32_t rows, cols, width, split, ctas;      // split: CTAs of a cluster; ctas: those that take columns; the others lay out `packs`
   int32_t activation;
   uint32_t accumulate, vectors;
   Packs packs;
@@ -147,27 +151,33 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_co
   __shared__ __align__(8) float s_all[kSlopeCtas][64];
   __shared__ uint64_t s_in;
   __shared__ int s_never;
-  const uint32_t rank = cluster_rank(), tid = threadIdx.x, lane = tid & 31u, groups = a.width / 8u;      // groups: threads side by side in a row
+  // (a launch without clusters - split = 1 - executes none of their instructions)
+  const bool clustered = a.split > 1;
+  const uint32_t rank = clustered ? cluster_rank() : 0u, tid = threadIdx.x, lane = tid & 31u, groups = a.width / 8u;      // groups: threads side by side in a row
   const bool pack = blockIdx.x >= a.ctas;
-  if (tid == 0) {
-    s_never = 0;
-    mbar_init(&s_in, 1u);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (rank == 0) mbar_arrive_expect_tx(&s_in, kSlopeCtas * a.width * 4u);
+  if (clustered) {
+    if (tid == 0) {
+      s_never = 0;
+      mbar_init(&s_in, 1u);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      if (rank == 0) mbar_arrive_expect_tx(&s_in, a.split * a.width * 4u);
+    }
+    __syncthreads();
+    cluster_arrive_relaxed();
   }
-  __syncthreads();
-  cluster_arrive_relaxed();
   pdl_wait();
   pdl_trigger();
   if (pack) {
     pack_rows(a.packs, (uint64_t)(blockIdx.x - a.ctas) * kSlopeThreads + tid, (uint64_t)(gridDim.x - a.ctas) * kSlopeThreads);
-    cluster_wait();
-    cluster_arrive_relaxed();
-    cluster_wait();
+    if (clustered) {
+      cluster_wait();
+      cluster_arrive_relaxed();
+      cluster_wait();
+    }
     return;
   }
-  const uint32_t col0 = blockIdx.x / kSlopeCtas * a.width, c = col0 + tid % groups * 8u, step = kSlopeThreads / groups;
-  const uint32_t per = (a.rows + kSlopeCtas - 1) / kSlopeCtas, r0 = min(rank * per, a.rows), r1 = min(r0 + per, a.rows);
+  const uint32_t col0 = blockIdx.x / a.split * a.width, c = col0 + tid % groups * 8u, step = kSlopeThreads / groups;
+  const uint32_t per = (a.rows + a.split - 1) / a.split, r0 = min(rank * per, a.rows), r1 = min(r0 + per, a.rows);
   const bool whole = a.vectors && c + 8 <= a.cols;
   float sum[8] = {};
   if (c < a.cols) {
@@ -225,6 +235,16 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_co
       for (int j = 0; j < 8; ++j) s_sum[tid >> 5][lane * 8u + j] = sum[j];
     }
     __syncthreads();
+    if (!clustered) {
+      if (tid < a.width) {
+        float t = 0.f;
+#pragma unroll
+        for (uint32_t w = 0; w < kSlopeWarps; ++w) t += s_sum[w][tid];
+        const uint32_t col = col0 + tid;
+        if (col < a.cols) a.db[col] = a.accumulate ? a.db[col] + t : t;
+      }
+      return;
+    }
     cluster_wait();                                  // (the first CTA's mbarrier exists)
     if (tid < a.width / 2) {
       float2 t = make_float2(0.f, 0.f);
@@ -234,32 +254,38 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_co
     }
     if (rank == 0 && tid < a.width) {
       float t = mbar_wait(&s_in, 0u, &s_never) ? 0.f : NAN;
-      for (uint32_t q = 0; q < kSlopeCtas; ++q) t += s_all[q][tid];
+      for (uint32_t q = 0; q < a.split; ++q) t += s_all[q][tid];
       const uint32_t col = col0 + tid;
       if (col < a.cols) a.db[col] = a.accumulate ? a.db[col] + t : t;
     }
-  } else {
+  } else if (clustered) {
     cluster_wait();
   }
-  cluster_arrive_relaxed();                          // (nobody leaves while something may still be on its way to it)
-  cluster_wait();
+  if (clustered) {
+    cluster_arrive_relaxed();                        // (nobody leaves while something may still be on its way to it)
+    cluster_wait();
+  }
 }
 cudaError_t launch_slope(SlopeArgs& a, int dtype, cudaStream_t stream) {
   ProfileScope ps(stream, PT_LINEAR_SLOPE);
+  // CTAs for every SM twice over, if there are rows enough for a CTA's threads
   a.width = (a.cols + 63) / 64 * kSlopeCtas < 2u * sm_count() ? 32 : 64;
-  a.ctas = (a.cols + a.width - 1) / a.width * kSlopeCtas;
+  const uint32_t tiles = (a.cols + a.width - 1) / a.width;
+  a.split = 1;
+  while (a.split < kSlopeCtas && tiles * a.split < 2u * sm_count() && a.rows > a.split * (kSlopeThreads * 8u / a.width)) a.split *= 2;
+  a.ctas = tiles * a.split;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.ctas + (pack_ctas(a.packs, kSlopeThreads) + kSlopeCtas - 1) / kSlopeCtas * kSlopeCtas);
+  cfg.gridDim = dim3(a.ctas + (pack_ctas(a.packs, kSlopeThreads) + a.split - 1) / a.split * a.split);
   cfg.blockDim = dim3(kSlopeThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kSlopeCtas;
+  attr[1].val.clusterDim.x = a.split;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = a.split > 1 ? 2 : 1;
   const cudaError_t e = dtype == GD_DTYPE_BF16 ? cudaLaunchKernelEx(&cfg, slope_kernel<GD_DTYPE_BF16>, a) : cudaLaunchKernelEx(&cfg, slope_kernel<GD_DTYPE_FP16>, a);
   if (e == cudaSuccess) note_launches(1);
   return e;
