@@ -41,8 +41,8 @@ struct AdamScalars {
   int32_t copy_dtype;
 };
 
-// Kernel arguments hold at most 32764 bytes.  The short table is for the usual model: a launch pays for its argument's bytes.
-constexpr uint32_t kFewTensors = 24, kMaxTensors = 400;
+// Kernel arguments hold at most 32764 bytes.  The shorter tables are there because a launch pays for its argument's bytes.
+constexpr uint32_t kFewTensors = 24, kSomeTensors = 110, kMaxTensors = 400;
 template <uint32_t CAP>
 struct AdamTable {
   AdamScalars s;
@@ -354,13 +354,17 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
       }
     }
   }
-  for (; at < end; at += kStride) {
-    load_ragged<PT, GT, BITS>(b, t, at, lane);
+  if (at < end) load_ragged<PT, GT, BITS>(b, t, at, lane);
+  while (at < end) {
+    Block<BITS> next;
+    if (at + kStride < end) load_ragged<PT, GT, BITS>(next, t, at + kStride, lane);
     update_block<true, BITS>(b, s, scale, t.decay, random_base, at, t.n, lane);
     if constexpr (BITS == 8) {
       if (lane == 0) t.m_scale[at >> 7] = b.ms, t.v_scale[at >> 7] = b.vs;
     }
     store_ragged<PT, BITS>(b, t, s.copy_dtype, at, lane);
+    b = next;
+    at += kStride;
   }
 }
 
@@ -368,11 +372,19 @@ template <int PT, int GT, int BITS>
 cudaError_t launch_cap(const AdamTable<kMaxTensors>& full, uint32_t chunks, cudaStream_t stream) {
   constexpr size_t smem = BITS == 8 ? kAdamThreads / 32 * kStages * kStageBytes : 0;
   static_assert(smem <= 48 * 1024, "without asking for more shared memory");
+  const auto with = [&](auto& table) {
+    table.s = full.s;
+    for (uint32_t i = 0; i < full.s.n_tensors; ++i) table.t[i] = full.t[i];
+  };
   if (full.s.n_tensors <= kFewTensors) {
     AdamTable<kFewTensors> few;
-    few.s = full.s;
-    for (uint32_t i = 0; i < full.s.n_tensors; ++i) few.t[i] = full.t[i];
+    with(few);
     return launch_dependent(adamw_kernel<PT, GT, BITS, kFewTensors>, dim3(chunks), dim3(kAdamThreads), smem, stream, few);
+  }
+  if (full.s.n_tensors <= kSomeTensors) {
+    AdamTable<kSomeTensors> some;
+    with(some);
+    return launch_dependent(adamw_kernel<PT, GT, BITS, kSomeTensors>, dim3(chunks), dim3(kAdamThreads), smem, stream, some);
   }
   return launch_dependent(adamw_kernel<PT, GT, BITS, kMaxTensors>, dim3(chunks), dim3(kAdamThreads), smem, stream, full);
 }

@@ -306,6 +306,12 @@ struct Workspace {
     return at <= size ? p : nullptr;
   }
 };
+// The partial sums' place, where a contraction is long enough to want one.
+int partial_place(uint64_t depth, Workspace& ws, float** p) {
+  if (depth < kLongDepth) return GD_OK;
+  *p = static_cast<float*>(ws.take(1, kPartialBytes / 2));
+  return *p ? GD_OK : GD_ERR_WORKSPACE;
+}
 // A leading dimension for one row is never used: a ragged one would only cause a copy.
 uint64_t row_step(uint64_t ld, uint64_t rows, uint64_t cols) { return rows > 1 ? ld : up(cols, 8); }
 
@@ -350,6 +356,7 @@ int forward(const gd_linear_forward_args* a, cudaStream_t stream) {
   packs.count = 0;
   Product p;
   std::memset(&p, 0, sizeof(p));
+  if ((rc = partial_place(a->k, ws, &p.partial)) != GD_OK) return rc;
   if ((rc = operand(a->x, a->ldx, a->m, a->k, ws, &packs, &p.a)) != GD_OK || (rc = operand(a->w, a->ldw, w_rows, w_cols, ws, &packs, &p.b)) != GD_OK) return rc;
   p.b.mn_major = in_out;
   p.depth = (uint32_t)a->k;
@@ -396,6 +403,8 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     dz.p = s.dz, dz.ld = s.ld_dz;
   }
   Operand w{}, x{};
+  float* partial = nullptr;
+  if ((rc = partial_place(std::max(has_dx ? n : 0, has_dw ? m : 0), ws, &partial)) != GD_OK) return rc;
   s.packs.count = 0;
   if (has_dx && n && (rc = operand(a->w, a->ldw, w_rows, w_cols, ws, &s.packs, &w)) != GD_OK) return rc;
   if (has_dw && m && (rc = operand(a->x, a->ldx, m, k, ws, &s.packs, &x)) != GD_OK) return rc;
@@ -420,6 +429,7 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     p.a = dz, p.a.mn_major = false;
     p.b = w, p.b.mn_major = !in_out;
     p.depth = (uint32_t)n;
+    p.partial = n >= kLongDepth ? partial : nullptr;
     p.ep.out = a->dx, p.ep.ld_out = a->ld_dx, p.ep.out_dtype = a->dtype;
     p.ep.rows = (uint32_t)m, p.ep.cols = (uint32_t)k;
     p.ep.vectors = vector_rows(a->dx, row_step(a->ld_dx, m, k), a->dtype);
@@ -429,6 +439,7 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     p.a = in_out ? x : dz, p.b = in_out ? dz : x;
     p.a.mn_major = p.b.mn_major = true;
     p.depth = (uint32_t)m;
+    p.partial = m >= kLongDepth ? partial : nullptr;     // (the product before this one has been joined by the time it is written)
     p.ep.out = a->dw, p.ep.ld_out = a->ld_dw, p.ep.out_dtype = a->dw_dtype;
     p.ep.rows = (uint32_t)w_rows, p.ep.cols = (uint32_t)w_cols;
     if (add) p.ep.add = a->dw, p.ep.ld_add = a->ld_dw, p.ep.add_dtype = GD_DTYPE_FP32;
@@ -449,6 +460,7 @@ int gd_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, int any_layout
   if (m >> 31 || n >> 31 || k >> 31) return GD_ERR_TOO_LARGE;
   auto matrix = [](uint64_t rows, uint64_t cols) { return up(rows * up(cols, 8) * 2, 256); };
   uint64_t b = kStatusBytes + matrix(m, n);                              // dz
+  if (std::max(m, std::max(n, k)) >= kLongDepth) b += kPartialBytes;      // partial sums of a long contraction
   if (any_layout || k % 8) b += matrix(m, k);                            // x
   if (any_layout || k % 8 || n % 8) b += std::max(matrix(k, n), matrix(n, k));   // w, in either layout
   *bytes_out = (size_t)b;

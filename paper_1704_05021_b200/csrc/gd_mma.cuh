@@ -328,7 +328,9 @@ struct Product {
   bool bf16;
   Epilogue ep;
   int* status;
+  float* partial;      // kPartialBytes of workspace where the depth is at least kLongDepth, else NULL
 };
+constexpr uint64_t kLongDepth = 16384, kPartialBytes = 2u << 20;
 // How many k blocks the tensor cores may sum in one go.  Their fp32 accumulator truncates: measured against 64 bits the relative
 // error of a product of normal numbers grows by 1.1e-9 per k (4.4e-6 at 4096, where fp32 additions in registers leave 6e-7).
 // Next to the 2^-9 of a 16-bit result that is nothing; an fp32 result is summed in chains of 512 k (5e-7) that are joined in
@@ -339,6 +341,7 @@ bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_
 struct SplitChoice {       // of the split kernel's tile
   bool transposed;         // D's lanes are the output's columns
   uint32_t bn, splits;
+  uint32_t outer;          // parts of k in clusters of their own, joined by a second launch
   double cost;             // estimated cycles
 };
 bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, int dtype);     // 32 rows x 128 bytes of a result

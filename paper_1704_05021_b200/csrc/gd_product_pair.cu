@@ -187,9 +187,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
         for (uint32_t i = 0; i < 4; ++i)
           if (4 * lane < kHalf && c0 + 4 * lane + i < ep.cols) bias[i] = load_as(ep.bias, c0 + 4 * lane + i, ep.bias_dtype);
       }
+      const bool through = ep.add && (!WIDE || ep.add_dtype == GD_DTYPE_FP32);      // the residual comes as pieces; one of 16 bits next to fp32 results does not fit
       // The residual of piece p, into the buffer whose place the result takes (buffer 0 alone where z also needs one).
       const auto ask_add = [&](uint32_t p) {
-        const uint32_t at = ep.pre ? 0u : p & 1u;
+        const uint32_t at = !WIDE && ep.pre ? 0u : p & 1u;
         mbar_arrive_expect_tx(&add_full[warp][at], kPieceBytes);
         tile_load(pieces + at * kPieceBytes, &g.add, (int32_t)(c0 + p * W), (int32_t)r0, &add_full[warp][at]);
       };
@@ -198,11 +199,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
         const uint32_t c = c0 + p * W;
         if constexpr (TILED) {
           const bool inside = r0 < ep.rows && c < ep.cols;
-          const uint32_t at = ep.pre ? 0u : p & 1u;
+          const bool two = !WIDE && ep.pre;          // z takes the second buffer
+          const uint32_t at = two ? 0u : p & 1u;
           unsigned char* mine = pieces + at * kPieceBytes + lane * 128u;
           unsigned char* z = pieces + kPieceBytes + lane * 128u;
-          if (!ep.add || ep.pre) {                   // (with a residual the buffer was free before its copy was asked for)
-            if (lane == 0) { if (ep.pre) stores_read<0>(); else stores_read<1>(); }
+          if (!through || two) {                     // (with a residual the buffer was free before its copy was asked for)
+            if (lane == 0) { if (two) stores_read<0>(); else stores_read<1>(); }
             __syncwarp();
           }
           if (ep.bias) {
@@ -218,8 +220,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
               if (lane == 0 && inside) tile_store(&g.pre, pieces + kPieceBytes, (int32_t)c, (int32_t)r0);
             }
           }
+          if constexpr (WIDE) {
+            if (ep.pre && r0 + lane < ep.rows) {     // 32 columns of 16 bits a lane: two sectors, written directly
+              uint16_t* to = static_cast<uint16_t*>(ep.pre) + (uint64_t)(r0 + lane) * ep.ld_pre + c;
+#pragma unroll
+              for (uint32_t j = 0; j < 4; ++j) {
+                if (c + 8 * j + 8 <= ep.cols) {
+                  *reinterpret_cast<uint4*>(to + 8 * j) = narrow8(v + 8 * j, ep.dtype);
+                } else {
+#pragma unroll
+                  for (uint32_t i = 0; i < 8; ++i)
+                    if (c + 8 * j + i < ep.cols) store_as(to, 8 * j + i, ep.dtype, v[8 * j + i]);
+                }
+              }
+            }
+          }
           activate_all<W>(v, ep.activation);
-          if (ep.add) {
+          if constexpr (WIDE) {
+            if (ep.add && !through && r0 + lane < ep.rows) {
+              const uint16_t* of = static_cast<const uint16_t*>(ep.add) + (uint64_t)(r0 + lane) * ep.ld_add + c;
+#pragma unroll
+              for (uint32_t j = 0; j < 4; ++j) {
+                float w[8] = {};
+                if (c + 8 * j + 8 <= ep.cols) {
+                  load8_as(of, 8 * j, ep.add_dtype, w);
+                } else {
+#pragma unroll
+                  for (uint32_t i = 0; i < 8; ++i)
+                    if (c + 8 * j + i < ep.cols) w[i] = load_as(of, 8 * j + i, ep.add_dtype);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * j + i] += w[i];
+              }
+            }
+          }
+          if (through) {
             good = mbar_wait(&add_full[warp][at], add_phase >> at & 1u, abort) && good;
             add_phase ^= 1u << at;
 #pragma unroll
@@ -248,8 +283,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           __syncwarp();
           if (lane == 0) {
             if (inside) tile_store(&g.out, pieces + at * kPieceBytes, (int32_t)c, (int32_t)r0);
-            if (ep.add && p + 1 < kPieces) {
-              if (ep.pre) stores_read<0>(); else stores_read<1>();
+            if (through && p + 1 < kPieces) {
+              if (two) stores_read<0>(); else stores_read<1>();
               ask_add(p + 1);
             }
           }
@@ -273,7 +308,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
         }
       };
       if constexpr (TILED) {
-        if (ep.add && lane == 0) {                   // the first piece's residual is under way while the sum is still being made
+        if (through && lane == 0) {                  // the first piece's residual is under way while the sum is still being made
           stores_read<0>();
           ask_add(0);
         }
@@ -323,7 +358,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       if (lane == 0) {
         // (a residual asked for by a tile whose sum never came still has to land)
         const int none = 0;
-        if (!good && ep.add) (void)mbar_wait(&add_full[warp][0], add_phase & 1u, &none, 1000000ull);
+        if (!good && ep.add && (!WIDE || ep.add_dtype == GD_DTYPE_FP32)) (void)mbar_wait(&add_full[warp][0], add_phase & 1u, &none, 1000000ull);
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
       }
     }
@@ -380,12 +415,11 @@ cudaError_t launch_product_pair(const Product& p, uint32_t bn, cudaStream_t stre
   g.desc = mma_desc(256, bn, p.bf16, p.a.mn_major, p.b.mn_major);
   g.tiles_r = (p.ep.rows + 255) / 256;
   g.tiles_c = (p.ep.cols + bn - 1) / bn;
-  // Results and residual as pieces of 32 rows x 128 bytes, where every row starts at a multiple of 16 bytes; a residual of another type
-  // than the results, or z next to fp32 results, does not fit a piece.
-  const bool wide = g.ep.out_dtype == GD_DTYPE_FP32;
-  const bool tiled = g.ep.vectors && !(wide && g.ep.pre) && (!g.ep.add || g.ep.add_dtype == g.ep.out_dtype);
-  if (tiled && (!encode_piece(&g.out, g.ep.out, g.ep.ld_out, g.ep, g.ep.out_dtype) || (g.ep.pre && !encode_piece(&g.pre, g.ep.pre, g.ep.ld_pre, g.ep, g.ep.dtype)) ||
-                (g.ep.add && !encode_piece(&g.add, g.ep.add, g.ep.ld_add, g.ep, g.ep.add_dtype))))
+  // results and residual as pieces of 32 rows x 128 bytes, where every row starts at a multiple of 16 bytes
+  const bool tiled = g.ep.vectors, wide = g.ep.out_dtype == GD_DTYPE_FP32;
+  if (tiled && (!encode_piece(&g.out, g.ep.out, g.ep.ld_out, g.ep, g.ep.out_dtype) ||
+                (g.ep.pre && !wide && !encode_piece(&g.pre, g.ep.pre, g.ep.ld_pre, g.ep, g.ep.dtype)) ||
+                (g.ep.add && g.ep.add_dtype == g.ep.out_dtype && !encode_piece(&g.add, g.ep.add, g.ep.ld_add, g.ep, g.ep.add_dtype))))
     return cudaErrorInvalidValue;
   return bn == 256 ? launch_bn<256>(p, g, tiled, stream) : launch_bn<128>(p, g, tiled, stream);
 }

@@ -42,6 +42,8 @@ struct SplitArgs {
   uint32_t blocks_k, tiles_i, desc;
   uint32_t chain;          // k blocks the tensor cores sum before the sum is joined to the others in fp32 registers
   uint32_t stages;         // blocks the shared memory holds
+  uint32_t tiles, outer;   // outer > 1: the results are partial sums, part o of them partial_step elements on
+  uint64_t partial_step;
   uint32_t transposed;     // D's lanes are the output's columns
 };
 
@@ -55,9 +57,10 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   constexpr uint32_t kColumns = BN < 32 ? 32 : 2 * BN;      // two accumulators
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
-  const uint32_t rank = SPLITS > 1 ? cluster_rank() : 0u, tile = blockIdx.x / SPLITS;
+  const uint32_t rank = SPLITS > 1 ? cluster_rank() : 0u, place = blockIdx.x / SPLITS, part_o = place / g.tiles, tile = place - part_o * g.tiles;
   const uint32_t i0 = tile % g.tiles_i * 128u, j0 = tile / g.tiles_i * BN;
-  const uint32_t k0 = g.blocks_k * rank / SPLITS, k1 = g.blocks_k * (rank + 1) / SPLITS;     // (blocks_k < 2^26: no overflow)
+  const uint32_t parts = g.outer * SPLITS, mine = part_o * SPLITS + rank;
+  const uint32_t k0 = (uint64_t)g.blocks_k * mine / parts, k1 = (uint64_t)g.blocks_k * (mine + 1) / parts;
   if (tid == 0) {
     for (uint32_t s = 0; s < kMaxStages; ++s) mbar_init(&full[s], 1u), mbar_init(&empty[s], 1u);
     for (uint32_t s = 0; s < 2; ++s) mbar_init(&sum_full[s], 1u), mbar_init(&sum_empty[s], kSumWarps);
@@ -177,7 +180,9 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
   const uint32_t rows = (g.transposed ? BN : 128u) / SPLITS, vecs = (g.transposed ? 128u : BN) / 8u;
   const uint32_t pitch = g.transposed ? S::kPitchLanes : S::kPitchCols;
   const uint32_t out_r = (g.transposed ? j0 : i0) + rank * rows, out_c = g.transposed ? i0 : j0;
-  if (g.ep.vectors) {
+  Epilogue ep = g.ep;
+  if (g.outer > 1) ep.out = static_cast<float*>(ep.out) + part_o * g.partial_step;
+  if (ep.vectors) {
     for (uint32_t t = tid; t < rows * vecs; t += kThreadsSplit) {
       const uint32_t r = t / vecs, c = t % vecs * 8u;
       const float* at = part + (rank * rows + r) * pitch + c;
@@ -196,7 +201,7 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
         const float4 x = *reinterpret_cast<const float4*>(at), y = *reinterpret_cast<const float4*>(at + 4);
         v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
       }
-      finish8(g.ep, out_r + r, out_c + c, v);
+      finish8(ep, out_r + r, out_c + c, v);
     }
   } else {
     // rows that start anywhere: a column per thread, up to eight rows of it at a time
@@ -204,8 +209,8 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
     for (uint32_t t = tid; t < rows / group * cols; t += kThreadsSplit) {
       const uint32_t r = t / cols * group, c = t % cols;
       const float* at = part + (rank * rows + r) * pitch + c;
-      if (out_c + c >= g.ep.cols || out_r + r >= g.ep.rows) continue;
-      const float bias = g.ep.bias ? load_as(g.ep.bias, out_c + c, g.ep.bias_dtype) : 0.f;
+      if (out_c + c >= ep.cols || out_r + r >= ep.rows) continue;
+      const float bias = ep.bias ? load_as(ep.bias, out_c + c, ep.bias_dtype) : 0.f;
       float v[8];
 #pragma unroll
       for (uint32_t u = 0; u < 8; ++u) {
@@ -222,7 +227,7 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
         }
         v[u] += bias;
       }
-      finish_column(g.ep, out_r + r, out_c + c, v, group);
+      finish_column(ep, out_r + r, out_c + c, v, group);
     }
   }
   if constexpr (SPLITS > 1) {
@@ -280,14 +285,31 @@ cudaError_t launch_bn(uint32_t bn, uint32_t splits, const SplitArgs& g, uint32_t
 }
 
 uint32_t tile_bytes(uint32_t bn, bool j_mn) { return kTileA + (j_mn && bn < 64 ? 64 : bn) * kBlockK * 2; }
+// out = epilogue of the sum of `outer` partial sums, in order.  A thread takes eight neighbours of a row.
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Epilogue ep, const float* partial, uint64_t step, uint32_t ld, uint32_t outer) {
+  pdl_wait();
+  pdl_trigger();
+  const uint64_t t = (uint64_t)blockIdx.x * 256u + threadIdx.x;
+  const uint32_t vecs = ld / 8u, r = (uint32_t)(t / vecs), c = (uint32_t)(t % vecs) * 8u;
+  if (r >= ep.rows) return;
+  float v[8] = {};
+  for (uint32_t o = 0; o < outer; ++o) {
+    float w[8];
+    load8_as(partial + o * step, (uint64_t)r * ld + c, GD_DTYPE_FP32, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += w[j];
+  }
+  finish8(ep, r, c, v);
+}
+
 // The tile shape and split with the smallest estimated time, in cycles of an SM.  A block takes the longer of its products (2 BN cycles)
 // and its copies (72 bytes per cycle) for as many CTAs as share the SM; a CTA costs its start, its first block's latency and its
 // epilogue besides, a split the exchange of the partial tiles.  The constants are a least-squares fit of the logarithms of 500 measured times
 // (20 shapes, all tiles and splits; within 15 % in the middle); the choice it makes is the fastest or within 10 % of it on all but
 // one of the shapes (10 outputs' gradient of 80 x 4096: 5.7 against 4.7 us).
-SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn) {
+SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn, bool can_join) {
   const uint32_t sms = (uint32_t)sm_count();
-  SplitChoice best{false, 128, 1, 1e300};
+  SplitChoice best{false, 128, 1, 1, 1e300};
   for (int t = 0; t < 2; ++t) {
     const uint32_t ei = t ? cols : rows, ej = t ? rows : cols;
     const bool j_mn = t ? a_mn : b_mn;
@@ -296,11 +318,16 @@ SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, b
       const double tiles = std::ceil(ei / 128.0) * std::ceil(ej / (double)bn);
       for (uint32_t splits = 1; splits <= 8; splits *= 2) {
         if (splits > 1 && blocks_k < 2 * splits) break;
-        const double ctas = tiles * splits, share = ctas <= sms ? 1.0 : 2.0, blocks = std::ceil(blocks_k / (double)splits);
-        const double block = share * std::max(2.0 * bn, bytes / 72.0);
-        const double exchange = splits == 1 ? 0.0 : splits == 2 ? 2200.0 : splits == 4 ? 3750.0 : 7400.0;
-        const double cost = 2600.0 + std::ceil(ctas / (share * sms)) * (blocks * block + share * 33.0 * bn + 3750.0 + exchange);
-        if (cost < best.cost) best = SplitChoice{t != 0, bn, splits, cost};
+        // outputs of so few tiles that eight CTAs each leave SMs idle over a long k: the join is a launch and a trip through L2
+        for (uint32_t outer = 1; outer <= 16; outer *= 2) {
+          if (outer > 1 && (!can_join || splits < 8 || blocks_k < 32 * outer || (uint64_t)outer * rows * ((cols + 7) / 8 * 8) * 4 > kPartialBytes)) break;
+          const double ctas = tiles * splits * outer, share = ctas <= sms ? 1.0 : 2.0, blocks = std::ceil(blocks_k / (double)(splits * outer));
+          const double block = share * std::max(2.0 * bn, bytes / 72.0);
+          const double exchange = splits == 1 ? 0.0 : splits == 2 ? 2200.0 : splits == 4 ? 3750.0 : 7400.0;
+          const double cost =
+              2600.0 + std::ceil(ctas / (share * sms)) * (blocks * block + share * 33.0 * bn + 3750.0 + exchange) + (outer > 1 ? 6000.0 : 0.0);
+          if (cost < best.cost) best = SplitChoice{t != 0, bn, splits, outer, cost};
+        }
       }
     }
   }
@@ -310,7 +337,7 @@ SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, b
 }  // namespace
 
 SplitChoice choose_product_split(const Product& p) {
-  return choose(p.ep.rows, p.ep.cols, (p.depth + kBlockK - 1) / kBlockK, p.a.mn_major, p.b.mn_major);
+  return choose(p.ep.rows, p.ep.cols, (p.depth + kBlockK - 1) / kBlockK, p.a.mn_major, p.b.mn_major, p.partial != nullptr);
 }
 
 cudaError_t launch_product_split(const Product& p, const SplitChoice& c, cudaStream_t stream) {
@@ -331,10 +358,27 @@ cudaError_t launch_product_split(const Product& p, const SplitChoice& c, cudaStr
   g.desc = mma_desc(128, c.bn, p.bf16, oi.mn_major, oj.mn_major);
   g.transposed = c.transposed;
   const uint64_t tiles = (uint64_t)g.tiles_i * ((ej + c.bn - 1) / c.bn);
-  if (tiles * c.splits > 0x7FFFFFFFull) return cudaErrorInvalidValue;
-  g.stages = stages_for(tile_bytes(c.bn, oj.mn_major), tiles * c.splits <= (uint64_t)sm_count());
-  if (oi.mn_major) return oj.mn_major ? launch_bn<true, true>(c.bn, c.splits, g, (uint32_t)tiles, stream) : launch_bn<true, false>(c.bn, c.splits, g, (uint32_t)tiles, stream);
-  return oj.mn_major ? launch_bn<false, true>(c.bn, c.splits, g, (uint32_t)tiles, stream) : launch_bn<false, false>(c.bn, c.splits, g, (uint32_t)tiles, stream);
+  if (tiles * c.splits * c.outer > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+  g.stages = stages_for(tile_bytes(c.bn, oj.mn_major), tiles * c.splits * c.outer <= (uint64_t)sm_count());
+  g.tiles = (uint32_t)tiles;
+  g.outer = c.outer;
+  const uint32_t ld = (p.ep.cols + 7) / 8 * 8;
+  if (c.outer > 1) {
+    g.partial_step = (uint64_t)p.ep.rows * ld;
+    Epilogue& e = g.ep;
+    e.out = p.partial, e.ld_out = ld, e.out_dtype = GD_DTYPE_FP32;
+    e.bias = e.add = nullptr, e.pre = nullptr;
+    e.activation = GD_ACT_NONE;
+    e.vectors = 1;
+    g.chain = kChainBlocks;                          // (partial sums are fp32 results)
+  }
+  const uint32_t groups = (uint32_t)tiles * c.outer;
+  cudaError_t e;
+  if (oi.mn_major) e = oj.mn_major ? launch_bn<true, true>(c.bn, c.splits, g, groups, stream) : launch_bn<true, false>(c.bn, c.splits, g, groups, stream);
+  else e = oj.mn_major ? launch_bn<false, true>(c.bn, c.splits, g, groups, stream) : launch_bn<false, false>(c.bn, c.splits, g, groups, stream);
+  if (e != cudaSuccess || c.outer == 1) return e;
+  note_launches(1);
+  return launch_dependent(join_kernel, dim3((uint32_t)((g.partial_step / 8 + 255) / 256)), dim3(256), 0, stream, p.ep, (const float*)p.partial, g.partial_step, ld, c.outer);
 }
 
 }  // namespace gd

@@ -108,6 +108,23 @@ def test_linear_forward_strided(cuda_device, shape, layout):
     _check_forward(cuda_device, *shape, torch.bfloat16, "silu", layout, torch.bfloat16, torch.float32, True, True, strided=True)
 
 
+@pytest.mark.parametrize("shape", [(5, 40000, 128), (1, 16384, 8), (17, 20001, 250)], ids=str)
+def test_linear_long_contractions(cuda_device, shape):
+    """Few results over a long sum, in every direction: the output layer of a small batch backward, a long input, many rows."""
+    m, n, k = shape
+    _check_backward(cuda_device, m, n, k, torch.bfloat16, "relu", "in_out", torch.float32)
+    _check_forward(cuda_device, m, k, n, torch.bfloat16, "gelu", "out_in", torch.bfloat16, torch.float32, True, True)
+    _check_backward(cuda_device, n, m, k, torch.bfloat16, "none", "out_in", torch.float32, accumulate=True)
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_linear_wide_results(cuda_device, act):
+    """fp32 results next to 16-bit pre-activations and residuals, whole tiles and cut ones."""
+    for m, n, k in [(2048, 2048, 64), (1100, 1304, 640)]:
+        _check_forward(cuda_device, m, n, k, torch.bfloat16, act, "out_in", torch.float32, torch.float32, True, True, seed=m)
+        _check_forward(cuda_device, m, n, k, torch.float16, act, "in_out", torch.float32, None, True, False, seed=n)
+
+
 def test_linear_residual_in_place(cuda_device):
     gen = _gen(cuda_device, 5)
     x, w, r = _rand(gen, 50, 64, dtype=torch.bfloat16), _rand(gen, 64, 72, dtype=torch.bfloat16, scale=0.1), _rand(gen, 50, 72, dtype=torch.bfloat16)
