@@ -51,7 +51,7 @@ struct AdamTable {
 static_assert(sizeof(AdamTable<kMaxTensors>) <= 32764, "a kernel argument");
 
 template <int DT>
-__device__ __forceinline__ void load4(const void* base, uint64_t at, float (&x)[4]) {
+__device__ __forceinline__ void load4(const void* base, uint32_t at, float (&x)[4]) {
   if constexpr (DT == GD_DTYPE_FP32) {
     const float4 q = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(base) + at));
     x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
@@ -62,18 +62,18 @@ __device__ __forceinline__ void load4(const void* base, uint64_t at, float (&x)[
   }
 }
 template <int DT>
-__device__ __forceinline__ void store4(void* base, uint64_t at, const float (&x)[4]) {
+__device__ __forceinline__ void store4(void* base, uint32_t at, const float (&x)[4]) {
   if constexpr (DT == GD_DTYPE_FP32)
     __stcs(reinterpret_cast<float4*>(static_cast<float*>(base) + at), make_float4(x[0], x[1], x[2], x[3]));
   else
     __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at), make_uint2(pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])));
 }
 template <int DT>
-__device__ __forceinline__ float load1(const void* base, uint64_t at) {
+__device__ __forceinline__ float load1(const void* base, uint32_t at) {
   return Elem<DT>::get(static_cast<const typename Elem<DT>::type*>(base)[at]);
 }
 template <int DT>
-__device__ __forceinline__ void store1(void* base, uint64_t at, float x) {
+__device__ __forceinline__ void store1(void* base, uint32_t at, float x) {
   static_cast<typename Elem<DT>::type*>(base)[at] = Elem<DT>::put(x);
 }
 
@@ -89,8 +89,9 @@ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
 // is its own bits (exponent and mantissa run on); below 2^-6 the step is fixed, and y / 2 + 2^-7 has the bits that continue the
 // normal numbers' downwards - it is also the larger of the two exactly there, so one maximum picks the case.  The code's seven bits
 // come out in the top byte, 0xC0 too high; four of them are put right together by pack_codes().
-__device__ __forceinline__ uint32_t encode_fp8(float y, uint32_t random_bits_8_to_23) {
-  return (__float_as_uint(fmaxf(y, fmaf(y, 0.5f, 0x1p-7f))) << 4) + random_bits_8_to_23;
+// `low` is y / 2 + 2^-7.
+__device__ __forceinline__ uint32_t encode_fp8(float y, float low, uint32_t random_bits_8_to_23) {
+  return (__float_as_uint(fmaxf(y, low)) << 4) + random_bits_8_to_23;
 }
 // (top byte - 0xC0) of each: a code is below 0x80, so that is the sixth bit turned over and the seventh cleared
 __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&x)[4]) {
@@ -128,14 +129,21 @@ __device__ __forceinline__ void block_scale(float top, float* scale, float* inve
   *inverse = __uint_as_float((uint32_t)(254 - e) << 23);
 }
 
-// the update in the order the header states; nothing may be contracted into a fused multiply-add
-__device__ __forceinline__ void update(float& p, float g, float& m, float& v, float& root, const AdamScalars& s, float scale, float decay) {
-  g = __fmul_rn(g, scale);
-  m = __fadd_rn(__fmul_rn(m, s.beta1), __fmul_rn(g, s.one_minus_beta1));
-  v = __fadd_rn(__fmul_rn(v, s.beta2), __fmul_rn(__fmul_rn(g, s.one_minus_beta2), g));
-  root = __fsqrt_rn(v);
-  const float d = __fadd_rn(__fmul_rn(root, s.root_factor), s.eps);
-  p = __fsub_rn(__fmul_rn(p, decay), __fmul_rn(__fdiv_rn(m, d), s.step_size));
+// The update of two elements, in the order the header states: sums in pairs, the products that go into them singly, so that nothing is
+// contracted.
+__device__ __forceinline__ float2 apart(float2 a, float b) { return make_float2(__fmul_rn(a.x, b), __fmul_rn(a.y, b)); }
+__device__ __forceinline__ void update(float* p, const float* grad, float* m, float* v, float* root, const AdamScalars& s, float scale, float decay) {
+  const float2 g = mul2(make_float2(grad[0], grad[1]), both(scale)), c = mul2(g, both(s.one_minus_beta2));
+  const float2 m2 = add2(apart(make_float2(m[0], m[1]), s.beta1), apart(g, s.one_minus_beta1));
+  const float2 v2 = add2(apart(make_float2(v[0], v[1]), s.beta2), make_float2(__fmul_rn(c.x, g.x), __fmul_rn(c.y, g.y)));
+  const float2 r = make_float2(__fsqrt_rn(v2.x), __fsqrt_rn(v2.y));
+  const float2 d = add2(apart(r, s.root_factor), both(s.eps));
+  const float2 q = apart(make_float2(__fdiv_rn(m2.x, d.x), __fdiv_rn(m2.y, d.y)), -s.step_size);
+  const float2 p2 = add2(apart(make_float2(p[0], p[1]), decay), q);
+  p[0] = p2.x, p[1] = p2.y;
+  m[0] = m2.x, m[1] = m2.y;
+  v[0] = v2.x, v[1] = v2.y;
+  root[0] = r.x, root[1] = r.y;
 }
 
 // What a lane holds of a block: four elements.
@@ -146,8 +154,19 @@ struct Block {
   float ms, vs;
 };
 
+// The chunk of a CTA: the tensor's pointers moved to its start, so that everything in it is a 32-bit offset from an address the whole CTA shares.
+struct Chunk {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  uint32_t n;
+};
 template <int PT, int GT>
-__device__ __forceinline__ void load_block(Block<32>& b, const TensorEntry& t, uint64_t at, uint32_t lane) {
+__device__ __forceinline__ void load_block(Block<32>& b, const Chunk& t, uint32_t at, uint32_t lane) {
   load4<PT>(t.param, at + 4 * lane, b.p);
   load4<GT>(t.grad, at + 4 * lane, b.g);
   load4<GD_DTYPE_FP32>(t.m, at + 4 * lane, b.m);
@@ -162,9 +181,9 @@ __device__ __forceinline__ void ask(void* dst, const void* src) {
   else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(BYTES) : "memory");
 }
 template <int PT, int GT>
-__device__ __forceinline__ void ask_block(unsigned char* stage, const TensorEntry& t, uint64_t at, uint32_t lane) {
+__device__ __forceinline__ void ask_block(unsigned char* stage, const Chunk& t, uint32_t at, uint32_t lane) {
   constexpr uint32_t pb = PT == GD_DTYPE_FP32 ? 16 : 8, gb = GT == GD_DTYPE_FP32 ? 16 : 8;
-  const uint64_t e = at / 4 + lane;
+  const uint32_t e = at / 4 + lane;
   ask<pb>(stage + pb * lane, static_cast<const unsigned char*>(t.param) + e * pb);
   ask<gb>(stage + 512 + gb * lane, static_cast<const unsigned char*>(t.grad) + e * gb);
   ask<4>(stage + 1024 + 4 * lane, static_cast<const unsigned char*>(t.m) + e * 4);
@@ -193,11 +212,11 @@ __device__ __forceinline__ void take_block(Block<8>& b, const unsigned char* sta
 }
 // Element by element: element j of a lane is at + lane + 32 j.  What lies past the end is held as zeros.
 template <int PT, int GT, int BITS>
-__device__ __forceinline__ void load_ragged(Block<BITS>& b, const TensorEntry& t, uint64_t at, uint32_t lane) {
+__device__ __forceinline__ void load_ragged(Block<BITS>& b, const Chunk& t, uint32_t at, uint32_t lane) {
   b.mc = b.vc = 0u;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint64_t e = at + lane + 32 * j;
+    const uint32_t e = at + lane + 32 * j;
     const bool in = e < t.n;
     b.p[j] = in ? load1<PT>(t.param, e) : 0.f;
     b.g[j] = in ? load1<GT>(t.grad, e) : 0.f;
@@ -217,19 +236,19 @@ __device__ __forceinline__ void load_ragged(Block<BITS>& b, const TensorEntry& t
 
 // The update of a block; with 8-bit moments also their new codes (mc, vc) and scales (ms, vs).
 template <bool RAGGED, int BITS>
-__device__ __forceinline__ void update_block(Block<BITS>& b, const AdamScalars& s, float scale, float decay, uint32_t random_base, uint64_t at, uint64_t n,
-                                             uint32_t lane) {
+__device__ __forceinline__ void update_block(Block<BITS>& b, const AdamScalars& s, float scale, float decay, uint32_t random_base, uint32_t first, uint32_t at,
+                                             uint32_t n, uint32_t lane) {
   float root[4];
   if constexpr (BITS == 8) {
     const float2 m01 = decode_fp8x2(b.mc & 0xFFFFu), m23 = decode_fp8x2(b.mc >> 16);
     const float2 v01 = decode_fp8x2(b.vc & 0xFFFFu), v23 = decode_fp8x2(b.vc >> 16);
-    b.m[0] = __fmul_rn(m01.x, b.ms), b.m[1] = __fmul_rn(m01.y, b.ms), b.m[2] = __fmul_rn(m23.x, b.ms), b.m[3] = __fmul_rn(m23.y, b.ms);
-    const float r[4] = {__fmul_rn(v01.x, b.vs), __fmul_rn(v01.y, b.vs), __fmul_rn(v23.x, b.vs), __fmul_rn(v23.y, b.vs)};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) b.v[j] = __fmul_rn(r[j], r[j]);
+    const float2 ma = mul2(m01, both(b.ms)), mb = mul2(m23, both(b.ms)), ra = mul2(v01, both(b.vs)), rb = mul2(v23, both(b.vs));
+    const float2 va = mul2(ra, ra), vb = mul2(rb, rb);
+    b.m[0] = ma.x, b.m[1] = ma.y, b.m[2] = mb.x, b.m[3] = mb.y;
+    b.v[0] = va.x, b.v[1] = va.y, b.v[2] = vb.x, b.v[3] = vb.y;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) update(b.p[j], b.g[j], b.m[j], b.v[j], root[j], s, scale, decay);
+  for (int j = 0; j < 4; j += 2) update(b.p + j, b.g + j, b.m + j, b.v + j, root + j, s, scale, decay);
   if constexpr (BITS == 8) {
     if constexpr (RAGGED) {
 #pragma unroll
@@ -243,13 +262,19 @@ __device__ __forceinline__ void update_block(Block<BITS>& b, const AdamScalars& 
     block_scale(v_top, &b.vs, &v_inverse);
     uint32_t cm[4], cv[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t e = (uint32_t)at + (RAGGED ? lane + 32 * j : 4 * lane + j);
-      const uint32_t h = mix32(e * 0x9E3779B9u + random_base);
-      cm[j] = encode_fp8(__fmul_rn(fabsf(b.m[j]), m_inverse), __byte_perm(h, 0u, 0x4324));
-      float y = __fmul_rn(root[j], v_inverse);
-      if (root[j] > 0.f) y = fmaxf(y, 0x1p-9f);          // at least the smallest positive code, whose step this is
-      cv[j] = encode_fp8(y, __byte_perm(h, 0u, 0x4104));
+    for (int j = 0; j < 4; j += 2) {
+      const float2 ym = mul2(make_float2(fabsf(b.m[j]), fabsf(b.m[j + 1])), both(m_inverse));
+      float2 yv = mul2(make_float2(root[j], root[j + 1]), both(v_inverse));
+      if (root[j] > 0.f) yv.x = fmaxf(yv.x, 0x1p-9f);        // at least the smallest positive code, whose step this is
+      if (root[j + 1] > 0.f) yv.y = fmaxf(yv.y, 0x1p-9f);
+      const float2 lm = fma2(ym, both(0.5f), both(0x1p-7f)), lv = fma2(yv, both(0.5f), both(0x1p-7f));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t e = first + at + (RAGGED ? lane + 32 * (j + i) : 4 * lane + j + i);
+        const uint32_t h = mix32(e * 0x9E3779B9u + random_base);
+        cm[j + i] = encode_fp8(i ? ym.y : ym.x, i ? lm.y : lm.x, __byte_perm(h, 0u, 0x4324));
+        cv[j + i] = encode_fp8(i ? yv.y : yv.x, i ? lv.y : lv.x, __byte_perm(h, 0u, 0x4104));
+      }
     }
     const uint32_t signs[4] = {__float_as_uint(b.m[0]), __float_as_uint(b.m[1]), __float_as_uint(b.m[2]), __float_as_uint(b.m[3])};
     b.mc = pack_codes(cm);
@@ -263,7 +288,7 @@ __device__ __forceinline__ void update_block(Block<BITS>& b, const AdamScalars& 
 }
 
 template <int PT, int BITS>
-__device__ __forceinline__ void store_block(const Block<BITS>& b, const TensorEntry& t, int copy_dtype, uint64_t at, uint32_t lane) {
+__device__ __forceinline__ void store_block(const Block<BITS>& b, const Chunk& t, int copy_dtype, uint32_t at, uint32_t lane) {
   store4<PT>(t.param, at + 4 * lane, b.p);
   if (t.copy) {
     if (copy_dtype == GD_DTYPE_BF16) store4<GD_DTYPE_BF16>(t.copy, at + 4 * lane, b.p);
@@ -279,10 +304,10 @@ __device__ __forceinline__ void store_block(const Block<BITS>& b, const TensorEn
   }
 }
 template <int PT, int BITS>
-__device__ __forceinline__ void store_ragged(const Block<BITS>& b, const TensorEntry& t, int copy_dtype, uint64_t at, uint32_t lane) {
+__device__ __forceinline__ void store_ragged(const Block<BITS>& b, const Chunk& t, int copy_dtype, uint32_t at, uint32_t lane) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint64_t e = at + lane + 32 * j;
+    const uint32_t e = at + lane + 32 * j;
     if (e >= t.n) continue;
     store1<PT>(t.param, e, b.p[j]);
     if (t.copy) {
@@ -309,19 +334,32 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     const uint32_t mid = (lo + hi) >> 1;
     if (table.t[mid].chunk0 <= blockIdx.x) lo = mid; else hi = mid;
   }
-  const TensorEntry t = table.t[lo];
-  const uint32_t lane = lane_id(), random_base = s.seed + t.index * 0x85EBCA77u;
-  uint64_t at = (uint64_t)(blockIdx.x - t.chunk0) * kChunk<BITS> + (threadIdx.x >> 5) * 128u;
-  const uint64_t end = min(t.n, (uint64_t)(blockIdx.x - t.chunk0 + 1) * kChunk<BITS>);
+  const TensorEntry& of = table.t[lo];
+  const uint64_t start = (uint64_t)(blockIdx.x - of.chunk0) * kChunk<BITS>;
+  const uint32_t end = (uint32_t)min(of.n - start, (uint64_t)kChunk<BITS>), first = (uint32_t)start;
+  const uint32_t pb = sizeof(typename Elem<PT>::type), gb = sizeof(typename Elem<GT>::type), cb = s.copy_dtype == GD_DTYPE_FP32 ? 4 : 2, sb = BITS / 8;
+  Chunk t;
+  t.param = static_cast<char*>(of.param) + start * pb;
+  t.grad = static_cast<const char*>(of.grad) + start * gb;
+  t.m = static_cast<char*>(of.m) + start * sb;
+  t.v = static_cast<char*>(of.v) + start * sb;
+  t.copy = of.copy ? static_cast<char*>(of.copy) + start * cb : nullptr;
+  t.m_scale = of.m_scale + start / 128;
+  t.v_scale = of.v_scale + start / 128;
+  t.n = end;
+  const float decay = of.decay;
+  const bool vectors = of.vectors;
+  const uint32_t lane = lane_id(), random_base = s.seed + of.index * 0x85EBCA77u;
+  uint32_t at = (threadIdx.x >> 5) * 128u;
   pdl_wait();
   pdl_trigger();
   const float scale = s.grad_scale_dev ? __fmul_rn(s.grad_scale, *s.grad_scale_dev) : s.grad_scale;
   Block<BITS> b;
   if constexpr (BITS == 8) {
     extern __shared__ __align__(16) unsigned char smem[];
-    if (t.vectors && at + 128u <= end) {
+    if (vectors && at + 128u <= end) {
       unsigned char* ring = smem + (threadIdx.x >> 5) * (kStages * kStageBytes);
-      uint64_t ask = at;
+      uint32_t ask = at;
 #pragma unroll
       for (int i = 0; i < kStages - 1; ++i, ask += kStride) {
         if (ask + 128u <= end) ask_block<PT, GT>(ring + i * kStageBytes, t, ask, lane);
@@ -333,20 +371,20 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
         if (ask + 128u <= end) ask_block<PT, GT>(ring + (i + kStages - 1) % kStages * kStageBytes, t, ask, lane);
         asm volatile("cp.async.commit_group;" ::: "memory");
         take_block<PT, GT>(b, ring + i % kStages * kStageBytes, lane);
-        update_block<false, BITS>(b, s, scale, t.decay, random_base, at, t.n, lane);
+        update_block<false, BITS>(b, s, scale, decay, random_base, first, at, end, lane);
         if (lane == 0) t.m_scale[at >> 7] = b.ms, t.v_scale[at >> 7] = b.vs;
         store_block<PT, BITS>(b, t, s.copy_dtype, at, lane);
       }
     }
   } else {
     Block<BITS> next;
-    if (t.vectors && at + 128u <= end) {
+    if (vectors && at + 128u <= end) {
       load_block<PT, GT>(b, t, at, lane);
       while (true) {
-        const uint64_t after = at + kStride;
+        const uint32_t after = at + kStride;
         const bool more = after + 128u <= end;
         if (more) load_block<PT, GT>(next, t, after, lane);        // under way while this block is worked on
-        update_block<false, BITS>(b, s, scale, t.decay, random_base, at, t.n, lane);
+        update_block<false, BITS>(b, s, scale, decay, random_base, first, at, end, lane);
         store_block<PT, BITS>(b, t, s.copy_dtype, at, lane);
         at = after;
         if (!more) break;
@@ -358,7 +396,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
   while (at < end) {
     Block<BITS> next;
     if (at + kStride < end) load_ragged<PT, GT, BITS>(next, t, at + kStride, lane);
-    update_block<true, BITS>(b, s, scale, t.decay, random_base, at, t.n, lane);
+    update_block<true, BITS>(b, s, scale, decay, random_base, first, at, end, lane);
     if constexpr (BITS == 8) {
       if (lane == 0) t.m_scale[at >> 7] = b.ms, t.v_scale[at >> 7] = b.vs;
     }
