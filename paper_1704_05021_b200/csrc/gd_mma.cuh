@@ -62,7 +62,7 @@ __device__ __forceinline__ void send_peer2(uint32_t address, float2 v, uint32_t 
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(address), "f"(v.x), "f"(v.y), "r"(barrier) : "memory");
 }
 
-// True in one thread of the (converged) warp.  The instructions that ask for copies and products take their operands from registers of
+// True in one thread of the (converged) warp, the same one every time.  The instructions that ask for copies and products take their operands from registers of
 // the whole warp; behind a branch on this the compiler knows that one thread is left and issues them directly.
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;

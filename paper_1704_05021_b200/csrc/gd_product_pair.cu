@@ -178,7 +178,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       const auto release = [&](uint32_t buf) {       // this warp has read its part of the sum
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_peer(peer_address(smem_u32(&sum_empty[buf]), 0));
+        if (elect_one()) mbar_arrive_peer(peer_address(smem_u32(&sum_empty[buf]), 0));
       };
       // Lane l holds the bias of columns 4 l .. 4 l + 3; asked for before the sum is there.
       float bias[4] = {0.f, 0.f, 0.f, 0.f};
@@ -204,7 +204,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           unsigned char* mine = pieces + at * kPieceBytes + lane * 128u;
           unsigned char* z = pieces + kPieceBytes + lane * 128u;
           if (!through || two) {                     // (with a residual the buffer was free before its copy was asked for)
-            if (lane == 0) { if (two) stores_read<0>(); else stores_read<1>(); }
+            if (elect_one()) { if (two) stores_read<0>(); else stores_read<1>(); }
             __syncwarp();
           }
           if (ep.bias) {
@@ -217,7 +217,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
               for (uint32_t j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(z + (j ^ (lane & 7u)) * 16u) = narrow8(v + 8 * j, ep.dtype);
               fence_async();
               __syncwarp();
-              if (lane == 0 && inside) tile_store(&g.pre, pieces + kPieceBytes, (int32_t)c, (int32_t)r0);
+              if (elect_one() && inside) tile_store(&g.pre, pieces + kPieceBytes, (int32_t)c, (int32_t)r0);
             }
           }
           if constexpr (WIDE) {
@@ -281,7 +281,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           }
           fence_async();
           __syncwarp();
-          if (lane == 0) {
+          if (elect_one()) {
             if (inside) tile_store(&g.out, pieces + at * kPieceBytes, (int32_t)c, (int32_t)r0);
             if (through && p + 1 < kPieces) {
               if (two) stores_read<0>(); else stores_read<1>();
@@ -308,7 +308,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
         }
       };
       if constexpr (TILED) {
-        if (through && lane == 0) {                  // the first piece's residual is under way while the sum is still being made
+        if (through && elect_one()) {                  // the first piece's residual is under way while the sum is still being made
           stores_read<0>();
           ask_add(0);
         }
@@ -355,7 +355,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       }
     }
     if constexpr (TILED) {
-      if (lane == 0) {
+      if (elect_one()) {
         // (a residual asked for by a tile whose sum never came still has to land)
         const int none = 0;
         if (!good && ep.add && (!WIDE || ep.add_dtype == GD_DTYPE_FP32)) (void)mbar_wait(&add_full[warp][0], add_phase & 1u, &none, 1000000ull);
