@@ -231,8 +231,8 @@ typedef struct gd_push {
  * entry's layer, or its layer and column in column-means mode).
  * One fused multiply-add in fp32 per entry; with alpha = 1 the result is fl32(p + value).
  * Pushes are applied one after another in stream order (unless GD_APPLY_ATOMIC is set); indices inside one push are unique.
- * Entries whose index lies outside every shard are skipped.  The optimiser is not part of
- * this library.
+ * Entries whose index lies outside every shard are skipped.  A server with another update than this
+ * adds the pushes into zeros and hands the sum to gd_adamw_step (gd_train.h).
  */
 /* gd_apply_args.flags */
 enum {

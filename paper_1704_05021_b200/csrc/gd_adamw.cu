@@ -1,12 +1,17 @@
 // One AdamW update of many tensors (gd_adamw_step): a stream over parameters, gradients and moments.
 //
 // The update is elementwise, so the bytes bound it: 28 per element with fp32 throughout, 16.1 with the moments in
-// 8 bits.  One launch takes up to kMaxTensors tensors, whose table travels as the kernel argument (no device copy, no
-// allocation); a CTA takes one chunk of kChunk consecutive elements of one tensor.  A warp works on blocks of 128 elements, four
-// per lane in one 16-byte access, because 128 is also the unit that shares a scale in the 8-bit moments: its largest
-// magnitude is one warp reduction, and nothing but the warp has to agree on it.
+// 8 bits - where the instructions (division and root to the last bit, random rounding, some 90 per element) come first.  One launch
+// takes up to kMaxTensors tensors, whose table travels as the kernel argument (no device copy, no allocation); a CTA takes one
+// chunk of kChunk consecutive elements of one tensor.  A warp works on blocks of 128 elements, four per lane in one 16-byte
+// access, because 128 is also the unit that shares a scale in the 8-bit moments: its largest magnitude is one warp
+// reduction, and nothing but the warp has to agree on it.  With 32-bit moments the next block waits in registers; with 8-bit ones,
+// whose arithmetic needs them, three blocks are on their way into shared memory.
 // A tensor whose buffers do not all start on a vector boundary (pieces of a flat vector do not), and a tensor's last,
 // partial block, go element by element, lane-contiguous, with the same arithmetic.
+//
+// Measured (one B200): 138 M elements, 32 bits 565 us = 6.8 TB/s; 8 bits with bf16 gradients and copy 425 us (460 under sustained load,
+// when the clocks fall; 706 with the loads through registers and codes made one by one), 90 % of the issue slots used.
 #include <cmath>
 
 #include "gd_train.cuh"

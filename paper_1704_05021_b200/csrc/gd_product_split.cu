@@ -1,13 +1,16 @@
-// The product for outputs of few tiles: one tile of 128 x BN per CTA, the
-// contraction split over a cluster of 1 .. 8 CTAs.
+// The product for outputs of few tiles: one tile of 128 x BN per CTA, the contraction split over a cluster of 1 .. 8 CTAs.
 //
 // What bounds these calls is not arithmetic but how many SMs take part and how many bytes each keeps in flight: one row through a
 // 4096 x 4096 layer is 33 MB of weights and next to no products.  So the longer side of the output lies on the tile's
 // 128 accumulator lanes and the shorter one on its BN columns (the output is then written transposed, which costs nothing: the lanes of
 // a warp are neighbours in memory), BN shrinks with the shorter side, and where there are fewer tiles than SMs the CTAs of
 // a cluster take a part of k each.  They put their partial tiles into shared memory and every one sums, in rank order, the slice of
-// rows it then finishes and stores: no workspace, no atomics, the same bits every time.  Two CTAs share an SM, so one's
-// copies run under the other's epilogue.
+// rows it then finishes and stores: no workspace, no atomics, the same bits every time.  Where even eight CTAs per tile leave SMs idle over
+// a long k, up to 16 such clusters take a part each and a second launch joins their sums (in workspace, in order).  Two CTAs share an SM
+// where there are enough, so one's copies run under the other's epilogue.
+//
+// Measured (one B200, passes back to back on the device): 1 x 4096 x 4096 8.7 us (5.2 of weights), 512 x 512 x 512 3.7 us,
+// 80 x 4096 x 784 5.0 us, 256 x 256 x 8192 8.8 us (24.6 without the split).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -15,7 +18,6 @@
 #include "gd_mma.cuh"
 
 namespace gd {
-
 namespace {
 
 constexpr uint32_t kSumWarps = 8, kThreadsSplit = (kSumWarps + 2) * 32;      // + one warp that asks for copies, one that issues products
