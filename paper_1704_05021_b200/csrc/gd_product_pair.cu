@@ -169,7 +169,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
     const uint32_t quarter = warp & 3u, half = (warp >> 2) * kHalf;
     unsigned char* pieces = smem + kPairStages * kPairStage + warp * 2 * kPieceBytes;
     const Epilogue& ep = g.ep;
-    uint32_t chain = 0, add_phase = 0;
+    uint32_t chain = 0, add_phase = 0, turn = 0;     // turn: pieces so far; they take the two buffers in turn, across tiles too
     for (uint32_t t = pair; good && t < tiles; t += pairs) {
       uint32_t tr, tc;
       tile_place(t, g.tiles_r, g.tiles_c, &tr, &tc);
@@ -188,9 +188,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           if (4 * lane < kHalf && c0 + 4 * lane + i < ep.cols) bias[i] = load_as(ep.bias, c0 + 4 * lane + i, ep.bias_dtype);
       }
       const bool through = ep.add && (!WIDE || ep.add_dtype == GD_DTYPE_FP32);      // the residual comes as pieces; one of 16 bits next to fp32 results does not fit
-      // The residual of piece p, into the buffer whose place the result takes (buffer 0 alone where z also needs one).
-      const auto ask_add = [&](uint32_t p) {
-        const uint32_t at = !WIDE && ep.pre ? 0u : p & 1u;
+      // The residual of piece p, `ahead` turns from now, into the buffer whose place the result takes (buffer 0 alone where z also needs one).
+      const auto ask_add = [&](uint32_t p, uint32_t ahead) {
+        const uint32_t at = !WIDE && ep.pre ? 0u : (turn + ahead) & 1u;
         mbar_arrive_expect_tx(&add_full[warp][at], kPieceBytes);
         tile_load(pieces + at * kPieceBytes, &g.add, (int32_t)(c0 + p * W), (int32_t)r0, &add_full[warp][at]);
       };
@@ -200,7 +200,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
         if constexpr (TILED) {
           const bool inside = r0 < ep.rows && c < ep.cols;
           const bool two = !WIDE && ep.pre;          // z takes the second buffer
-          const uint32_t at = two ? 0u : p & 1u;
+          const uint32_t at = two ? 0u : turn & 1u;
           unsigned char* mine = pieces + at * kPieceBytes + lane * 128u;
           unsigned char* z = pieces + kPieceBytes + lane * 128u;
           if (!through || two) {                     // (with a residual the buffer was free before its copy was asked for)
@@ -285,9 +285,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
             if (inside) tile_store(&g.out, pieces + at * kPieceBytes, (int32_t)c, (int32_t)r0);
             if (through && p + 1 < kPieces) {
               if (two) stores_read<0>(); else stores_read<1>();
-              ask_add(p + 1);
+              ask_add(p + 1, 1);
             }
           }
+          ++turn;
         } else {
           // any pitch: a row of the piece at a time, one column per lane
           float* piece = reinterpret_cast<float*>(pieces);
@@ -310,7 +311,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       if constexpr (TILED) {
         if (through && elect_one()) {                  // the first piece's residual is under way while the sum is still being made
           stores_read<0>();
-          ask_add(0);
+          ask_add(0, 0);
         }
       }
       if constexpr (CHAINED) {
@@ -358,7 +359,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       if (elect_one()) {
         // (a residual asked for by a tile whose sum never came still has to land)
         const int none = 0;
-        if (!good && ep.add && (!WIDE || ep.add_dtype == GD_DTYPE_FP32)) (void)mbar_wait(&add_full[warp][0], add_phase & 1u, &none, 1000000ull);
+        if (!good && ep.add && (!WIDE || ep.add_dtype == GD_DTYPE_FP32)) (void)mbar_wait(&add_full[warp][!WIDE && ep.pre ? 0 : turn & 1u], add_phase >> (!WIDE && ep.pre ? 0 : turn & 1u) & 1u, &none, 1000000ull);
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
       }
     }

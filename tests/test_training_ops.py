@@ -269,6 +269,23 @@ def test_linear_repeats_bit_for_bit(cuda_device):
         assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
 
 
+@pytest.mark.parametrize("shape", [(4000, 1500, 1000), (8192, 1280, 128), (6000, 1000, 64)], ids=str)
+def test_linear_many_tiles_repeat_bit_for_bit(cuda_device, shape):
+    """Many tiles per pair of CTAs with little to sum: what leaves one tile must not meet what the next one writes."""
+    m, n, k = shape
+    gen = _gen(cuda_device, 12)
+    for layout in ("in_out", "out_in"):
+        x, w = _rand(gen, m, k, dtype=torch.bfloat16), _rand(gen, *((k, n) if layout == "in_out" else (n, k)), dtype=torch.bfloat16)
+        r = _rand(gen, m, n, dtype=torch.bfloat16)
+        s = T.LinearSession(k, n, m, w_layout=layout, device=cuda_device, any_layout=True)
+        for residual in (None, r):
+            first = s.forward(x, w, residual=residual)
+            plain = x.float() @ (w if layout == "in_out" else w.t()).float() + (0 if residual is None else residual.float())
+            assert float((first.float() - plain).abs().max()) <= 2.0 ** -7 * float(plain.abs().max())
+            for _ in range(10):
+                assert torch.equal(first, s.forward(x, w, residual=residual, out=torch.empty_like(first)))
+
+
 def test_linear_on_another_stream(cuda_device):
     gen = _gen(cuda_device, 4)
     x, w = _rand(gen, 33, 72, dtype=torch.bfloat16), _rand(gen, 72, 40, dtype=torch.bfloat16)
