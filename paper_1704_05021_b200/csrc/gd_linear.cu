@@ -18,7 +18,7 @@ namespace {
 // pairs without work: weights of 1500 x 1000 over 4000 rows 28.9 against 35.2 us (split kernel 33.4); 8192 x 4096 x 4096 262 against 175.
 double cost_product_pair(const Product& p, uint32_t bn) {
   const double tiles = std::ceil(p.ep.rows / 256.0) * std::ceil(p.ep.cols / (double)bn), blocks_k = std::ceil(p.depth / (double)kBlockK);
-  const double waves = std::ceil(tiles / (sm_count() / 2));
+  const double full = tiles / (sm_count() / 2), waves = p.followed ? std::max(1.0, full) : std::ceil(full);
   return bn == 256 ? 12600.0 + waves * std::max(600.0 * blocks_k, 9000.0) : 10500.0 + waves * std::max(440.0 * blocks_k, 6000.0);
 }
 }  // namespace
@@ -430,6 +430,7 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     p.b = w, p.b.mn_major = !in_out;
     p.depth = (uint32_t)n;
     p.partial = n >= kLongDepth ? partial : nullptr;
+    p.followed = has_dw && n < kLongDepth;
     p.ep.out = a->dx, p.ep.ld_out = a->ld_dx, p.ep.out_dtype = a->dtype;
     p.ep.rows = (uint32_t)m, p.ep.cols = (uint32_t)k;
     p.ep.vectors = vector_rows(a->dx, row_step(a->ld_dx, m, k), a->dtype);
@@ -442,6 +443,8 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     p.partial = m >= kLongDepth ? partial : nullptr;     // (the product before this one has been joined by the time it is written)
     p.ep.out = a->dw, p.ep.ld_out = a->ld_dw, p.ep.out_dtype = a->dw_dtype;
     p.ep.rows = (uint32_t)w_rows, p.ep.cols = (uint32_t)w_cols;
+    p.followed = false;
+    p.beside = has_dx && n < kLongDepth;                  // (a joined dx has a launch in between, and the partial sums' place)
     if (add) p.ep.add = a->dw, p.ep.ld_add = a->ld_dw, p.ep.add_dtype = GD_DTYPE_FP32;
     p.ep.vectors = vector_rows(a->dw, row_step(a->ld_dw, w_rows, w_cols), a->dw_dtype);
     if (launch_product(p, stream) != cudaSuccess) return GD_ERR_CUDA;

@@ -329,6 +329,10 @@ struct Product {
   Epilogue ep;
   int* status;
   float* partial;      // kPartialBytes of workspace where the depth is at least kLongDepth, else NULL
+  // The launch before this one in the stream is a product too, waits for all before it, and neither touches what the other writes: this one
+  // runs on the SMs that the other leaves idle in its last wave (pdl_wait stands at its end, so that whatever follows has both).
+  bool beside;
+  bool followed;       // the launch after this one is such a product: what this one's last wave leaves idle is no loss
 };
 constexpr uint64_t kLongDepth = 16384, kPartialBytes = 2u << 20;
 // How many k blocks the tensor cores may sum in one go.  Their fp32 accumulator truncates: measured against 64 bits the relative

@@ -38,6 +38,7 @@ struct PairArgs {
   int* status;
   uint32_t blocks_k, chain, desc;
   uint32_t tiles_r, tiles_c;
+  uint32_t beside;
 };
 
 __device__ __forceinline__ void tile_load_pair(void* dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t barrier) {
@@ -98,7 +99,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
   const uint32_t tmem = s_tmem;
   const volatile int* abort = &s_abort;
   bool good = true;
-  pdl_wait();
+  if (!g.beside) pdl_wait();                         // (the other product's CTAs are past theirs: all have triggered)
   pdl_trigger();
 
   if (warp == kPairWarps) {                          // copies: each CTA its halves, all counted on the leader's barrier
@@ -371,6 +372,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
   cluster_arrive();                                  // neither CTA leaves while the other's products read its memory or its warps signal
   cluster_wait();
   if (warp == kPairWarps) tmem_free<2>(tmem, 2 * BN);
+  if (g.beside) pdl_wait();
 }
 
 template <int BN, bool A_MN, bool B_MN, bool CHAINED, bool TILED, bool WIDE>
@@ -411,6 +413,7 @@ cudaError_t launch_product_pair(const Product& p, uint32_t bn, cudaStream_t stre
     return cudaErrorInvalidValue;
   g.ep = p.ep;
   g.status = p.status;
+  g.beside = p.beside;
   g.blocks_k = (p.depth + kBlockK - 1) / kBlockK;
   g.chain = chain_blocks(p);
   g.desc = mma_desc(256, bn, p.bf16, p.a.mn_major, p.b.mn_major);

@@ -47,6 +47,7 @@ struct SplitArgs {
   uint32_t tiles, outer;   // outer > 1: the results are partial sums, part o of them partial_step elements on
   uint64_t partial_step;
   uint32_t transposed;     // D's lanes are the output's columns
+  uint32_t beside;
 };
 
 template <bool A_MN, bool B_MN, int BN, int SPLITS>
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
   fence_after();
   const uint32_t tmem = s_tmem;
   const volatile int* abort = &s_abort;
-  pdl_wait();
+  if (!g.beside) pdl_wait();                         // (the other product's CTAs are past theirs: all have triggered)
   pdl_trigger();
 
   float* part = reinterpret_cast<float*>(smem);
@@ -239,6 +240,7 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
     __syncthreads();
   }
   if (warp == kSumWarps) tmem_free<1>(tmem, kColumns);
+  if (g.beside) pdl_wait();
 }
 
 template <bool A_MN, bool B_MN, int BN, int SPLITS>
@@ -309,7 +311,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Epilo
 // epilogue besides, a split the exchange of the partial tiles.  The constants are a least-squares fit of the logarithms of 500 measured times
 // (20 shapes, all tiles and splits; within 15 % in the middle); the choice it makes is the fastest or within 10 % of it on all but
 // one of the shapes (10 outputs' gradient of 80 x 4096: 5.7 against 4.7 us).
-SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn, bool can_join) {
+SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, bool b_mn, bool can_join, bool followed) {
   const uint32_t sms = (uint32_t)sm_count();
   SplitChoice best{false, 128, 1, 1, 1e300};
   for (int t = 0; t < 2; ++t) {
@@ -327,7 +329,7 @@ SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, b
           const double block = share * std::max(2.0 * bn, bytes / 72.0);
           const double exchange = splits == 1 ? 0.0 : splits == 2 ? 2200.0 : splits == 4 ? 3750.0 : 7400.0;
           const double cost =
-              2600.0 + std::ceil(ctas / (share * sms)) * (blocks * block + share * 33.0 * bn + 3750.0 + exchange) + (outer > 1 ? 6000.0 : 0.0);
+              2600.0 + (followed ? std::max(1.0, ctas / (share * sms)) : std::ceil(ctas / (share * sms))) * (blocks * block + share * 33.0 * bn + 3750.0 + exchange) + (outer > 1 ? 6000.0 : 0.0);
           if (cost < best.cost) best = SplitChoice{t != 0, bn, splits, outer, cost};
         }
       }
@@ -339,7 +341,7 @@ SplitChoice choose(uint32_t rows, uint32_t cols, uint32_t blocks_k, bool a_mn, b
 }  // namespace
 
 SplitChoice choose_product_split(const Product& p) {
-  return choose(p.ep.rows, p.ep.cols, (p.depth + kBlockK - 1) / kBlockK, p.a.mn_major, p.b.mn_major, p.partial != nullptr);
+  return choose(p.ep.rows, p.ep.cols, (p.depth + kBlockK - 1) / kBlockK, p.a.mn_major, p.b.mn_major, p.partial != nullptr, p.followed);
 }
 
 cudaError_t launch_product_split(const Product& p, const SplitChoice& c, cudaStream_t stream) {
@@ -354,6 +356,7 @@ cudaError_t launch_product_split(const Product& p, const SplitChoice& c, cudaStr
     return cudaErrorInvalidValue;
   g.ep = p.ep;
   g.status = p.status;
+  g.beside = p.beside;
   g.blocks_k = blocks_k;
   g.chain = chain_blocks(p);
   g.tiles_i = (ei + 127) / 128;
