@@ -133,7 +133,7 @@ cudaError_t launch_pack(const Packs& all, cudaStream_t stream) {
 // thread takes 8 neighbouring columns of every so many rows.  The threads' sums meet by shuffles and in shared memory, the CTAs' are sent
 // to the first of the cluster and counted there, always in the same order: no atomics, no second launch.  Bound by the bytes (dy and
 // pre read, dz written) where there are many columns, by the 25 instructions an entry of GELU or SiLU takes where there are few.
-constexpr uint32_t kSlopeCtas = 8, kSlopeThreads = 512, kSlopeWarps = kSlopeThreads / 32, kAhead = 2;
+constexpr uint32_t kSlopeCtas = 8, kSlopeThreads = 512, kSlopeWarps = kSlopeThreads / 32;
 struct SlopeArgs {
   const void* dy;
   const void* pre;
@@ -145,8 +145,33 @@ struct SlopeArgs {
   uint32_t accumulate, vectors;
   Packs packs;
 };
-template <int DT>
+// Eight 16-bit elements from column c of a row that starts anywhere: the two aligned vectors around them, moved into place. Both lie within
+// the row where `inner` holds; a row's ends are read element by element.
+__device__ __forceinline__ bool inner(uint32_t c, uint32_t cols) { return c >= 8 && c + 16 <= cols; }
+struct Around {
+  uint4 lo, hi;
+};
+__device__ __forceinline__ Around load_around(const uint16_t* s) {
+  const uint4* at = reinterpret_cast<const uint4*>((uintptr_t)s & ~(uintptr_t)15);
+  return Around{at[0], at[1]};
+}
+__device__ __forceinline__ uint4 into_place(const Around& a, const uint16_t* s) {
+  const uint32_t off = (uint32_t)(uintptr_t)s & 15u;
+  uint32_t w[8] = {a.lo.x, a.lo.y, a.lo.z, a.lo.w, a.hi.x, a.hi.y, a.hi.z, a.hi.w};
+#pragma unroll
+  for (int j = 0; j < 6; ++j) w[j] = off & 8u ? w[j + 2] : w[j];
+#pragma unroll
+  for (int j = 0; j < 5; ++j) w[j] = off & 4u ? w[j + 1] : w[j];
+  const uint32_t bits = (off & 2u) * 8u;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+// RAGGED: rows of kWideRow columns and more that start anywhere, read by `load_around`; shorter ones are read element by element, two rows at a
+// time.  Backward of 6563 x 1120 <- 3347 155 against 197 us, column sums of 2000 x 85001 138 against 182; slopes of 6214 x 38 14.6
+// against 12.6, of 11506 x 433 26.9 against 25.2 (few loads in hand and many ends).
+constexpr uint32_t kWideRow = 1024;
+template <int DT, bool RAGGED>
 __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_constant__ SlopeArgs a) {
+  constexpr uint32_t kAhead = RAGGED ? 1 : 2;         // rows in hand (two ragged ones do not fit the registers)
   __shared__ float s_sum[kSlopeWarps][64];
   __shared__ __align__(8) float s_all[kSlopeCtas][64];
   __shared__ uint64_t s_in;
@@ -178,19 +203,26 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_co
   }
   const uint32_t col0 = blockIdx.x / a.split * a.width, c = col0 + tid % groups * 8u, step = kSlopeThreads / groups;
   const uint32_t per = (a.rows + a.split - 1) / a.split, r0 = min(rank * per, a.rows), r1 = min(r0 + per, a.rows);
-  const bool whole = a.vectors && c + 8 <= a.cols;
+  const bool whole = RAGGED ? inner(c, a.cols) : a.vectors && c + 8 <= a.cols;
+  const uint16_t *dy = static_cast<const uint16_t*>(a.dy) + c, *pre = static_cast<const uint16_t*>(a.pre) + c;
   float sum[8] = {};
   if (c < a.cols) {
     for (uint32_t first = r0 + tid / groups; first < r1; first += kAhead * step) {
       uint4 gq[kAhead], zq[kAhead];
+      Around ga[kAhead], za[kAhead];
       float g[8], z[8];
       if (whole) {
 #pragma unroll
         for (uint32_t u = 0; u < kAhead; ++u) {      // these rows' loads are under way together
           const uint64_t r = first + u * step;
           if (r >= r1) break;
-          gq[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.dy) + r * a.ld_dy + c));
-          if (a.activation != GD_ACT_NONE) zq[u] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.pre) + r * a.ld_pre + c));
+          if constexpr (RAGGED) {
+            ga[u] = load_around(dy + r * a.ld_dy);
+            if (a.activation != GD_ACT_NONE) za[u] = load_around(pre + r * a.ld_pre);
+          } else {
+            gq[u] = __ldcs(reinterpret_cast<const uint4*>(dy + r * a.ld_dy));
+            if (a.activation != GD_ACT_NONE) zq[u] = __ldcs(reinterpret_cast<const uint4*>(pre + r * a.ld_pre));
+          }
         }
       }
 #pragma unroll
@@ -198,6 +230,10 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_co
         const uint64_t r = first + u * step;
         if (r >= r1) break;
         if (whole) {
+          if constexpr (RAGGED) {
+            gq[u] = into_place(ga[u], dy + r * a.ld_dy);
+            if (a.activation != GD_ACT_NONE) zq[u] = into_place(za[u], pre + r * a.ld_pre);
+          }
           widen8(gq[u], DT, g);
           if (a.activation != GD_ACT_NONE) widen8(zq[u], DT, z);
         } else {
@@ -286,7 +322,9 @@ cudaError_t launch_slope(SlopeArgs& a, int dtype, cudaStream_t stream) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.split > 1 ? 2 : 1;
-  const cudaError_t e = dtype == GD_DTYPE_BF16 ? cudaLaunchKernelEx(&cfg, slope_kernel<GD_DTYPE_BF16>, a) : cudaLaunchKernelEx(&cfg, slope_kernel<GD_DTYPE_FP16>, a);
+  const bool bf16 = dtype == GD_DTYPE_BF16, ragged = !a.vectors && a.cols >= kWideRow;
+  const cudaError_t e = !ragged ? cudaLaunchKernelEx(&cfg, bf16 ? slope_kernel<GD_DTYPE_BF16, false> : slope_kernel<GD_DTYPE_FP16, false>, a)
+                                : cudaLaunchKernelEx(&cfg, bf16 ? slope_kernel<GD_DTYPE_BF16, true> : slope_kernel<GD_DTYPE_FP16, true>, a);
   if (e == cudaSuccess) note_launches(1);
   return e;
 }

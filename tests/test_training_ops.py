@@ -193,6 +193,42 @@ def test_linear_backward_strided_and_accumulated(cuda_device, layout):
         _check_backward(cuda_device, *shape, torch.bfloat16, "relu", layout, torch.float32, accumulate=True)
 
 
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("n", [1024, 1025, 1031, 1540, 3347])
+def test_linear_backward_wide_ragged_rows(cuda_device, n, act):
+    """Rows of dy and pre that start at every 16-bit place of an aligned vector, their ends inside one."""
+    _check_backward(cuda_device, 37, n, 24, torch.bfloat16, act, "in_out", torch.float32, seed=n, strided=True)
+    _check_backward(cuda_device, 300, n, 40, torch.float16, act, "out_in", torch.float16, seed=n)
+
+
+@pytest.mark.parametrize("shape", [(4000, 1000, 1500), (80, 10, 4096), (300, 200, 100), (20000, 24, 600), (500, 17000, 72)], ids=str)
+def test_linear_backward_products_side_by_side(cuda_device, shape):
+    """Both gradients from one call, time and again with changing inputs: the bits of a call for each alone, and of the first time."""
+    m, n, k = shape
+    gen = _gen(cuda_device, 13)
+    w = _rand(gen, k, n, dtype=torch.bfloat16, scale=0.05)
+    s = T.LinearSession(k, n, m, activation="relu", device=cuda_device, any_layout=True)
+    sets = [(_rand(gen, m, n, dtype=torch.bfloat16), _rand(gen, m, k, dtype=torch.bfloat16), _rand(gen, m, n, dtype=torch.bfloat16)) for _ in range(2)]
+    alone, first = [], [None, None]
+    for dy, x, pre in sets:
+        dw, db = torch.empty(k, n, device=cuda_device), torch.empty(n, device=cuda_device)
+        s.backward(dy, x, w, pre, dw=dw, db=db)
+        alone.append((dw, db))
+    for i in range(20):
+        dy, x, pre = sets[i & 1]
+        dx = torch.full((m, k), float("nan"), dtype=torch.bfloat16, device=cuda_device)
+        dw, db = torch.full((k, n), float("nan"), device=cuda_device), torch.full((n,), float("nan"), device=cuda_device)
+        s.backward(dy, x, w, pre, dx=dx, dw=dw, db=db)
+        kept = (dx + 0, dw + 0)                          # (read by the kernel behind the call: it must find both complete)
+        assert torch.equal(dw, alone[i & 1][0]) and torch.equal(db, alone[i & 1][1])
+        if first[i & 1] is None:
+            first[i & 1] = dx
+            plain = (dy.float() * (pre > 0)) @ w.float().T
+            assert float((dx.float() - plain).abs().max()) <= 2.0 ** -7 * float(plain.abs().max())
+        assert torch.equal(dx, first[i & 1]) and torch.equal(kept[0], dx) and torch.equal(kept[1], dw)
+    assert s.status() == B.GD_OK
+
+
 def test_linear_empty_sizes(cuda_device):
     """No rows, no inputs, no outputs: sums over nothing are 0, and nothing else is touched."""
     dev, dt = cuda_device, torch.bfloat16
