@@ -335,6 +335,9 @@ bool tiles_as_it_is(const void* p, uint64_t ld) { return aligned_to(p, 16) && ld
 // 16-byte accesses at columns that are multiples of 8 stay aligned
 bool vector_rows(const void* p, uint64_t ld, int dt) { return !p || (aligned_to(p, 16) && ld * dtype_bytes(dt) % 16 == 0); }
 
+// 16-bit rows that take 4-byte accesses at even columns
+bool paired_rows(const void* p, uint64_t ld, int dt) { return !p || (dt != GD_DTYPE_FP32 && aligned_to(p, 4) && ld % 2 == 0); }
+
 struct Workspace {
   unsigned char* base;
   size_t at, size;
@@ -410,6 +413,7 @@ int forward(const gd_linear_forward_args* a, cudaStream_t stream) {
   const bool one = a->m == 1;
   e.vectors = vector_rows(e.out, one ? 8 : e.ld_out, e.out_dtype) && vector_rows(e.bias, 8, GD_DTYPE_FP32) && vector_rows(e.add, one ? 8 : e.ld_add, e.add_dtype) &&
               vector_rows(e.pre, one ? 8 : e.ld_pre, e.dtype);
+  e.pairs = paired_rows(e.out, one ? 8 : e.ld_out, e.out_dtype) && paired_rows(e.add, one ? 8 : e.ld_add, e.add_dtype) && paired_rows(e.pre, one ? 8 : e.ld_pre, e.dtype);
   return launch_pack(packs, stream) == cudaSuccess && launch_product(p, stream) == cudaSuccess ? GD_OK : GD_ERR_CUDA;
 }
 
@@ -472,6 +476,7 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     p.ep.out = a->dx, p.ep.ld_out = a->ld_dx, p.ep.out_dtype = a->dtype;
     p.ep.rows = (uint32_t)m, p.ep.cols = (uint32_t)k;
     p.ep.vectors = vector_rows(a->dx, row_step(a->ld_dx, m, k), a->dtype);
+    p.ep.pairs = paired_rows(a->dx, row_step(a->ld_dx, m, k), a->dtype);
     if (launch_product(p, stream) != cudaSuccess) return GD_ERR_CUDA;
   }
   if (has_dw) {                       // dw = x^T dz, or its transpose: contraction over m
@@ -485,6 +490,7 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
     p.beside = has_dx && n < kLongDepth;                  // (a joined dx has a launch in between, and the partial sums' place)
     if (add) p.ep.add = a->dw, p.ep.ld_add = a->ld_dw, p.ep.add_dtype = GD_DTYPE_FP32;
     p.ep.vectors = vector_rows(a->dw, row_step(a->ld_dw, w_rows, w_cols), a->dw_dtype);
+    p.ep.pairs = paired_rows(a->dw, row_step(a->ld_dw, w_rows, w_cols), a->dw_dtype);
     if (launch_product(p, stream) != cudaSuccess) return GD_ERR_CUDA;
   }
   return GD_OK;

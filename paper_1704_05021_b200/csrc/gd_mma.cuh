@@ -193,6 +193,7 @@ struct Epilogue {
   int32_t out_dtype, bias_dtype, add_dtype;
   int32_t activation;
   uint32_t vectors;     // every buffer above takes 16-byte accesses at columns that are multiples of 8
+  uint32_t pairs;       // out, add and pre are of 16 bits and take 4-byte accesses at even columns
 };
 
 __device__ __forceinline__ float load_as(const void* p, uint64_t i, int dt) {
@@ -282,6 +283,35 @@ __device__ __forceinline__ void finish_column(const Epilogue& e, uint32_t r, uin
       if (u < rows) static_cast<uint16_t*>(e.out)[at + u * e.ld_out] = (uint16_t)w;
     }
   }
+}
+// The same of columns c and c + 1, c even, where e.pairs holds: one access for both (c may be the last column).
+__device__ __forceinline__ void finish_columns(const Epilogue& e, uint32_t r, uint32_t c, float (&z)[8], float (&y)[8], uint32_t most = 8) {
+  const uint32_t rows = min(e.rows - min(r, e.rows), most);
+  const bool bf16 = e.out_dtype == GD_DTYPE_BF16, both = c + 1 < e.cols;      // (the type of all three)
+  const auto put = [&](void* to, uint64_t ld) {
+    uint16_t* at = static_cast<uint16_t*>(to) + (uint64_t)r * ld + c;
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u) {
+      const uint32_t w = bf16 ? pack2<GD_DTYPE_BF16>(z[u], y[u]) : pack2<GD_DTYPE_FP16>(z[u], y[u]);
+      if (u < rows && both) *reinterpret_cast<uint32_t*>(at + u * ld) = w;
+      if (u < rows && !both) at[u * ld] = (uint16_t)w;
+    }
+  };
+  if (e.pre) put(e.pre, e.ld_pre);
+  activate_all<8>(z, e.activation);
+  activate_all<8>(y, e.activation);
+  if (e.add) {
+    const uint16_t* at = static_cast<const uint16_t*>(e.add) + (uint64_t)r * e.ld_add + c;
+    uint32_t w[8];
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u) w[u] = u < rows ? (both ? *reinterpret_cast<const uint32_t*>(at + u * e.ld_add) : at[u * e.ld_add]) : 0u;
+#pragma unroll
+    for (uint32_t u = 0; u < 8; ++u) {
+      const float2 f = bf16 ? unpack2<GD_DTYPE_BF16>(w[u]) : unpack2<GD_DTYPE_FP16>(w[u]);
+      z[u] += f.x, y[u] += f.y;
+    }
+  }
+  put(e.out, e.ld_out);
 }
 // Eight neighbours of one output row, c a multiple of 8.
 __device__ __forceinline__ void finish8(const Epilogue& e, uint32_t r, uint32_t c, float (&v)[8]) {

@@ -206,6 +206,34 @@ __global__ void __launch_bounds__(kThreadsSplit, 2) product_split_kernel(const _
       }
       finish8(ep, out_r + r, out_c + c, v);
     }
+  } else if (ep.pairs) {
+    // rows that start at a multiple of 4 bytes: two columns per thread, up to eight rows of them at a time
+    const uint32_t cols = vecs * 4u, group = rows < 8u ? rows : 8u;
+    for (uint32_t t = tid; t < rows / group * cols; t += kThreadsSplit) {
+      const uint32_t r = t / cols * group, c = t % cols * 2u;
+      const float* at = part + (rank * rows + r) * pitch + c;
+      if (out_c + c >= ep.cols || out_r + r >= ep.rows) continue;
+      const float b0 = ep.bias ? load_as(ep.bias, out_c + c, ep.bias_dtype) : 0.f;
+      const float b1 = ep.bias && out_c + c + 1 < ep.cols ? load_as(ep.bias, out_c + c + 1, ep.bias_dtype) : 0.f;
+      float v[8], y[8];
+#pragma unroll
+      for (uint32_t u = 0; u < 8; ++u) {
+        if (u >= group) continue;
+        float2 f;
+        if constexpr (SPLITS > 1) {
+          const uint32_t address = smem_u32(at + u * pitch);
+#pragma unroll
+          for (uint32_t q = 0; q < SPLITS; ++q) {
+            const float2 w = peer_load2(peer_address(address, q));
+            f = q == 0 ? w : make_float2(f.x + w.x, f.y + w.y);
+          }
+        } else {
+          f = *reinterpret_cast<const float2*>(at + u * pitch);
+        }
+        v[u] = f.x + b0, y[u] = f.y + b1;
+      }
+      finish_columns(ep, out_r + r, out_c + c, v, y, group);
+    }
   } else {
     // rows that start anywhere: a column per thread, up to eight rows of it at a time
     const uint32_t cols = vecs * 8u, group = rows < 8u ? rows : 8u;

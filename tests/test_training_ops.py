@@ -125,6 +125,35 @@ def test_linear_wide_results(cuda_device, act):
         _check_forward(cuda_device, m, n, k, torch.float16, act, "in_out", torch.float32, None, True, False, seed=n)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("shape", [(1, 33, 40), (50, 70, 72), (77, 1001, 136), (1500, 1502, 200), (4100, 2051, 64)], ids=str)
+def test_linear_rows_of_four_bytes(cuda_device, shape, dtype):
+    """Results, z and residual in rows that start at multiples of 4 bytes only, with odd and even widths: right inside, untouched outside."""
+    m, n, k = shape
+    gen = _gen(cuda_device, n)
+    pitch = (n + 1) // 2 * 2 + (2 if (n + 1) // 2 % 4 == 0 else 0)
+    x, w, b = _rand(gen, m, k, dtype=dtype), _rand(gen, k, n, dtype=dtype, scale=k ** -0.5), _rand(gen, n)
+
+    def wide():
+        return torch.full((m * pitch + 2,), 77.0, dtype=dtype, device=cuda_device)
+
+    bufs = [wide() for _ in range(3)]
+    y, z, r = (t[2:].view(m, pitch)[:, :n] for t in bufs)
+    r.copy_(_rand(gen, m, n, dtype=dtype))
+    s = T.LinearSession(k, n, m, dtype=dtype, activation="relu", device=cuda_device, any_layout=True)
+    s.forward(x, w, b, residual=r, pre=z, out=y)
+    z64 = x.double() @ w.double() + b.double()
+    room = (k / 16 + 8) * 2.0 ** -22 * (x.double().abs() @ w.double().abs() + b.double().abs())
+    _within(z, z64, room + z64.abs() * HALF_ULP[dtype] + TINY[dtype], "z")
+    ref = z64.clamp_min(0) + r.double()
+    _within(y, ref, room + ref.abs() * HALF_ULP[dtype] + 2.0 ** -23 * r.double().abs() + TINY[dtype], "y")
+    for t in bufs:
+        assert bool((t[:2] == 77).all()) and bool((t[2:].view(m, pitch)[:, n:] == 77).all())
+    kept = y.clone()
+    s.forward(x, w, b, residual=r, pre=z, out=r)
+    assert torch.equal(r, kept)
+
+
 def test_linear_residual_in_place(cuda_device):
     gen = _gen(cuda_device, 5)
     x, w, r = _rand(gen, 50, 64, dtype=torch.bfloat16), _rand(gen, 64, 72, dtype=torch.bfloat16, scale=0.1), _rand(gen, 50, 72, dtype=torch.bfloat16)
