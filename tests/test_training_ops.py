@@ -258,6 +258,30 @@ def test_linear_backward_products_side_by_side(cuda_device, shape):
     assert s.status() == B.GD_OK
 
 
+@pytest.mark.parametrize("shape", [(4000, 1000, 1500), (80, 10, 4096)], ids=str)
+def test_linear_backward_in_a_graph(cuda_device, shape):
+    """A captured backward call, replayed over new inputs, gives the bits of the call itself."""
+    m, n, k = shape
+    gen = _gen(cuda_device, 14)
+    w = _rand(gen, k, n, dtype=torch.bfloat16, scale=0.05)
+    s = T.LinearSession(k, n, m, activation="relu", device=cuda_device, any_layout=True)
+    dy, x, pre = (_rand(gen, m, c, dtype=torch.bfloat16) for c in (n, k, n))
+    dx, dw, db = torch.empty_like(x), torch.empty(k, n, device=cuda_device), torch.empty(n, device=cuda_device)
+    s.backward(dy, x, w, pre, dx=dx, dw=dw, db=db)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.backward(dy, x, w, pre, dx=dx, dw=dw, db=db)
+    for seed in range(4):
+        for t in (dy, x, pre):
+            t.copy_(_rand(gen, *t.shape, dtype=torch.bfloat16))
+        graph.replay()
+        replayed = [t + 0 for t in (dx, dw, db)]
+        s.backward(dy, x, w, pre, dx=dx, dw=dw, db=db)
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (dx, dw, db)))
+    assert s.status() == B.GD_OK
+
+
 def test_linear_empty_sizes(cuda_device):
     """No rows, no inputs, no outputs: sums over nothing are 0, and nothing else is touched."""
     dev, dt = cuda_device, torch.bfloat16
