@@ -345,7 +345,8 @@ int gd_compress_static(const gd_compress_args* args, void* stream, const void** 
  * 10 means division, 11 quantisation-error feedback, 12 candidate selection and compaction in one launch,
  * 13 setup and prediction in one launch, 14 dense histogram pass, 15 walk of the dense histogram,
  * 16 add, selection and compaction of a short vector in one launch; the operators of gd_train.h: 17 layout of a
- * ragged operand, 18 activation slope and bias gradient, 19 product, 20 cross-entropy, 21 AdamW), then forgets them.
+ * ragged operand, 18 activation slope and bias gradient, 19 product of few tiles, 20 cross-entropy, 21 AdamW, 22 and 23 product of many tiles,
+ * 256 x 256 and 256 x 128), then forgets them.
  * At most 4096 pairs are held between two collects; later launches are not recorded.  Not thread-safe.
  */
 int gd_profile_enable(int mode);

@@ -285,7 +285,7 @@ def gd_step_host(call: CompressCall, apply: Optional[ApplyCall], grad_host: torc
 
 PROFILE_TAGS = ["setup", "sample_select", "add_emit", "dense_select", "dense_compact", "cand_select", "cand_compact",
                 "finalize", "apply", "pack_sampled", "means", "feedback", "cand_select_compact", "setup_predict", "dense_hist", "dense_find", "dense_fused",
-                "linear_pack", "linear_slope", "linear", "cross_entropy", "adamw"]
+                "linear_pack", "linear_slope", "linear", "cross_entropy", "adamw", "linear_pair", "linear_pair_narrow"]
 # Kernels one gd_compress launches, in order, by the path the call takes (each is one launch and, with
 # gd_profile_enable(2), one tagged event pair); gd_decompress_apply adds one "apply" per push.
 STEP_KERNELS = {

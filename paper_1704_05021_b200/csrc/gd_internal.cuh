@@ -367,7 +367,8 @@ enum ProfileTag : uint32_t { PT_SETUP = 0, PT_PACK_SAMPLED = 9, PT_MEANS = 10, P
                              PT_CAND_SELECT = 5, PT_CAND_COMPACT = 6, PT_FINALIZE = 7, PT_APPLY = 8, PT_FEEDBACK = 11,
                              PT_CAND_SELECT_COMPACT = 12, PT_SETUP_PREDICT = 13,
                              PT_DENSE_HIST = 14, PT_DENSE_FIND = 15, PT_DENSE_FUSED = 16,
-                             PT_LINEAR_PACK = 17, PT_LINEAR_SLOPE = 18, PT_LINEAR = 19, PT_XENT = 20, PT_ADAMW = 21 };
+                             PT_LINEAR_PACK = 17, PT_LINEAR_SLOPE = 18, PT_LINEAR = 19, PT_XENT = 20, PT_ADAMW = 21,
+                             PT_LINEAR_PAIR = 22, PT_LINEAR_PAIR_NARROW = 23 };
 void profile_mark(cudaStream_t stream, bool begin, uint32_t tag);
 struct ProfileScope {   // records an event pair around the launches made during its lifetime
   cudaStream_t stream;

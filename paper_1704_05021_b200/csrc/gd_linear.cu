@@ -54,10 +54,10 @@ bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& 
 
 cudaError_t launch_product(const Product& p, cudaStream_t stream) {
   if (p.ep.rows == 0 || p.ep.cols == 0) return cudaSuccess;
-  ProfileScope ps(stream, PT_LINEAR);
   const SplitChoice split = choose_product_split(p);
   const double wide = cost_product_pair(p, 256), narrow = cost_product_pair(p, 128);
   const bool pair = p.depth && std::min(wide, narrow) < split.cost;
+  ProfileScope ps(stream, !pair ? PT_LINEAR : wide <= narrow ? PT_LINEAR_PAIR : PT_LINEAR_PAIR_NARROW);
   const cudaError_t e = pair ? launch_product_pair(p, wide <= narrow ? 256 : 128, stream) : launch_product_split(p, split, stream);
   if (e == cudaSuccess) note_launches(1);
   return e;

@@ -56,8 +56,10 @@ __device__ __forceinline__ void mbar_arrive_peer(uint32_t address) {
 
 __device__ __forceinline__ void tile_store(const CUtensorMap* map, const void* src, int32_t x, int32_t y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(smem_u32(src)) : "memory");
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
+// Closes a group of stores.  Every piece closes one, whether it was stored or lies outside the matrix (an empty group is done at once): the pieces
+// take the buffers in turn and stores_read() counts groups, so the two counts have to run together.
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int LEFT>
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }   // all but LEFT have left shared memory
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -218,7 +220,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
               for (uint32_t j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(z + (j ^ (lane & 7u)) * 16u) = narrow8(v + 8 * j, ep.dtype);
               fence_async();
               __syncwarp();
-              if (elect_one() && inside) tile_store(&g.pre, pieces + kPieceBytes, (int32_t)c, (int32_t)r0);
+              if (elect_one()) {
+                if (inside) tile_store(&g.pre, pieces + kPieceBytes, (int32_t)c, (int32_t)r0);
+                stores_commit();
+              }
             }
           }
           if constexpr (WIDE) {
@@ -284,6 +289,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
           __syncwarp();
           if (elect_one()) {
             if (inside) tile_store(&g.out, pieces + at * kPieceBytes, (int32_t)c, (int32_t)r0);
+            stores_commit();
             if (through && p + 1 < kPieces) {
               if (two) stores_read<0>(); else stores_read<1>();
               ask_add(p + 1, 1);

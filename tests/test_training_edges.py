@@ -1,0 +1,125 @@
+"""The training operators where a result or a row ends inside what a kernel works on at a time: cut tiles of the large products, lengths at
+the limits of shared memory, rows worked on in place, values that are not finite.
+
+Tolerances are bounds on the stated arithmetic: a product accumulates in fp32 in steps of 16 products, each rounding (possibly truncating)
+once, at most (depth / 16 + 8) 2^-22 of the sum of magnitudes; a result rounds once to its type; a residual is one more fp32 sum.
+"""
+import pytest
+import torch
+
+from paper_1704_05021_b200 import binding as B
+from paper_1704_05021_b200 import training as T
+
+pytestmark = pytest.mark.gpu
+
+ROUND = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+
+
+def _rand(gen, *shape, dtype=torch.float32, scale=1.0):
+    return (torch.randn(*shape, generator=gen, device=gen.device) * scale).to(dtype)
+
+
+def _gen(device, seed):
+    return torch.Generator(device=device).manual_seed(seed)
+
+
+def _kernels(call):
+    """The kernels a call launches, by their tags."""
+    B.gd_profile_enable(0)
+    B.gd_profile_collect()
+    B.gd_profile_enable(2)
+    try:
+        call()
+        return [name for name, _ in B.gd_profile_collect(with_tags=True)]
+    finally:
+        B.gd_profile_enable(0)
+
+
+def _within(got, ref, room, what):
+    over = (got.double() - ref).abs() - room
+    assert bool((over <= 0).all()), f"{what}: {float(over.max())} past the bound at {int(over.argmax())}"
+
+
+def _repeats(call, result, times=20):
+    """The call once more and again: the same bits every time.  `call` puts back whatever it adds to."""
+    first = result.clone()
+    for _ in range(times):
+        call()
+        assert torch.equal(result, first)
+
+
+# ------------------------------------------------------------------------------------------ products whose last tiles are cut
+
+CUTS = [8, 32, 40, 64, 72, 96]
+
+
+@pytest.mark.parametrize("more_rows", [8, 136])
+@pytest.mark.parametrize("cut", CUTS)
+@pytest.mark.parametrize("width, kernel", [(4096, "linear_pair"), (2048, "linear_pair_narrow")])
+def test_cut_tiles_of_the_forward_product(cuda_device, width, kernel, cut, more_rows):
+    """Two to three tiles per pair of CTAs, the last column of them ending after any number of 32-column pieces, the last row of them after
+    part of one CTA's half: what is stored of one piece must have left before the next takes its place, stored or not."""
+    m, n, k, dt = 2560 + more_rows, width + cut, 200, torch.bfloat16
+    gen = _gen(cuda_device, cut)
+    x, w, r = _rand(gen, m, k, dtype=dt), _rand(gen, k, n, dtype=dt, scale=k ** -0.5), _rand(gen, m, n, dtype=dt)
+    s = T.LinearSession(k, n, m, device=cuda_device)
+    ref, size = x.double() @ w.double(), x.double().abs() @ w.double().abs()
+    for out_dt in (torch.float32, dt):
+        for residual in (None, r):
+            for with_pre in (False, True):
+                y = torch.full((m, n), float("nan"), dtype=out_dt, device=cuda_device)
+                z = torch.full((m, n), float("nan"), dtype=dt, device=cuda_device) if with_pre else None
+                call = lambda: s.forward(x, w, residual=residual, out=y, pre=z)  # noqa: B023, E731
+                assert _kernels(call) == [kernel]
+                want = ref if residual is None else ref + residual.double()
+                room = (k / 16 + 8) * 2.0 ** -22 * size + 2.0 ** -23 * (ref.abs() + want.abs())
+                _within(y, want, room + ROUND[out_dt] * want.abs(), (out_dt, residual is None, with_pre))
+                if with_pre:
+                    _within(z, ref, room + ROUND[dt] * ref.abs(), "pre")
+                _repeats(call, y)
+    assert s.status() == B.GD_OK
+
+
+def _check_weights(device, m, n, k, layout, accumulate, dtype=torch.bfloat16, kernel="linear_pair"):
+    gen = _gen(device, m + n)
+    x, dy = _rand(gen, m, k, dtype=dtype), _rand(gen, m, n, dtype=dtype, scale=1e-2)
+    shape = (k, n) if layout == "in_out" else (n, k)
+    start = _rand(gen, *shape) if accumulate else torch.full(shape, float("nan"), device=device)
+    dw = torch.empty_like(start)
+    s = T.LinearSession(k, n, m, dtype=dtype, w_layout=layout, device=device)
+
+    def call():
+        dw.copy_(start)
+        s.backward(dy, x, None, dw=dw, accumulate=accumulate)
+
+    launched = _kernels(call)
+    assert launched[-1] == kernel, launched
+    ref, size = x.double().T @ dy.double(), x.double().abs().T @ dy.double().abs()
+    if layout == "out_in":
+        ref, size = ref.T, size.T
+    want = ref + start.double() if accumulate else ref
+    _within(dw, want, (m / 16 + 8) * 2.0 ** -22 * size + 2.0 ** -23 * (ref.abs() + want.abs()), "dw")
+    _repeats(call, dw)
+    assert s.status() == B.GD_OK
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("layout", ["in_out", "out_in"])
+@pytest.mark.parametrize("cut", CUTS)
+def test_cut_tiles_of_the_weight_gradient(cuda_device, cut, layout, accumulate):
+    """The same for fp32 gradients of the weights, written and added to: chains of one and of two."""
+    k, n = (2568, 4096 + cut) if layout == "in_out" else (4096 + cut, 2696)
+    for m in (200, 648):
+        _check_weights(cuda_device, m, n, k, layout, accumulate)
+    k, n = (2568, 2048 + cut) if layout == "in_out" else (2048 + cut, 2696)
+    _check_weights(cuda_device, 200, n, k, layout, accumulate, kernel="linear_pair_narrow")
+
+
+def test_weight_gradient_of_the_vocabulary(cuda_device):
+    """The output projection of the translation model, 500 x 85000 over 4000 rows: the last column tile has eight columns."""
+    _check_weights(cuda_device, 4000, 85000, 500, "in_out", False)
+    _check_weights(cuda_device, 4000, 85000, 500, "in_out", True)
+
+
+def test_weight_gradient_added_to_a_large_matrix(cuda_device):
+    _check_weights(cuda_device, 8192, 4104, 4096, "in_out", True)
