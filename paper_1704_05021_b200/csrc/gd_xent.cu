@@ -324,17 +324,21 @@ cudaError_t launch_short(const XentArgs& a, cudaStream_t stream) {
   return launch_dependent(xent_short_kernel<DT, G, PER>, dim3((uint32_t)blocks), dim3(128), 0, stream, a);
 }
 
-using RowKernel = void (*)(XentArgs, uint32_t, uint32_t, uint32_t);
-cudaError_t launch_clusters(RowKernel kernel, uint64_t ctas, uint32_t threads, size_t smem, uint32_t cluster, cudaStream_t stream, const XentArgs& a, uint32_t slice,
-                            uint32_t stage) {
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxStage);
+template <int DT, uint32_t THREADS>
+cudaError_t launch_clusters(const XentArgs& a, uint32_t cluster, uint32_t slice, uint32_t stage, cudaStream_t stream) {
+  auto kernel = xent_row_kernel<DT, THREADS>;
+  // Always: without it a CTA has 48 KB for its static and its dynamic shared memory together, and the slice alone may be that long.
+  static PerDeviceInt ready;
+  int dev;
+  if (!ready.get(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxStage);
     if (e != cudaSuccess) return e;
+    ready.set(dev, 1);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((uint32_t)ctas);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.gridDim = dim3((uint32_t)(a.rows * cluster));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = stage * sizeof(typename Elem<DT>::type);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -365,10 +369,10 @@ cudaError_t launch_rows(const XentArgs& a, cudaStream_t stream) {
   const uint32_t stage = std::min(slice * item, kMaxStage) / item;
   // threads by what each has to do: a short slice would pay for more of them in synchronisation, not gain by them
   const uint32_t vecs = slice * item / 16;
-  if (vecs <= kVecs32) return launch_clusters(xent_row_kernel<DT, 32>, a.rows * cluster, 32, stage * item, cluster, stream, a, slice, stage);
-  if (vecs <= kVecs64) return launch_clusters(xent_row_kernel<DT, 64>, a.rows * cluster, 64, stage * item, cluster, stream, a, slice, stage);
-  if (vecs <= kVecs128) return launch_clusters(xent_row_kernel<DT, 128>, a.rows * cluster, 128, stage * item, cluster, stream, a, slice, stage);
-  return launch_clusters(xent_row_kernel<DT, 256>, a.rows * cluster, 256, stage * item, cluster, stream, a, slice, stage);
+  if (vecs <= kVecs32) return launch_clusters<DT, 32>(a, cluster, slice, stage, stream);
+  if (vecs <= kVecs64) return launch_clusters<DT, 64>(a, cluster, slice, stage, stream);
+  if (vecs <= kVecs128) return launch_clusters<DT, 128>(a, cluster, slice, stage, stream);
+  return launch_clusters<DT, 256>(a, cluster, slice, stage, stream);
 }
 
 }  // namespace
