@@ -175,6 +175,7 @@ __global__ void __launch_bounds__(THREADS) xent_row_kernel(const __grid_constant
   __shared__ float2 s_warp[THREADS / 32];
   __shared__ __align__(8) float2 s_pairs[8];
   __shared__ uint64_t s_full[kParts], s_pairs_in;
+  __shared__ float s_target;
   const uint32_t tid = threadIdx.x, rank = cluster > 1 ? cluster_rank() : 0u;
   const uint64_t row = blockIdx.x / cluster;
   const uint32_t c0 = min(rank * slice, a.classes), c1 = min(c0 + slice, a.classes), len = c1 - c0;
@@ -208,7 +209,8 @@ __global__ void __launch_bounds__(THREADS) xent_row_kernel(const __grid_constant
   }
   const int64_t target = target_of(a, row);
   const float scale = a.grad_scale_dev ? a.grad_scale * *a.grad_scale_dev : a.grad_scale;
-  const float target_logit = target >= 0 ? Elem<DT>::get(static_cast<const T*>(a.logits)[row * a.ld_logits + target]) : 0.f;
+  const bool answers = tid == 0 && rank == 0;      // writes the row's loss, and so reads the target's logit, wherever it lies
+  const float target_logit = answers && target >= 0 ? Elem<DT>::get(static_cast<const T*>(a.logits)[row * a.ld_logits + target]) : 0.f;
   bool landed = true;
 
   // Each thread's running maximum and sum: the sum is rescaled when a piece raises the maximum.
@@ -234,6 +236,9 @@ __global__ void __launch_bounds__(THREADS) xent_row_kernel(const __grid_constant
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) join(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o));
   if ((tid & 31u) == 0u) s_warp[tid >> 5] = make_float2(m, s);
+  // In place, the target's logit is overwritten by whichever CTA has it in its slice, once that has this one's pair: the read is over
+  // before the pair is sent (its value goes through shared memory ahead of the barrier), not merely begun.
+  if (answers) s_target = target_logit;
   __syncthreads();
   m = s_warp[0].x, s = s_warp[0].y;
 #pragma unroll
@@ -247,8 +252,8 @@ __global__ void __launch_bounds__(THREADS) xent_row_kernel(const __grid_constant
     for (uint32_t r = 0; r < cluster; ++r) join(m, s, s_pairs[r].x, s_pairs[r].y);
     cluster_arrive_relaxed();                    // the pairs have been received; waited for before this CTA ends
   }
-  const RowResult r = finish(m, s, target, target_logit, scale);
-  if (tid == 0 && rank == 0) {
+  const RowResult r = finish(m, s, target, answers ? s_target : 0.f, scale);
+  if (answers) {
     if (a.loss) a.loss[row] = r.loss;
     if (a.lse) a.lse[row] = r.lse;
   }

@@ -49,3 +49,19 @@ def test_slices_as_long_as_shared_memory(cuda_device, dtype):
             f"for n in {sizes}: e.check(200, n, {dtype})\n")
     res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=ROOT)
     assert res.returncode == 0, res.stderr[-2000:]
+
+
+@pytest.mark.parametrize("rows, classes", [(3, 40000), (150, 85000), (1, 200000)], ids=str)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_in_place_with_the_target_in_any_slice(cuda_device, dtype, rows, classes):
+    """Rows that several CTAs share, worked on in place, the target in every part of them: the bits of a call into another buffer.  (The
+    CTA that writes the loss reads the target's logit from the slice of another, which overwrites it.)"""
+    gen = torch.Generator(device=cuda_device).manual_seed(classes)
+    logits = (torch.randn(rows, classes, generator=gen, device=cuda_device) * 3).to(dtype)
+    for at in range(16):
+        t = (torch.arange(rows, device=cuda_device) * 7919 + at * (classes // 16) + 13 * at) % classes
+        apart, loss, inside = torch.empty_like(logits), [torch.empty(rows, device=cuda_device) for _ in range(2)], logits.clone()
+        T.cross_entropy(logits, t, loss=loss[0], grad=apart)
+        T.cross_entropy(inside, t, loss=loss[1], grad=inside)
+        assert torch.equal(loss[0], loss[1]) and torch.equal(apart, inside)
+    check(rows, classes, dtype, in_place=True)
