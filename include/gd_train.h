@@ -112,7 +112,8 @@ int gd_linear_status(const void* workspace, void* stream);
  * A row whose target is ignore_index has loss 0 and gradient 0 whatever its logits are.  Logits of -inf are masked classes: they
  * take no part and their gradient is 0.  In a row with a target, where every class is masked, or with +inf or NaN among
  * the logits, loss and gradient are NaN; so are those of a row whose target is neither ignore_index nor in [0, classes).
- * grad may be logits itself (same address and leading dimension) or NULL; loss and lse may be NULL.
+ * grad may be logits itself (same address and leading dimension) or NULL; loss and lse may be NULL.  The call has no workspace and
+ * so no status word: a device-side wait that gives up leaves NaN in its row's results.
  */
 typedef struct gd_cross_entropy_args {
   uint64_t rows, classes;     /* classes >= 1, each < 2^31 */

@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(THREADS) xent_row_kernel(const __grid_constant
   for (uint32_t i = kept + tid; i < n_vec; i += THREADS) take(__ldcg(x_vec + i));
   const int never = 0;
   for (uint32_t p = 0; p < kParts; ++p) {
-    landed = landed && mbar_wait(&s_full[p], 0u, &never);
+    landed = mbar_wait(&s_full[p], 0u, &never) && landed;       // (also behind a wait that ran out: the CTA must not end with copies under way)
     const uint32_t v1 = min((p + 1) * part, kept);
     for (uint32_t i = p * part + tid; i < v1; i += THREADS) take(held_vec[i]);
   }
