@@ -105,6 +105,13 @@ int gd_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, int any_layout
 int gd_linear_status(const void* workspace, void* stream);
 
 /*
+ * Self-test of a bounded wait, as gd_selftest_bounded_wait is in gd.h: zeroes the workspace (256-byte aligned, at least 16896 bytes) and runs the
+ * sum of a bias gradient by two CTAs, of which one waits at most budget_ns for eight bytes more than the other sends.  Afterwards
+ * gd_linear_status(workspace) is GD_ERR_DEVICE_TIMEOUT and the 32 fp32 sums at its byte 256 are NaN.  The context stays usable.
+ */
+int gd_selftest_linear_wait(void* workspace, size_t workspace_bytes, uint64_t budget_ns, void* stream);
+
+/*
  * gd_cross_entropy - for every row i of logits [rows, classes] with target t = targets[i]:
  *     lse[i]    = log sum_j exp(logits[i, j])
  *     loss[i]   = lse[i] - logits[i, t]

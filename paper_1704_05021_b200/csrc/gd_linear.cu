@@ -143,6 +143,9 @@ struct SlopeArgs {
   uint32_t rows, cols, width, split, ctas;      // split: CTAs of a cluster; ctas: those that take columns; the others lay out `packs`
   int32_t activation;
   uint32_t accumulate, vectors;
+  int* status;
+  uint64_t budget_ns;  // of the wait for the other CTAs' sums
+  uint32_t missing;    // bytes awaited that nobody sends (0; the self-test's 8)
   Packs packs;
 };
 // Eight 16-bit elements from column c of a row that starts anywhere: the two aligned vectors around them, moved into place. Both lie within
@@ -185,7 +188,7 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_co
       s_never = 0;
       mbar_init(&s_in, 1u);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      if (rank == 0) mbar_arrive_expect_tx(&s_in, a.split * a.width * 4u);
+      if (rank == 0) mbar_arrive_expect_tx(&s_in, a.split * a.width * 4u + a.missing);
     }
     __syncthreads();
     cluster_arrive_relaxed();
@@ -289,7 +292,9 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) slope_kernel(const __grid_co
       send_peer2(peer_address(smem_u32(&s_all[rank][2 * tid]), 0), t, peer_address(smem_u32(&s_in), 0));
     }
     if (rank == 0 && tid < a.width) {
-      float t = mbar_wait(&s_in, 0u, &s_never) ? 0.f : NAN;
+      const bool there = mbar_wait(&s_in, 0u, &s_never, a.budget_ns);
+      if (!there) atomicExch(a.status, GD_ERR_DEVICE_TIMEOUT);
+      float t = there ? 0.f : NAN;
       for (uint32_t q = 0; q < a.split; ++q) t += s_all[q][tid];
       const uint32_t col = col0 + tid;
       if (col < a.cols) a.db[col] = a.accumulate ? a.db[col] + t : t;
@@ -451,6 +456,8 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
   if (has_dx && n && (rc = operand(a->w, a->ldw, w_rows, w_cols, ws, &s.packs, &w)) != GD_OK) return rc;
   if (has_dw && m && (rc = operand(a->x, a->ldx, m, k, ws, &s.packs, &x)) != GD_OK) return rc;
   if (make || has_db) {
+    s.status = (int*)a->workspace;
+    s.budget_ns = kWaitBudgetNs;
     s.dy = a->dy, s.ld_dy = a->ld_dy;
     s.pre = a->pre, s.ld_pre = a->ld_pre;
     s.db = has_db ? a->db : nullptr;
@@ -520,6 +527,26 @@ int gd_linear_status(const void* workspace, void* stream) {
   if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return GD_ERR_CUDA;
   if (cudaMemcpy(&status, workspace, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return GD_ERR_CUDA;
   return status;
+}
+
+int gd_selftest_linear_wait(void* workspace, size_t workspace_bytes, uint64_t budget_ns, void* stream) {
+  using namespace gd;
+  constexpr uint32_t rows = 256, cols = 32;              // two CTAs in a cluster
+  constexpr size_t sums = kStatusBytes, values = sums + 256;
+  if (check_workspace(workspace, workspace_bytes) != GD_OK || workspace_bytes < values + rows * cols * 2) return GD_ERR_WORKSPACE;
+  unsigned char* base = (unsigned char*)workspace;
+  if (cudaMemsetAsync(base, 0, values + rows * cols * 2, (cudaStream_t)stream) != cudaSuccess) return GD_ERR_CUDA;
+  SlopeArgs s;
+  std::memset(&s, 0, sizeof(s));
+  s.dy = base + values, s.ld_dy = cols;
+  s.db = (float*)(base + sums);
+  s.rows = rows, s.cols = cols;
+  s.activation = GD_ACT_NONE;
+  s.vectors = 1;
+  s.status = (int*)workspace;
+  s.budget_ns = budget_ns;
+  s.missing = 8;
+  return launch_slope(s, GD_DTYPE_BF16, (cudaStream_t)stream) == cudaSuccess ? GD_OK : GD_ERR_CUDA;
 }
 
 int gd_linear_forward(const gd_linear_forward_args* a, void* stream) { return gd::forward(a, (cudaStream_t)stream); }

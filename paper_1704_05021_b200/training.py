@@ -21,7 +21,8 @@ GD_ACT_NONE, GD_ACT_RELU, GD_ACT_GELU, GD_ACT_SILU = 0, 1, 2, 3
 GD_W_IN_OUT, GD_W_OUT_IN = 0, 1
 GD_LINEAR_ACCUMULATE = 1
 
-EXPORTS = ["gd_linear_forward", "gd_linear_backward", "gd_linear_workspace_bytes", "gd_linear_status", "gd_cross_entropy", "gd_adamw_step"]
+EXPORTS = ["gd_linear_forward", "gd_linear_backward", "gd_linear_workspace_bytes", "gd_linear_status", "gd_selftest_linear_wait", "gd_cross_entropy",
+           "gd_adamw_step"]
 
 _DTYPES = {torch.float32: GD_DTYPE_FP32, torch.bfloat16: GD_DTYPE_BF16, torch.float16: GD_DTYPE_FP16}
 _ACTIVATIONS = {"none": GD_ACT_NONE, "relu": GD_ACT_RELU, "gelu": GD_ACT_GELU, "silu": GD_ACT_SILU}
@@ -85,6 +86,7 @@ def load_library():
         lib.gd_linear_backward.argtypes = [C.c_void_p, C.c_void_p]
         lib.gd_linear_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.c_int, C.POINTER(C.c_size_t)]
         lib.gd_linear_status.argtypes = [C.c_void_p, C.c_void_p]
+        lib.gd_selftest_linear_wait.argtypes = [C.c_void_p, C.c_size_t, C.c_uint64, C.c_void_p]
         lib.gd_cross_entropy.argtypes = [C.c_void_p, C.c_void_p]
         lib.gd_adamw_step.argtypes = [C.POINTER(_AdamwArgs), C.c_void_p]
         for name in EXPORTS:

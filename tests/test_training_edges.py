@@ -123,3 +123,22 @@ def test_weight_gradient_of_the_vocabulary(cuda_device):
 
 def test_weight_gradient_added_to_a_large_matrix(cuda_device):
     _check_weights(cuda_device, 8192, 4104, 4096, "in_out", True)
+
+
+# ------------------------------------------------------------------------------------------ waits that run out
+
+def test_a_wait_that_runs_out_reaches_the_status(cuda_device):
+    """The sum of a bias gradient by two CTAs, one waiting (a millisecond) for more than the other sends: the status says so, the sums are NaN,
+    and the next call works once the word is zeroed."""
+    s = T.LinearSession(32, 32, 512, device=cuda_device)
+    ws, lib = s.workspace, T.load_library()
+    assert ws.numel() >= 16896
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.gd_selftest_linear_wait(ws.data_ptr(), 16895, 1_000_000, stream) == B.GD_ERR_WORKSPACE
+    assert lib.gd_selftest_linear_wait(ws.data_ptr(), ws.numel(), 1_000_000, stream) == B.GD_OK
+    assert s.status() == B.GD_ERR_DEVICE_TIMEOUT
+    assert bool(torch.isnan(ws[256:384].view(torch.float32)).all())
+    ws[:256].zero_()
+    dy, db = torch.ones(512, 32, dtype=torch.bfloat16, device=cuda_device), torch.empty(32, device=cuda_device)
+    s.backward(dy, None, None, db=db)
+    assert bool((db == 512).all()) and s.status() == B.GD_OK
