@@ -136,13 +136,18 @@ def _cuda_index(device) -> int:
     return torch.cuda.current_device() if device.index is None else device.index
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # the current stream's handle without a Stream object around it
+# the current stream's handle without a Stream object around it, and the current device without initialising anything
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _stream(stream, index: int):
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(index)
-    return B._stream_handle(stream)
+def _issue(call, args, stream, index: int) -> int:
+    """call(args, stream's handle) with the tensors' device current: the library launches on the current device, and the handle of a default
+    stream does not say which device's it is."""
+    if _current_device() != index:
+        with torch.cuda.device(index):
+            return call(args, _raw_stream(index) if stream is None else B._stream_handle(stream))
+    return call(args, _raw_stream(index) if stream is None else B._stream_handle(stream))
 
 
 class LinearSession:
@@ -166,13 +171,17 @@ class LinearSession:
         self._lib = load_library()
         size = C.c_size_t(0)
         B._check(self._lib.gd_linear_workspace_bytes(self.max_rows, self.n_out, self.n_in, int(any_layout), C.byref(size)), "gd_linear_workspace_bytes")
-        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        self._bind(torch.empty(size.value, dtype=torch.uint8, device=self.device))
         self.workspace[:256].zero_()
+
+    def _bind(self, workspace: torch.Tensor) -> None:
+        """The arguments that stay the same from call to call."""
+        self.workspace = workspace
         self._forward, self._backward = _LinearForwardArgs(), _LinearBackwardArgs()
         for a in (self._forward, self._backward):
-            a.workspace, a.workspace_bytes = self.workspace.data_ptr(), size.value
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
         self._forward_at, self._backward_at = C.addressof(self._forward), C.addressof(self._backward)
-        self._codes = (self.n_out, self.n_in, _DTYPES[dtype], _ACTIVATIONS[activation], _LAYOUTS[w_layout])
+        self._codes = (self.n_out, self.n_in, _DTYPES[self.dtype], _ACTIVATIONS[self.activation], _LAYOUTS[self.w_layout])
 
     def _rows(self, t: torch.Tensor) -> int:
         m = t.shape[0] if t.dim() == 2 else -1
@@ -198,7 +207,7 @@ class LinearSession:
         _FORWARD_FIELDS.pack_into(self._forward, 0, m, *self._codes, bias_code, _DTYPES[out_dt], 0,
                                   x.data_ptr(), _matrix(x, "x", m, self.n_in, dt, index), w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, index), bias_at,
                                   residual_at, ld_residual, out.data_ptr(), _matrix(out, "out", m, n, out_dt, index), pre_at, ld_pre)
-        code = self._lib.gd_linear_forward(self._forward_at, _stream(stream, index))
+        code = _issue(self._lib.gd_linear_forward, self._forward_at, stream, index)
         if code:
             raise B.GdError(code, "gd_linear_forward")
         return out
@@ -232,13 +241,13 @@ class LinearSession:
             db_at = db.data_ptr()
         _BACKWARD_FIELDS.pack_into(self._backward, 0, m, *self._codes, dw_code, GD_LINEAR_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
                                    _matrix(dy, "dy", m, n, dt, index), pre_at, ld_pre, x_at, ldx, w_at, ldw, dx_at, ld_dx, dw_at, ld_dw, db_at)
-        code = self._lib.gd_linear_backward(self._backward_at, _stream(stream, index))
+        code = _issue(self._lib.gd_linear_backward, self._backward_at, stream, index)
         if code:
             raise B.GdError(code, "gd_linear_backward")
 
     def status(self, stream=None) -> int:
         """GD_OK, or GD_ERR_DEVICE_TIMEOUT if a device-side wait of any call so far gave up (waits for the stream)."""
-        return self._lib.gd_linear_status(self.workspace.data_ptr(), _stream(stream, self._index))
+        return _issue(self._lib.gd_linear_status, self.workspace.data_ptr(), stream, self._index)
 
 
 def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
@@ -264,7 +273,7 @@ def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, loss: Optional[to
                              ignore_index, grad_scale, 0, _scalar(grad_scale_dev, "grad_scale_dev", index), 0 if loss is None else loss.data_ptr(),
                              0 if lse is None else lse.data_ptr(), 0 if grad is None else grad.data_ptr(),
                              0 if grad is None else _matrix(grad, "grad", rows, classes, dtype, index))
-    code = load_library().gd_cross_entropy(args, _stream(stream, index))
+    code = _issue(load_library().gd_cross_entropy, args, stream, index)
     if code:
         raise B.GdError(code, "gd_cross_entropy")
 
@@ -346,6 +355,6 @@ class AdamWSession:
         a.step, a.lr, a.beta1, a.beta2, a.eps = step, lr, beta1, beta2, eps
         a.grad_scale, a.seed = grad_scale, seed & 0xFFFFFFFF
         a.grad_scale_dev = _scalar(grad_scale_dev, "grad_scale_dev", self._index)
-        code = load_library().gd_adamw_step(C.byref(a), _stream(stream, self._index))
+        code = _issue(load_library().gd_adamw_step, C.byref(a), stream, self._index)
         if code:
             raise B.GdError(code, "gd_adamw_step")

@@ -1,0 +1,86 @@
+"""What the Python calls of the training operators do around the library's: which device is current, whose arguments are passed, what is
+refused.  No GPU: tensors on the CPU stand in for tensors on device 1, and the library's entry points are replaced."""
+
+import pytest
+import torch
+
+from paper_1704_05021_b200 import binding as B
+from paper_1704_05021_b200 import training as T
+
+
+class OnDevice1(torch.Tensor):
+    def get_device(self):
+        return 1
+
+
+def _on_device_1(t):
+    return t.as_subclass(OnDevice1)
+
+
+class Library:
+    """Entry points that note which device was current and what they were given."""
+
+    def __init__(self, state):
+        self.state, self.seen = state, []
+
+    def __getattr__(self, name):
+        def call(args, stream):
+            self.seen.append((name, self.state["current"], stream))
+            return B.GD_OK
+        return call
+
+
+@pytest.fixture
+def machine(monkeypatch):
+    """Two devices, 0 current; the streams' handles are 100 + device."""
+    state = {"current": 0}
+
+    class Guard:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, state["current"] = state["current"], self.index
+
+        def __exit__(self, *_):
+            state["current"] = self.before
+
+    lib = Library(state)
+    monkeypatch.setattr(T, "_current_device", lambda: state["current"])
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(T, "_raw_stream", lambda index: 100 + index)
+    monkeypatch.setattr(T, "load_library", lambda: lib)
+    state["library"] = lib
+    return state
+
+
+def _session(lib, n_in=16, n_out=24, rows=4):
+    """A LinearSession of device 1 as its constructor leaves it, without the device."""
+    s = object.__new__(T.LinearSession)
+    s._index, s.device = 1, torch.device("cuda", 1)
+    s.n_in, s.n_out, s.max_rows, s.dtype, s.activation, s.w_layout = n_in, n_out, rows, torch.bfloat16, "none", "in_out"
+    s.w_shape, s._lib = (n_in, n_out), lib
+    s._bind(_on_device_1(torch.zeros(4096, dtype=torch.uint8)))
+    return s
+
+
+def _bf16(*shape):
+    return _on_device_1(torch.zeros(*shape, dtype=torch.bfloat16))
+
+
+def test_calls_make_the_tensors_device_current(machine):
+    lib = machine["library"]
+    s = _session(lib)
+    x, w, y = _bf16(4, 16), _bf16(16, 24), _bf16(4, 24)
+    s.forward(x, w, out=y)
+    s.backward(y, x, w, dx=_bf16(4, 16))
+    s.status()
+    T.cross_entropy(_on_device_1(torch.zeros(4, 8)), _on_device_1(torch.zeros(4, dtype=torch.int64)), loss=_on_device_1(torch.zeros(4)))
+    a = object.__new__(T.AdamWSession)
+    a._index, a._args = 1, T._AdamwArgs()
+    a.step(step=1, lr=1e-3)
+    assert lib.seen == [(name, 1, 101) for name in ("gd_linear_forward", "gd_linear_backward", "gd_linear_status", "gd_cross_entropy", "gd_adamw_step")]
+    assert machine["current"] == 0
+    machine["current"] = 1
+    s.status()
+    assert lib.seen[-1] == ("gd_linear_status", 1, 101)
