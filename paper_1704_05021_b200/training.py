@@ -68,10 +68,10 @@ class _AdamwArgs(C.Structure):
                 ("grad_scale", C.c_float), ("reserved", C.c_int32), ("grad_scale_dev", C.c_void_p)]
 
 
-# The parts of the first three that change from call to call, written in one go (setting ctypes fields one by one costs more than the launch):
-# m .. y_dtype .. ld_pre of the first, m .. db of the second, all of the third.
-_FORWARD_FIELDS, _BACKWARD_FIELDS, _LOSS_FIELDS = struct.Struct("<3Q6i11Q"), struct.Struct("<3Q4iIi13Q"), struct.Struct("<2Q2i3Qqfi5Q")
-assert _FORWARD_FIELDS.size == _LinearForwardArgs.workspace.offset and _BACKWARD_FIELDS.size == _LinearBackwardArgs.workspace.offset
+# The first three, written in one go (setting ctypes fields one by one costs more than the launch), anew for every call: the library reads
+# them while other threads may run.
+_FORWARD_FIELDS, _BACKWARD_FIELDS, _LOSS_FIELDS = struct.Struct("<3Q6i13Q"), struct.Struct("<3Q4iIi15Q"), struct.Struct("<2Q2i3Qqfi5Q")
+assert _FORWARD_FIELDS.size == C.sizeof(_LinearForwardArgs) and _BACKWARD_FIELDS.size == C.sizeof(_LinearBackwardArgs)
 assert _LOSS_FIELDS.size == C.sizeof(_CrossEntropyArgs)
 
 _lib = None
@@ -82,7 +82,7 @@ def load_library():
     global _lib
     if _lib is None:
         lib = B.load_library()
-        lib.gd_linear_forward.argtypes = [C.c_void_p, C.c_void_p]         # (the address of the arguments, or byref of a structure)
+        lib.gd_linear_forward.argtypes = [C.c_void_p, C.c_void_p]         # (the bytes of the arguments, or byref of a structure)
         lib.gd_linear_backward.argtypes = [C.c_void_p, C.c_void_p]
         lib.gd_linear_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.c_int, C.POINTER(C.c_size_t)]
         lib.gd_linear_status.argtypes = [C.c_void_p, C.c_void_p]
@@ -177,10 +177,7 @@ class LinearSession:
     def _bind(self, workspace: torch.Tensor) -> None:
         """The arguments that stay the same from call to call."""
         self.workspace = workspace
-        self._forward, self._backward = _LinearForwardArgs(), _LinearBackwardArgs()
-        for a in (self._forward, self._backward):
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-        self._forward_at, self._backward_at = C.addressof(self._forward), C.addressof(self._backward)
+        self._space = (workspace.data_ptr(), workspace.numel())
         self._codes = (self.n_out, self.n_in, _DTYPES[self.dtype], _ACTIVATIONS[self.activation], _LAYOUTS[self.w_layout])
 
     def _rows(self, t: torch.Tensor) -> int:
@@ -204,10 +201,10 @@ class LinearSession:
             residual_at, ld_residual = residual.data_ptr(), _matrix(residual, "residual", m, n, dt, index)
         if pre is not None:
             pre_at, ld_pre = pre.data_ptr(), _matrix(pre, "pre", m, n, dt, index)
-        _FORWARD_FIELDS.pack_into(self._forward, 0, m, *self._codes, bias_code, _DTYPES[out_dt], 0,
-                                  x.data_ptr(), _matrix(x, "x", m, self.n_in, dt, index), w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, index), bias_at,
-                                  residual_at, ld_residual, out.data_ptr(), _matrix(out, "out", m, n, out_dt, index), pre_at, ld_pre)
-        code = _issue(self._lib.gd_linear_forward, self._forward_at, stream, index)
+        args = _FORWARD_FIELDS.pack(m, *self._codes, bias_code, _DTYPES[out_dt], 0, x.data_ptr(), _matrix(x, "x", m, self.n_in, dt, index),
+                                    w.data_ptr(), _matrix(w, "w", *self.w_shape, dt, index), bias_at, residual_at, ld_residual,
+                                    out.data_ptr(), _matrix(out, "out", m, n, out_dt, index), pre_at, ld_pre, *self._space)
+        code = _issue(self._lib.gd_linear_forward, args, stream, index)
         if code:
             raise B.GdError(code, "gd_linear_forward")
         return out
@@ -239,9 +236,10 @@ class LinearSession:
         if db is not None:
             _vector(db, "db", n, (torch.float32,), index)
             db_at = db.data_ptr()
-        _BACKWARD_FIELDS.pack_into(self._backward, 0, m, *self._codes, dw_code, GD_LINEAR_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
-                                   _matrix(dy, "dy", m, n, dt, index), pre_at, ld_pre, x_at, ldx, w_at, ldw, dx_at, ld_dx, dw_at, ld_dw, db_at)
-        code = _issue(self._lib.gd_linear_backward, self._backward_at, stream, index)
+        args = _BACKWARD_FIELDS.pack(m, *self._codes, dw_code, GD_LINEAR_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
+                                     _matrix(dy, "dy", m, n, dt, index), pre_at, ld_pre, x_at, ldx, w_at, ldw, dx_at, ld_dx, dw_at, ld_dw, db_at,
+                                     *self._space)
+        code = _issue(self._lib.gd_linear_backward, args, stream, index)
         if code:
             raise B.GdError(code, "gd_linear_backward")
 

@@ -1,6 +1,9 @@
 """What the Python calls of the training operators do around the library's: which device is current, whose arguments are passed, what is
 refused.  No GPU: tensors on the CPU stand in for tensors on device 1, and the library's entry points are replaced."""
 
+import ctypes as C
+import threading
+
 import pytest
 import torch
 
@@ -84,3 +87,38 @@ def test_calls_make_the_tensors_device_current(machine):
     machine["current"] = 1
     s.status()
     assert lib.seen[-1] == ("gd_linear_status", 1, 101)
+
+
+@pytest.mark.parametrize("direction", ["forward", "backward"])
+def test_threads_on_one_session_do_not_exchange_arguments(machine, direction):
+    """A call into the library lets other threads run before it has read its arguments: they are its own."""
+    entered, released, read = threading.Event(), threading.Event(), []
+
+    class Slow:
+        def __getattr__(self, name):
+            def call(args, stream):
+                if threading.current_thread() is not threading.main_thread():
+                    entered.set()
+                    assert released.wait(30)
+                    read.append(args if isinstance(args, bytes) else C.string_at(args, 128))
+                return B.GD_OK
+            return call
+
+    s = _session(Slow())
+    w, mine, other = _bf16(16, 24), [_bf16(3, 16), _bf16(3, 24)], [_bf16(4, 16), _bf16(4, 24)]
+
+    def use(x, y):
+        if direction == "forward":
+            s.forward(x, w, out=y)
+        else:
+            s.backward(y, x, w, dx=x)
+
+    thread = threading.Thread(target=use, args=mine)
+    thread.start()
+    assert entered.wait(30)
+    use(*other)
+    released.set()
+    thread.join()
+    args = (T._LinearForwardArgs if direction == "forward" else T._LinearBackwardArgs).from_buffer_copy(read[0].ljust(256, b"\0"))
+    assert args.m == 3 and (args.x if direction == "forward" else args.dx) == mine[0].data_ptr()
+    assert (args.y if direction == "forward" else args.dy) == mine[1].data_ptr()
