@@ -8,6 +8,7 @@ stream, or the one passed as `stream`.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import struct
 from typing import Optional, Sequence, Union
@@ -150,6 +151,10 @@ def _issue(call, args, stream, index: int) -> int:
     return call(args, _raw_stream(index) if stream is None else B._stream_handle(stream))
 
 
+def _stream_object(stream, index: int):
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=index)
+
+
 class LinearSession:
     """One linear layer's shape - n_in inputs, n_out outputs, up to max_rows rows at a time - and its workspace.
 
@@ -188,10 +193,13 @@ class LinearSession:
 
     def forward(self, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        """act(x W + bias) + residual, into `out` (float32, or the session's type; made here if None) and, if `pre` is given, x W + bias."""
+        """act(x W + bias) + residual, into `out` (float32, or the session's type; made here, on the call's stream, if None) and, if `pre`
+        is given, x W + bias."""
         m, n, dt, index = self._rows(x), self.n_out, self.dtype, self._index
         if out is None:
-            out = torch.empty(m, n, dtype=dt, device=self.device)
+            # on the stream of the call: memory that other streams gave back may still be in use there
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(_stream_object(stream, index)):
+                out = torch.empty(m, n, dtype=dt, device=self.device)
         out_dt = out.dtype if out.dtype is torch.float32 else dt
         bias_at = bias_code = residual_at = ld_residual = pre_at = ld_pre = 0
         if bias is not None:

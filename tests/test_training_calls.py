@@ -122,3 +122,39 @@ def test_threads_on_one_session_do_not_exchange_arguments(machine, direction):
     args = (T._LinearForwardArgs if direction == "forward" else T._LinearBackwardArgs).from_buffer_copy(read[0].ljust(256, b"\0"))
     assert args.m == 3 and (args.x if direction == "forward" else args.dx) == mine[0].data_ptr()
     assert (args.y if direction == "forward" else args.dy) == mine[1].data_ptr()
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_a_result_made_by_the_call_belongs_to_its_stream(machine, monkeypatch, as_handle):
+    """`out` left out with a stream given: the allocator must take its memory from that stream's, not from what the current stream has freed
+    and its kernels may still be using."""
+    class Stream:
+        def __init__(self, handle, device=None):
+            self.cuda_stream = handle
+
+    current = [7]
+
+    class Using:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            current.append(self.stream.cuda_stream)
+
+        def __exit__(self, *_):
+            current.pop()
+
+    made, empty = [], torch.empty
+
+    def make(*shape, dtype, device):
+        made.append(current[-1])
+        return _on_device_1(empty(*shape, dtype=dtype))
+
+    monkeypatch.setattr(torch.cuda, "stream", Using)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(T.torch, "empty", make)
+    s = _session(machine["library"])
+    x, w = _bf16(4, 16), _bf16(16, 24)
+    s.forward(x, w)
+    s.forward(x, w, stream=55 if as_handle else Stream(55))
+    assert made == [7, 55] and [seen[2] for seen in machine["library"].seen] == [101, 55]

@@ -142,3 +142,19 @@ def test_a_wait_that_runs_out_reaches_the_status(cuda_device):
     dy, db = torch.ones(512, 32, dtype=torch.bfloat16, device=cuda_device), torch.empty(32, device=cuda_device)
     s.backward(dy, None, None, db=db)
     assert bool((db == 512).all()) and s.status() == B.GD_OK
+
+
+# ------------------------------------------------------------------------------------------ results made by the call
+
+def test_result_made_on_another_stream(cuda_device):
+    """Without `out`, on a stream other than the current one, given as an object and as a handle."""
+    gen = _gen(cuda_device, 3)
+    x, w = _rand(gen, 33, 72, dtype=torch.bfloat16), _rand(gen, 72, 40, dtype=torch.bfloat16)
+    s = T.LinearSession(72, 40, 33, device=cuda_device)
+    here = s.forward(x, w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (side, side.cuda_stream, torch.cuda.default_stream()):
+        there = s.forward(x, w, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(here, there)
