@@ -357,6 +357,8 @@ class AdamWSession:
     def step(self, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
              grad_scale_dev: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
         """Update number `step` (from 1).  seed: another one every step for the 8-bit moments' rounding; not used with 32 bits."""
+        if step < 0:                         # (would reach the library as a step near 2^64; 0 is refused there)
+            raise ValueError(f"steps count from 1, got {step}")
         a = self._args
         a.step, a.lr, a.beta1, a.beta2, a.eps = step, lr, beta1, beta2, eps
         a.grad_scale, a.seed = grad_scale, seed & 0xFFFFFFFF

@@ -158,3 +158,12 @@ def test_a_result_made_by_the_call_belongs_to_its_stream(machine, monkeypatch, a
     s.forward(x, w)
     s.forward(x, w, stream=55 if as_handle else Stream(55))
     assert made == [7, 55] and [seen[2] for seen in machine["library"].seen] == [101, 55]
+
+
+def test_a_negative_step_is_refused(machine):
+    """Not passed on as the unsigned number that its bits are."""
+    a = object.__new__(T.AdamWSession)
+    a._index, a._args = 1, T._AdamwArgs()
+    with pytest.raises(ValueError):
+        a.step(step=-1, lr=1e-3)
+    assert machine["library"].seen == []
