@@ -153,7 +153,7 @@ int gd_cross_entropy(const gd_cross_entropy_args* args, void* stream);
  *
  * state_bits = 8: m and the ROOT of v are held as fp8 (1 sign, 4 exponent, 3 mantissa bits, bias 7) times a scale that a block of
  * 128 consecutive elements of a tensor shares: m_scale and v_scale, ceil(n / 128) fp32 powers of two, 2^(E - 7) with 2^E
- * <= the block's largest magnitude < 2^(E + 1) (at least 2^-126).  v is the square of its held root.  A magnitude is rounded up
+ * <= the block's largest finite magnitude < 2^(E + 1) (at least 2^-126).  v is the square of its held root.  A magnitude is rounded up
  * to its upper neighbour with a probability of 1 in 2^16 for every 2^-16 of the way it lies past the lower one, so that
  * moments that change by less than a step still change on average; the 16 random bits are the upper (m) and lower (v) half of
  * mix(i * 0x9E3779B9 + seed + t * 0x85EBCA77) mod 2^32 for element i of tensor t, with mix as in gd.h's sampled-threshold mode.

@@ -127,6 +127,13 @@ __device__ __forceinline__ float warp_largest(float x) {
   asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
+// The same without what is not finite: an element that is held as NaN must not take the scale with it, which the other 127 need.
+__device__ __forceinline__ float largest_finite(const float* x) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(x[j]) < INFINITY ? fabsf(x[j]) : 0.f);
+  return warp_largest(top);
+}
 // The scale of a block from its largest magnitude, and its reciprocal: powers of two, so both products are exact.
 __device__ __forceinline__ void block_scale(float top, float* scale, float* inverse) {
   const int e = max((int)(__float_as_uint(top) >> 23) - 7, 1);
@@ -260,8 +267,10 @@ __device__ __forceinline__ void update_block(Block<BITS>& b, const AdamScalars& 
       for (int j = 0; j < 4; ++j)
         if (at + lane + 32 * j >= n) b.m[j] = root[j] = 0.f;
     }
-    const float m_top = warp_largest(largest(largest(b.m[0], b.m[1]), largest(b.m[2], b.m[3])));
-    const float v_top = warp_largest(largest(largest(root[0], root[1]), largest(root[2], root[3])));
+    float m_top = warp_largest(largest(largest(b.m[0], b.m[1]), largest(b.m[2], b.m[3])));
+    float v_top = warp_largest(largest(largest(root[0], root[1]), largest(root[2], root[3])));
+    const bool finite = m_top < INFINITY && v_top < INFINITY;      // the same for the whole warp
+    if (!finite) m_top = largest_finite(b.m), v_top = largest_finite(root);
     float m_inverse, v_inverse;
     block_scale(m_top, &b.ms, &m_inverse);
     block_scale(v_top, &b.vs, &v_inverse);
@@ -284,7 +293,7 @@ __device__ __forceinline__ void update_block(Block<BITS>& b, const AdamScalars& 
     const uint32_t signs[4] = {__float_as_uint(b.m[0]), __float_as_uint(b.m[1]), __float_as_uint(b.m[2]), __float_as_uint(b.m[3])};
     b.mc = pack_codes(cm);
     b.vc = pack_codes(cv);
-    if (!(m_top < INFINITY && v_top < INFINITY)) {       // the same for the whole warp
+    if (!finite) {
       b.mc = nan_codes(b.mc, b.m);
       b.vc = nan_codes(b.vc, root);
     }

@@ -158,3 +158,33 @@ def test_result_made_on_another_stream(cuda_device):
         there = s.forward(x, w, stream=stream)
         torch.cuda.synchronize()
         assert torch.equal(here, there)
+
+
+# ------------------------------------------------------------------------------------------ values that are not finite
+
+@pytest.mark.parametrize("offset", [0, 1])
+def test_a_moment_that_is_not_finite_leaves_its_block_alone(cuda_device, offset):
+    """8-bit moments: the 127 elements that share a scale with an infinite or NaN gradient go on as they would next to a gradient of 0, with the
+    same scales, bit for bit; the element itself is NaN from then on."""
+    n, bad = 1000, [5, 200, 201, 999]
+    gen = _gen(cuda_device, 21)
+    grad, start = _rand(gen, n, scale=1e-2), _rand(gen, n, scale=0.1)
+    runs = []
+    for values in ([0.0] * 4, [float("inf"), float("nan"), -float("inf"), float("inf")]):
+        flat = [torch.zeros(n + 4, device=cuda_device) for _ in range(2)]
+        p, g = (t[offset:offset + n] for t in flat)
+        p.copy_(start), g.copy_(grad)
+        s = T.AdamWSession([p], [g], weight_decay=0.01, state_bits=8)
+        for step in range(1, 6):
+            g[bad] = torch.tensor(values if step == 2 else [0.0] * 4, device=cuda_device)
+            s.step(step=step, lr=1e-3, seed=step)
+        runs.append([p, s.m[0].float(), s.v[0].float(), s.m_scale[0], s.v_scale[0]])
+    others = torch.ones(n, dtype=torch.bool, device=cuda_device)
+    others[bad] = False
+    for plain, hit in zip(runs[0][:3], runs[1][:3]):
+        assert torch.equal(plain[others], hit[others])
+        assert bool(torch.isfinite(hit[others]).all())
+    for held in runs[1][1:3]:
+        assert bool(torch.isnan(held[bad]).all())
+    for plain, hit in zip(runs[0][3:], runs[1][3:]):
+        assert torch.equal(plain, hit)
