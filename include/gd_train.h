@@ -116,8 +116,9 @@ int gd_selftest_linear_wait(void* workspace, size_t workspace_bytes, uint64_t bu
  *     lse[i]    = log sum_j exp(logits[i, j])
  *     loss[i]   = lse[i] - logits[i, t]
  *     grad[i,j] = (exp(logits[i, j] - lse[i]) - (j == t)) * grad_scale * (*grad_scale_dev)
- * A row whose target is ignore_index has loss 0 and gradient 0 whatever its logits are.  Logits of -inf are masked classes: they
- * take no part and their gradient is 0.  In a row with a target, where every class is masked, or with +inf or NaN among
+ * A row whose target is ignore_index has loss 0 and gradient 0 whatever its logits are (its lse is theirs).  Logits of -inf are masked classes:
+ * they take no part and their gradient is 0, unless the target is one: the row's loss is then +inf, and the gradient as the formula
+ * says, -grad_scale * (*grad_scale_dev) at the target.  In a row with a target, where every class is masked, or with +inf or NaN among
  * the logits, loss and gradient are NaN; so are those of a row whose target is neither ignore_index nor in [0, classes).
  * grad may be logits itself (same address and leading dimension) or NULL; loss and lse may be NULL.  The call has no workspace and
  * so no status word: a device-side wait that gives up leaves NaN in its row's results.

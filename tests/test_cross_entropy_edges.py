@@ -1,4 +1,4 @@
-"""The cross-entropy at row lengths where a slice of a row is as long as shared memory without asking for more, as the first calls of a process.
+"""The cross-entropy at its edges: slices of a row as long as shared memory without asking for more, rows in place, a masked target.
 
 Bounds: exp of a difference d in fp32 is off by |d| 2^-23 for the argument and 2^-21 for the function, sums and the logarithm by a few
 2^-23, a gradient rounds once to its type.
@@ -65,3 +65,24 @@ def test_in_place_with_the_target_in_any_slice(cuda_device, dtype, rows, classes
         T.cross_entropy(inside, t, loss=loss[1], grad=inside)
         assert torch.equal(loss[0], loss[1]) and torch.equal(apart, inside)
     check(rows, classes, dtype, in_place=True)
+
+
+@pytest.mark.parametrize("classes", [10, 700, 5000, 85000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "fp16", "fp32"])
+def test_a_masked_target(cuda_device, dtype, classes):
+    """The target's own logit is -inf while other classes are not masked: loss +inf, the gradient that of the formula; ignored, the row is 0."""
+    gen = torch.Generator(device=cuda_device).manual_seed(classes)
+    x = torch.randn(90, classes, generator=gen, device=cuda_device).to(dtype)
+    x[:, classes // 2:] = -float("inf")
+    t = torch.full((90,), classes - 1, device=cuda_device)
+    t[1::3], t[2::3] = 0, -100
+    loss, lse, grad = torch.empty(90, device=cuda_device), torch.empty(90, device=cuda_device), torch.empty_like(x)
+    T.cross_entropy(x, t, loss=loss, lse=lse, grad=grad, grad_scale=0.5)
+    assert bool((loss[0::3] == float("inf")).all()) and bool(torch.isfinite(loss[1::3]).all()) and bool((loss[2::3] == 0).all())
+    assert bool(((lse.double() - torch.logsumexp(x.double(), 1)).abs() <= 2.0 ** -18).all())
+    p = torch.softmax(x.double(), 1) * 0.5
+    room = p * (2.0 ** -18 + ROUND[dtype]) + 2.0 ** -126 + TINY[dtype]
+    half = slice(0, classes // 2)
+    assert bool(((grad[0::3, half].double() - p[0::3, half]).abs() <= room[0::3, half]).all())
+    assert bool((grad[0::3, classes // 2:classes - 1] == 0).all()) and bool((grad[0::3, classes - 1] == -0.5).all())
+    assert bool((grad[1::3, classes // 2:] == 0).all()) and bool((grad[2::3] == 0).all())
