@@ -47,9 +47,9 @@ bool encode_tile(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t w
 bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_t depth, uint32_t box_extent, bool bf16) {
   return encode_tile(map, o.p, o.ld * 2, o.mn_major ? extent : depth, o.mn_major ? depth : extent, 64, box_extent, bf16 ? GD_DTYPE_BF16 : GD_DTYPE_FP16);
 }
-bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, int dtype) {
+bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, uint32_t cols, int dtype) {
   const uint64_t item = dtype == GD_DTYPE_FP32 ? 4 : 2;
-  return encode_tile(map, p, (ep.rows > 1 ? ld : (ep.cols + 7) / 8 * 8) * item, ep.cols, ep.rows, (uint32_t)(128 / item), 32, dtype);
+  return encode_tile(map, p, (ep.rows > 1 ? ld : (ep.cols + 7) / 8 * 8) * item, cols, ep.rows, (uint32_t)(128 / item), 32, dtype);
 }
 
 cudaError_t launch_product(const Product& p, cudaStream_t stream) {

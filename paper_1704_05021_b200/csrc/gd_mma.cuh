@@ -378,7 +378,7 @@ struct SplitChoice {       // of the split kernel's tile
   uint32_t outer;          // parts of k in clusters of their own, joined by a second launch
   double cost;             // estimated cycles
 };
-bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, int dtype);     // 32 rows x 128 bytes of a result
+bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, uint32_t cols, int dtype);     // 32 rows x 128 bytes of a result, up to `cols`
 cudaError_t launch_product(const Product& p, cudaStream_t stream);
 
 }  // namespace gd

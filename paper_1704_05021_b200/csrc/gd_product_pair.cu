@@ -7,7 +7,9 @@
 // memory, 128 columns of 32 lanes each, and finish the tile while the next one is summed into the other half of it: 2 x 256
 // columns, all there are.  A lane holds a row, so results leave through shared memory: a piece of 32 rows x 128 bytes per warp, two of
 // them in turn, stored by the copy engine, which cuts what lies outside the matrix and takes any row pitch that is a multiple of 16 bytes; the
-// residual comes in the same way, into the piece the result is then written over.  Other pitches: element by element, a row at a time.
+// residual comes in the same way, into the piece the result is then written over.  Stores are cut to whole 16 bytes only (measured: 4096 x 4097
+// results in 16 bits put zeros into the seven elements behind each row; loads are cut to the element), so their map ends at the row's last whole 16
+// bytes and each lane writes what is left of its row.  Other pitches: element by element, a row at a time.
 //
 // Tiles are taken in groups of kGroup tile rows, column by column, so that what the pairs read at one time stays in L2.
 #include <algorithm>
@@ -60,6 +62,8 @@ __device__ __forceinline__ void tile_store(const CUtensorMap* map, const void* s
 // Closes a group of stores.  Every piece closes one, whether it was stored or lies outside the matrix (an empty group is done at once): the pieces
 // take the buffers in turn and stores_read() counts groups, so the two counts have to run together.
 __device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// columns that make up whole 16 bytes of a row
+__host__ __device__ constexpr uint32_t whole_columns(uint32_t cols, uint32_t item) { return cols & ~(16u / item - 1u); }
 template <int LEFT>
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }   // all but LEFT have left shared memory
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -201,7 +205,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
       const auto finish = [&](uint32_t p, float* v) {
         const uint32_t c = c0 + p * W;
         if constexpr (TILED) {
-          const bool inside = r0 < ep.rows && c < ep.cols;
+          const uint32_t whole = whole_columns(ep.cols, WIDE ? 4 : 2);
+          const bool inside = r0 < ep.rows && c < whole;
+          // the row's last columns, short of 16 bytes, from the lane's own row of a piece
+          const auto finish_row = [&](void* to, uint64_t ld, const unsigned char* from) {
+            if (whole == ep.cols || c >= ep.cols || whole >= c + W || r0 + lane >= ep.rows) return;
+            const uint4 q = *reinterpret_cast<const uint4*>(from + ((whole - c) / (W / 8) ^ (lane & 7u)) * 16u);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            const uint64_t at = (uint64_t)(r0 + lane) * ld + whole;
+#pragma unroll
+            for (uint32_t i = 0; i < W / 8; ++i) {
+              if (whole + i >= ep.cols) continue;
+              if constexpr (WIDE) static_cast<uint32_t*>(to)[at + i] = w[i];
+              else static_cast<uint16_t*>(to)[at + i] = (uint16_t)(w[i / 2] >> (i & 1u) * 16u);
+            }
+          };
           const bool two = !WIDE && ep.pre;          // z takes the second buffer
           const uint32_t at = two ? 0u : turn & 1u;
           unsigned char* mine = pieces + at * kPieceBytes + lane * 128u;
@@ -218,6 +236,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
             if (ep.pre) {
 #pragma unroll
               for (uint32_t j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(z + (j ^ (lane & 7u)) * 16u) = narrow8(v + 8 * j, ep.dtype);
+              finish_row(ep.pre, ep.ld_pre, z);
               fence_async();
               __syncwarp();
               if (elect_one()) {
@@ -285,6 +304,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) pro
             else
               *chunk = narrow8(v + 8 * j, ep.dtype);
           }
+          finish_row(ep.out, ep.ld_out, mine);
           fence_async();
           __syncwarp();
           if (elect_one()) {
@@ -447,10 +467,11 @@ cudaError_t launch_product_pair(const Product& p, uint32_t bn, cudaStream_t stre
   g.tiles_r = (p.ep.rows + 255) / 256;
   g.tiles_c = (p.ep.cols + bn - 1) / bn;
   // results and residual as pieces of 32 rows x 128 bytes, where every row starts at a multiple of 16 bytes
-  const bool tiled = g.ep.vectors, wide = g.ep.out_dtype == GD_DTYPE_FP32;
-  if (tiled && (!encode_piece(&g.out, g.ep.out, g.ep.ld_out, g.ep, g.ep.out_dtype) ||
-                (g.ep.pre && !wide && !encode_piece(&g.pre, g.ep.pre, g.ep.ld_pre, g.ep, g.ep.dtype)) ||
-                (g.ep.add && g.ep.add_dtype == g.ep.out_dtype && !encode_piece(&g.add, g.ep.add, g.ep.ld_add, g.ep, g.ep.add_dtype))))
+  const bool wide = g.ep.out_dtype == GD_DTYPE_FP32, tiled = g.ep.vectors && whole_columns(g.ep.cols, wide ? 4 : 2);
+  const uint32_t whole = whole_columns(g.ep.cols, wide ? 4 : 2);
+  if (tiled && (!encode_piece(&g.out, g.ep.out, g.ep.ld_out, g.ep, whole, g.ep.out_dtype) ||
+                (g.ep.pre && !wide && !encode_piece(&g.pre, g.ep.pre, g.ep.ld_pre, g.ep, whole, g.ep.dtype)) ||
+                (g.ep.add && g.ep.add_dtype == g.ep.out_dtype && !encode_piece(&g.add, g.ep.add, g.ep.ld_add, g.ep, g.ep.cols, g.ep.add_dtype))))
     return cudaErrorInvalidValue;
   return bn == 256 ? launch_bn<256>(p, g, tiled, stream) : launch_bn<128>(p, g, tiled, stream);
 }

@@ -125,6 +125,59 @@ def test_weight_gradient_added_to_a_large_matrix(cuda_device):
     _check_weights(cuda_device, 8192, 4104, 4096, "in_out", True)
 
 
+def _slice_of_a_wider_matrix(rows, cols, dtype, device):
+    """[rows, cols] in rows at multiples of 16 bytes, everything around it 77, and a check that it still is."""
+    item = 4 if dtype is torch.float32 else 2
+    pitch = (cols * item // 16 + 2) * 16 // item
+    buf = torch.full(((rows + 1) * pitch,), 77.0, dtype=dtype, device=device)
+    view = buf[:rows * pitch].view(rows, pitch)[:, :cols]
+
+    def untouched():
+        return bool((buf[:rows * pitch].view(rows, pitch)[:, cols:] == 77).all()) and bool((buf[rows * pitch:] == 77).all())
+    return view, untouched
+
+
+@pytest.mark.parametrize("width, kernel", [(4096, "linear_pair"), (2048, "linear_pair_narrow"), (2400, None)])
+@pytest.mark.parametrize("more", [1, 2, 3, 5, 7, 39, 126])
+def test_results_in_a_slice_of_a_wider_matrix(cuda_device, width, kernel, more):
+    """Widths that are no multiple of 16 bytes in rows that are: nothing behind a row is written, whatever the type, with and without z
+    and residual, written and added to.  (The last width comes in 100 rows: the kernel for few tiles.)"""
+    m, n, k, dt = (2560 if kernel else 100), width + more, 136, torch.bfloat16
+    gen = _gen(cuda_device, more)
+    x, w, r = _rand(gen, m, k, dtype=dt), _rand(gen, k, n, dtype=dt, scale=k ** -0.5), _rand(gen, m, n, dtype=dt)
+    ref, size = x.double() @ w.double(), x.double().abs() @ w.double().abs()
+    s = T.LinearSession(k, n, m, device=cuda_device, any_layout=True)
+    for out_dt in (torch.float32, dt):
+        for with_residual in (False, True):
+            for with_pre in (False, True):
+                y, y_kept = _slice_of_a_wider_matrix(m, n, out_dt, cuda_device)
+                z, z_kept = _slice_of_a_wider_matrix(m, n, dt, cuda_device)
+                res, res_kept = _slice_of_a_wider_matrix(m, n, dt, cuda_device)
+                res.copy_(r)
+                call = lambda: s.forward(x, w, residual=res if with_residual else None, out=y, pre=z if with_pre else None)  # noqa: B023, E731
+                assert kernel is None or _kernels(call)[-1] == kernel
+                call()
+                assert y_kept() and z_kept() and res_kept(), (out_dt, with_residual, with_pre)
+                want = ref + r.double() if with_residual else ref
+                room = (k / 16 + 8) * 2.0 ** -22 * size + 2.0 ** -23 * (ref.abs() + want.abs())
+                _within(y, want, room + ROUND[out_dt] * want.abs(), "y")
+                if with_pre:
+                    _within(z, ref, room + ROUND[dt] * ref.abs(), "z")
+    # the weights' gradient of a layer with m inputs and n outputs over k rows
+    xs, dy = _rand(gen, k, m, dtype=dt), _rand(gen, k, n, dtype=dt)
+    ref, size = xs.double().T @ dy.double(), xs.double().abs().T @ dy.double().abs()
+    s = T.LinearSession(m, n, k, device=cuda_device, any_layout=True)
+    start = _rand(gen, m, n)
+    for dw_dt, accumulate in ((torch.float32, False), (torch.float32, True), (dt, False)):
+        dw, kept = _slice_of_a_wider_matrix(m, n, dw_dt, cuda_device)
+        if accumulate:
+            dw.copy_(start)
+        s.backward(dy, xs, None, dw=dw, accumulate=accumulate)
+        assert kept(), (dw_dt, accumulate)
+        want = ref + start.double() if accumulate else ref
+        _within(dw, want, (k / 16 + 8) * 2.0 ** -22 * size + 2.0 ** -23 * (ref.abs() + want.abs()) + ROUND[dw_dt] * want.abs(), "dw")
+
+
 # ------------------------------------------------------------------------------------------ waits that run out
 
 def test_a_wait_that_runs_out_reaches_the_status(cuda_device):
