@@ -1,5 +1,5 @@
 // The linear layer (gd_linear_forward, gd_linear_backward): argument checks, the layout of ragged operands, the activation's
-// slope with the bias gradient, and the products (gd_product_split.cu, gd_product_large.cu).
+// slope with the bias gradient, and the products (gd_product_split.cu, gd_product_pair.cu).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
