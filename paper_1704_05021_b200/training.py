@@ -349,9 +349,11 @@ class AdamWSession:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError("one gradient per tensor is needed")
-        self._args.grad_dtype = _dtype_of(grads[0].dtype)
-        for i, g in enumerate(grads):
-            self._tensors[i].grad = self._flat(g, "grads", self.params[i].numel(), grads[0].dtype)
+        grad_dtype = _dtype_of(grads[0].dtype)
+        addresses = [self._flat(g, "grads", t.n, grads[0].dtype) for g, t in zip(grads, self._tensors)]
+        self._args.grad_dtype = grad_dtype            # (all of them or, where one is refused, none: their type is one for all)
+        for t, address in zip(self._tensors, addresses):
+            t.grad = address
         self.grads = grads
 
     def step(self, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,

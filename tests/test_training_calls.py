@@ -167,3 +167,22 @@ def test_a_negative_step_is_refused(machine):
     with pytest.raises(ValueError):
         a.step(step=-1, lr=1e-3)
     assert machine["library"].seen == []
+
+
+def test_refused_gradients_leave_the_old_ones():
+    """A list of which one tensor is refused changes nothing: neither the type, by which all are read, nor the addresses before that one."""
+    s = object.__new__(T.AdamWSession)
+    s._device, s.params, s._args = torch.device("cpu"), [torch.zeros(8), torch.zeros(5)], T._AdamwArgs()
+    s._tensors = (T._AdamwTensor * 2)()
+    for t, p in zip(s._tensors, s.params):
+        t.n = p.numel()
+    first = [torch.zeros(8, dtype=torch.bfloat16), torch.zeros(5, dtype=torch.bfloat16)]
+    s.set_grads(first)
+    for bad in ([torch.zeros(8), torch.zeros(4)], [torch.zeros(8), torch.zeros(5, dtype=torch.bfloat16)], [torch.zeros(8)], [torch.zeros(8).double()] * 2):
+        with pytest.raises(ValueError):
+            s.set_grads(bad)
+        assert s._args.grad_dtype == T.GD_DTYPE_BF16 and [t.grad for t in s._tensors] == [g.data_ptr() for g in first]
+        assert all(a is b for a, b in zip(s.grads, first))
+    second = [torch.zeros(8), torch.zeros(5)]
+    s.set_grads(second)
+    assert s._args.grad_dtype == T.GD_DTYPE_FP32 and [t.grad for t in s._tensors] == [g.data_ptr() for g in second]
