@@ -290,7 +290,8 @@ class AdamWSession:
     params and grads are lists of contiguous tensors of one type each (float32, bfloat16 or float16; any starting address).  m and v are
     lists of float32 tensors, or - the 8-bit form - of float8_e4m3fn tensors (v holds the root of the second moment) with
     m_scale and v_scale, ceil(n / 128) float32 each; without them the session makes zero moments of state_bits.  copies: 16-bit (or
-    float32) tensors that receive the updated parameters, or None.  weight_decay: one number or one per tensor.
+    float32) tensors that receive the updated parameters, or None.  weight_decay: one number or one per tensor.  Addresses are
+    taken once and the memory behind them is kept: a tensor that is pointed at other memory later (`t.data = ...`) needs a new session.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Optional[Sequence[torch.Tensor]] = None,
@@ -327,22 +328,28 @@ class AdamWSession:
         a.tensors, a.n_tensors, a.state_bits = self._tensors, len(sizes), state_bits
         a.param_dtype = _dtype_of(self.params[0].dtype)
         a.copy_dtype = GD_DTYPE_FP32 if self.copies is None else _dtype_of(self.copies[0].dtype)
+        self._held = []
         for i, n in enumerate(sizes):
             t = self._tensors[i]
             t.n, t.weight_decay = n, float(decay[i])
-            t.param = self._flat(self.params[i], "params", n, self.params[0].dtype)
-            t.m, t.v = (self._flat(s[i], name, n, held) for s, name in ((self.m, "m"), (self.v, "v")))
+            t.param = self._take(self.params[i], "params", n, self.params[0].dtype)
+            t.m, t.v = (self._take(s[i], name, n, held) for s, name in ((self.m, "m"), (self.v, "v")))
             if state_bits == 8:
-                t.m_scale, t.v_scale = (self._flat(s[i], name, -(-n // _SCALE_BLOCK), torch.float32)
+                t.m_scale, t.v_scale = (self._take(s[i], name, -(-n // _SCALE_BLOCK), torch.float32)
                                         for s, name in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale")))
             if self.copies is not None:
-                t.copy = self._flat(self.copies[i], "copies", n, self.copies[0].dtype)
+                t.copy = self._take(self.copies[i], "copies", n, self.copies[0].dtype)
         self.set_grads(grads)
 
-    def _flat(self, t: torch.Tensor, name: str, n: int, dtype) -> int:
+    def _flat(self, t: torch.Tensor, name: str, n: int, dtype) -> torch.Tensor:
+        """The checked tensor's memory under a name of its own, which lives whatever becomes of the tensor."""
         if t.numel() != n or t.dtype != dtype or t.device != self._device or not t.is_contiguous():
             raise ValueError(f"{name}: expected {n} contiguous {dtype} on {self._device}, got {t.dtype} {list(t.shape)} on {t.device}")
-        return t.data_ptr()
+        return t.detach()
+
+    def _take(self, *what) -> int:
+        self._held.append(self._flat(*what))
+        return self._held[-1].data_ptr()
 
     def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
         """The gradients the next steps read (the same buffers are read every step until other ones are set)."""
@@ -350,11 +357,11 @@ class AdamWSession:
         if len(grads) != len(self.params):
             raise ValueError("one gradient per tensor is needed")
         grad_dtype = _dtype_of(grads[0].dtype)
-        addresses = [self._flat(g, "grads", t.n, grads[0].dtype) for g, t in zip(grads, self._tensors)]
+        held = [self._flat(g, "grads", t.n, grads[0].dtype) for g, t in zip(grads, self._tensors)]
         self._args.grad_dtype = grad_dtype            # (all of them or, where one is refused, none: their type is one for all)
-        for t, address in zip(self._tensors, addresses):
-            t.grad = address
-        self.grads = grads
+        for t, g in zip(self._tensors, held):
+            t.grad = g.data_ptr()
+        self.grads, self._held_grads = grads, held
 
     def step(self, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
              grad_scale_dev: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:

@@ -241,3 +241,18 @@ def test_a_moment_that_is_not_finite_leaves_its_block_alone(cuda_device, offset)
         assert bool(torch.isnan(held[bad]).all())
     for plain, hit in zip(runs[0][3:], runs[1][3:]):
         assert torch.equal(plain, hit)
+
+
+# ------------------------------------------------------------------------------------------ memory the session was given
+
+def test_adamw_keeps_the_memory_it_was_given(cuda_device):
+    """The session holds addresses: after a tensor has been pointed at other memory, a step must not write what the allocator has made of the old."""
+    n = 1 << 20
+    p, g, copy = (torch.nn.Parameter(torch.ones(n, device=cuda_device), requires_grad=False) for _ in range(3))
+    s = T.AdamWSession([p], [g], copies=[copy])
+    for t in (p, g, copy):
+        t.data = torch.zeros(4, device=cuda_device)
+    others = [torch.full((n,), 7.0, device=cuda_device) for _ in range(6)]
+    s.step(step=1, lr=0.1)
+    assert all(bool((t == 7).all()) for t in others)
+    assert bool((p == 0).all())
