@@ -68,6 +68,9 @@ int gd_linear_forward(const gd_linear_forward_args* args, void* stream);
  *     db = column sums of dz, fp32
  * Any of dx, dw, db may be NULL.  The products take dz rounded to dtype: exact for GD_ACT_NONE and GD_ACT_RELU (the slope
  * is 0 or 1; 0 at pre = 0), one rounding of at most 2^-8 (bf16) or 2^-11 (fp16) of an entry for GELU and SiLU; db sums the unrounded dz.
+ *
+ * In both calls the tensor cores' fp32 accumulator truncates: a 16-bit result is off by about 1.1e-9 of its size per step of the contraction
+ * before its own rounding (9e-5 over 85000), an fp32 result, summed in chains of 512, by 5e-7 at any depth.
  */
 typedef struct gd_linear_backward_args {
   uint64_t m, n, k;

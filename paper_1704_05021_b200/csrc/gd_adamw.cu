@@ -10,8 +10,8 @@
 // A tensor whose buffers do not all start on a vector boundary (pieces of a flat vector do not), and a tensor's last,
 // partial block, go element by element, lane-contiguous, with the same arithmetic.
 //
-// Measured (one B200): 138 M elements, 32 bits 565 us = 6.8 TB/s; 8 bits with bf16 gradients and copy 425 us (460 under sustained load,
-// when the clocks fall; 706 with the loads through registers and codes made one by one), 90 % of the issue slots used.
+// Measured (one B200): 138 M elements, 32 bits 575 us = 6.7 TB/s; 8 bits with bf16 gradients and copy 446 - 477 us by the clocks under sustained load
+// (425 in short runs; 706 with the loads through registers and codes made one by one), 90 % of the issue slots used.
 #include <cmath>
 
 #include "gd_train.cuh"

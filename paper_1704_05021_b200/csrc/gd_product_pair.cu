@@ -3,7 +3,7 @@
 // Bound by the tensor cores, if they are fed, and by the power the GPU may draw.  A 128 x 256 x 64 block takes an SM 512 cycles; the
 // pair's instruction (cta_group::2) lets each SM bring only its own half of A and of B, 32 KB, so an SM draws 64 bytes per cycle
 // from L2 where a tile of its own of that size would draw 96, and 128 x 128 tiles 128.  Ten warps: one thread asks for the copies
-// (kPairStages blocks deep), one thread of the leading CTA issues the products for both, eight warps take finished sums out of tensor
+// (kStages blocks deep), one thread of the leading CTA issues the products for both, eight warps take finished sums out of tensor
 // memory, 128 columns of 32 lanes each, and finish the tile while the next one is summed into the other half of it: 2 x 256
 // columns, all there are.  A lane holds a row, so results leave through shared memory: a piece of 32 rows x 128 bytes per warp, two of
 // them in turn, stored by the copy engine, which cuts what lies outside the matrix and takes any row pitch that is a multiple of 16 bytes; the

@@ -10,8 +10,8 @@
 // lanes holds a row in registers.  exp(x - m) subtracts first, in fp32: the difference is exact where it matters, and masked or
 // lowest-value logits give 0 and never a NaN.
 //
-// Measured (one B200): 4000 x 85000 in bf16 246 us = 5.5 TB/s (plain loads, two passes over shared memory and cluster barriers: 361);
-// 1.0 GB of fp32 rows of 2048 .. 85000 6.3 - 6.7 TB/s.
+// Measured (one B200): 4000 x 85000 in bf16 266 us = 5.1 TB/s under sustained load, 246 in short runs (361 by plain loads,
+// two passes over shared memory and cluster barriers); 1.0 GB of fp32 rows of 2048 .. 85000 6.3 - 6.7 TB/s.
 #include <algorithm>
 #include <type_traits>
 
