@@ -1,0 +1,315 @@
+"""The layers of a language model around the linear layer and the loss: ctypes binding of include/gd_layers.h and the objects that hold what its
+calls need between them.
+
+`EmbeddingSession` (a table's shape, and the workspace of its gradient), `LayerNormSession`, `recurrence_forward` and `recurrence_backward`, and
+`GatedLinearSession` check the tensors they are given, marshal addresses and issue the calls, as training.py does: all
+arithmetic happens inside libgd.so.  Tensors must live on the device of the call and be ready on its stream: the current stream, or the
+one passed as `stream`.  A session's workspace is part of it: calls on different streams must be ordered with respect to each other, or use
+sessions of their own; a captured graph uses the workspace of the session that was called.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+import struct
+from typing import Optional
+
+import torch
+
+from . import binding as B
+from . import training as T
+from .training import _ACTIVATIONS, _DTYPES, _LAYOUTS, _cuda_index, _dtype_of, _issue, _matrix, _stream_object, _vector
+
+GD_EMBEDDING_ACCUMULATE = 1
+GD_LAYER_NORM_ACCUMULATE = 1
+
+EXPORTS = ["gd_embedding_forward", "gd_embedding_backward", "gd_embedding_workspace_bytes", "gd_layer_norm_forward", "gd_layer_norm_backward",
+           "gd_layer_norm_workspace_bytes", "gd_recurrence_forward", "gd_recurrence_backward", "gd_recurrence_marks_rows"]
+
+
+class _EmbeddingForwardArgs(C.Structure):
+    _fields_ = [("tokens", C.c_uint64), ("vocab", C.c_uint64), ("width", C.c_uint64), ("table_dtype", C.c_int32), ("y_dtype", C.c_int32),
+                ("id_bits", C.c_int32), ("scale", C.c_float), ("ignore_index", C.c_int64), ("table", C.c_void_p), ("ld_table", C.c_uint64),
+                ("ids", C.c_void_p), ("y", C.c_void_p), ("ld_y", C.c_uint64)]
+
+
+class _EmbeddingBackwardArgs(C.Structure):
+    _fields_ = [("tokens", C.c_uint64), ("vocab", C.c_uint64), ("width", C.c_uint64), ("dtype", C.c_int32), ("dtable_dtype", C.c_int32),
+                ("id_bits", C.c_int32), ("scale", C.c_float), ("ignore_index", C.c_int64), ("flags", C.c_uint32), ("reserved", C.c_int32),
+                ("dy", C.c_void_p), ("ld_dy", C.c_uint64), ("ids", C.c_void_p), ("dtable", C.c_void_p), ("ld_dtable", C.c_uint64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class _LayerNormForwardArgs(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("width", C.c_uint64), ("dtype", C.c_int32), ("param_dtype", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32),
+                ("x", C.c_void_p), ("ldx", C.c_uint64), ("weight", C.c_void_p), ("bias", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_uint64),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p)]
+
+
+class _LayerNormBackwardArgs(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("width", C.c_uint64), ("dtype", C.c_int32), ("param_dtype", C.c_int32), ("flags", C.c_uint32), ("reserved", C.c_int32),
+                ("dy", C.c_void_p), ("ld_dy", C.c_uint64), ("x", C.c_void_p), ("ldx", C.c_uint64), ("weight", C.c_void_p), ("mean", C.c_void_p),
+                ("rstd", C.c_void_p), ("add", C.c_void_p), ("ld_add", C.c_uint64), ("dx", C.c_void_p), ("ld_dx", C.c_uint64),
+                ("dweight", C.c_void_p), ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class _RecurrenceForwardArgs(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("sequences", C.c_uint64), ("width", C.c_uint64), ("dtype", C.c_int32), ("offset_bits", C.c_int32),
+                ("offsets", C.c_void_p), ("gate", C.c_void_p), ("ld_gate", C.c_uint64), ("value", C.c_void_p), ("ld_value", C.c_uint64),
+                ("y", C.c_void_p), ("ld_y", C.c_uint64), ("h0", C.c_void_p), ("h_last", C.c_void_p), ("marks", C.c_void_p)]
+
+
+class _RecurrenceBackwardArgs(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("sequences", C.c_uint64), ("width", C.c_uint64), ("dtype", C.c_int32), ("offset_bits", C.c_int32),
+                ("offsets", C.c_void_p), ("dy", C.c_void_p), ("ld_dy", C.c_uint64), ("gate", C.c_void_p), ("ld_gate", C.c_uint64),
+                ("value", C.c_void_p), ("ld_value", C.c_uint64), ("marks", C.c_void_p), ("dgate", C.c_void_p), ("ld_dgate", C.c_uint64),
+                ("dvalue", C.c_void_p), ("ld_dvalue", C.c_uint64), ("dh_last", C.c_void_p), ("dh0", C.c_void_p)]
+
+
+# written in one go for every call, as in training.py
+_FIELDS = {_EmbeddingForwardArgs: struct.Struct("<3Q3ifq5Q"), _EmbeddingBackwardArgs: struct.Struct("<3Q3ifqIi7Q"),
+           _LayerNormForwardArgs: struct.Struct("<2Q2ifi8Q"), _LayerNormBackwardArgs: struct.Struct("<2Q2iIi15Q"),
+           _RecurrenceForwardArgs: struct.Struct("<3Q2i10Q"), _RecurrenceBackwardArgs: struct.Struct("<3Q2i14Q")}
+assert all(fields.size == C.sizeof(args) for args, fields in _FIELDS.items())
+_EMBED, _EMBED_BACK, _NORM, _NORM_BACK, _SCAN, _SCAN_BACK = _FIELDS.values()
+
+_lib = None
+
+
+def load_library():
+    """libgd.so with the prototypes of gd_layers.h (see binding.load_library)."""
+    global _lib
+    if _lib is None:
+        lib = T.load_library()
+        for name in EXPORTS:
+            function = getattr(lib, name)
+            function.argtypes, function.restype = [C.c_void_p, C.c_void_p], C.c_int      # (the bytes of the arguments, or byref of a structure)
+        lib.gd_embedding_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.POINTER(C.c_size_t)]
+        lib.gd_layer_norm_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.POINTER(C.c_size_t)]
+        lib.gd_recurrence_marks_rows.argtypes = [C.c_uint64, C.c_uint64, C.POINTER(C.c_uint64)]
+        _lib = lib
+    return _lib
+
+
+def _call(function, name: str, args: bytes, stream, index: int) -> None:
+    code = _issue(function, args, stream, index)
+    if code:
+        raise B.GdError(code, name)
+
+
+def _new(rows: int, cols: int, dtype, stream, index: int) -> torch.Tensor:
+    """A result made by a call, from the call's stream: memory that other streams gave back may still be in use there."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(_stream_object(stream, index)):
+        return torch.empty(rows, cols, dtype=dtype, device=torch.device("cuda", index))
+
+
+def _opt_matrix(t: Optional[torch.Tensor], name: str, rows: int, cols: int, dtype, index: int):
+    return (0, 0) if t is None else (t.data_ptr(), _matrix(t, name, rows, cols, dtype, index))
+
+
+def _opt_vector(t: Optional[torch.Tensor], name: str, n: int, dtypes, index: int) -> int:
+    if t is None:
+        return 0
+    _vector(t, name, n, dtypes, index)
+    return t.data_ptr()
+
+
+def _opt_state(t: Optional[torch.Tensor], name: str, rows: int, cols: int, index: int) -> int:
+    if t is None:
+        return 0
+    if t.dtype is not torch.float32 or t.shape != (rows, cols) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous torch.float32 [{rows}, {cols}] on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+_F32 = (torch.float32,)
+_INTS = (torch.int64, torch.int32)
+
+
+class EmbeddingSession:
+    """The shape of an embedding table - vocab rows of width elements - and the workspace that its gradient for up to max_tokens positions takes
+    (gradient=False: none, for a program that only looks up).
+
+    ids are vectors of int32 or int64.  A position whose id is ignore_index is padding: its row is zeros and its gradient counts nowhere.  An
+    id that is not in the table gives a row of NaN and has no part in the gradient.
+    """
+
+    def __init__(self, vocab: int, width: int, max_tokens: int, device="cuda", gradient: bool = True):
+        self._index = index = _cuda_index(device)
+        self.device = torch.device("cuda", index)
+        self.vocab, self.width, self.max_tokens = int(vocab), int(width), int(max_tokens)
+        self._lib = load_library()
+        size = C.c_size_t(0)
+        B._check(self._lib.gd_embedding_workspace_bytes(self.max_tokens, self.vocab, self.width, C.byref(size)), "gd_embedding_workspace_bytes")
+        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device) if gradient else None
+
+    def _ids(self, ids: torch.Tensor) -> int:
+        n = ids.shape[0] if ids.dim() == 1 else -1
+        if not 0 <= n <= self.max_tokens:
+            raise ValueError(f"at most {self.max_tokens} positions in a vector of ids, got {list(ids.shape)}")
+        _vector(ids, "ids", n, _INTS, self._index)
+        return n
+
+    def forward(self, table: torch.Tensor, ids: torch.Tensor, out: Optional[torch.Tensor] = None, scale: float = 1.0, ignore_index: int = -100,
+                stream=None) -> torch.Tensor:
+        """scale * table[ids], into `out` (the table's type, or float32; from a float32 table any; made here if None)."""
+        n, index, width = self._ids(ids), self._index, self.width
+        ld = _matrix(table, "table", self.vocab, width, table.dtype, index)
+        if out is None:
+            out = _new(n, width, table.dtype, stream, index)
+        args = _EMBED.pack(n, self.vocab, width, _dtype_of(table.dtype), _dtype_of(out.dtype), 64 if ids.dtype is torch.int64 else 32, scale, ignore_index,
+                           table.data_ptr(), ld, ids.data_ptr(), out.data_ptr(), _matrix(out, "out", n, width, out.dtype, index))
+        _call(self._lib.gd_embedding_forward, "gd_embedding_forward", args, stream, index)
+        return out
+
+    def backward(self, dy: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, scale: float = 1.0, accumulate: bool = False, ignore_index: int = -100,
+                 stream=None) -> None:
+        """dtable (float32, or dy's type) receives scale times the sums of dy's rows of equal ids, zeros elsewhere; accumulate adds them to what a
+        float32 dtable holds and leaves the other rows as they are."""
+        n, index, width = self._ids(ids), self._index, self.width
+        if self.workspace is None:
+            raise ValueError("a session made with gradient=False has no workspace for backward")
+        args = _EMBED_BACK.pack(n, self.vocab, width, _dtype_of(dy.dtype), _dtype_of(dtable.dtype), 64 if ids.dtype is torch.int64 else 32, scale, ignore_index,
+                                GD_EMBEDDING_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(), _matrix(dy, "dy", n, width, dy.dtype, index),
+                                ids.data_ptr(), dtable.data_ptr(), _matrix(dtable, "dtable", self.vocab, width, dtable.dtype, index),
+                                self.workspace.data_ptr(), self.workspace.numel())
+        _call(self._lib.gd_embedding_backward, "gd_embedding_backward", args, stream, index)
+
+
+class LayerNormSession:
+    """Layer norm over rows of `width` elements of one type (float32, bfloat16 or float16), up to max_rows at a time, and the workspace for the sums
+    of its parameters' gradients.  weight and bias are float32 or of the rows' type, both the same."""
+
+    def __init__(self, width: int, max_rows: int, dtype=torch.bfloat16, eps: float = 1e-5, device="cuda"):
+        self._index = index = _cuda_index(device)
+        self.device = torch.device("cuda", index)
+        self._code = _dtype_of(dtype)
+        if not eps >= 0:
+            raise ValueError(f"eps is not negative, got {eps}")
+        self.width, self.max_rows, self.dtype, self.eps = int(width), int(max_rows), dtype, float(eps)
+        self._lib = load_library()
+        size = C.c_size_t(0)
+        B._check(self._lib.gd_layer_norm_workspace_bytes(self.max_rows, self.width, C.byref(size)), "gd_layer_norm_workspace_bytes")
+        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+
+    def _rows(self, t: torch.Tensor) -> int:
+        rows = t.shape[0] if t.dim() == 2 else -1
+        if not 0 <= rows <= self.max_rows:
+            raise ValueError(f"at most {self.max_rows} rows of a matrix, got {list(t.shape)}")
+        return rows
+
+    def _params(self, *params):
+        """The type code of the parameters given, and their addresses."""
+        given = [p for p in params if p is not None]
+        dtype = given[0].dtype if given else torch.float32
+        if dtype not in (torch.float32, self.dtype):
+            raise ValueError(f"weight and bias are float32 or {self.dtype}, got {dtype}")
+        return _DTYPES[dtype], [_opt_vector(p, "weight or bias", self.width, (dtype,), self._index) for p in params]
+
+    def forward(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """(x - mean) * rstd * weight + bias into `out` (may be x; made here if None), and each row's mean and rstd (float32) if given."""
+        rows, width, dt, index = self._rows(x), self.width, self.dtype, self._index
+        ldx = _matrix(x, "x", rows, width, dt, index)
+        if out is None:
+            out = _new(rows, width, dt, stream, index)
+        code, (weight_at, bias_at) = self._params(weight, bias)
+        args = _NORM.pack(rows, width, self._code, code, self.eps, 0, x.data_ptr(), ldx, weight_at, bias_at, out.data_ptr(),
+                          _matrix(out, "out", rows, width, dt, index), _opt_vector(mean, "mean", rows, _F32, index), _opt_vector(rstd, "rstd", rows, _F32, index))
+        _call(self._lib.gd_layer_norm_forward, "gd_layer_norm_forward", args, stream, index)
+        return out
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                 dx: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                 dbias: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None) -> None:
+        """The gradients whose buffers are given.  add is the gradient that reaches x past the norm and is added to dx; dx may be dy or add itself.
+        dweight and dbias are float32; accumulate adds to what they hold."""
+        rows, width, dt, index = self._rows(dy), self.width, self.dtype, self._index
+        code, (weight_at,) = self._params(weight)
+        sums = [_opt_vector(t, name, width, _F32, index) for t, name in ((dweight, "dweight"), (dbias, "dbias"))]
+        _vector(mean, "mean", rows, _F32, index)
+        _vector(rstd, "rstd", rows, _F32, index)
+        args = _NORM_BACK.pack(rows, width, self._code, code, GD_LAYER_NORM_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
+                               _matrix(dy, "dy", rows, width, dt, index), x.data_ptr(), _matrix(x, "x", rows, width, dt, index), weight_at, mean.data_ptr(),
+                               rstd.data_ptr(), *_opt_matrix(add, "add", rows, width, dt, index), *_opt_matrix(dx, "dx", rows, width, dt, index), *sums,
+                               self.workspace.data_ptr(), self.workspace.numel())
+        _call(self._lib.gd_layer_norm_backward, "gd_layer_norm_backward", args, stream, index)
+
+
+def _spans(rows: int, offsets: Optional[torch.Tensor], sequences: int, index: int):
+    """offset_bits and the address of offsets."""
+    if offsets is None:
+        if sequences < 1 or rows % sequences:
+            raise ValueError(f"without offsets {rows} rows are equal parts for {sequences} sequences")
+        return 64, 0
+    _vector(offsets, "offsets", sequences + 1, _INTS, index)
+    return 64 if offsets.dtype is torch.int64 else 32, offsets.data_ptr()
+
+
+def _matrix_index(t: torch.Tensor, name: str) -> int:
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected a matrix, got {list(t.shape)}")
+    if t.get_device() < 0:
+        raise RuntimeError("a CUDA device is needed: the library has no CPU path")
+    return t.get_device()
+
+
+def recurrence_marks(rows: int, sequences: int, width: int, device="cuda") -> torch.Tensor:
+    """Room for the states that recurrence_forward keeps for recurrence_backward, for up to this many rows and sequences."""
+    count = C.c_uint64(0)
+    B._check(load_library().gd_recurrence_marks_rows(rows, sequences, C.byref(count)), "gd_recurrence_marks_rows")
+    return torch.empty(count.value, width, dtype=torch.float32, device=torch.device("cuda", _cuda_index(device)))
+
+
+def _marks(marks: Optional[torch.Tensor], rows: int, sequences: int, width: int, index: int) -> int:
+    if marks is None:
+        return 0
+    count = C.c_uint64(0)
+    B._check(load_library().gd_recurrence_marks_rows(rows, sequences, C.byref(count)), "gd_recurrence_marks_rows")
+    if marks.dtype is not torch.float32 or marks.dim() != 2 or marks.shape[1] != width or marks.shape[0] < count.value or marks.get_device() != index or \
+            not marks.is_contiguous():
+        raise ValueError(f"marks: expected contiguous torch.float32 [{count.value}, {width}] on cuda:{index}, got {marks.dtype} {list(marks.shape)} on {marks.device}")
+    return marks.data_ptr()
+
+
+def recurrence_forward(gate: torch.Tensor, value: torch.Tensor, out: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                       sequences: int = 1, h0: Optional[torch.Tensor] = None, h_last: Optional[torch.Tensor] = None,
+                       marks: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """h[t] = f h[t-1] + (1 - f) value[t] with f = sigmoid(gate[t]), per column, over sequences that lie one behind the other in the rows.
+
+    offsets (int32 or int64, sequences + 1): where each begins and the last one ends; None: equal parts.  h0 and h_last: [sequences, width]
+    float32, the states before and after; they may be one tensor, as in a model that answers token by token (one row per sequence).
+    `out` (of value's type; made here if None) receives the states; rows that belong to no sequence are left as they are.  marks (from
+    recurrence_marks) are what recurrence_backward takes.
+    """
+    index = _matrix_index(value, "value")
+    rows, width = value.shape
+    dt = value.dtype
+    code = _dtype_of(dt)
+    bits, offsets_at = _spans(rows, offsets, sequences, index)
+    gate_ld, value_ld = _matrix(gate, "gate", rows, width, dt, index), _matrix(value, "value", rows, width, dt, index)
+    if out is None:
+        out = _new(rows, width, dt, stream, index)
+    args = _SCAN.pack(rows, sequences, width, code, bits, offsets_at, gate.data_ptr(), gate_ld, value.data_ptr(), value_ld, out.data_ptr(),
+                      _matrix(out, "out", rows, width, dt, index), _opt_state(h0, "h0", sequences, width, index),
+                      _opt_state(h_last, "h_last", sequences, width, index), _marks(marks, rows, sequences, width, index))
+    _call(load_library().gd_recurrence_forward, "gd_recurrence_forward", args, stream, index)
+    return out
+
+
+def recurrence_backward(dy: torch.Tensor, gate: torch.Tensor, value: torch.Tensor, marks: torch.Tensor, dgate: torch.Tensor, dvalue: torch.Tensor,
+                        offsets: Optional[torch.Tensor] = None, sequences: int = 1, dh_last: Optional[torch.Tensor] = None,
+                        dh0: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of recurrence_forward for dy and dh_last (the gradients of its result and of h_last), with the marks, offsets and sequences of that
+    call.  dgate may be gate or dy itself, dvalue value."""
+    index = _matrix_index(value, "value")
+    rows, width = value.shape
+    dt = value.dtype
+    code = _dtype_of(dt)
+    bits, offsets_at = _spans(rows, offsets, sequences, index)
+    matrices = []
+    for t, name in ((dy, "dy"), (gate, "gate"), (value, "value"), (dgate, "dgate"), (dvalue, "dvalue")):
+        matrices += (t.data_ptr(), _matrix(t, name, rows, width, dt, index))
+    args = _SCAN_BACK.pack(rows, sequences, width, code, bits, offsets_at, *matrices[:6], _marks(marks, rows, sequences, width, index), *matrices[6:],
+                           _opt_state(dh_last, "dh_last", sequences, width, index), _opt_state(dh0, "dh0", sequences, width, index))
+    _call(load_library().gd_recurrence_backward, "gd_recurrence_backward", args, stream, index)
