@@ -4,6 +4,7 @@
  *   gd_embedding_forward / _backward    lookup of scaled rows, and their gradient by sorted tokens
  *   gd_layer_norm_forward / _backward   layer norm of rows
  *   gd_recurrence_forward / _backward   a gated linear recurrence over packed sequences
+ *   gd_gated_forward / _backward        the gated feed-forward block: two projections, activation and product
  *
  * The conventions of gd_train.h hold: device pointers, a stream as void*, calls only enqueue and never allocate, argument errors are
  * found on the host before anything is enqueued and returned as a gd_status_t.  All sums, statistics and states are fp32; a result is
@@ -187,6 +188,68 @@ typedef struct gd_recurrence_backward_args {
 } gd_recurrence_backward_args;
 
 int gd_recurrence_backward(const gd_recurrence_backward_args* args, void* stream);
+
+/*
+ * gd_gated_forward - the gated feed-forward block up to its hidden layer.  x [m, k], W given as w [k, 2 n] or [2 n, k] (w_layout): the first n
+ * outputs are the gate, the others are multiplied by it.
+ *     z = x W + bias  [m, 2 n]        y = act(z[:, :n]) * z[:, n:]  [m, n]        pre = z, rounded to dtype
+ * fp32 accumulation; y is made from the unrounded z.  m, n and k may be 0 (an empty sum is 0).
+ */
+typedef struct gd_gated_forward_args {
+  uint64_t m, n, k;                /* each < 2^30 */
+  int32_t dtype;                   /* of x, w, y and pre: GD_DTYPE_BF16 or GD_DTYPE_FP16 */
+  int32_t activation;              /* GD_ACT_* */
+  int32_t w_layout;                /* GD_W_* */
+  int32_t bias_dtype;              /* GD_DTYPE_FP32, or dtype */
+  const void* x;
+  uint64_t ldx;
+  const void* w;
+  uint64_t ldw;
+  const void* bias;                /* 2 n, or NULL */
+  void* y;                         /* [m, n] */
+  uint64_t ldy;
+  void* pre;                       /* [m, 2 n], or NULL */
+  uint64_t ld_pre;
+  void* workspace;                 /* 256-byte aligned, >= gd_gated_workspace_bytes(); zeroed once before its first use */
+  size_t workspace_bytes;
+} gd_gated_forward_args;
+
+int gd_gated_forward(const gd_gated_forward_args* args, void* stream);
+
+/*
+ * gd_gated_backward - gradients of the above for dy, the gradient of y, with a = pre[:, :n] and u = pre[:, n:]:
+ *     dz = [dy * u * act'(a), dy * act(a)]  [m, 2 n]
+ *     dx = dz W^T  [m, k], dtype      dw = x^T dz in w's layout, dw_dtype      db = column sums of dz, 2 n fp32
+ * Any of dx, dw, db may be NULL.  The products take dz rounded to dtype (one rounding of at most 2^-8 (bf16) or 2^-11 (fp16) of an
+ * entry); db sums the unrounded dz.  With GD_LINEAR_ACCUMULATE dw (GD_DTYPE_FP32 then) and db are added to what their buffers hold.
+ */
+typedef struct gd_gated_backward_args {
+  uint64_t m, n, k;
+  int32_t dtype, activation, w_layout;
+  int32_t dw_dtype;                /* dtype, or GD_DTYPE_FP32 */
+  uint32_t flags;                  /* GD_LINEAR_ACCUMULATE or 0 */
+  int32_t reserved;                /* 0 */
+  const void* dy;                  /* [m, n] */
+  uint64_t ld_dy;
+  const void* pre;                 /* [m, 2 n] */
+  uint64_t ld_pre;
+  const void* x;                   /* may be NULL without dw */
+  uint64_t ldx;
+  const void* w;                   /* may be NULL without dx */
+  uint64_t ldw;
+  void* dx;
+  uint64_t ld_dx;
+  void* dw;
+  uint64_t ld_dw;
+  float* db;
+  void* workspace;
+  size_t workspace_bytes;
+} gd_gated_backward_args;
+
+int gd_gated_backward(const gd_gated_backward_args* args, void* stream);
+
+/* Workspace of the two calls above for up to m rows; any_layout and the status word as in gd_linear_workspace_bytes(), read by gd_linear_status(). */
+int gd_gated_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, int any_layout, size_t* bytes_out);
 
 #ifdef __cplusplus
 }

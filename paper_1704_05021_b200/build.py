@@ -11,7 +11,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libgd.so")
 SOURCES = ["gd_emit.cu", "gd_emit_pipe.cu", "gd_select.cu", "gd_compact.cu", "gd_candidates.cu", "gd_predict.cu", "gd_dense.cu", "gd_apply.cu", "gd_api.cu",
-           "gd_adamw.cu", "gd_xent.cu", "gd_linear.cu", "gd_product_split.cu", "gd_product_pair.cu", "gd_norm.cu", "gd_embed.cu", "gd_recurrence.cu"]
+           "gd_adamw.cu", "gd_xent.cu", "gd_linear.cu", "gd_product_split.cu", "gd_product_pair.cu", "gd_norm.cu", "gd_embed.cu", "gd_recurrence.cu", "gd_gated.cu",
+           "gd_gated_product.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-shared", "-Xcompiler", "-fPIC", "-cudart", "static", "--threads", "0",

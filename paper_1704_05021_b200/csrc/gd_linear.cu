@@ -4,7 +4,7 @@
 #include <cmath>
 #include <cstring>
 
-#include "gd_mma.cuh"
+#include "gd_linear.cuh"
 
 namespace gd {
 
@@ -65,65 +65,11 @@ cudaError_t launch_product(const Product& p, cudaStream_t stream) {
 
 namespace {
 
-constexpr uint32_t kStatusBytes = 256;
-
-// ---------------------------------------------------------------- ragged operands
-// A matrix of 16-bit elements whose rows are no multiple of 16 bytes (or start anywhere), laid out with rows of 8 `vecs` elements; the
-// columns between are zeros.  A thread makes 16 bytes of the result: bound by the bytes, read and written once.
-struct Pack {
-  const uint16_t* src;
-  uint4* dst;
-  uint64_t ld;
-  uint32_t rows, cols, vecs;
-};
-struct Packs {
-  Pack p[2];
-  uint32_t count;
-};
-__device__ __forceinline__ void pack_rows(const Packs& all, uint64_t first, uint64_t step) {
-  for (uint32_t i = 0; i < all.count; ++i) {
-    const Pack& k = all.p[i];
-    const uint64_t total = (uint64_t)k.rows * k.vecs;
-#pragma unroll 4
-    for (uint64_t t = first; t < total; t += step) {
-      // (64-bit division only where 32 bits do not hold the position)
-      const uint32_t r = total >> 32 ? (uint32_t)(t / k.vecs) : (uint32_t)t / k.vecs, c = ((uint32_t)t - r * k.vecs) * 8u;
-      const uint16_t* s = k.src + r * k.ld + c;
-      uint32_t w[4];
-      if (c + 8 <= k.cols && ((uintptr_t)s & 7u) == 0) {
-        const uint2 lo = __ldcs(reinterpret_cast<const uint2*>(s)), hi = __ldcs(reinterpret_cast<const uint2*>(s) + 1);
-        w[0] = lo.x, w[1] = lo.y, w[2] = hi.x, w[3] = hi.y;
-      } else if (c + 8 <= k.cols && ((uintptr_t)s & 3u) == 0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = reinterpret_cast<const uint32_t*>(s)[j];
-      } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-          const uint32_t a = c + 2 * j < k.cols ? s[2 * j] : 0u, b = c + 2 * j + 1 < k.cols ? s[2 * j + 1] : 0u;
-          w[j] = a | b << 16;
-        }
-      }
-      k.dst[t] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  }
-}
 constexpr uint32_t kPackThreads = 256;
 __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constant__ Packs all) {
   pdl_wait();
   pdl_trigger();
   pack_rows(all, (uint64_t)blockIdx.x * kPackThreads + threadIdx.x, (uint64_t)gridDim.x * kPackThreads);
-}
-uint32_t pack_ctas(const Packs& all, uint32_t threads) {
-  uint64_t most = 0;
-  for (uint32_t i = 0; i < all.count; ++i) most = std::max(most, ((uint64_t)all.p[i].rows * all.p[i].vecs + threads - 1) / threads);
-  return (uint32_t)std::min<uint64_t>(most, (uint64_t)sm_count() * 1024 / threads);
-}
-cudaError_t launch_pack(const Packs& all, cudaStream_t stream) {
-  if (all.count == 0) return cudaSuccess;
-  ProfileScope ps(stream, PT_LINEAR_PACK);
-  const cudaError_t e = launch_dependent(pack_kernel, dim3(pack_ctas(all, kPackThreads)), dim3(kPackThreads), 0, stream, all);
-  if (e == cudaSuccess) note_launches(1);
-  return e;
 }
 
 // ---------------------------------------------------------------- dz and db
@@ -148,26 +94,6 @@ struct SlopeArgs {
   uint32_t missing;    // bytes awaited that nobody sends (0; the self-test's 8)
   Packs packs;
 };
-// Eight 16-bit elements from column c of a row that starts anywhere: the two aligned vectors around them, moved into place. Both lie within
-// the row where `inner` holds; a row's ends are read element by element.
-__device__ __forceinline__ bool inner(uint32_t c, uint32_t cols) { return c >= 8 && c + 16 <= cols; }
-struct Around {
-  uint4 lo, hi;
-};
-__device__ __forceinline__ Around load_around(const uint16_t* s) {
-  const uint4* at = reinterpret_cast<const uint4*>((uintptr_t)s & ~(uintptr_t)15);
-  return Around{at[0], at[1]};
-}
-__device__ __forceinline__ uint4 into_place(const Around& a, const uint16_t* s) {
-  const uint32_t off = (uint32_t)(uintptr_t)s & 15u;
-  uint32_t w[8] = {a.lo.x, a.lo.y, a.lo.z, a.lo.w, a.hi.x, a.hi.y, a.hi.z, a.hi.w};
-#pragma unroll
-  for (int j = 0; j < 6; ++j) w[j] = off & 8u ? w[j + 2] : w[j];
-#pragma unroll
-  for (int j = 0; j < 5; ++j) w[j] = off & 4u ? w[j + 1] : w[j];
-  const uint32_t bits = (off & 2u) * 8u;
-  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
-}
 // RAGGED: rows of kWideRow columns and more that start anywhere, read by `load_around`; shorter ones are read element by element, two rows at a
 // time.  Backward of 6563 x 1120 <- 3347 155 against 197 us, column sums of 2000 x 85001 138 against 182; slopes of 6214 x 38 14.6
 // against 12.6, of 11506 x 433 26.9 against 25.2 (few loads in hand and many ends).
@@ -335,53 +261,11 @@ cudaError_t launch_slope(SlopeArgs& a, int dtype, cudaStream_t stream) {
 }
 
 // ---------------------------------------------------------------- host side
-uint64_t up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
-bool tiles_as_it_is(const void* p, uint64_t ld) { return aligned_to(p, 16) && ld % 8 == 0; }
-// 16-byte accesses at columns that are multiples of 8 stay aligned
-bool vector_rows(const void* p, uint64_t ld, int dt) { return !p || (aligned_to(p, 16) && ld * dtype_bytes(dt) % 16 == 0); }
-
-// 16-bit rows that take 4-byte accesses at even columns
-bool paired_rows(const void* p, uint64_t ld, int dt) { return !p || (dt != GD_DTYPE_FP32 && aligned_to(p, 4) && ld % 2 == 0); }
-
-struct Workspace {
-  unsigned char* base;
-  size_t at, size;
-  void* take(uint64_t rows, uint64_t cols) {
-    unsigned char* p = base + at;
-    at += up(rows * up(cols, 8) * 2, 256);
-    return at <= size ? p : nullptr;
-  }
-};
-// The partial sums' place, where a contraction is long enough to want one.
-int partial_place(uint64_t depth, Workspace& ws, float** p) {
-  if (depth < kLongDepth) return GD_OK;
-  *p = static_cast<float*>(ws.take(1, kPartialBytes / 2));
-  return *p ? GD_OK : GD_ERR_WORKSPACE;
-}
-// A leading dimension for one row is never used: a ragged one would only cause a copy.
-uint64_t row_step(uint64_t ld, uint64_t rows, uint64_t cols) { return rows > 1 ? ld : up(cols, 8); }
-
-// `p` as an operand the tiled copies can read, added to what has to be laid out in the workspace if need be.
-int operand(const void* p, uint64_t ld, uint64_t rows, uint64_t cols, Workspace& ws, Packs* packs, Operand* o) {
-  o->p = p;
-  o->ld = row_step(ld, rows, cols);
-  if (rows == 0 || cols == 0 || tiles_as_it_is(p, o->ld)) return GD_OK;
-  void* q = ws.take(rows, cols);
-  if (!q) return GD_ERR_WORKSPACE;
-  packs->p[packs->count++] = Pack{static_cast<const uint16_t*>(p), static_cast<uint4*>(q), ld, (uint32_t)rows, (uint32_t)cols, (uint32_t)((cols + 7) / 8)};
-  o->p = q;
-  o->ld = up(cols, 8);
-  return GD_OK;
-}
-bool good_rows(const void* p, uint64_t ld, uint64_t rows, uint64_t cols, size_t item) {
-  return p && aligned_to(p, item) && (rows <= 1 || ld >= cols) && !(ld >> 40);
-}
 int check_shape(uint64_t m, uint64_t n, uint64_t k, int dtype, int act, int layout) {
   if (!is_16bit(dtype) || act < GD_ACT_NONE || act > GD_ACT_SILU || (layout != GD_W_IN_OUT && layout != GD_W_OUT_IN)) return GD_ERR_INVALID_ARG;
   if (m >> 31 || n >> 31 || k >> 31) return GD_ERR_TOO_LARGE;
   return GD_OK;
 }
-int check_workspace(const void* ws, size_t bytes) { return !ws || !aligned_to(ws, 256) || bytes < kStatusBytes ? GD_ERR_WORKSPACE : GD_OK; }
 
 int forward(const gd_linear_forward_args* a, cudaStream_t stream) {
   if (!a || a->reserved != 0) return GD_ERR_INVALID_ARG;
@@ -469,41 +353,67 @@ int backward(const gd_linear_backward_args* a, cudaStream_t stream) {
   } else if (launch_pack(s.packs, stream) != cudaSuccess) {
     return GD_ERR_CUDA;
   }
-  Product p;
-  std::memset(&p, 0, sizeof(p));
-  p.bf16 = a->dtype == GD_DTYPE_BF16;
-  p.status = (int*)a->workspace;
-  p.ep.dtype = a->dtype;
-  if (has_dx) {                       // dx = dz W^T: contraction over n
-    p.a = dz, p.a.mn_major = false;
-    p.b = w, p.b.mn_major = !in_out;
-    p.depth = (uint32_t)n;
-    p.partial = n >= kLongDepth ? partial : nullptr;
-    p.followed = has_dw && n < kLongDepth;
-    p.ep.out = a->dx, p.ep.ld_out = a->ld_dx, p.ep.out_dtype = a->dtype;
-    p.ep.rows = (uint32_t)m, p.ep.cols = (uint32_t)k;
-    p.ep.vectors = vector_rows(a->dx, row_step(a->ld_dx, m, k), a->dtype);
-    p.ep.pairs = paired_rows(a->dx, row_step(a->ld_dx, m, k), a->dtype);
-    if (launch_product(p, stream) != cudaSuccess) return GD_ERR_CUDA;
-  }
-  if (has_dw) {                       // dw = x^T dz, or its transpose: contraction over m
-    p.a = in_out ? x : dz, p.b = in_out ? dz : x;
-    p.a.mn_major = p.b.mn_major = true;
-    p.depth = (uint32_t)m;
-    p.partial = m >= kLongDepth ? partial : nullptr;     // (the product before this one has been joined by the time it is written)
-    p.ep.out = a->dw, p.ep.ld_out = a->ld_dw, p.ep.out_dtype = a->dw_dtype;
-    p.ep.rows = (uint32_t)w_rows, p.ep.cols = (uint32_t)w_cols;
-    p.followed = false;
-    p.beside = has_dx && n < kLongDepth;                  // (a joined dx has a launch in between, and the partial sums' place)
-    if (add) p.ep.add = a->dw, p.ep.ld_add = a->ld_dw, p.ep.add_dtype = GD_DTYPE_FP32;
-    p.ep.vectors = vector_rows(a->dw, row_step(a->ld_dw, w_rows, w_cols), a->dw_dtype);
-    p.ep.pairs = paired_rows(a->dw, row_step(a->ld_dw, w_rows, w_cols), a->dw_dtype);
-    if (launch_product(p, stream) != cudaSuccess) return GD_ERR_CUDA;
-  }
-  return GD_OK;
+  BackProducts q;
+  q.dz = dz, q.w = w, q.x = x;
+  q.partial = partial;
+  q.m = m, q.n = n, q.k = k;
+  q.in_out = in_out, q.add = add;
+  q.dtype = a->dtype, q.dw_dtype = a->dw_dtype;
+  q.dx = has_dx ? a->dx : nullptr, q.ld_dx = a->ld_dx;
+  q.dw = has_dw ? a->dw : nullptr, q.ld_dw = a->ld_dw;
+  q.status = (int*)a->workspace;
+  return launch_back_products(q, stream) == cudaSuccess ? GD_OK : GD_ERR_CUDA;
 }
 
 }  // namespace
+
+cudaError_t launch_pack(const Packs& all, cudaStream_t stream) {
+  if (all.count == 0) return cudaSuccess;
+  ProfileScope ps(stream, PT_LINEAR_PACK);
+  const cudaError_t e = launch_dependent(pack_kernel, dim3(pack_ctas(all, kPackThreads)), dim3(kPackThreads), 0, stream, all);
+  if (e == cudaSuccess) note_launches(1);
+  return e;
+}
+
+cudaError_t launch_back_products(const BackProducts& q, cudaStream_t stream) {
+  const uint64_t m = q.m, n = q.n, k = q.k, w_rows = q.in_out ? k : n, w_cols = q.in_out ? n : k;
+  const bool has_dx = q.dx != nullptr, has_dw = q.dw != nullptr;
+  Product p;
+  std::memset(&p, 0, sizeof(p));
+  p.bf16 = q.dtype == GD_DTYPE_BF16;
+  p.status = q.status;
+  p.ep.dtype = q.dtype;
+  if (has_dx) {                       // dx = dz W^T: contraction over n
+    p.a = q.dz, p.a.mn_major = false;
+    p.b = q.w, p.b.mn_major = !q.in_out;
+    p.depth = (uint32_t)n;
+    p.partial = n >= kLongDepth ? q.partial : nullptr;
+    p.followed = has_dw && n < kLongDepth;
+    p.ep.out = q.dx, p.ep.ld_out = q.ld_dx, p.ep.out_dtype = q.dtype;
+    p.ep.rows = (uint32_t)m, p.ep.cols = (uint32_t)k;
+    p.ep.vectors = vector_rows(q.dx, row_step(q.ld_dx, m, k), q.dtype);
+    p.ep.pairs = paired_rows(q.dx, row_step(q.ld_dx, m, k), q.dtype);
+    const cudaError_t e = launch_product(p, stream);
+    if (e != cudaSuccess) return e;
+  }
+  if (has_dw) {                       // dw = x^T dz, or its transpose: contraction over m
+    p.a = q.in_out ? q.x : q.dz, p.b = q.in_out ? q.dz : q.x;
+    p.a.mn_major = p.b.mn_major = true;
+    p.depth = (uint32_t)m;
+    p.partial = m >= kLongDepth ? q.partial : nullptr;     // (the product before this one has been joined by the time it is written)
+    p.ep.out = q.dw, p.ep.ld_out = q.ld_dw, p.ep.out_dtype = q.dw_dtype;
+    p.ep.rows = (uint32_t)w_rows, p.ep.cols = (uint32_t)w_cols;
+    p.followed = false;
+    p.beside = has_dx && n < kLongDepth;                  // (a joined dx has a launch in between, and the partial sums' place)
+    if (q.add) p.ep.add = q.dw, p.ep.ld_add = q.ld_dw, p.ep.add_dtype = GD_DTYPE_FP32;
+    p.ep.vectors = vector_rows(q.dw, row_step(q.ld_dw, w_rows, w_cols), q.dw_dtype);
+    p.ep.pairs = paired_rows(q.dw, row_step(q.ld_dw, w_rows, w_cols), q.dw_dtype);
+    const cudaError_t e = launch_product(p, stream);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 }  // namespace gd
 
 extern "C" {

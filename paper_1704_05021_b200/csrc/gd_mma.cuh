@@ -143,6 +143,32 @@ __device__ __forceinline__ void tmem_load32(uint32_t address, float* r) {
 }
 __device__ __forceinline__ void tmem_ready() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+// ---------------------------------------------------------------- pairs of CTAs, tiled stores
+__device__ __forceinline__ void tile_load_pair(void* dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t barrier) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
+               "l"(map), "r"(x), "r"(y), "r"(barrier)
+               : "memory");
+}
+// b, in both CTAs of the pair, receives one arrive when the products issued so far have been done
+__device__ __forceinline__ void mma_commit_pair(uint64_t* b) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(b)), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_peer(uint32_t address) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(address) : "memory");
+}
+
+__device__ __forceinline__ void tile_store(const CUtensorMap* map, const void* src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(smem_u32(src)) : "memory");
+}
+// Closes a group of stores.  Every piece closes one, whether it was stored or lies outside the matrix (an empty group is done at once): the pieces
+// take the buffers in turn and stores_read() counts groups, so the two counts have to run together.
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// columns that make up whole 16 bytes of a row
+__host__ __device__ constexpr uint32_t whole_columns(uint32_t cols, uint32_t item) { return cols & ~(16u / item - 1u); }
+template <int LEFT>
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }   // all but LEFT have left shared memory
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // ---------------------------------------------------------------- activations and epilogue
 // x Phi(x) and x / (1 + exp(-x)), and their slopes.  Phi by formula 7.1.26 of Abramowitz and Stegun (erf to 1.5e-7, one
 // exponential that is also the density's): a third of the instructions of erff, which a tile's 65536 values pay for.

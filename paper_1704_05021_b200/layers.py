@@ -24,7 +24,8 @@ GD_EMBEDDING_ACCUMULATE = 1
 GD_LAYER_NORM_ACCUMULATE = 1
 
 EXPORTS = ["gd_embedding_forward", "gd_embedding_backward", "gd_embedding_workspace_bytes", "gd_layer_norm_forward", "gd_layer_norm_backward",
-           "gd_layer_norm_workspace_bytes", "gd_recurrence_forward", "gd_recurrence_backward", "gd_recurrence_marks_rows"]
+           "gd_layer_norm_workspace_bytes", "gd_recurrence_forward", "gd_recurrence_backward", "gd_recurrence_marks_rows",
+           "gd_gated_forward", "gd_gated_backward", "gd_gated_workspace_bytes"]
 
 
 class _EmbeddingForwardArgs(C.Structure):
@@ -66,12 +67,28 @@ class _RecurrenceBackwardArgs(C.Structure):
                 ("dvalue", C.c_void_p), ("ld_dvalue", C.c_uint64), ("dh_last", C.c_void_p), ("dh0", C.c_void_p)]
 
 
+class _GatedForwardArgs(C.Structure):
+    _fields_ = [("m", C.c_uint64), ("n", C.c_uint64), ("k", C.c_uint64), ("dtype", C.c_int32), ("activation", C.c_int32), ("w_layout", C.c_int32),
+                ("bias_dtype", C.c_int32), ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("ldw", C.c_uint64), ("bias", C.c_void_p),
+                ("y", C.c_void_p), ("ldy", C.c_uint64), ("pre", C.c_void_p), ("ld_pre", C.c_uint64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class _GatedBackwardArgs(C.Structure):
+    _fields_ = [("m", C.c_uint64), ("n", C.c_uint64), ("k", C.c_uint64), ("dtype", C.c_int32), ("activation", C.c_int32), ("w_layout", C.c_int32),
+                ("dw_dtype", C.c_int32), ("flags", C.c_uint32), ("reserved", C.c_int32), ("dy", C.c_void_p), ("ld_dy", C.c_uint64),
+                ("pre", C.c_void_p), ("ld_pre", C.c_uint64), ("x", C.c_void_p), ("ldx", C.c_uint64), ("w", C.c_void_p), ("ldw", C.c_uint64),
+                ("dx", C.c_void_p), ("ld_dx", C.c_uint64), ("dw", C.c_void_p), ("ld_dw", C.c_uint64), ("db", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 # written in one go for every call, as in training.py
 _FIELDS = {_EmbeddingForwardArgs: struct.Struct("<3Q3ifq5Q"), _EmbeddingBackwardArgs: struct.Struct("<3Q3ifqIi7Q"),
            _LayerNormForwardArgs: struct.Struct("<2Q2ifi8Q"), _LayerNormBackwardArgs: struct.Struct("<2Q2iIi15Q"),
-           _RecurrenceForwardArgs: struct.Struct("<3Q2i10Q"), _RecurrenceBackwardArgs: struct.Struct("<3Q2i14Q")}
+           _RecurrenceForwardArgs: struct.Struct("<3Q2i10Q"), _RecurrenceBackwardArgs: struct.Struct("<3Q2i14Q"),
+           _GatedForwardArgs: struct.Struct("<3Q4i11Q"), _GatedBackwardArgs: struct.Struct("<3Q4iIi15Q")}
 assert all(fields.size == C.sizeof(args) for args, fields in _FIELDS.items())
-_EMBED, _EMBED_BACK, _NORM, _NORM_BACK, _SCAN, _SCAN_BACK = _FIELDS.values()
+_EMBED, _EMBED_BACK, _NORM, _NORM_BACK, _SCAN, _SCAN_BACK, _GATED, _GATED_BACK = _FIELDS.values()
 
 _lib = None
 
@@ -86,6 +103,7 @@ def load_library():
             function.argtypes, function.restype = [C.c_void_p, C.c_void_p], C.c_int      # (the bytes of the arguments, or byref of a structure)
         lib.gd_embedding_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.POINTER(C.c_size_t)]
         lib.gd_layer_norm_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.POINTER(C.c_size_t)]
+        lib.gd_gated_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.c_int, C.POINTER(C.c_size_t)]
         lib.gd_recurrence_marks_rows.argtypes = [C.c_uint64, C.c_uint64, C.POINTER(C.c_uint64)]
         _lib = lib
     return _lib
@@ -313,3 +331,77 @@ def recurrence_backward(dy: torch.Tensor, gate: torch.Tensor, value: torch.Tenso
     args = _SCAN_BACK.pack(rows, sequences, width, code, bits, offsets_at, *matrices[:6], _marks(marks, rows, sequences, width, index), *matrices[6:],
                            _opt_state(dh_last, "dh_last", sequences, width, index), _opt_state(dh0, "dh0", sequences, width, index))
     _call(load_library().gd_recurrence_backward, "gd_recurrence_backward", args, stream, index)
+
+
+class GatedLinearSession:
+    """The gated feed-forward block's two projections - n_in inputs, n_out outputs each, up to max_rows rows at a time - and its workspace.
+
+    W is one matrix, [n_in, 2 n_out] or [2 n_out, n_in] (w_layout): the first n_out outputs are the gate, the others are multiplied by it.  dtype is
+    that of x, w, the result and pre (bfloat16 or float16).  any_layout=True makes room for operands that are not contiguous or start at odd
+    addresses.  The block's last projection is a LinearSession.
+    """
+
+    def __init__(self, n_in: int, n_out: int, max_rows: int, dtype=torch.bfloat16, activation: str = "silu", w_layout: str = "in_out", device="cuda",
+                 any_layout: bool = False):
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("GatedLinearSession takes bfloat16 or float16")
+        if activation not in _ACTIVATIONS or w_layout not in _LAYOUTS:
+            raise ValueError(f"activation is one of {sorted(_ACTIVATIONS)}, w_layout one of {sorted(_LAYOUTS)}")
+        self._index = index = _cuda_index(device)
+        self.device = torch.device("cuda", index)
+        self.n_in, self.n_out, self.max_rows, self.dtype, self.activation, self.w_layout = int(n_in), int(n_out), int(max_rows), dtype, activation, w_layout
+        self.w_shape = (self.n_in, 2 * self.n_out) if w_layout == "in_out" else (2 * self.n_out, self.n_in)
+        self._lib = load_library()
+        size = C.c_size_t(0)
+        B._check(self._lib.gd_gated_workspace_bytes(self.max_rows, self.n_out, self.n_in, int(any_layout), C.byref(size)), "gd_gated_workspace_bytes")
+        self._bind(torch.empty(size.value, dtype=torch.uint8, device=self.device))
+        self.workspace[:256].zero_()
+
+    def _bind(self, workspace: torch.Tensor) -> None:
+        """The arguments that stay the same from call to call."""
+        self.workspace = workspace
+        self._space = (workspace.data_ptr(), workspace.numel())
+        self._codes = (self.n_out, self.n_in, _DTYPES[self.dtype], _ACTIVATIONS[self.activation], _LAYOUTS[self.w_layout])
+
+    def _rows(self, t: torch.Tensor) -> int:
+        m = t.shape[0] if t.dim() == 2 else -1
+        if not 0 <= m <= self.max_rows:
+            raise ValueError(f"at most {self.max_rows} rows of a matrix, got {list(t.shape)}")
+        return m
+
+    def forward(self, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                pre: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """act(z[:, :n_out]) * z[:, n_out:] with z = x W + bias (float32 or the session's type), into `out` (made here if None) and, if `pre`
+        ([rows, 2 n_out]) is given, z."""
+        m, n, dt, index = self._rows(x), self.n_out, self.dtype, self._index
+        if out is None:
+            out = _new(m, n, dt, stream, index)
+        bias_at = _opt_vector(bias, "bias", 2 * n, (torch.float32, dt), index)
+        args = _GATED.pack(m, *self._codes, 0 if bias is None else _DTYPES[bias.dtype], x.data_ptr(), _matrix(x, "x", m, self.n_in, dt, index), w.data_ptr(),
+                           _matrix(w, "w", *self.w_shape, dt, index), bias_at, out.data_ptr(), _matrix(out, "out", m, n, dt, index),
+                           *_opt_matrix(pre, "pre", m, 2 * n, dt, index), *self._space)
+        _call(self._lib.gd_gated_forward, "gd_gated_forward", args, stream, index)
+        return out
+
+    def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor], pre: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                 dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None) -> None:
+        """The gradients whose buffers are given, for dy, the gradient of forward's result, and the pre that it wrote.
+
+        dw has w's shape, in float32 or the session's type; db is float32, 2 n_out.  accumulate adds to dw (float32) and db.
+        """
+        m, n, k, dt, index = self._rows(dy), self.n_out, self.n_in, self.dtype, self._index
+        if dx is not None and w is None:
+            raise ValueError("dx needs w")
+        if dw is not None and x is None:
+            raise ValueError("dw needs x")
+        dw_dt = dt if dw is None or dw.dtype is not torch.float32 else torch.float32
+        args = _GATED_BACK.pack(m, *self._codes, _DTYPES[dw_dt], T.GD_LINEAR_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
+                                _matrix(dy, "dy", m, n, dt, index), pre.data_ptr(), _matrix(pre, "pre", m, 2 * n, dt, index),
+                                *_opt_matrix(x if dw is not None else None, "x", m, k, dt, index),
+                                *_opt_matrix(w if dx is not None else None, "w", *self.w_shape, dt, index), *_opt_matrix(dx, "dx", m, k, dt, index),
+                                *_opt_matrix(dw, "dw", *self.w_shape, dw_dt, index), _opt_vector(db, "db", 2 * n, _F32, index), *self._space)
+        _call(self._lib.gd_gated_backward, "gd_gated_backward", args, stream, index)
+
+    def status(self, stream=None) -> int:
+        """GD_OK, or GD_ERR_DEVICE_TIMEOUT if a device-side wait of any call so far gave up (waits for the stream)."""
+        return _issue(self._lib.gd_linear_status, self.workspace.data_ptr(), stream, self._index)

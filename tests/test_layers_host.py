@@ -94,7 +94,36 @@ def _scan_back():
     return a
 
 
+def _gated():
+    a = L._GatedForwardArgs()
+    a.m, a.n, a.k, a.dtype, a.activation = 4, 8, 16, 1, 3
+    a.x, a.ldx, a.w, a.ldw, a.bias, a.y, a.ldy, a.pre, a.ld_pre, a.workspace, a.workspace_bytes = 0x1000, 16, 0x2000, 16, 0x3000, 0x4000, 8, 0x5000, 16, 0x6000, 256
+    return a
+
+
+def _gated_back():
+    a = L._GatedBackwardArgs()
+    a.m, a.n, a.k, a.dtype, a.activation = 4, 8, 16, 1, 3
+    a.dy, a.ld_dy, a.pre, a.ld_pre, a.x, a.ldx, a.w, a.ldw = 0x1000, 8, 0x2000, 16, 0x3000, 16, 0x4000, 16
+    a.dx, a.ld_dx, a.dw, a.ld_dw, a.db, a.workspace, a.workspace_bytes = 0x5000, 16, 0x6000, 16, 0x7000, 0x8000, 512
+    return a
+
+
 @pytest.mark.parametrize("call, make, changes, code", [
+    ("gd_gated_forward", _gated, dict(dtype=0), INVALID), ("gd_gated_forward", _gated, dict(activation=4), INVALID),
+    ("gd_gated_forward", _gated, dict(w_layout=2), INVALID), ("gd_gated_forward", _gated, dict(bias_dtype=2), INVALID),
+    ("gd_gated_forward", _gated, dict(x=None), INVALID), ("gd_gated_forward", _gated, dict(w=0x2001), INVALID), ("gd_gated_forward", _gated, dict(ldw=15), INVALID),
+    ("gd_gated_forward", _gated, dict(y=None), INVALID), ("gd_gated_forward", _gated, dict(ld_pre=15), INVALID), ("gd_gated_forward", _gated, dict(m=1 << 30), LARGE),
+    ("gd_gated_forward", _gated, dict(workspace=None), SPACE), ("gd_gated_forward", _gated, dict(workspace_bytes=255), SPACE),
+    ("gd_gated_forward", _gated, dict(ldx=17), SPACE), ("gd_gated_forward", _gated, dict(ldw=17), SPACE), ("gd_gated_forward", _gated, dict(w=0x2002), SPACE),
+    ("gd_gated_forward", _gated, dict(n=0), 0), ("gd_gated_backward", _gated_back, dict(dtype=0), INVALID),
+    ("gd_gated_backward", _gated_back, dict(flags=2), INVALID), ("gd_gated_backward", _gated_back, dict(reserved=1), INVALID),
+    ("gd_gated_backward", _gated_back, dict(dw_dtype=2), INVALID), ("gd_gated_backward", _gated_back, dict(flags=1, dw_dtype=1), INVALID),
+    ("gd_gated_backward", _gated_back, dict(dy=None), INVALID), ("gd_gated_backward", _gated_back, dict(pre=None), INVALID),
+    ("gd_gated_backward", _gated_back, dict(x=None), INVALID), ("gd_gated_backward", _gated_back, dict(w=None), INVALID),
+    ("gd_gated_backward", _gated_back, dict(db=0x7002), INVALID), ("gd_gated_backward", _gated_back, dict(ld_dw=15), INVALID),
+    ("gd_gated_backward", _gated_back, dict(workspace_bytes=511 - 128), SPACE), ("gd_gated_backward", _gated_back, dict(ldx=19), SPACE),
+    ("gd_gated_backward", _gated_back, dict(k=1 << 30), LARGE), ("gd_gated_backward", _gated_back, dict(dx=None, dw=None, db=None), 0),
     ("gd_embedding_forward", _embedding, dict(table_dtype=3), INVALID), ("gd_embedding_forward", _embedding, dict(y_dtype=2), INVALID),
     ("gd_embedding_forward", _embedding, dict(id_bits=16), INVALID), ("gd_embedding_forward", _embedding, dict(table=None), INVALID),
     ("gd_embedding_forward", _embedding, dict(table=0x1001), INVALID), ("gd_embedding_forward", _embedding, dict(ld_table=7), INVALID),
@@ -150,6 +179,13 @@ def test_workspaces_and_marks(lib):
     size = C.c_size_t(0)
     assert lib.gd_layer_norm_workspace_bytes(4, 8, C.byref(size)) == B.GD_OK and size.value == 4 * 2 * 8 * 4
     assert lib.gd_layer_norm_workspace_bytes(1 << 31, 8, C.byref(size)) == LARGE and lib.gd_layer_norm_workspace_bytes(1, 1, None) == INVALID
+
+    def gated(m, n, k, any_layout=0):
+        assert lib.gd_gated_workspace_bytes(m, n, k, any_layout, C.byref(size)) == B.GD_OK
+        return size.value
+
+    assert 256 <= gated(0, 0, 0) < gated(80, 64, 64) < gated(80, 65, 64) < gated(80, 65, 65) and gated(80, 64, 64) < gated(80, 64, 64, 1)
+    assert lib.gd_gated_workspace_bytes(1, 1 << 30, 1, 0, C.byref(size)) == LARGE and lib.gd_gated_workspace_bytes(1, 1, 1, 0, None) == INVALID
     count = C.c_uint64(0)
     assert lib.gd_recurrence_marks_rows(640, 3, C.byref(count)) == B.GD_OK and count.value == 13
     assert lib.gd_recurrence_marks_rows(1, 1 << 31, C.byref(count)) == LARGE and lib.gd_recurrence_marks_rows(1, 1, None) == INVALID
@@ -157,7 +193,7 @@ def test_workspaces_and_marks(lib):
 
 def test_sessions_and_calls_want_a_gpu():
     x = torch.zeros(4, 8)
-    for make in (lambda: L.EmbeddingSession(4, 8, 4, device="cpu"), lambda: L.LayerNormSession(8, 4, device="cpu"), lambda: L.recurrence_forward(x, x),
+    for make in (lambda: L.EmbeddingSession(4, 8, 4, device="cpu"), lambda: L.LayerNormSession(8, 4, device="cpu"), lambda: L.GatedLinearSession(8, 8, 4, device="cpu"), lambda: L.recurrence_forward(x, x),
                  lambda: L.recurrence_marks(4, 1, 8, device="cpu"), lambda: L.recurrence_backward(x, x, x, x, x, x)):
         with pytest.raises(RuntimeError, match="CUDA device is needed"):
             make()
@@ -197,6 +233,22 @@ def test_tensors_that_do_not_fit_are_refused():
                 dict(add=torch.zeros(8, 4, dtype=torch.bfloat16).t())):
         with pytest.raises(ValueError):
             n.backward(**{**dict(dy=x, x=x, weight=None, mean=stats, rstd=stats), **bad})
+
+
+def test_gated_tensors_that_do_not_fit_are_refused():
+    for wrong in (dict(dtype=torch.float32), dict(activation="sigmoid"), dict(w_layout="out")):
+        with pytest.raises(ValueError):
+            L.GatedLinearSession(8, 16, 4, **wrong)
+    s = _without_gpu(L.GatedLinearSession, n_in=8, n_out=16, max_rows=4, dtype=torch.bfloat16, activation="silu", w_layout="in_out", w_shape=(8, 32))
+    s._bind(s.workspace)
+    x, w, y, pre = (torch.zeros(*shape, dtype=torch.bfloat16) for shape in ((4, 8), (8, 32), (4, 16), (4, 32)))
+    for bad in (dict(x=x.float()), dict(x=torch.zeros(5, 8).bfloat16()), dict(w=w[:, :16]), dict(w=w.t()), dict(bias=torch.zeros(16)), dict(bias=torch.zeros(32).half()),
+                dict(out=torch.zeros(4, 16)), dict(pre=y)):
+        with pytest.raises(ValueError):
+            s.forward(**{**dict(x=x, w=w, out=y), **bad})
+    for bad in (dict(dy=x), dict(pre=y), dict(dx=x, w=None), dict(dw=w, x=None), dict(dw=w.half()), dict(db=torch.zeros(16)), dict(dx=y)):
+        with pytest.raises(ValueError):
+            s.backward(**{**dict(dy=y, x=x, w=w, pre=pre), **bad})
 
 
 def test_recurrence_arguments_that_do_not_fit_are_refused(monkeypatch):
