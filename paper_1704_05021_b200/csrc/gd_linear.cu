@@ -25,7 +25,8 @@ double cost_product_pair(const Product& p, uint32_t bn) {
 
 // Tiled-copy map of an operand.  The encoder is the driver's; it is asked for through the runtime, so that the library does not link
 // against libcuda and loads on a machine without a GPU.
-bool encode_tile(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t width, uint64_t height, uint32_t box_width, uint32_t box_height, int dtype) {
+static bool encode(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t width, uint64_t height, uint32_t box_width, uint32_t box_height, int dtype,
+                   CUtensorMapSwizzle swizzle) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   static std::atomic<void*> found{nullptr};
@@ -41,8 +42,14 @@ bool encode_tile(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t w
   const CUtensorMapDataType type = dtype == GD_DTYPE_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                    : dtype == GD_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                             : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  return reinterpret_cast<Encode>(f)(map, type, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return reinterpret_cast<Encode>(f)(map, type, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+static bool encode_tile(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t width, uint64_t height, uint32_t box_width, uint32_t box_height, int dtype) {
+  return encode(map, p, row_bytes, width, height, box_width, box_height, dtype, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+bool encode_matrix(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t width, uint64_t height, uint32_t box_width, uint32_t box_height, int dtype) {
+  return encode(map, p, row_bytes, width, height, box_width, box_height, dtype, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 bool encode_operand(CUtensorMap* map, const Operand& o, uint32_t extent, uint32_t depth, uint32_t box_extent, bool bf16) {
   return encode_tile(map, o.p, o.ld * 2, o.mn_major ? extent : depth, o.mn_major ? depth : extent, 64, box_extent, bf16 ? GD_DTYPE_BF16 : GD_DTYPE_FP16);

@@ -405,6 +405,7 @@ struct SplitChoice {       // of the split kernel's tile
   double cost;             // estimated cycles
 };
 bool encode_piece(CUtensorMap* map, const void* p, uint64_t ld, const Epilogue& ep, uint32_t cols, int dtype);     // 32 rows x 128 bytes of a result, up to `cols`
+bool encode_matrix(CUtensorMap* map, const void* p, uint64_t row_bytes, uint64_t width, uint64_t height, uint32_t box_width, uint32_t box_height, int dtype);  // as it lies
 cudaError_t launch_product(const Product& p, cudaStream_t stream);
 
 }  // namespace gd

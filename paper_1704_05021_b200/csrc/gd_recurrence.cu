@@ -1,14 +1,14 @@
 // A gated linear recurrence over packed sequences (gd_recurrence_forward, gd_recurrence_backward).
 //
 // h[t] = f[t] h[t-1] + s[t] v[t] with f = sigmoid(gate), s = 1 - f is a composition of affine maps, column by column: rows t0 .. t1 take a state h to
-// A h + B, and maps compose.  A CTA takes a slab of columns of one sequence, kTileRows rows at a time: each warp makes the map of its kRows rows
+// A h + B, and maps compose.  A CTA takes a slab of columns of one sequence, kMarkRows rows at a time: each warp makes the map of its kRows rows
 // in registers, the warps' maps meet in shared memory, and from the state that enters the tile every warp goes through its rows again, still
 // in registers, and writes them.  So gate and value are read once and y is written once, whatever the length: bound by the bytes.  The next tile's
 // rows are asked for before this one's are worked on.  Where sequences and slabs alone would leave SMs idle, a cluster of 2 .. 8 CTAs takes
 // neighbouring tiles of a sequence and exchanges their maps (sent and counted, as the cross-entropy does).
 //
 // Backwards dh runs through the same maps from the other end: with C the map's constant, the gradient that leaves rows t0 .. t1 towards the past is
-// A (what came in) + C.  The states h[t-1] that dgate needs are made again from the marks, the states before every kTileRows-th row of a sequence
+// A (what came in) + C.  The states h[t-1] that dgate needs are made again from the marks, the states before every kMarkRows-th row of a sequence
 // which the forward call keeps in fp32: y is rounded and would not do where h[t-1] and value nearly agree.
 //
 // Sequences of few rows (kShortRows on average, the single step among them): a thread takes a sequence's columns through all its rows.
@@ -21,7 +21,7 @@
 namespace gd {
 namespace {
 
-constexpr uint32_t kWarps = 8, kRows = 8, kTileRows = kWarps * kRows;      // kTileRows is part of the marks' layout
+constexpr uint32_t kWarps = 8, kRows = 8, kMarkRows = kWarps * kRows;      // kMarkRows is part of the marks' layout
 constexpr uint32_t kShortRows = 24;
 constexpr uint32_t kMostCluster = 8;
 
@@ -70,69 +70,390 @@ struct ScanBackArgs {
   uint64_t items;
 };
 // the row of marks that holds the state before row 0 of a sequence
-__device__ __forceinline__ uint64_t first_mark(uint32_t sequence, uint32_t first_row) { return (uint64_t)first_row / kTileRows + sequence; }
+__device__ __forceinline__ uint64_t first_mark(uint32_t sequence, uint32_t first_row) { return (uint64_t)first_row / kMarkRows + sequence; }
 
 // f = 1 / (1 + exp(-g)) and s = 1 - f, each to its own relative accuracy
+__device__ __forceinline__ float exp2_of(float x) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  return e;
+}
+__device__ __forceinline__ float inverse_of(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
 template <int DT>
 __device__ __forceinline__ void gate_of(float g, float* f, float* s) {
-  const float e = DT == GD_DTYPE_FP32 ? expf(-fabsf(g)) : __expf(-fabsf(g));
-  const float big = __fdividef(1.f, 1.f + e), small = e * big;
+  const float e = DT == GD_DTYPE_FP32 ? expf(-fabsf(g)) : exp2_of(-fabsf(g) * kLog2e);
+  const float big = inverse_of(1.f + e), small = e * big;
   *f = g < 0.f ? small : big;      // (a NaN stays one)
   *s = g < 0.f ? big : small;
 }
+// Of two gates, for 16-bit types: with e = exp(-g), held at 2^126, f = 1 / (1 + e) and s = e f.  Where e is held f is 2^-126 too much: taken
+// off again, which changes no f above 2^-102.  6.5 instructions an element where the above takes 8 and the instructions bound the kernel.
+__device__ __forceinline__ void gate_pair(float2 g, float2* f, float2* s) {
+  constexpr float kMost = 126.f, kLeast = 1.17549435e-38f;
+  float2 t = mul2(g, both(-kLog2e));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(t.x) : "f"(kMost));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(t.y) : "f"(kMost));
+  const float2 e = make_float2(exp2_of(t.x), exp2_of(t.y)), d = add2(e, both(1.f)), r = make_float2(inverse_of(d.x), inverse_of(d.y));
+  *s = mul2(e, r);
+  *f = add2(r, both(-kLeast));
+}
+// f and s of N elements side by side
+template <int DT, int N>
+__device__ __forceinline__ void gates_of(const float (&g)[N], float (&f)[N], float (&s)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; j += 2) {
+    if constexpr (DT == GD_DTYPE_FP32) {
+      gate_of<DT>(g[j], &f[j], &s[j]);
+      gate_of<DT>(g[j + 1], &f[j + 1], &s[j + 1]);
+    } else {
+      float2 p, q;
+      gate_pair(make_float2(g[j], g[j + 1]), &p, &q);
+      f[j] = p.x, f[j + 1] = p.y, s[j] = q.x, s[j + 1] = q.y;
+    }
+  }
+}
+// The products of N elements side by side.
+template <int N>
+__device__ __forceinline__ void times(const float (&a)[N], const float (&b)[N], float (&c)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; j += 2) {
+    const float2 p = mul2(make_float2(a[j], a[j + 1]), make_float2(b[j], b[j + 1]));
+    c[j] = p.x, c[j + 1] = p.y;
+  }
+}
+// V columns' a * b + c, and a * b
+template <int V>
+__device__ __forceinline__ void fma_v(const float* a, const float* b, const float* c, float* r) {
+  if constexpr (V == 2) {
+    const float2 p = fma2(make_float2(a[0], a[1]), make_float2(b[0], b[1]), make_float2(c[0], c[1]));
+    r[0] = p.x, r[1] = p.y;
+  } else {
+    r[0] = fmaf(a[0], b[0], c[0]);
+  }
+}
+template <int V>
+__device__ __forceinline__ void mul_v(const float* a, const float* b, float* r) {
+  if constexpr (V == 2) {
+    const float2 p = mul2(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
+    r[0] = p.x, r[1] = p.y;
+  } else {
+    r[0] = a[0] * b[0];
+  }
+}
+template <int V>
+__device__ __forceinline__ void add_v(const float* a, const float* b, float* r) {
+  if constexpr (V == 2) {
+    const float2 p = add2(make_float2(a[0], a[1]), make_float2(b[0], b[1]));
+    r[0] = p.x, r[1] = p.y;
+  } else {
+    r[0] = a[0] + b[0];
+  }
+}
+// The maps of the warps, in shared memory: a lane's V columns of A, then of B.
+template <int V>
+struct __align__(8 * V) Map {
+  float a[V], b[V];
+};
+// first <- what the rows of `first` and then those of m make of a state
+template <int V>
+__device__ __forceinline__ void append(Map<V>& first, const Map<V>& m) {
+  fma_v<V>(m.a, first.b, m.b, first.b);
+  mul_v<V>(m.a, first.a, first.a);
+}
+template <int V>
+__device__ __forceinline__ Map<V> identity() {
+  Map<V> m;
+#pragma unroll
+  for (int i = 0; i < V; ++i) m.a[i] = 1.f, m.b[i] = 0.f;
+  return m;
+}
 
 // ---------------------------------------------------------------- exchange of a cluster's maps
-// Two places in turn for the pairs of all CTAs, each counted on an mbarrier of its own.
-template <int V>
+// A CTA sends the map of a tile to all CTAs of its cluster as soon as it has it, one tile before it needs theirs, so that nobody waits for a
+// message under way.  Four places in turn, each counted on an mbarrier of its own: while a CTA reads the maps of tile set t the others may have
+// sent those of t + 1 .. t + 3, which take its maps of up to t + 2 to have come that far.
+constexpr uint32_t kPlaces = 4;
+template <int V, int CL, int L>
 struct Exchange {
-  float2 pair[2][kMostCluster][32 * V];
-  uint64_t full[2];
+  Map<V> map[kPlaces][CL][L];
+  uint64_t full[kPlaces];
 };
-template <int V>
-__device__ __forceinline__ void exchange_begin(Exchange<V>& x, uint32_t cluster) {
+template <int V, int CL, int L>
+__device__ __forceinline__ void exchange_begin(Exchange<V, CL, L>& x) {
   if (threadIdx.x == 0) {
-    for (int b = 0; b < 2; ++b) {
+    for (uint32_t b = 0; b < kPlaces; ++b) {
       mbar_init(&x.full[b], 1u);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      mbar_arrive_expect_tx(&x.full[b], cluster * 32u * V * 8u);
+      mbar_arrive_expect_tx(&x.full[b], CL * L * (uint32_t)sizeof(Map<V>));
     }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
   cluster_arrive();
   cluster_wait();
 }
-// Sends this CTA's (a, b) to all and waits for everybody's.  Warp w sends to CTA w; all threads hold the same values for their lane's columns.
-template <int V>
-__device__ __forceinline__ bool exchange(Exchange<V>& x, uint32_t cluster, uint32_t rank, uint32_t round, const float (&a)[V], const float (&b)[V]) {
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, at = round & 1u;
-  if (warp < cluster) {
-    const uint32_t full = peer_address(smem_u32(&x.full[at]), warp);
+// One group of threads sends this CTA's map to all.
+template <int V, int CL, int L>
+__device__ __forceinline__ void exchange_send(Exchange<V, CL, L>& x, uint32_t rank, uint32_t round, const Map<V>& m) {
+  const uint32_t at = round % kPlaces, to = smem_u32(&x.map[at][rank][threadIdx.x % L]), full = smem_u32(&x.full[at]);
 #pragma unroll
-    for (int i = 0; i < V; ++i) send_peer2(peer_address(smem_u32(&x.pair[at][rank][lane * V + i]), warp), make_float2(a[i], b[i]), full);
+  for (uint32_t q = 0; q < CL; ++q) {
+    const uint32_t peer = peer_address(to, q), bar = peer_address(full, q);
+    if constexpr (V == 2) {
+      send_peer2(peer, make_float2(m.a[0], m.a[1]), bar);
+      send_peer2(peer + 8u, make_float2(m.b[0], m.b[1]), bar);
+    } else {
+      send_peer2(peer, make_float2(m.a[0], m.b[0]), bar);
+    }
   }
-  const int never = 0;
-  return mbar_wait(&x.full[at], (round >> 1) & 1u, &never);
 }
-// after all threads are past the wait of `round`, and before they send for round + 2
-template <int V>
-__device__ __forceinline__ void exchange_again(Exchange<V>& x, uint32_t cluster, uint32_t round) {
-  if (threadIdx.x == 0) mbar_arrive_expect_tx(&x.full[round & 1u], cluster * 32u * V * 8u);
+// Waits for everybody's maps of `round` and makes the place ready for round + kPlaces (nobody sends for that before all threads here are past
+// a barrier behind this call).  From the state that enters the cluster's tiles, `carry`: what enters this CTA's, and `carry` behind the last.
+template <int V, int CL, bool BACKWARD, int L>
+__device__ __forceinline__ void exchange_fold(Exchange<V, CL, L>& x, uint32_t rank, uint32_t round, float (&mine)[V], float (&carry)[V]) {
+  const uint32_t lane = threadIdx.x % L, at = round % kPlaces;
+  const int never = 0;
+  const bool good = mbar_wait(&x.full[at], (round / kPlaces) & 1u, &never);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (!good) carry[i] = NAN;                       // (a map that never came: the results say so)
+    mine[i] = carry[i];
+  }
+#pragma unroll
+  for (uint32_t n = 0; n < CL; ++n) {
+    const uint32_t q = BACKWARD ? CL - 1u - n : n;
+    if (q == rank) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) mine[i] = carry[i];
+    }
+    const Map<V> m = x.map[at][q][lane];
+    fma_v<V>(m.a, carry, m.b, carry);
+  }
+  if (threadIdx.x == 0) mbar_arrive_expect_tx(&x.full[at], CL * L * (uint32_t)sizeof(Map<V>));
 }
 
+// ---------------------------------------------------------------- tiles in shared memory
+// A group of L threads has V columns each of kRows rows; a tile is the groups' rows x L V columns of every input, brought by tiled copies (which cut
+// at the matrix' end; what a tile holds beyond its sequence is masked) into one of a few stages.
+template <int DT, int V, int L, int INPUTS, int CL>
+struct TileShape {
+  static constexpr uint32_t kGroups = kWarps * 32 / L, kTileRows = kGroups * kRows, kColumns = L * V;
+  static constexpr uint32_t kInput = kTileRows * kColumns * sizeof(typename Elem<DT>::type), kStage = INPUTS * kInput;
+  static constexpr uint32_t kDepth = INPUTS == 3 && CL > 1 ? 3 : 4;
+  static constexpr uint32_t kBytes = kDepth * kStage + (CL > 1 ? (uint32_t)sizeof(Exchange<V, CL, L>) : 0u) + 128u;
+};
+constexpr uint32_t kMarkGroups = kMarkRows / kRows;      // groups from one mark to the next
+
 // ---------------------------------------------------------------- forward
-template <int DT, int V, bool CLUSTER>
-__global__ void __launch_bounds__(kWarps * 32) scan_kernel(const __grid_constant__ ScanArgs a, uint32_t cluster) {
+// Rows that tiled copies can read: 16-byte aligned.
+struct ScanMaps {
+  CUtensorMap gate, value;
+};
+template <int DT, int V, int L, int CL>
+__global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel(const __grid_constant__ ScanArgs a, const __grid_constant__ ScanMaps maps) {
+  using P = Piece<DT, V>;
+  using T = typename Elem<DT>::type;
+  using S = TileShape<DT, V, L, 2, CL>;
+  constexpr uint32_t kDepth = S::kDepth, kGroups = S::kGroups, kTileRows = S::kTileRows, kColumns = S::kColumns;
+  constexpr int R = kRows, N = R * V;                // row k's columns at k V
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+  __shared__ Map<V> s_map[2][kGroups][L];
+  __shared__ float s_state[2][L][V];                // the state behind a tile, of the last group (without a cluster)
+  Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
+  __shared__ uint64_t s_full[kDepth];
+  const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&maps.gate), prefetch_map(&maps.value);
+  }
+  if constexpr (CL > 1) exchange_begin(s_x);
+  else __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  uint32_t round = 0, asked = 0, taken = 0, turn = 0;
+  const uint64_t stride = gridDim.x / CL;
+  for (uint64_t item = blockIdx.x / CL; item < a.items; item += stride) {
+    const uint32_t seq = (uint32_t)(item / a.slabs), col0 = (uint32_t)(item % a.slabs) * kColumns, c = col0 + lane * V;
+    uint32_t first, count;
+    a.spans.of(seq, &first, &count);
+    const bool in = c < a.width;
+    T* y = static_cast<T*>(a.y) + (uint64_t)first * a.ld_y + c;
+    const uint64_t mark0 = first_mark(seq, first);
+    const uint32_t tiles = (count + kTileRows - 1) / kTileRows, sets = (tiles + CL - 1) / CL;
+    const auto ask = [&](uint32_t set) {             // one thread: the copies of this CTA's tile of a set
+      const uint32_t tile = set * CL + rank, s = asked % kDepth;
+      if (tile >= tiles) return;
+      mbar_arrive_expect_tx(&s_full[s], S::kStage);
+      tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
+      tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
+      ++asked;
+    };
+    if (threadIdx.x == 0)
+      for (uint32_t n = 0; n < kDepth; ++n) ask(n);
+    float h[V];                                      // the state that enters the tile, or the cluster's tiles
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = in && a.h0 ? a.h0[(uint64_t)seq * a.width + c + i] : 0.f;
+    const auto rows_of = [&](uint32_t tile) {
+      const uint32_t r0 = tile * kTileRows + group * R;
+      return tile < tiles && r0 < count ? min((uint32_t)R, count - r0) : 0u;
+    };
+    // f and s v of this group's rows of a tile, and their map, which is left for the other groups
+    const auto evaluate = [&](uint32_t tile, float (&f)[N], float (&sv)[N]) __attribute__((always_inline)) {
+      const uint32_t rows = rows_of(tile), s = taken % kDepth;
+      bool good = true;
+      if (tile < tiles) {
+        const int never = 0;
+        good = mbar_wait(&s_full[s], (taken / kDepth) & 1u, &never);
+        ++taken;
+      }
+      if (rows) {
+        const T* from = reinterpret_cast<const T*>(smem + s * S::kStage) + (group * R * L + lane) * V;
+        float g[N], v[N];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          P::widen(*reinterpret_cast<const typename P::Raw*>(from + k * L * V), g + k * V);
+          P::widen(*reinterpret_cast<const typename P::Raw*>(from + S::kInput / sizeof(T) + k * L * V), v + k * V);
+        }
+        gates_of<DT>(g, f, sv);
+        times(sv, v, sv);
+      }
+      if (rows < R) {                                // behind the sequence: nothing changes
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          if (e / V >= (int)rows) f[e] = 1.f, sv[e] = 0.f;
+        }
+      }
+      Map<V> m;
+#pragma unroll
+      for (int i = 0; i < V; ++i) m.a[i] = f[i], m.b[i] = good ? sv[i] : NAN;
+#pragma unroll
+      for (int k = 1; k < R; ++k) {
+        fma_v<V>(f + k * V, m.b, sv + k * V, m.b);
+        mul_v<V>(f + k * V, m.a, m.a);
+      }
+      s_map[turn & 1u][group][lane] = m;
+      return m;
+    };
+    const auto apply = [&](uint32_t tile, const float (&f)[N], const float (&sv)[N], float (&state)[V]) __attribute__((always_inline)) {
+      const uint32_t r0 = tile * kTileRows + group * R, rows = in ? rows_of(tile) : 0u;
+      if (a.marks && group % kMarkGroups == 0 && rows) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) a.marks[(mark0 + r0 / kMarkRows) * a.width + c + i] = state[i];
+      }
+      T* to = y + (uint64_t)r0 * a.ld_y;
+      if (rows == R) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          fma_v<V>(f + k * V, state, sv + k * V, state);
+          P::store(to, P::narrow(state));
+          to += a.ld_y;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          fma_v<V>(f + k * V, state, sv + k * V, state);
+          if (k < (int)rows) P::store(to, P::narrow(state));
+          to += a.ld_y;
+        }
+      }
+    };
+    if constexpr (CL > 1) {
+      // the map of the next tile is under way to the others while this one's rows are written
+      float f[2][N], sv[2][N];
+      Map<V> before[2];                              // of the tile's rows before this group's
+      const auto begin = [&](uint32_t set, float (&fn)[N], float (&svn)[N], Map<V>& before_n) __attribute__((always_inline)) {
+        const Map<V> own = evaluate(set * CL + rank, fn, svn);
+        __syncthreads();
+        if (threadIdx.x == 0) ask(set + kDepth);
+        before_n = identity<V>();
+#pragma unroll
+        for (uint32_t w = 0; w < kGroups - 1; ++w) {
+          if (w == group) break;
+          append(before_n, s_map[turn & 1u][w][lane]);
+        }
+        ++turn;
+        if (group == kGroups - 1) {                    // (it has the tile's)
+          Map<V> all = before_n;
+          append(all, own);
+          exchange_send(s_x, rank, round + set, all);
+        }
+      };
+      const auto end = [&](uint32_t set, const float (&fn)[N], const float (&svn)[N], const Map<V>& before_n) __attribute__((always_inline)) {
+        float state[V];
+        exchange_fold<V, CL, false>(s_x, rank, round + set, state, h);
+        fma_v<V>(before_n.a, state, before_n.b, state);
+        apply(set * CL + rank, fn, svn, state);
+      };
+      if (sets) begin(0, f[0], sv[0], before[0]);
+      for (uint32_t set = 0; set < sets; set += 2) {
+        if (set + 1 < sets) begin(set + 1, f[1], sv[1], before[1]);
+        end(set, f[0], sv[0], before[0]);
+        if (set + 1 >= sets) break;
+        if (set + 2 < sets) begin(set + 2, f[0], sv[0], before[0]);
+        end(set + 1, f[1], sv[1], before[1]);
+      }
+      round += sets;
+      cluster_arrive();                              // (h_last may be h0: written when all have read it)
+      cluster_wait();
+    } else {
+      for (uint32_t tile = 0; tile < tiles; ++tile) {
+        float f[N], sv[N];
+        const Map<V> own = evaluate(tile, f, sv);
+        __syncthreads();
+        if (threadIdx.x == 0) ask(tile + kDepth);
+        if (tile) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) h[i] = s_state[turn & 1u][lane][i];
+        }
+#pragma unroll
+        for (uint32_t w = 0; w < kGroups - 1; ++w) {
+          if (w == group) break;
+          const Map<V> m = s_map[turn & 1u][w][lane];
+          fma_v<V>(m.a, h, m.b, h);
+        }
+        ++turn;
+        if (group == kGroups - 1) {
+          float behind[V];
+          fma_v<V>(own.a, h, own.b, behind);
+#pragma unroll
+          for (int i = 0; i < V; ++i) s_state[turn & 1u][lane][i] = behind[i];      // (read behind the next barrier)
+        }
+        apply(tile, f, sv, h);
+      }
+      __syncthreads();
+      if (tiles) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = s_state[turn & 1u][lane][i];
+      }
+    }
+    if (a.h_last && in && group == 0 && rank == 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) a.h_last[(uint64_t)seq * a.width + c + i] = h[i];
+    }
+  }
+  if constexpr (CL > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+}
+
+// Any other rows: read by each thread, the next tile's before this one's are worked on.
+template <int DT, int V>
+__global__ void __launch_bounds__(kWarps * 32) scan_kernel(const __grid_constant__ ScanArgs a) {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
   __shared__ float2 s_map[2][kWarps][32 * V];
-  __shared__ Exchange<CLUSTER ? V : 1> s_x;
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, rank = CLUSTER ? cluster_rank() : 0u;
-  if constexpr (CLUSTER) exchange_begin(s_x, cluster);
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  uint32_t turn = 0, round = 0;
-  const uint64_t stride = gridDim.x / cluster;
-  for (uint64_t item = blockIdx.x / cluster; item < a.items; item += stride) {
+  uint32_t turn = 0;
+  for (uint64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
     const uint32_t seq = (uint32_t)(item / a.slabs), c = ((uint32_t)(item % a.slabs) * 32u + lane) * V;
     uint32_t first, count;
     a.spans.of(seq, &first, &count);
@@ -144,10 +465,10 @@ __global__ void __launch_bounds__(kWarps * 32) scan_kernel(const __grid_constant
     float h[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) h[i] = in && a.h0 ? a.h0[(uint64_t)seq * a.width + c + i] : 0.f;
-    const uint32_t tiles = (count + kTileRows - 1) / kTileRows;
+    const uint32_t tiles = (count + kMarkRows - 1) / kMarkRows;
     typename P::Raw next_g[kRows], next_v[kRows];
     const auto ask = [&](uint32_t tile) {
-      const uint32_t r0 = tile * kTileRows + warp * kRows;
+      const uint32_t r0 = tile * kMarkRows + warp * kRows;
 #pragma unroll
       for (uint32_t k = 0; k < kRows; ++k) {
         const bool there = in && tile < tiles && r0 + k < count;
@@ -155,10 +476,10 @@ __global__ void __launch_bounds__(kWarps * 32) scan_kernel(const __grid_constant
         next_v[k] = there ? P::load(value + (uint64_t)(r0 + k) * a.ld_value) : P::none();
       }
     };
-    ask(rank);
-    for (uint32_t tile = rank; tile - rank < tiles; tile += cluster) {
-      const uint32_t r0 = tile * kTileRows + warp * kRows, rows = tile < tiles && r0 < count ? min(kRows, count - r0) : 0u;
-      float f[kRows][V], sv[kRows][V], A[V], B[V];
+    ask(0);
+    for (uint32_t tile = 0; tile < tiles; ++tile) {
+      const uint32_t r0 = tile * kMarkRows + warp * kRows, rows = r0 < count ? min(kRows, count - r0) : 0u;
+      float f[kRows][V], sv[kRows][V], A[V], B[V], mine[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) A[i] = 1.f, B[i] = 0.f;
 #pragma unroll
@@ -176,96 +497,36 @@ __global__ void __launch_bounds__(kWarps * 32) scan_kernel(const __grid_constant
           B[i] = fmaf(f[k][i], B[i], sv[k][i]);
         }
       }
-      ask(tile + cluster);
-      float2(*map)[32 * V] = s_map[turn & 1u];
-      ++turn;
+      ask(tile + 1);
+      float2(*map)[32 * V] = s_map[turn++ & 1u];
 #pragma unroll
       for (int i = 0; i < V; ++i) map[warp][lane * V + i] = make_float2(A[i], B[i]);
       __syncthreads();
-      if constexpr (CLUSTER) {
-        // the tile's map; from the others' the state that enters this tile, and the one behind the cluster's tiles
+      if (a.marks && in && warp == 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) a.marks[(mark0 + tile) * a.width + c + i] = h[i];
+      }
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          A[i] = 1.f, B[i] = 0.f;
-#pragma unroll
-          for (uint32_t w = 0; w < kWarps; ++w) {
-            const float2 m = map[w][lane * V + i];
-            A[i] *= m.x, B[i] = fmaf(m.x, B[i], m.y);
-          }
-        }
-        const bool good = exchange(s_x, cluster, rank, round, A, B);
-        float after[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float e = good ? h[i] : NAN, mine = e;
-          for (uint32_t q = 0; q < cluster; ++q) {
-            if (q == rank) mine = e;
-            const float2 m = s_x.pair[round & 1u][q][lane * V + i];
-            e = fmaf(m.x, e, m.y);
-          }
-          h[i] = mine, after[i] = e;
-        }
-        if (a.marks && in && tile < tiles && warp == 0) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) a.marks[(mark0 + tile) * a.width + c + i] = h[i];
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-#pragma unroll
-          for (uint32_t w = 0; w < kWarps; ++w) {
-            const float2 m = map[w][lane * V + i];
-            h[i] = w < warp ? fmaf(m.x, h[i], m.y) : h[i];
-          }
-        }
-#pragma unroll
-        for (uint32_t k = 0; k < kRows; ++k) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) h[i] = fmaf(f[k][i], h[i], sv[k][i]);
-          if (in && k < rows) P::store(y + (uint64_t)(r0 + k) * a.ld_y, P::narrow(h));
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) h[i] = after[i];
-        exchange_again(s_x, cluster, round);
-        ++round;
-      } else {
-        if (a.marks && in && warp == 0) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) a.marks[(mark0 + tile) * a.width + c + i] = h[i];
-        }
-        float mine[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          mine[i] = h[i];
-#pragma unroll
-          for (uint32_t w = 0; w < kWarps; ++w) {
-            if (w == warp) mine[i] = h[i];
-            const float2 m = map[w][lane * V + i];
-            h[i] = fmaf(m.x, h[i], m.y);
-          }
-        }
-#pragma unroll
-        for (uint32_t k = 0; k < kRows; ++k) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) mine[i] = fmaf(f[k][i], mine[i], sv[k][i]);
-          if (in && k < rows) P::store(y + (uint64_t)(r0 + k) * a.ld_y, P::narrow(mine));
+          if (w == warp) mine[i] = h[i];
+          const float2 m = map[w][lane * V + i];
+          h[i] = fmaf(m.x, h[i], m.y);
         }
       }
+#pragma unroll
+      for (uint32_t k = 0; k < kRows; ++k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) mine[i] = fmaf(f[k][i], mine[i], sv[k][i]);
+        if (in && k < rows) P::store(y + (uint64_t)(r0 + k) * a.ld_y, P::narrow(mine));
+      }
     }
-    // (h_last may be h0: written when all have read it)
-    if constexpr (CLUSTER) {
-      cluster_arrive();
-      cluster_wait();
-    } else {
-      __syncthreads();
-    }
-    if (a.h_last && in && warp == 0 && rank == 0) {
+    __syncthreads();                                 // (h_last may be h0: written when all have read it)
+    if (a.h_last && in && warp == 0) {
 #pragma unroll
       for (int i = 0; i < V; ++i) a.h_last[(uint64_t)seq * a.width + c + i] = h[i];
     }
-  }
-  if constexpr (CLUSTER) {
-    cluster_arrive();
-    cluster_wait();
   }
 }
 
@@ -290,9 +551,9 @@ __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const __grid_
 #pragma unroll
     for (int i = 0; i < V; ++i) h[i] = a.h0 ? a.h0[(uint64_t)seq * a.width + c + i] : 0.f;
     for (uint32_t r = 0; r < count; r += kShortAhead) {
-      if (a.marks && r % kTileRows == 0) {
+      if (a.marks && r % kMarkRows == 0) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) a.marks[(mark0 + r / kTileRows) * a.width + c + i] = h[i];
+        for (int i = 0; i < V; ++i) a.marks[(mark0 + r / kMarkRows) * a.width + c + i] = h[i];
       }
       typename P::Raw g_raw[kShortAhead], v_raw[kShortAhead];
 #pragma unroll
@@ -324,20 +585,273 @@ __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------- backward
-template <int DT, int V, bool CLUSTER>
-__global__ void __launch_bounds__(kWarps * 32, 2) scan_back_kernel(const __grid_constant__ ScanBackArgs a, uint32_t cluster) {
+struct ScanBackMaps {
+  CUtensorMap gate, value, dy;
+};
+// With a cluster a tile's rows are evaluated twice, from shared memory: for the maps that the others wait for, and a set later for the results.
+template <int DT, int V, int L, int CL>
+__global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const __grid_constant__ ScanBackArgs a, const __grid_constant__ ScanBackMaps maps) {
+  using P = Piece<DT, V>;
+  using T = typename Elem<DT>::type;
+  using S = TileShape<DT, V, L, 3, CL>;
+  constexpr uint32_t kDepth = S::kDepth, kGroups = S::kGroups, kTileRows = S::kTileRows, kColumns = S::kColumns;
+  constexpr int R = kRows, N = R * V;                // row k's columns at k V
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+  __shared__ Map<V> s_map[2][kGroups][L], s_back[2][kGroups][L];       // of the states, and of the gradient
+  __shared__ float s_carry[2][L][V];                // what leaves a tile towards the past, of the first group (without a cluster)
+  Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
+  __shared__ uint64_t s_full[kDepth];
+  const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&maps.gate), prefetch_map(&maps.value), prefetch_map(&maps.dy);
+  }
+  if constexpr (CL > 1) exchange_begin(s_x);
+  else __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  uint32_t round = 0, asked = 0, taken = 0, turn = 0;
+  const uint64_t stride = gridDim.x / CL;
+  for (uint64_t item = blockIdx.x / CL; item < a.items; item += stride) {
+    const uint32_t seq = (uint32_t)(item / a.slabs), col0 = (uint32_t)(item % a.slabs) * kColumns, c = col0 + lane * V;
+    uint32_t first, count;
+    a.spans.of(seq, &first, &count);
+    const bool in = c < a.width;
+    T* dgate = static_cast<T*>(a.dgate) + (uint64_t)first * a.ld_dgate + c;
+    T* dvalue = static_cast<T*>(a.dvalue) + (uint64_t)first * a.ld_dvalue + c;
+    const float* marks = a.marks + first_mark(seq, first) * a.width + c;
+    const uint32_t tiles = (count + kTileRows - 1) / kTileRows, sets = (tiles + CL - 1) / CL;
+    // sets are counted from the last one: set n holds the tiles (sets - 1 - n) CL + 0 .. CL - 1
+    const auto ask = [&](uint32_t n) {               // one thread
+      const uint32_t tile = (sets - 1u - n) * CL + rank, s = asked % kDepth;
+      if (n >= sets || tile >= tiles) return;
+      const int32_t row = (int32_t)(first + tile * kTileRows);
+      mbar_arrive_expect_tx(&s_full[s], S::kStage);
+      tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, row, &s_full[s]);
+      tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, row, &s_full[s]);
+      tile_load(smem + s * S::kStage + 2 * S::kInput, &maps.dy, (int32_t)col0, row, &s_full[s]);
+      ++asked;
+    };
+    // With a cluster a set's tile is read again one set later: while the maps of set n are made, n and n - 1 hold a stage each and n + 1 may be
+    // on its way.
+    constexpr uint32_t kAhead = CL > 1 ? kDepth - 2 : kDepth;
+    if (threadIdx.x == 0)
+      for (uint32_t n = 0; n < kAhead; ++n) ask(n);
+    float carry[V];                                  // f[t+1] dh[t+1] of the row behind the tile, or the cluster's tiles
+#pragma unroll
+    for (int i = 0; i < V; ++i) carry[i] = in && a.dh_last ? a.dh_last[(uint64_t)seq * a.width + c + i] : 0.f;
+    struct Rows {
+      float f[N], s[N], v[N], d[N];
+    };
+    const auto rows_of = [&](uint32_t tile) {
+      const uint32_t r0 = tile * kTileRows + group * R;
+      return tile < tiles && r0 < count ? min((uint32_t)R, count - r0) : 0u;
+    };
+    const auto read = [&](uint32_t stage, uint32_t rows, Rows& x) __attribute__((always_inline)) {
+      if (rows) {
+        const T* from = reinterpret_cast<const T*>(smem + stage * S::kStage) + (group * R * L + lane) * V;
+        float g[N];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          P::widen(*reinterpret_cast<const typename P::Raw*>(from + k * L * V), g + k * V);
+          P::widen(*reinterpret_cast<const typename P::Raw*>(from + S::kInput / sizeof(T) + k * L * V), x.v + k * V);
+          P::widen(*reinterpret_cast<const typename P::Raw*>(from + 2 * S::kInput / sizeof(T) + k * L * V), x.d + k * V);
+        }
+        gates_of<DT>(g, x.f, x.s);
+      }
+      if (rows < R) {                                // behind the sequence: nothing changes
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          if (e / V >= (int)rows) x.f[e] = 1.f, x.s[e] = x.v[e] = x.d[e] = 0.f;
+        }
+      }
+    };
+    // Leaves the maps of this group's rows for the others: h -> A h + B of the states, and of the gradient C = sum of d[k] f[0] .. f[k], which is
+    // A times what reaches the last row, plus C, at the first.  Returns the latter.
+    const auto leave = [&](const Rows& x, bool good) __attribute__((always_inline)) {
+      Map<V> m, b;
+      float sv[N];
+      times(x.s, x.v, sv);
+#pragma unroll
+      for (int i = 0; i < V; ++i) m.a[i] = x.f[i], m.b[i] = good ? sv[i] : NAN, b.b[i] = good ? 0.f : NAN;
+      fma_v<V>(m.a, x.d, b.b, b.b);
+#pragma unroll
+      for (int k = 1; k < R; ++k) {
+        fma_v<V>(x.f + k * V, m.b, sv + k * V, m.b);
+        mul_v<V>(x.f + k * V, m.a, m.a);
+        fma_v<V>(m.a, x.d + k * V, b.b, b.b);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) b.a[i] = m.a[i];
+      s_map[turn & 1u][group][lane] = m;
+      s_back[turn & 1u][group][lane] = b;
+      return b;
+    };
+    // the state at the last mark before this group's rows
+    const uint32_t group0 = group / kMarkGroups * kMarkGroups;
+    const auto mark_of = [&](uint32_t tile, float (&h)[V]) {
+      const uint32_t r0 = tile * kTileRows + group0 * R;
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[i] = in && tile < tiles && r0 < count ? marks[(uint64_t)(r0 / kMarkRows) * a.width + i] : 0.f;
+    };
+    const auto wait = [&](uint32_t tile, uint32_t* stage) {
+      *stage = taken % kDepth;
+      if (tile >= tiles) return true;
+      const int never = 0;
+      const bool good = mbar_wait(&s_full[*stage], (taken / kDepth) & 1u, &never);
+      ++taken;
+      return good;
+    };
+    // from there to the state before this group's rows
+    const auto state_of = [&](float (&h)[V]) __attribute__((always_inline)) {
+#pragma unroll
+      for (uint32_t n = 0; n < kMarkGroups - 1; ++n) {
+        if (group0 + n == group) break;
+        const Map<V> m = s_map[turn & 1u][group0 + n][lane];
+        fma_v<V>(m.a, h, m.b, h);
+      }
+    };
+    // g: what reaches this group's last row from behind it
+    const auto write = [&](uint32_t tile, Rows& x, float (&h)[V], float (&g)[V]) __attribute__((always_inline)) {
+      const uint32_t rows = in ? rows_of(tile) : 0u, r0 = tile * kTileRows + group * R;
+      float sv[N];
+      times(x.s, x.v, sv);
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x.v[k * V + i] = h[i] - x.v[k * V + i];
+        fma_v<V>(x.f + k * V, h, sv + k * V, h);
+      }
+      times(x.v, x.f, x.v);
+      T *to_g = dgate + (uint64_t)(r0 + R - 1) * a.ld_dgate, *to_v = dvalue + (uint64_t)(r0 + R - 1) * a.ld_dvalue;
+#pragma unroll
+      for (int k = R - 1; k >= 0; --k) {
+        float dg[V], dv[V], dh[V];
+        add_v<V>(x.d + k * V, g, dh);
+        mul_v<V>(x.s + k * V, dh, dv);
+        mul_v<V>(x.f + k * V, dh, g);
+        mul_v<V>(x.v + k * V, dv, dg);
+        if (k < (int)rows) {
+          P::store(to_g, P::narrow(dg));
+          P::store(to_v, P::narrow(dv));
+        }
+        to_g -= a.ld_dgate, to_v -= a.ld_dvalue;
+      }
+    };
+    if constexpr (CL > 1) {
+      float h[V], next_h[V];
+      Map<V> behind, next_behind;                    // of the tile's rows behind this group's
+      uint32_t stage = 0, next_stage = 0;
+      const auto start = [&](uint32_t n) __attribute__((always_inline)) {
+        const uint32_t tile = (sets - 1u - n) * CL + rank;
+        mark_of(tile, next_h);
+        const bool good = wait(tile, &next_stage);
+        Map<V> own;
+        {
+          Rows x;
+          read(next_stage, rows_of(tile), x);
+          own = leave(x, good);
+        }
+        __syncthreads();
+        // (all are past finish of set n - 2: its stage is free)
+        if (threadIdx.x == 0) ask(n + kAhead);
+        next_behind = identity<V>();
+#pragma unroll
+        for (uint32_t w = kGroups - 1; w > 0; --w) {
+          if (w == group) break;
+          append(next_behind, s_back[turn & 1u][w][lane]);
+        }
+        state_of(next_h);
+        ++turn;
+        if (group == 0) {
+          Map<V> all = next_behind;
+          append(all, own);
+          exchange_send(s_x, rank, round + n, all);
+        }
+      };
+      for (uint32_t n = 0; n <= sets && sets; ++n) {
+        // the maps of set n go out while set n - 1 is finished
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = next_h[i];
+        behind = next_behind, stage = next_stage;
+        if (n < sets) start(n);
+        if (n == 0) continue;
+        const uint32_t tile = (sets - n) * CL + rank;
+        float g[V];
+        exchange_fold<V, CL, true>(s_x, rank, round + n - 1, g, carry);
+        fma_v<V>(behind.a, g, behind.b, g);
+        if (rows_of(tile)) {
+          Rows x;
+          read(stage, rows_of(tile), x);
+          write(tile, x, h, g);
+        }
+      }
+      round += sets;
+      cluster_arrive();                              // (dh0 may be dh_last: written when all have read it)
+      cluster_wait();
+    } else {
+      for (uint32_t n = 0; n < sets; ++n) {
+        const uint32_t tile = sets - 1u - n;
+        Rows x;
+        float h[V];
+        uint32_t stage;
+        mark_of(tile, h);
+        const bool good = wait(tile, &stage);
+        read(stage, rows_of(tile), x);
+        const Map<V> own = leave(x, good);
+        __syncthreads();
+        if (threadIdx.x == 0) ask(n + kAhead);
+        if (n) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) carry[i] = s_carry[turn & 1u][lane][i];
+        }
+#pragma unroll
+        for (uint32_t w = kGroups - 1; w > 0; --w) {
+          if (w == group) break;
+          const Map<V> m = s_back[turn & 1u][w][lane];
+          fma_v<V>(m.a, carry, m.b, carry);
+        }
+        state_of(h);
+        ++turn;
+        if (group == 0) {
+          float before[V];
+          fma_v<V>(own.a, carry, own.b, before);
+#pragma unroll
+          for (int i = 0; i < V; ++i) s_carry[turn & 1u][lane][i] = before[i];       // (read behind the next barrier)
+        }
+        write(tile, x, h, carry);
+      }
+      __syncthreads();
+      if (sets) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) carry[i] = s_carry[turn & 1u][lane][i];
+      }
+    }
+    if (a.dh0 && in && group == 0 && rank == 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) a.dh0[(uint64_t)seq * a.width + c + i] = carry[i];
+    }
+  }
+  if constexpr (CL > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+}
+
+// Any other rows, read by each thread.
+template <int DT, int V>
+__global__ void __launch_bounds__(kWarps * 32, 2) scan_back_kernel(const __grid_constant__ ScanBackArgs a) {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
   __shared__ float2 s_map[2][kWarps][32 * V];       // (A, B): of the states
   __shared__ float s_back[2][kWarps][32 * V];       // C: of the gradient
-  __shared__ Exchange<CLUSTER ? V : 1> s_x;
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, rank = CLUSTER ? cluster_rank() : 0u;
-  if constexpr (CLUSTER) exchange_begin(s_x, cluster);
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  uint32_t turn = 0, round = 0;
-  const uint64_t stride = gridDim.x / cluster;
-  for (uint64_t item = blockIdx.x / cluster; item < a.items; item += stride) {
+  uint32_t turn = 0;
+  for (uint64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
     const uint32_t seq = (uint32_t)(item / a.slabs), c = ((uint32_t)(item % a.slabs) * 32u + lane) * V;
     uint32_t first, count;
     a.spans.of(seq, &first, &count);
@@ -351,25 +865,24 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_kernel(const __grid_
     float carry[V];                                  // f[t+1] dh[t+1] of the row behind the tile
 #pragma unroll
     for (int i = 0; i < V; ++i) carry[i] = in && a.dh_last ? a.dh_last[(uint64_t)seq * a.width + c + i] : 0.f;
-    const uint32_t tiles = (count + kTileRows - 1) / kTileRows, sets = (tiles + cluster - 1) / cluster;
+    const uint32_t tiles = (count + kMarkRows - 1) / kMarkRows;
     typename P::Raw next_g[kRows], next_v[kRows], next_d[kRows];
     float next_h[V];
-    const auto ask = [&](uint32_t set) {             // of the set-th group of tiles, counted from 1
-      const uint32_t tile = (set - 1) * cluster + rank, r0 = tile * kTileRows + warp * kRows;
+    const auto ask = [&](uint32_t behind) {          // of the tile before that one
+      const uint32_t tile = behind - 1, r0 = tile * kMarkRows + warp * kRows;
 #pragma unroll
       for (uint32_t k = 0; k < kRows; ++k) {
-        const bool there = in && set && tile < tiles && r0 + k < count;
+        const bool there = in && behind && r0 + k < count;
         next_g[k] = there ? P::load(gate + (uint64_t)(r0 + k) * a.ld_gate) : P::none();
         next_v[k] = there ? P::load(value + (uint64_t)(r0 + k) * a.ld_value) : P::none();
         next_d[k] = there ? P::load(dy + (uint64_t)(r0 + k) * a.ld_dy) : P::none();
       }
 #pragma unroll
-      for (int i = 0; i < V; ++i) next_h[i] = in && set && tile < tiles ? marks[(uint64_t)tile * a.width + i] : 0.f;
+      for (int i = 0; i < V; ++i) next_h[i] = in && behind ? marks[(uint64_t)tile * a.width + i] : 0.f;
     };
-    ask(sets);
-    for (uint32_t set = sets; set > 0; --set) {
-      const uint32_t tile = (set - 1) * cluster + rank, r0 = tile * kTileRows + warp * kRows;
-      const uint32_t rows = tile < tiles && r0 < count ? min(kRows, count - r0) : 0u;
+    ask(tiles);
+    for (uint32_t behind = tiles; behind > 0; --behind) {
+      const uint32_t r0 = (behind - 1) * kMarkRows + warp * kRows, rows = r0 < count ? min(kRows, count - r0) : 0u;
       float f[kRows][V], s[kRows][V], v[kRows][V], A[V], B[V], C[V], h[V];
       typename P::Raw d_raw[kRows];
 #pragma unroll
@@ -395,53 +908,24 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_kernel(const __grid_
 #pragma unroll
         for (int i = 0; i < V; ++i) C[i] = f[k][i] * (d[i] + C[i]);
       }
-      ask(set - 1);
+      ask(behind - 1);
       float2(*map)[32 * V] = s_map[turn & 1u];
       float(*back)[32 * V] = s_back[turn & 1u];
       ++turn;
 #pragma unroll
       for (int i = 0; i < V; ++i) map[warp][lane * V + i] = make_float2(A[i], B[i]), back[warp][lane * V + i] = C[i];
       __syncthreads();
-      float behind[V];                               // what reaches the tile's last row
-      if constexpr (CLUSTER) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          A[i] = 1.f, C[i] = 0.f;
-#pragma unroll
-          for (uint32_t w = kWarps; w-- > 0;) {
-            const float m = map[w][lane * V + i].x;
-            A[i] *= m, C[i] = fmaf(m, C[i], back[w][lane * V + i]);
-          }
-        }
-        const bool good = exchange(s_x, cluster, rank, round, A, C);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float e = good ? carry[i] : NAN;
-          behind[i] = e;
-          for (uint32_t q = cluster; q-- > 0;) {
-            if (q == rank) behind[i] = e;
-            const float2 m = s_x.pair[round & 1u][q][lane * V + i];
-            e = fmaf(m.x, e, m.y);
-          }
-          carry[i] = e;
-        }
-        exchange_again(s_x, cluster, round);
-        ++round;
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) behind[i] = carry[i];
-      }
       float g[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        float e = behind[i];
+        float e = carry[i];
         g[i] = e;
 #pragma unroll
         for (uint32_t w = kWarps; w-- > 0;) {
           if (w == warp) g[i] = e;
           e = fmaf(map[w][lane * V + i].x, e, back[w][lane * V + i]);
         }
-        if (!CLUSTER) carry[i] = e;
+        carry[i] = e;
 #pragma unroll
         for (uint32_t w = 0; w < kWarps; ++w) {
           const float2 m = map[w][lane * V + i];
@@ -474,20 +958,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_kernel(const __grid_
         }
       }
     }
-    if constexpr (CLUSTER) {
-      cluster_arrive();
-      cluster_wait();
-    } else {
-      __syncthreads();
-    }
-    if (a.dh0 && in && warp == 0 && rank == 0) {
+    __syncthreads();                                 // (dh0 may be dh_last: written when all have read it)
+    if (a.dh0 && in && warp == 0) {
 #pragma unroll
       for (int i = 0; i < V; ++i) a.dh0[(uint64_t)seq * a.width + c + i] = carry[i];
     }
-  }
-  if constexpr (CLUSTER) {
-    cluster_arrive();
-    cluster_wait();
   }
 }
 
@@ -516,9 +991,9 @@ __global__ void __launch_bounds__(kShortThreads) scan_back_short_kernel(const __
       const uint32_t r0 = (end - 1) / kShortAhead * kShortAhead, rows = end - r0;
       float h[V], f[kShortAhead][V], s[kShortAhead][V], v[kShortAhead][V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[i] = marks[(uint64_t)(r0 / kTileRows) * a.width + i];
+      for (int i = 0; i < V; ++i) h[i] = marks[(uint64_t)(r0 / kMarkRows) * a.width + i];
       // the state before r0 (a sequence this long among short ones goes through its rows several times)
-      for (uint32_t r = r0 / kTileRows * kTileRows; r < r0; ++r) {
+      for (uint32_t r = r0 / kMarkRows * kMarkRows; r < r0; ++r) {
         float x[V], w[V];
         P::widen(P::load_kept(gate + (uint64_t)r * a.ld_gate), x);
         P::widen(P::load_kept(value + (uint64_t)r * a.ld_value), w);
@@ -570,11 +1045,19 @@ __global__ void __launch_bounds__(kShortThreads) scan_back_short_kernel(const __
 }
 
 // ---------------------------------------------------------------- host side
-template <typename Args>
-cudaError_t launch_clusters(void (*kernel)(Args, uint32_t), const Args& a, uint32_t cluster, cudaStream_t stream) {
+// The launch of a kernel over tiles that copies bring, in clusters of `cluster`.
+template <typename Args, typename Maps>
+cudaError_t launch_tiled(void (*kernel)(Args, Maps), PerDeviceInt& ready, const Args& a, const Maps& maps, uint32_t bytes, uint32_t cluster, cudaStream_t stream) {
+  int dev;
+  if (!ready.get(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
+    ready.set(dev, 1);
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(a.items, 1u << 24) * cluster);
   cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = bytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -584,39 +1067,98 @@ cudaError_t launch_clusters(void (*kernel)(Args, uint32_t), const Args& a, uint3
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a, cluster);
+  return cudaLaunchKernelEx(&cfg, kernel, a, maps);
 }
-// CTAs per sequence and slab: more while SMs would be idle and every CTA has two tiles or more
-uint32_t choose_cluster(uint64_t items, const Spans& s) {
+uint32_t capped(uint64_t ctas) { return (uint32_t)std::min<uint64_t>(ctas, 1u << 24); }
+template <typename Args>
+void cut(Args& a, uint32_t columns) {
+  a.slabs = (a.width + columns - 1) / columns;
+  a.items = (uint64_t)a.spans.sequences * a.slabs;
+}
+// CTAs per sequence and slab: more while two of them would still fit every SM and each has two tiles or more.
+uint32_t choose_cluster(uint64_t items, const Spans& s, uint32_t tile_rows) {
   uint32_t cluster = 1;
-  while (cluster < kMostCluster && items * cluster * 2 <= 2ull * sm_count() && s.rows / s.sequences >= 4ull * cluster * kTileRows) cluster *= 2;
+  while (cluster < kMostCluster && items * cluster * 2 <= 2ull * sm_count() && s.rows / s.sequences >= 4ull * cluster * tile_rows) cluster *= 2;
   return cluster;
 }
-template <int DT, int V>
-cudaError_t launch_forward(ScanArgs a, cudaStream_t stream) {
-  if (a.spans.rows / a.spans.sequences < kShortRows) {
-    a.slabs = a.width / V;
-    a.items = (uint64_t)a.spans.sequences * a.slabs;
-    const uint64_t ctas = std::min<uint64_t>((a.items + kShortThreads - 1) / kShortThreads, 1u << 24);
-    return launch_dependent(scan_short_kernel<DT, V>, dim3((uint32_t)ctas), dim3(kShortThreads), 0, stream, a);
-  }
-  a.slabs = (a.width + 32 * V - 1) / (32 * V);
-  a.items = (uint64_t)a.spans.sequences * a.slabs;
-  const uint32_t cluster = choose_cluster(a.items, a.spans);
-  return launch_clusters<ScanArgs>(cluster > 1 ? scan_kernel<DT, V, true> : scan_kernel<DT, V, false>, a, cluster, stream);
+// Half as many columns and twice the rows to a tile where wide ones in the largest clusters would leave SMs with one CTA or none (one sequence of
+// 65536 rows of 1024: MEASURED).
+template <typename Args>
+bool narrow_tiles(const Args& a, uint32_t columns) {
+  return (uint64_t)a.spans.sequences * ((a.width + columns - 1) / columns) * kMostCluster <= (uint64_t)sm_count() && a.spans.rows / a.spans.sequences >= 8u * kMarkRows;
 }
-template <int DT, int V>
-cudaError_t launch_backward(ScanBackArgs a, cudaStream_t stream) {
-  if (a.spans.rows / a.spans.sequences < kShortRows) {
-    a.slabs = a.width / V;
-    a.items = (uint64_t)a.spans.sequences * a.slabs;
-    const uint64_t ctas = std::min<uint64_t>((a.items + kShortThreads - 1) / kShortThreads, 1u << 24);
-    return launch_dependent(scan_back_short_kernel<DT, V>, dim3((uint32_t)ctas), dim3(kShortThreads), 0, stream, a);
+// Rows that tiled copies take: the map's box is the tile.
+template <int DT, typename Shape>
+bool encode_rows(CUtensorMap* map, const void* p, uint64_t ld, const Spans& s, uint32_t width) {
+  constexpr uint64_t item = sizeof(typename Elem<DT>::type);
+  return encode_matrix(map, p, (s.rows > 1 ? ld : (width + 7) / 8 * 8) * item, width, s.rows, Shape::kColumns, Shape::kTileRows, DT);
+}
+bool tiles_take(const void* p, uint64_t ld, uint64_t rows, size_t item) { return aligned_to(p, 16) && (rows <= 1 || ld * item % 16 == 0); }
+template <int DT, int V, int L, int CL>
+cudaError_t forward_in(const ScanArgs& a, const ScanMaps& m, cudaStream_t stream) {
+  static PerDeviceInt ready;
+  return launch_tiled<ScanArgs, ScanMaps>(scan_tiled_kernel<DT, V, L, CL>, ready, a, m, TileShape<DT, V, L, 2, CL>::kBytes, CL, stream);
+}
+template <int DT, int V, int L>
+cudaError_t forward_tiled(ScanArgs a, cudaStream_t stream) {
+  using S = TileShape<DT, V, L, 2, 1>;
+  cut(a, S::kColumns);
+  ScanMaps m;
+  if (!encode_rows<DT, S>(&m.gate, a.gate, a.ld_gate, a.spans, a.width) || !encode_rows<DT, S>(&m.value, a.value, a.ld_value, a.spans, a.width)) return cudaErrorInvalidValue;
+  switch (choose_cluster(a.items, a.spans, S::kTileRows)) {
+    case 1: return forward_in<DT, V, L, 1>(a, m, stream);
+    case 2: return forward_in<DT, V, L, 2>(a, m, stream);
+    case 4: return forward_in<DT, V, L, 4>(a, m, stream);
+    default: return forward_in<DT, V, L, 8>(a, m, stream);
   }
-  a.slabs = (a.width + 32 * V - 1) / (32 * V);
-  a.items = (uint64_t)a.spans.sequences * a.slabs;
-  const uint32_t cluster = choose_cluster(a.items, a.spans);
-  return launch_clusters<ScanBackArgs>(cluster > 1 ? scan_back_kernel<DT, V, true> : scan_back_kernel<DT, V, false>, a, cluster, stream);
+}
+template <int DT>
+cudaError_t launch_forward(ScanArgs a, bool two, cudaStream_t stream) {
+  constexpr size_t item = sizeof(typename Elem<DT>::type);
+  constexpr int W = item == 2 ? 2 : 1;
+  if (a.spans.rows / a.spans.sequences < kShortRows) {
+    cut(a, two ? W : 1);
+    const dim3 grid(capped((a.items + kShortThreads - 1) / kShortThreads)), block(kShortThreads);
+    return two ? launch_dependent(scan_short_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_short_kernel<DT, 1>, grid, block, 0, stream, a);
+  }
+  if ((two || item == 4) && tiles_take(a.gate, a.ld_gate, a.spans.rows, item) && tiles_take(a.value, a.ld_value, a.spans.rows, item))
+    return narrow_tiles(a, 32 * W) ? forward_tiled<DT, W, 16>(a, stream) : forward_tiled<DT, W, 32>(a, stream);
+  cut(a, 32 * (two ? W : 1));
+  const dim3 grid(capped(a.items)), block(kWarps * 32);
+  return two ? launch_dependent(scan_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_kernel<DT, 1>, grid, block, 0, stream, a);
+}
+template <int DT, int V, int L, int CL>
+cudaError_t backward_in(const ScanBackArgs& a, const ScanBackMaps& m, cudaStream_t stream) {
+  static PerDeviceInt ready;
+  return launch_tiled<ScanBackArgs, ScanBackMaps>(scan_back_tiled_kernel<DT, V, L, CL>, ready, a, m, TileShape<DT, V, L, 3, CL>::kBytes, CL, stream);
+}
+template <int DT, int V, int L>
+cudaError_t backward_tiled(ScanBackArgs a, cudaStream_t stream) {
+  using S = TileShape<DT, V, L, 3, 1>;
+  cut(a, S::kColumns);
+  ScanBackMaps m;
+  if (!encode_rows<DT, S>(&m.gate, a.gate, a.ld_gate, a.spans, a.width) || !encode_rows<DT, S>(&m.value, a.value, a.ld_value, a.spans, a.width) || !encode_rows<DT, S>(&m.dy, a.dy, a.ld_dy, a.spans, a.width)) return cudaErrorInvalidValue;
+  switch (choose_cluster(a.items, a.spans, S::kTileRows)) {
+    case 1: return backward_in<DT, V, L, 1>(a, m, stream);
+    case 2: return backward_in<DT, V, L, 2>(a, m, stream);
+    case 4: return backward_in<DT, V, L, 4>(a, m, stream);
+    default: return backward_in<DT, V, L, 8>(a, m, stream);
+  }
+}
+template <int DT>
+cudaError_t launch_backward(ScanBackArgs a, bool two, cudaStream_t stream) {
+  constexpr size_t item = sizeof(typename Elem<DT>::type);
+  constexpr int W = item == 2 ? 2 : 1;
+  if (a.spans.rows / a.spans.sequences < kShortRows) {
+    cut(a, two ? W : 1);
+    const dim3 grid(capped((a.items + kShortThreads - 1) / kShortThreads)), block(kShortThreads);
+    return two ? launch_dependent(scan_back_short_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_back_short_kernel<DT, 1>, grid, block, 0, stream, a);
+  }
+  if ((two || item == 4) && tiles_take(a.gate, a.ld_gate, a.spans.rows, item) && tiles_take(a.value, a.ld_value, a.spans.rows, item) && tiles_take(a.dy, a.ld_dy, a.spans.rows, item))
+    return narrow_tiles(a, 32 * W) ? backward_tiled<DT, W, 16>(a, stream) : backward_tiled<DT, W, 32>(a, stream);
+  cut(a, 32 * (two ? W : 1));
+  const dim3 grid(capped(a.items)), block(kWarps * 32);
+  return two ? launch_dependent(scan_back_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_back_kernel<DT, 1>, grid, block, 0, stream, a);
 }
 
 int check_shape(uint64_t rows, uint64_t sequences, uint64_t width, int dtype, const void* offsets, int offset_bits) {
@@ -650,9 +1192,8 @@ int forward(const gd_recurrence_forward_args* g, cudaStream_t stream) {
   const bool two = g->width % 2 == 0 && pairs(g->gate, g->ld_gate) && pairs(g->value, g->ld_value) && pairs(g->y, g->ld_y);
   ProfileScope ps(stream, PT_RECURRENCE);
   cudaError_t e;
-  if (g->dtype == GD_DTYPE_FP32) e = launch_forward<GD_DTYPE_FP32, 1>(a, stream);
-  else if (g->dtype == GD_DTYPE_BF16) e = two ? launch_forward<GD_DTYPE_BF16, 2>(a, stream) : launch_forward<GD_DTYPE_BF16, 1>(a, stream);
-  else e = two ? launch_forward<GD_DTYPE_FP16, 2>(a, stream) : launch_forward<GD_DTYPE_FP16, 1>(a, stream);
+  if (g->dtype == GD_DTYPE_FP32) e = launch_forward<GD_DTYPE_FP32>(a, false, stream);
+  else e = g->dtype == GD_DTYPE_BF16 ? launch_forward<GD_DTYPE_BF16>(a, two, stream) : launch_forward<GD_DTYPE_FP16>(a, two, stream);
   if (e != cudaSuccess) return GD_ERR_CUDA;
   note_launches(1);
   return GD_OK;
@@ -688,9 +1229,8 @@ int backward(const gd_recurrence_backward_args* g, cudaStream_t stream) {
   const bool two = g->width % 2 == 0 && pairs(g->dy, g->ld_dy) && pairs(g->gate, g->ld_gate) && pairs(g->value, g->ld_value) && pairs(g->dgate, g->ld_dgate) && pairs(g->dvalue, g->ld_dvalue);
   ProfileScope ps(stream, PT_RECURRENCE_BACK);
   cudaError_t e;
-  if (g->dtype == GD_DTYPE_FP32) e = launch_backward<GD_DTYPE_FP32, 1>(a, stream);
-  else if (g->dtype == GD_DTYPE_BF16) e = two ? launch_backward<GD_DTYPE_BF16, 2>(a, stream) : launch_backward<GD_DTYPE_BF16, 1>(a, stream);
-  else e = two ? launch_backward<GD_DTYPE_FP16, 2>(a, stream) : launch_backward<GD_DTYPE_FP16, 1>(a, stream);
+  if (g->dtype == GD_DTYPE_FP32) e = launch_backward<GD_DTYPE_FP32>(a, false, stream);
+  else e = g->dtype == GD_DTYPE_BF16 ? launch_backward<GD_DTYPE_BF16>(a, two, stream) : launch_backward<GD_DTYPE_FP16>(a, two, stream);
   if (e != cudaSuccess) return GD_ERR_CUDA;
   note_launches(1);
   return GD_OK;
@@ -704,7 +1244,7 @@ extern "C" {
 int gd_recurrence_marks_rows(uint64_t rows, uint64_t sequences, uint64_t* rows_out) {
   if (!rows_out) return GD_ERR_INVALID_ARG;
   if (rows >> 31 || sequences >> 31) return GD_ERR_TOO_LARGE;
-  *rows_out = rows / gd::kTileRows + sequences;
+  *rows_out = rows / gd::kMarkRows + sequences;
   return GD_OK;
 }
 int gd_recurrence_forward(const gd_recurrence_forward_args* a, void* stream) { return gd::forward(a, (cudaStream_t)stream); }
