@@ -19,21 +19,23 @@ namespace gd {
 namespace {
 
 constexpr uint32_t kDigitBits = 9, kDigits = 1u << kDigitBits;
-constexpr uint32_t kPer = 8;                       // positions a thread ranks
-constexpr uint32_t kOneThreads = 1024, kOneMost = kOneThreads * kPer;      // the sort of one CTA
-constexpr uint32_t kTileThreads = 512, kSortTile = kTileThreads * kPer, kMostTiles = 256;      // the sort of many: each takes a share of whole tiles
-constexpr uint32_t kChunk = 32;
+constexpr uint32_t kOnePer = 8, kOneThreads = 1024, kOneMost = kOneThreads * kOnePer;           // the sort of one CTA: positions a thread ranks
+constexpr uint32_t kTilePer = 4, kTileThreads = 512, kSortTile = kTileThreads * kTilePer;       // the sort of many: each takes a share of whole tiles
+constexpr uint32_t kMostTiles = 128;                   // (every one reads the counts of all)
+constexpr uint32_t kChunk = 32, kShortChunk = 8;       // positions of a chunk; of lists that one CTA sorts (more CTAs, each with less to wait for)
 constexpr uint32_t kFillCtasPerSm = 2;
 
 // ---------------------------------------------------------------- lookup
+// A group of `lanes` neighbouring threads (a power of two, up to a warp) takes a row, pieces of up to 16 bytes, kLookAhead of them in hand; the next
+// row's id is asked for before this one's pieces.
 struct EmbedArgs {
   const void* table;
   const void* ids;
   void* y;
-  uint64_t ld_table, ld_y, vocab, pieces_total;
+  uint64_t ld_table, ld_y, vocab;
   int64_t ignore_index;
-  uint32_t pieces;             // of a row
-  uint32_t id_bits;
+  uint32_t tokens, pieces;     // rows, and pieces of a row
+  uint32_t lanes, id_bits;
   float scale;
 };
 __device__ __forceinline__ int64_t id_at(const void* ids, uint64_t i, uint32_t bits) {
@@ -44,37 +46,37 @@ template <int DT, int OT, int V>
 __global__ void __launch_bounds__(kLookThreads) embed_kernel(const __grid_constant__ EmbedArgs a) {
   using P = Piece<DT, V>;
   using Q = Piece<OT, V>;
-  const auto* table = static_cast<const typename Elem<DT>::type*>(a.table);
-  auto* y = static_cast<typename Elem<OT>::type*>(a.y);
   pdl_wait();
   pdl_trigger();
-  const uint64_t stride = (uint64_t)gridDim.x * kLookThreads;
-  for (uint64_t t0 = (uint64_t)blockIdx.x * kLookThreads + threadIdx.x; t0 < a.pieces_total; t0 += stride * kLookAhead) {
-    typename P::Raw raw[kLookAhead];
-    uint64_t to[kLookAhead];
-    float fill[kLookAhead];                       // what a position without a row gives: 0 (padding) or NaN
-    bool have[kLookAhead];
+  const uint32_t t = blockIdx.x * kLookThreads + threadIdx.x, lane = t & (a.lanes - 1u), step = gridDim.x * kLookThreads / a.lanes;
+  uint32_t r = t / a.lanes;
+  int64_t next = r < a.tokens ? id_at(a.ids, r, a.id_bits) : 0;
+  for (; r < a.tokens; r += step) {
+    const int64_t id = next;
+    if (r + step < a.tokens) next = id_at(a.ids, r + step, a.id_bits);
+    auto* y = static_cast<typename Elem<OT>::type*>(a.y) + r * a.ld_y;
+    if (id != a.ignore_index && id >= 0 && (uint64_t)id < a.vocab) {
+      const auto* from = static_cast<const typename Elem<DT>::type*>(a.table) + (uint64_t)id * a.ld_table;
+      for (uint32_t c = lane; c < a.pieces; c += kLookAhead * a.lanes) {
+        typename P::Raw raw[kLookAhead];
 #pragma unroll
-    for (uint32_t u = 0; u < kLookAhead; ++u) {
-      const uint64_t t = t0 + u * stride;
-      have[u] = false, fill[u] = 0.f;
-      if (t >= a.pieces_total) continue;
-      const uint64_t r = t >> 32 ? t / a.pieces : (uint32_t)t / a.pieces;
-      const uint32_t c = (uint32_t)(t - r * a.pieces) * V;
-      const int64_t id = id_at(a.ids, r, a.id_bits);
-      to[u] = r * a.ld_y + c;
-      have[u] = id != a.ignore_index && id >= 0 && (uint64_t)id < a.vocab;
-      fill[u] = id == a.ignore_index ? 0.f : NAN;
-      if (have[u]) raw[u] = P::load_kept(table + (uint64_t)id * a.ld_table + c);
-    }
+        for (uint32_t u = 0; u < kLookAhead; ++u)
+          if (c + u * a.lanes < a.pieces) raw[u] = P::load_kept(from + (c + u * a.lanes) * V);
 #pragma unroll
-    for (uint32_t u = 0; u < kLookAhead; ++u) {
-      if (t0 + u * stride >= a.pieces_total) continue;
+        for (uint32_t u = 0; u < kLookAhead; ++u) {
+          if (c + u * a.lanes >= a.pieces) continue;
+          float x[V];
+          P::widen(raw[u], x);
+#pragma unroll
+          for (int i = 0; i < V; ++i) x[i] *= a.scale;
+          Q::store(y + (c + u * a.lanes) * V, Q::narrow(x));
+        }
+      }
+    } else {                                      // padding, or an id that is not in the table
       float x[V];
-      if (have[u]) P::widen(raw[u], x);
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = have[u] ? x[i] * a.scale : fill[u];
-      Q::store(y + to[u], Q::narrow(x));
+      for (int i = 0; i < V; ++i) x[i] = id == a.ignore_index ? 0.f : NAN;
+      for (uint32_t c = lane; c < a.pieces; c += a.lanes) Q::store(y + c * V, Q::narrow(x));
     }
   }
 }
@@ -126,7 +128,8 @@ struct SortArgs {
   const uint32_t* at_in;
   uint32_t* keys_out;
   uint32_t* at_out;
-  uint32_t* hist;              // [tiles][kDigits]
+  uint32_t* hist;              // [tiles][kDigits]: of this pass
+  uint32_t* next_hist;         // of the next one, counted while this one places (NULL: there is none)
   uint32_t* splits;            // splits[0]: how many chunks begin a run that is joined later, zeroed here
   int64_t ignore_index;
   uint32_t n, vocab, id_bits;
@@ -166,7 +169,7 @@ __device__ __forceinline__ uint32_t digit_scan(uint32_t x, uint32_t* s_warp) {
 // Stable ranks of THREADS x kPer positions by a digit: rank[u] is the place of position warp * 32 kPer + 32 u + lane among those of the same digit
 // in the warps' positions up to it; counts[w][d] afterwards is the number of positions of digit d in the warps before w.
 // Returns, in threads d < kDigits, the number of positions of digit d.  `live`: this thread's positions that exist, as bits.
-template <uint32_t THREADS>
+template <uint32_t THREADS, uint32_t kPer>
 __device__ __forceinline__ uint32_t rank_digits(const uint32_t (&key)[kPer], uint32_t live, uint32_t shift, uint32_t mask, uint32_t (*counts)[kDigits], uint32_t (&rank)[kPer]) {
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   for (uint32_t i = threadIdx.x; i < THREADS / 32 * kDigits; i += THREADS) (&counts[0][0])[i] = 0;
@@ -201,6 +204,7 @@ struct OneSmem {
   uint32_t keys[kOneMost], at[kOneMost];
 };
 __global__ void __launch_bounds__(kOneThreads) sort_one_kernel(const __grid_constant__ SortArgs a) {
+  constexpr uint32_t kPer = kOnePer;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ uint32_t s_base[kDigits], s_warp[kOneThreads / 32];
   OneSmem& s = *reinterpret_cast<OneSmem*>(smem);
@@ -222,7 +226,7 @@ __global__ void __launch_bounds__(kOneThreads) sort_one_kernel(const __grid_cons
   }
   const uint32_t mask = (1u << a.bits) - 1u;
   for (uint32_t p = 0; p < a.passes; ++p) {
-    const uint32_t total = rank_digits<kOneThreads>(key, live, p * a.bits, mask, s.counts, rank);
+    const uint32_t total = rank_digits<kOneThreads, kPer>(key, live, p * a.bits, mask, s.counts, rank);
     const uint32_t base = digit_scan(total, s_warp);
     if (threadIdx.x < kDigits) s_base[threadIdx.x] = base;
     __syncthreads();
@@ -244,8 +248,8 @@ __global__ void __launch_bounds__(kOneThreads) sort_one_kernel(const __grid_cons
   }
 }
 
-// More positions: per pass one launch counts the digits of every share, one places the positions.
-template <bool FIRST>
+// More positions: one launch counts the first digits of every share, then one per pass places the positions and counts the next digits of the
+// shares they come to (whole numbers: the order of these additions does not matter).
 __global__ void __launch_bounds__(kTileThreads) sort_count_kernel(const __grid_constant__ SortArgs a) {
   __shared__ uint32_t s_count[kDigits];
   pdl_wait();
@@ -254,15 +258,18 @@ __global__ void __launch_bounds__(kTileThreads) sort_count_kernel(const __grid_c
     fill_share(a, a.tiles);
     return;
   }
-  if (FIRST && blockIdx.x == 0 && threadIdx.x == 0) a.splits[0] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.splits[0] = 0;
   for (uint32_t d = threadIdx.x; d < kDigits; d += kTileThreads) s_count[d] = 0;
   __syncthreads();
   const uint64_t i0 = (uint64_t)blockIdx.x * a.per_tile, i1 = min(i0 + a.per_tile, (uint64_t)a.n);
   const uint32_t mask = (1u << a.bits) - 1u;
 #pragma unroll 4
-  for (uint64_t i = i0 + threadIdx.x; i < i1; i += kTileThreads) atomicAdd(&s_count[(FIRST ? key_of(a, (uint32_t)i) : a.keys_in[i]) >> a.shift & mask], 1u);
+  for (uint64_t i = i0 + threadIdx.x; i < i1; i += kTileThreads) atomicAdd(&s_count[key_of(a, (uint32_t)i) & mask], 1u);
   __syncthreads();
-  for (uint32_t d = threadIdx.x; d < kDigits; d += kTileThreads) a.hist[blockIdx.x * kDigits + d] = s_count[d];
+  for (uint32_t d = threadIdx.x; d < kDigits; d += kTileThreads) {
+    a.hist[blockIdx.x * kDigits + d] = s_count[d];
+    for (uint32_t p = 1; p < a.passes; ++p) a.hist[(p * kMostTiles + blockIdx.x) * kDigits + d] = 0;
+  }
 }
 struct TileSmem {
   uint32_t counts[kTileThreads / 32][kDigits];
@@ -270,6 +277,7 @@ struct TileSmem {
 template <bool FIRST>
 __global__ void __launch_bounds__(kTileThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
   static_assert(kTileThreads == kDigits, "a thread per digit");
+  constexpr uint32_t kPer = kTilePer;
   __shared__ TileSmem s;
   __shared__ uint32_t s_base[kDigits], s_warp[kTileThreads / 32];
   pdl_wait();
@@ -279,17 +287,10 @@ __global__ void __launch_bounds__(kTileThreads) sort_place_kernel(const __grid_c
     return;
   }
   const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, mask = (1u << a.bits) - 1u;
-  uint32_t before = 0, total = 0;      // positions of digit `tid` in the shares before this one, and in all
-#pragma unroll 8
-  for (uint32_t t = 0; t < a.tiles; ++t) {
-    const uint32_t c = a.hist[t * kDigits + tid];
-    before += t < blockIdx.x ? c : 0u;
-    total += c;
-  }
-  s_base[tid] = digit_scan(total, s_warp) + before;
   const uint64_t i0 = (uint64_t)blockIdx.x * a.per_tile, i1 = min(i0 + a.per_tile, (uint64_t)a.n);
-  for (uint64_t from = i0; from < i1; from += kSortTile) {
-    uint32_t key[kPer], at[kPer], rank[kPer], live = 0;
+  uint32_t key[kPer], at[kPer], rank[kPer], live = 0;
+  const auto take = [&](uint64_t from) {
+    live = 0;
 #pragma unroll
     for (uint32_t u = 0; u < kPer; ++u) {
       const uint64_t i = from + warp * 32u * kPer + 32u * u + lane;
@@ -298,14 +299,34 @@ __global__ void __launch_bounds__(kTileThreads) sort_place_kernel(const __grid_c
       key[u] = !in ? 0u : FIRST ? key_of(a, (uint32_t)i) : a.keys_in[i];
       at[u] = !in ? 0u : FIRST ? (uint32_t)i : a.at_in[i];
     }
-    const uint32_t here = rank_digits<kTileThreads>(key, live, a.shift, mask, s.counts, rank);
+  };
+  take(i0);
+  uint32_t before = 0, total = 0;      // positions of digit `tid` in the shares before this one, and in all
+#pragma unroll 32
+  for (uint32_t t = 0; t < a.tiles; ++t) {
+    const uint32_t c = a.hist[t * kDigits + tid];
+    before += t < blockIdx.x ? c : 0u;
+    total += c;
+  }
+  s_base[tid] = digit_scan(total, s_warp) + before;
+  for (uint64_t from = i0; from < i1; from += kSortTile) {
+    if (from != i0) take(from);
+    const uint32_t here = rank_digits<kTileThreads, kPer>(key, live, a.shift, mask, s.counts, rank);
     __syncthreads();
 #pragma unroll
     for (uint32_t u = 0; u < kPer; ++u) {
-      if (!(live >> u & 1u)) continue;
-      const uint32_t d = key[u] >> a.shift & mask, to = s_base[d] + s.counts[warp][d] + rank[u];
-      a.keys_out[to] = key[u];
-      a.at_out[to] = at[u];
+      const bool in = live >> u & 1u;
+      uint32_t count_at = 0xFFFFFFFFu;
+      if (in) {
+        const uint32_t d = key[u] >> a.shift & mask, to = s_base[d] + s.counts[warp][d] + rank[u];
+        a.keys_out[to] = key[u];
+        a.at_out[to] = at[u];
+        count_at = to / a.per_tile * kDigits + (key[u] >> (a.shift + a.bits) & mask);
+      }
+      if (a.next_hist) {                               // (frequent ids have their upper digit in common: one addition for all that a warp has)
+        const uint32_t peers = __match_any_sync(0xFFFFFFFFu, count_at);
+        if (in && lane == (uint32_t)__ffs(peers) - 1u) atomicAdd(&a.next_hist[count_at], (uint32_t)__popc(peers));
+      }
     }
     __syncthreads();
     s_base[tid] += here;
@@ -340,7 +361,7 @@ __device__ __forceinline__ void put_row(const SumArgs& a, uint32_t key, uint32_t
   *reinterpret_cast<typename Q::Raw*>(to) = Q::narrow(sum);
 }
 constexpr uint32_t kSumAhead = 8;
-template <int DT, int GT, int V>
+template <int DT, int GT, int V, uint32_t kChunk>
 __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArgs a) {
   using P = Piece<DT, V>;
   __shared__ uint32_t s_key[3 * kChunk + 2], s_at[2 * kChunk];      // s_key[j]: of sorted position i0 - kChunk - 1 + j
@@ -395,9 +416,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
       if (j + u + 1 < end && key[j + u + 1] == k) continue;
       // the run's last row here
       if ((came && k == key[-1]) || (goes && k == last)) {
-        float* to = part + (came && k == key[-1] ? 0u : a.part_ld);
-#pragma unroll
-        for (int i = 0; i < V; ++i) to[i] = sum[i];
+        Piece<GD_DTYPE_FP32, V>::store(part + (came && k == key[-1] ? 0u : a.part_ld), Piece<GD_DTYPE_FP32, V>::narrow(sum));
       } else {
         put_row<GT, V>(a, k, c, sum);
       }
@@ -411,20 +430,21 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
 // The runs of more than two chunks: the part of the chunk they begin in, then those of the chunks that follow, shared out to the warps in order.
 constexpr uint32_t kJoinWarps = 8;
 template <int GT, int V>
-__global__ void __launch_bounds__(32 * kJoinWarps) sum_join_kernel(const __grid_constant__ SumArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps) sum_join_kernel(const __grid_constant__ SumArgs a, uint32_t chunk_rows) {
+  using F = Piece<GD_DTYPE_FP32, V>;                  // (the parts' rows are multiples of four apart)
   __shared__ float s_sum[kJoinWarps][32 * V];
   __shared__ uint32_t s_more;
   pdl_wait();
   pdl_trigger();
   const uint32_t count = a.splits[0], lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, c = (blockIdx.y * 32u + lane) * V;
   for (uint32_t e = blockIdx.x; e < count; e += gridDim.x) {
-    const uint32_t chunk = a.splits[1u + e], key = a.keys[(uint64_t)chunk * kChunk + kChunk - 1];
+    const uint32_t chunk = a.splits[1u + e], key = a.keys[(uint64_t)chunk * chunk_rows + chunk_rows - 1];
     // how many chunks follow that begin inside the run
     uint32_t more = 0;
     for (bool on = true; on; ) {
       if (threadIdx.x == 0) s_more = 0;
       __syncthreads();
-      const uint64_t i = ((uint64_t)chunk + 1 + more + threadIdx.x) * kChunk;
+      const uint64_t i = ((uint64_t)chunk + 1 + more + threadIdx.x) * chunk_rows;
       const uint32_t inside = __ballot_sync(0xFFFFFFFFu, i < a.n && a.keys[i < a.n ? i : 0] == key);
       if (lane == 0) atomicAdd(&s_more, (uint32_t)__popc(inside));
       __syncthreads();
@@ -438,16 +458,15 @@ __global__ void __launch_bounds__(32 * kJoinWarps) sum_join_kernel(const __grid_
     for (int i = 0; i < V; ++i) sum[i] = 0.f;
     if (c < a.width) {
       if (warp == 0) {
-        const float* from = a.part + ((uint64_t)chunk * 2 + 1) * a.part_ld + c;
-#pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] = from[i];
+        F::widen(F::load_kept(a.part + ((uint64_t)chunk * 2 + 1) * a.part_ld + c), sum);
       }
       const uint32_t m0 = (uint64_t)more * warp / kJoinWarps, m1 = (uint64_t)more * (warp + 1) / kJoinWarps;
 #pragma unroll 8
       for (uint32_t m = m0; m < m1; ++m) {
-        const float* from = a.part + ((uint64_t)chunk + 1 + m) * 2 * a.part_ld + c;
+        float x[V];
+        F::widen(F::load_kept(a.part + ((uint64_t)chunk + 1 + m) * 2 * a.part_ld + c), x);
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] += from[i];
+        for (int i = 0; i < V; ++i) sum[i] += x[i];
       }
     }
 #pragma unroll
@@ -472,6 +491,7 @@ uint32_t bits_of(uint64_t x) {      // of the largest key
   while (x >> b) ++b;
   return b;
 }
+uint32_t chunk_of(uint64_t n) { return n <= kOneMost ? kShortChunk : kChunk; }
 // Where everything is in the workspace.
 struct Layout {
   uint64_t keys[2], at[2], hist, splits, part, part_ld, end;
@@ -484,25 +504,33 @@ struct Layout {
     };
     const bool one = n <= kOneMost;
     for (int i = 0; i < 2; ++i) keys[i] = i && one ? 0 : take(4 * n), at[i] = i && one ? 0 : take(4 * n);
-    hist = take(one ? 0 : (uint64_t)kMostTiles * kDigits * 4);
-    const uint64_t chunks = (n + kChunk - 1) / kChunk;
+    hist = take(one ? 0 : 4ull * kMostTiles * kDigits * 4);        // (31 bits are four passes)
+    const uint32_t chunk = chunk_of(n);
+    const uint64_t chunks = (n + chunk - 1) / chunk;
     splits = take(4 * (chunks + 1));
     part_ld = up(width, 4);
-    part = take(n > 2 * kChunk ? chunks * 2 * part_ld * 4 : 0);
+    part = take(n > 2 * chunk ? chunks * 2 * part_ld * 4 : 0);
     end = std::max<uint64_t>(o, 256);
   }
 };
 
+template <int DT, int OT, int V>
+cudaError_t launch_pieces(EmbedArgs a, uint32_t width, cudaStream_t stream) {
+  a.pieces = width / V;
+  a.lanes = 1;
+  while (a.lanes < 32 && a.lanes < a.pieces) a.lanes *= 2;
+  const uint64_t ctas = ((uint64_t)a.tokens * a.lanes + kLookThreads - 1) / kLookThreads;
+  return launch_dependent(embed_kernel<DT, OT, V>, dim3((uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * 8)), dim3(kLookThreads), 0, stream, a);
+}
 template <int DT, int OT>
-cudaError_t launch_lookup(EmbedArgs a, const gd_embedding_forward_args* g, cudaStream_t stream) {
-  const bool four = in_pieces(a.table, a.ld_table, 2, g->width, sizeof(typename Elem<DT>::type), 4) &&
-                    in_pieces(a.y, a.ld_y, g->tokens, g->width, sizeof(typename Elem<OT>::type), 4);
-  a.pieces = (uint32_t)(four ? g->width / 4 : g->width);
-  a.pieces_total = g->tokens * a.pieces;
-  const uint64_t per = kLookThreads * kLookAhead;
-  const uint32_t ctas = (uint32_t)std::min<uint64_t>((a.pieces_total + per - 1) / per, (uint64_t)sm_count() * 8);
-  return four ? launch_dependent(embed_kernel<DT, OT, 4>, dim3(ctas), dim3(kLookThreads), 0, stream, a)
-              : launch_dependent(embed_kernel<DT, OT, 1>, dim3(ctas), dim3(kLookThreads), 0, stream, a);
+cudaError_t launch_lookup(const EmbedArgs& a, const gd_embedding_forward_args* g, cudaStream_t stream) {
+  constexpr size_t in = sizeof(typename Elem<DT>::type), out = sizeof(typename Elem<OT>::type);
+  const uint32_t width = (uint32_t)g->width;
+  const auto takes = [&](uint32_t v) { return in_pieces(a.table, a.ld_table, 2, width, in, v) && in_pieces(a.y, a.ld_y, g->tokens, width, out, v); };
+  if constexpr (in == 2 && out == 2) {
+    if (takes(8)) return launch_pieces<DT, OT, 8>(a, width, stream);
+  }
+  return takes(4) ? launch_pieces<DT, OT, 4>(a, width, stream) : takes(2) ? launch_pieces<DT, OT, 2>(a, width, stream) : launch_pieces<DT, OT, 1>(a, width, stream);
 }
 
 int forward(const gd_embedding_forward_args* g, cudaStream_t stream) {
@@ -518,7 +546,7 @@ int forward(const gd_embedding_forward_args* g, cudaStream_t stream) {
   a.table = g->table, a.ld_table = g->vocab > 1 ? g->ld_table : g->width;
   a.ids = g->ids, a.id_bits = (uint32_t)g->id_bits;
   a.y = g->y, a.ld_y = g->ld_y;
-  a.vocab = g->vocab;
+  a.vocab = g->vocab, a.tokens = (uint32_t)g->tokens;
   a.ignore_index = g->ignore_index;
   a.scale = g->scale;
   ProfileScope ps(stream, PT_EMBED);
@@ -556,25 +584,28 @@ cudaError_t launch_sort(SortArgs& a, const Layout& l, unsigned char* ws, const u
     a.fill_part = 0, a.fill_parts = 1;
     *keys = a.keys_out, *at = a.at_out;
     note_launches(1);
-    return launch_dependent(sort_one_kernel, dim3(1 + fillers(1, 1)), dim3(kOneThreads), sizeof(OneSmem), stream, a);
+    return launch_dependent(sort_one_kernel, dim3(1 + std::min(fillers(1, 1), (uint32_t)std::max(1, sm_count() - 1))), dim3(kOneThreads), sizeof(OneSmem), stream, a);
   }
   const uint32_t whole = (a.n + kSortTile - 1) / kSortTile, per = (whole + kMostTiles - 1) / kMostTiles;
   a.per_tile = per * kSortTile;
   a.tiles = (whole + per - 1) / per;
-  a.hist = reinterpret_cast<uint32_t*>(ws + l.hist);
-  a.fill_parts = 2 * a.passes;
+  uint32_t* hist = reinterpret_cast<uint32_t*>(ws + l.hist);
+  a.hist = hist;
+  a.fill_parts = 1 + a.passes;
   const dim3 grid(a.tiles + fillers(a.fill_parts, kFillCtasPerSm)), block(kTileThreads);
+  cudaError_t e = launch_dependent(sort_count_kernel, grid, block, 0, stream, a);
+  if (e != cudaSuccess) return e;
+  note_launches(1);
   for (uint32_t p = 0; p < a.passes; ++p) {
     a.shift = p * a.bits;
+    a.hist = hist + (uint64_t)p * kMostTiles * kDigits;
+    a.next_hist = p + 1 < a.passes ? hist + (uint64_t)(p + 1) * kMostTiles * kDigits : nullptr;
     if (p) a.keys_in = keys_at((p - 1) & 1u), a.at_in = at_at((p - 1) & 1u);
     a.keys_out = keys_at(p & 1u), a.at_out = at_at(p & 1u);
-    a.fill_part = 2 * p;
-    cudaError_t e = launch_dependent(p ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, stream, a);
-    if (e != cudaSuccess) return e;
-    a.fill_part = 2 * p + 1;
+    a.fill_part = p + 1;
     e = launch_dependent(p ? sort_place_kernel<false> : sort_place_kernel<true>, grid, block, 0, stream, a);
     if (e != cudaSuccess) return e;
-    note_launches(2);
+    note_launches(1);
   }
   *keys = a.keys_out, *at = a.at_out;
   return cudaSuccess;
@@ -582,14 +613,14 @@ cudaError_t launch_sort(SortArgs& a, const Layout& l, unsigned char* ws, const u
 
 template <int DT, int GT, int V>
 cudaError_t launch_sums(const SumArgs& a, cudaStream_t stream) {
-  const uint32_t pieces = (a.width + V - 1) / V, chunks = (a.n + kChunk - 1) / kChunk;
+  const uint32_t pieces = (a.width + V - 1) / V, chunk = chunk_of(a.n), chunks = (a.n + chunk - 1) / chunk;
   const uint32_t threads = std::min(256u, (pieces + 31) / 32 * 32), across = (pieces + threads - 1) / threads;
-  cudaError_t e = launch_dependent(sum_kernel<DT, GT, V>, dim3(chunks, across), dim3(threads), 0, stream, a);
+  cudaError_t e = launch_dependent(chunk == kShortChunk ? sum_kernel<DT, GT, V, kShortChunk> : sum_kernel<DT, GT, V, kChunk>, dim3(chunks, across), dim3(threads), 0, stream, a);
   if (e != cudaSuccess) return e;
   note_launches(1);
-  if (a.n <= 2 * kChunk) return e;                   // (no run can be longer)
+  if (a.n <= 2 * chunk) return e;                    // (no run can be longer)
   const uint32_t blocks = (a.width + 32 * V - 1) / (32 * V);
-  e = launch_dependent(sum_join_kernel<GT, V>, dim3(std::min(chunks, std::max(1u, 4u * (uint32_t)sm_count() / blocks)), blocks), dim3(32 * kJoinWarps), 0, stream, a);
+  e = launch_dependent(sum_join_kernel<GT, V>, dim3(std::min(chunks, std::max(1u, 16u * (uint32_t)sm_count() / blocks)), blocks), dim3(32 * kJoinWarps), 0, stream, a, chunk);
   if (e == cudaSuccess) note_launches(1);
   return e;
 }

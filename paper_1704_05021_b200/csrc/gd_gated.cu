@@ -15,7 +15,7 @@ namespace {
 // cluster of 1 .. 8 CTAs takes `width` columns of dy, each CTA a share of the rows, a thread 8 neighbouring columns of every so many rows; the
 // sums meet by shuffles, in shared memory and, sent and counted, in the cluster's first CTA, always in the same order.
 // Bound by the bytes: three values read and two written for each of dy.
-constexpr uint32_t kSlopeCtas = 8, kSlopeThreads = 512, kSlopeWarps = kSlopeThreads / 32;
+constexpr uint32_t kSlopeCtas = 8, kSlopeThreads = 256, kSlopeWarps = kSlopeThreads / 32;
 struct SlopeArgs {
   const void* dy;
   const void* pre;
@@ -30,31 +30,28 @@ struct SlopeArgs {
 };
 // (a, u, g) -> the two halves of dz, in a's and u's place
 __device__ __forceinline__ void back8(float (&a)[8], float (&u)[8], const float (&g)[8], int act) {
-  float s[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) s[j] = a[j];
-  activate_all<8>(s, act);
+  float v[8];
   if (act == GD_ACT_RELU) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = a[j] > 0.f ? 1.f : 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = a[j] < 0.f ? 0.f : a[j], a[j] = a[j] > 0.f ? 1.f : 0.f;
   } else if (act == GD_ACT_GELU) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = gelu_slope(a[j]);
+    for (int j = 0; j < 8; ++j) a[j] = gelu_both(a[j], &v[j]);
   } else if (act == GD_ACT_SILU) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = silu_slope(a[j]);
+    for (int j = 0; j < 8; ++j) a[j] = silu_both(a[j], &v[j]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = 1.f;
+    for (int j = 0; j < 8; ++j) v[j] = a[j], a[j] = 1.f;
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     a[j] *= g[j] * u[j];
-    u[j] = g[j] * s[j];
+    u[j] = g[j] * v[j];
   }
 }
 template <int DT>
-__global__ void __launch_bounds__(kSlopeThreads, 2) gated_slope_kernel(const __grid_constant__ SlopeArgs a) {
+__global__ void __launch_bounds__(kSlopeThreads, 3) gated_slope_kernel(const __grid_constant__ SlopeArgs a) {
   __shared__ float s_sum[kSlopeWarps][2][64];
   __shared__ __align__(8) float s_all[kSlopeCtas][128];
   __shared__ uint64_t s_in;
@@ -91,24 +88,32 @@ __global__ void __launch_bounds__(kSlopeThreads, 2) gated_slope_kernel(const __g
   float sum[2][8] = {};
   if (c < a.cols) {
     if (a.vectors) {
-      uint4 gq, aq, uq;
-      const auto ask = [&](uint64_t r) {
-        gq = __ldcs(reinterpret_cast<const uint4*>(dy + r * a.ld_dy));
-        aq = __ldcs(reinterpret_cast<const uint4*>(pre + r * a.ld_pre));
-        uq = __ldcs(reinterpret_cast<const uint4*>(pre + r * a.ld_pre + a.cols));
+      constexpr uint32_t kInHand = 2;                  // rows
+      uint4 gq[kInHand], aq[kInHand], uq[kInHand];
+      const auto ask = [&](uint64_t r, uint32_t q) {
+        if (r >= r1) return;
+        gq[q] = __ldcs(reinterpret_cast<const uint4*>(dy + r * a.ld_dy));
+        aq[q] = __ldcs(reinterpret_cast<const uint4*>(pre + r * a.ld_pre));
+        uq[q] = __ldcs(reinterpret_cast<const uint4*>(pre + r * a.ld_pre + a.cols));
       };
-      uint64_t r = r0 + tid / groups;
-      if (r < r1) ask(r);
-      for (; r < r1; r += step) {
-        float g[8], z[8], u[8];
-        widen8_t<DT>(gq, g), widen8_t<DT>(aq, z), widen8_t<DT>(uq, u);
-        if (r + step < r1) ask(r + step);
-        back8(z, u, g, a.activation);
+      const uint64_t from = r0 + tid / groups;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[0][j] += z[j], sum[1][j] += u[j];
-        if (dz) {
-          *reinterpret_cast<uint4*>(dz + r * a.ld_dz) = narrow8_t<DT>(z);
-          *reinterpret_cast<uint4*>(dz + r * a.ld_dz + a.cols) = narrow8_t<DT>(u);
+      for (uint32_t q = 0; q < kInHand; ++q) ask(from + q * step, q);
+      for (uint64_t first = from; first < r1; first += kInHand * step) {
+#pragma unroll
+        for (uint32_t q = 0; q < kInHand; ++q) {
+          const uint64_t r = first + q * step;
+          if (r >= r1) break;
+          float g[8], z[8], u[8];
+          widen8_t<DT>(gq[q], g), widen8_t<DT>(aq[q], z), widen8_t<DT>(uq[q], u);
+          ask(r + kInHand * step, q);
+          back8(z, u, g, a.activation);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[0][j] += z[j], sum[1][j] += u[j];
+          if (dz) {
+            *reinterpret_cast<uint4*>(dz + r * a.ld_dz) = narrow8_t<DT>(z);
+            *reinterpret_cast<uint4*>(dz + r * a.ld_dz + a.cols) = narrow8_t<DT>(u);
+          }
         }
       }
     } else {

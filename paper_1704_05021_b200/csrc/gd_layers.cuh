@@ -62,6 +62,16 @@ inline bool good_matrix(const void* p, uint64_t ld, uint64_t rows, uint64_t widt
   return p && aligned_to(p, item) && (rows <= 1 || ld >= width) && !(ld >> 40);
 }
 
+// Copies of 4, 8 or 16 bytes into shared memory that a thread asks for and waits for by itself.
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }   // all groups but the last LEFT
+
 // The lanes' sum, the same in all of them.
 __device__ __forceinline__ float warp_sum(float s) {
 #pragma unroll

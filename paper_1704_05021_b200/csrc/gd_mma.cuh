@@ -198,6 +198,18 @@ __device__ __forceinline__ float silu_slope(float x) {
   const float s = __fdividef(1.f, 1.f + __expf(-x));
   return s * (1.f + x * (1.f - s));
 }
+// Both at once: the value in *v.
+__device__ __forceinline__ float gelu_both(float x, float* v) {
+  float e;
+  const float phi = normal_cdf(x, &e);
+  *v = x * phi;
+  return fmaf(x * 0.39894228040143268f, e, phi);
+}
+__device__ __forceinline__ float silu_both(float x, float* v) {
+  const float s = __fdividef(1.f, 1.f + __expf(-x));
+  *v = x * s;
+  return s * (1.f + x * (1.f - s));
+}
 __device__ __forceinline__ float activate(float z, int act) {
   switch (act) {
     case GD_ACT_RELU: return z < 0.f ? 0.f : z;      // (a NaN stays one)

@@ -1,9 +1,12 @@
 // Layer norm of rows (gd_layer_norm_forward, gd_layer_norm_backward).
 //
-// Bound by the bytes: a row is read once and waits in registers, kEach elements a thread, until its statistics are known.  A group of
-// G threads holds a row: a warp (four rows a CTA then) or a whole CTA of 64 .. 512 threads; groups take rows in turn and ask for the next
-// one before they work on this one.  The variance is the sum of squares about the mean, a second sum over the registers, not a
-// difference of large numbers.
+// Bound by the bytes.  Forward: a row is read once and waits in registers, as it lies in memory, until its statistics are known: up to
+// 64 elements a thread, so that a warp has rows of up to 2048, or several short ones, by itself; weight and bias lie in shared memory; the next row's
+// pieces are copied into shared memory by the threads that take them meanwhile.  The variance is the sum of squares about the mean, a second
+// sum over the registers, not a difference of large numbers.  (32768 x 4096 in bf16: 98 us = 5.5 TB/s; 300000 x 64 22 us, 65 with a
+// warp to each row; 8000 x 8192 58 us, 74 with 16 elements to a thread: instructions, 19 an element there, and not bytes were the time.)
+//
+// Backward: each thread keeps the sums of its columns, 16 of each gradient, which is why a row is spread over 32 .. 512 threads there.
 #include <algorithm>
 #include <cstring>
 
@@ -12,9 +15,9 @@
 namespace gd {
 namespace {
 
-constexpr int kEach = 16;                     // elements of a row a thread holds
+constexpr int kEach = 16;                      // backward: elements of a row a thread holds
 constexpr uint32_t kMostThreads = 1024;
-constexpr uint32_t kHeldWidth = kEach * 512;               // longer rows are read again for every sum
+constexpr uint32_t kHeldWidth = 8192;                      // longer rows are read again for every sum
 constexpr uint32_t kColumnCtas = 296;         // most CTAs that hold sums of columns
 
 struct NormArgs {
@@ -43,24 +46,34 @@ struct NormBackArgs {
   uint32_t wide_params;
 };
 
+__device__ __forceinline__ uint64_t row_at(uint32_t r, uint64_t ld) { return r * ld; }
 template <int DT>
 __device__ __forceinline__ float param(const void* p, uint32_t i, uint32_t wide) {
   return wide ? static_cast<const float*>(p)[i] : Elem<DT>::get(static_cast<const typename Elem<DT>::type*>(p)[i]);
 }
 
+template <int G>
+constexpr int kGroupThreads = G > 256 ? G : 256;       // of a CTA: one group, or several side by side
+constexpr uint32_t kAhead = 4;                          // rows of a group under way
+
 // Sum over a group's N values each; every thread of it gets the same.  `turn` alternates between calls: one barrier each suffices.
 template <int G, int N>
 __device__ __forceinline__ void group_sum(float (&s)[N], float (*place)[N], uint32_t turn) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) s[i] = warp_sum(s[i]);
+  for (int o = (G < 32 ? G : 32) / 2; o > 0; o >>= 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], o);
+  }
   if constexpr (G > 32) {
     constexpr int W = G / 32;
-    float(*at)[N] = place + (turn & 1u) * W;
+    const uint32_t group = threadIdx.x / G;
+    float(*at)[N] = place + (group * 2u + (turn & 1u)) * W;
     if ((threadIdx.x & 31u) == 0u) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) at[threadIdx.x >> 5][i] = s[i];
+      for (int i = 0; i < N; ++i) at[(threadIdx.x % G) >> 5][i] = s[i];
     }
-    __syncthreads();
+    if constexpr (G > 256) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1u), "n"(G) : "memory");
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float t = 0.f;
@@ -70,81 +83,195 @@ __device__ __forceinline__ void group_sum(float (&s)[N], float (*place)[N], uint
     }
   }
 }
-
 template <int G>
-constexpr int kGroupThreads = G > 32 ? G : 128;
+constexpr int kSumPlaces = G > 32 ? 2 * kGroupThreads<G> / 32 : 1;
 
-// ---------------------------------------------------------------- forward
-template <int DT, int V, int G>
-__global__ void __launch_bounds__(kGroupThreads<G>) norm_kernel(const __grid_constant__ NormArgs a) {
+// A thread's pieces of `INPUTS` matrices' rows, kAhead rows under way in shared memory: it asks for and reads its own, so nobody else waits.
+// (Pieces of two bytes, which cannot be copied so, are held in registers, a row ahead.)
+template <int DT, int V, int G, int INPUTS>
+struct RowsAhead {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
-  constexpr int kPieces = kEach / V, kThreads = kGroupThreads<G>, kGroups = kThreads / G;
-  __shared__ float s_sum[G > 32 ? 2 * G / 32 : 1][1];
+  static constexpr int kPieces = kEach / V, kBytes = V * (int)sizeof(T), kThreads = kGroupThreads<G>;
+  static constexpr bool kCopies = kBytes >= 4;
+  // (backward: as many as let two CTAs of 256 threads, or one of 512, have their place on an SM)
+  static constexpr uint32_t kDepth = !kCopies ? 1 : INPUTS == 1 ? kAhead : sizeof(T) == 4 ? 2 : kThreads == 256 ? 3 : 4;
+  static constexpr uint32_t kSmem = kCopies ? kDepth * INPUTS * kPieces * kThreads * kBytes : 0;
+  const T* from[INPUTS];
+  uint64_t ld[INPUTS];
+  uint32_t tid, rows, width, smem;
+  typename P::Raw held[kCopies ? 1 : INPUTS][kCopies ? 1 : kPieces];
+  __device__ __forceinline__ uint32_t place(uint32_t slot, int input, int j) const {
+    return smem + (((slot * INPUTS + input) * kPieces + j) * kThreads + threadIdx.x) * kBytes;
+  }
+  __device__ __forceinline__ void ask(uint32_t row, uint32_t slot) {
+#pragma unroll
+    for (int input = 0; input < INPUTS; ++input) {
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        const uint32_t c = (tid + j * G) * V;
+        const bool there = row < rows && c < width && from[input];
+        const T* p = from[input] + row * ld[input] + c;
+        if constexpr (kCopies) {
+          if (there) copy_ahead<kBytes>(place(slot, input, j), p);
+        } else {
+          held[input][j] = there ? P::load(p) : P::none();
+        }
+      }
+    }
+    if constexpr (kCopies) copies_commit();
+  }
+  // x[input]: the row's elements (0 where there are none); `slot` may be asked for anew afterwards
+  __device__ __forceinline__ void take(uint32_t slot, int input, float* x) const {
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const uint32_t c = (tid + j * G) * V;
+      if constexpr (kCopies) {
+        typename P::Raw r = P::none();
+        if (c < width && from[input]) r = *reinterpret_cast<const typename P::Raw*>(__cvta_shared_to_generic(place(slot, input, j)));
+        P::widen(r, x + j * V);
+      } else {
+        P::widen(held[input][j], x + j * V);
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------- forward
+// E elements of a row to each of G threads, held as they lie; G > 32: groups of a CTA meet at barriers of their own.
+template <int DT, int V, int E, int G>
+struct RowShape {
+  using T = typename Elem<DT>::type;
+  static constexpr int kPieces = E / V, kBytes = V * (int)sizeof(T), kThreads = 256;
+  static constexpr bool kCopies = kBytes >= 4;         // (pieces of two bytes cannot be copied ahead)
+  static constexpr uint32_t kSmem = kCopies ? kPieces * kBytes * kThreads : 0;      // weight and bias come behind this
+};
+// two neighbours (or one and a zero) of a piece
+template <int DT, int V>
+__device__ __forceinline__ float2 pair_of(const typename Piece<DT, V>::Raw& r, int i) {
+  if constexpr (V == 1) {
+    float x;
+    Piece<DT, V>::widen(r, &x);
+    return make_float2(x, 0.f);
+  } else if constexpr (DT == GD_DTYPE_FP32) {
+    const float* f = reinterpret_cast<const float*>(&r);
+    return make_float2(f[2 * i], f[2 * i + 1]);
+  } else {
+    return unpack2<DT>(reinterpret_cast<const uint32_t*>(&r)[i]);
+  }
+}
+template <int DT, int V, int E, int G>
+__global__ void __launch_bounds__(RowShape<DT, V, E, G>::kThreads, E <= 32 ? 3 : 2) norm_kernel(const __grid_constant__ NormArgs a) {
+  using P = Piece<DT, V>;
+  using T = typename Elem<DT>::type;
+  using S = RowShape<DT, V, E, G>;
+  constexpr int kPieces = S::kPieces, kGroups = S::kThreads / G, kPairs = V == 1 ? 1 : V / 2;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ float s_sum[G > 32 ? 2 * S::kThreads / 32 : 1][1];
+  float *s_w = reinterpret_cast<float*>(smem + S::kSmem), *s_b = s_w + (a.width + 3u & ~3u);
   const uint32_t tid = threadIdx.x % G;
   const T* x = static_cast<const T*>(a.x);
   T* y = static_cast<T*>(a.y);
   pdl_wait();
   pdl_trigger();
-  float w[kEach], b[kEach];
-#pragma unroll
-  for (int j = 0; j < kPieces; ++j) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const uint32_t c = (tid + j * G) * V + i;
-      w[j * V + i] = a.weight && c < a.width ? param<DT>(a.weight, c, a.wide_params) : 1.f;
-      b[j * V + i] = a.bias && c < a.width ? param<DT>(a.bias, c, a.wide_params) : 0.f;
-    }
-  }
-  const uint32_t step = gridDim.x * kGroups;
-  uint32_t r = blockIdx.x * kGroups + threadIdx.x / G, turn = 0;
-  typename P::Raw next[kPieces];
+  // pieces of a row this thread has: the first `mine` of kPieces
+  const uint32_t whole = a.width / V, mine = tid < whole ? (whole - tid + G - 1) / G : 0u;
+  const uint32_t at = smem_u32(smem) + threadIdx.x * S::kBytes;
   const auto ask = [&](uint32_t row) {
+    if constexpr (S::kCopies) {
+      if (row < a.rows) {
+        const T* from = x + row * a.ldx + tid * V;
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const uint32_t c = (tid + j * G) * V;
-      next[j] = row < a.rows && c < a.width ? P::load(x + row * a.ldx + c) : P::none();
+        for (int j = 0; j < kPieces; ++j)
+          if (j < (int)mine) copy_ahead<S::kBytes>(at + j * (S::kThreads * S::kBytes), from + j * G * V);
+      }
+      copies_commit();
     }
   };
+  const uint32_t step = gridDim.x * kGroups;
+  uint32_t r = blockIdx.x * kGroups + threadIdx.x / G, turn = 0;
   ask(r);
+  for (uint32_t c = threadIdx.x; c < a.width; c += S::kThreads) {
+    s_w[c] = a.weight ? param<DT>(a.weight, c, a.wide_params) : 1.f;
+    s_b[c] = a.bias ? param<DT>(a.bias, c, a.wide_params) : 0.f;
+  }
+  __syncthreads();
   const float count = (float)a.width;
-  for (; r < a.rows; r += step) {
-    float v[kEach];
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) P::widen(next[j], v + j * V);
-    ask(r + step);
-    float s[1] = {0.f};
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) s[0] += v[j];
-    group_sum<G>(s, s_sum, turn++);
-    const float mean = s[0] / count;
-    s[0] = 0.f;
+  // (the groups of a warp stay together: those behind the last row go through the motions)
+  for (uint32_t first = blockIdx.x * kGroups + (G < 32 ? threadIdx.x / 32 * (32 / G) : threadIdx.x / G); first < a.rows; first += step, r += step) {
+    const bool live = r < a.rows;
+    typename P::Raw raw[kPieces];
+    if constexpr (S::kCopies) copies_wait<0>();
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
-      const bool in = (tid + j * G) * V < a.width;
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float& e = v[j * V + i];
-        e -= mean;
-        s[0] = in ? fmaf(e, e, s[0]) : s[0];
+      raw[j] = P::none();
+      if (j < (int)mine && live) {
+        if constexpr (S::kCopies) raw[j] = *reinterpret_cast<const typename P::Raw*>(smem + threadIdx.x * S::kBytes + j * (S::kThreads * S::kBytes));
+        else raw[j] = P::load(x + row_at(r, a.ldx) + (tid + j * G) * V);
       }
     }
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) sum = add2(sum, pair_of<DT, V>(raw[j], i));
+    }
+    float s[1] = {sum.x + sum.y};
+    group_sum<G>(s, s_sum, turn++);
+    ask(r + step);                                     // (the sum has this row's values: they have been read)
+    const float mean = s[0] / count;                   // (a product with 1 / count would not give a constant row's value back)
+    const float2 less = both(-mean);
+    sum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      if (j < (int)mine) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          float2 d = add2(pair_of<DT, V>(raw[j], i), less);
+          if constexpr (V == 1) d.y = 0.f;
+          sum = fma2(d, d, sum);
+        }
+      }
+    }
+    s[0] = sum.x + sum.y;
     group_sum<G>(s, s_sum, turn++);
     const float rstd = __frsqrt_rn(s[0] / count + a.eps);
+    if (!live) continue;
     if (tid == 0) {
       if (a.mean) a.mean[r] = mean;
       if (a.rstd) a.rstd[r] = rstd;
     }
+    T* to = y + row_at(r, a.ldy) + tid * V;
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
-      const uint32_t c = (tid + j * G) * V;
-      if (c < a.width) {
+      if (j < (int)mine) {
+        const uint32_t c = (tid + j * G) * V;
+        float w[V], b[V], o[V];
+        if constexpr (V >= 4) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j * V + i] = fmaf(v[j * V + i] * rstd, w[j * V + i], b[j * V + i]);
-        P::store(y + r * a.ldy + c, P::narrow(v + j * V));
+          for (int i = 0; i < V; i += 4) {
+            const float4 p = *reinterpret_cast<const float4*>(s_w + c + i), q = *reinterpret_cast<const float4*>(s_b + c + i);
+            w[i] = p.x, w[i + 1] = p.y, w[i + 2] = p.z, w[i + 3] = p.w, b[i] = q.x, b[i + 1] = q.y, b[i + 2] = q.z, b[i + 3] = q.w;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; ++i) w[i] = s_w[c + i], b[i] = s_b[c + i];
+        }
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          const float2 d = mul2(add2(pair_of<DT, V>(raw[j], i), less), both(rstd));
+          if constexpr (V == 1) {
+            o[0] = fmaf(d.x, w[0], b[0]);
+          } else {
+            const float2 e = fma2(d, make_float2(w[2 * i], w[2 * i + 1]), make_float2(b[2 * i], b[2 * i + 1]));
+            o[2 * i] = e.x, o[2 * i + 1] = e.y;
+          }
+        }
+        P::store(to + j * G * V, P::narrow(o));
       }
     }
   }
+  if constexpr (S::kCopies) copies_wait<0>();
 }
 
 // Rows longer than the registers of a CTA: read once per sum and once for the result, from L2 after the first time.
@@ -161,7 +288,7 @@ __global__ void __launch_bounds__(kMostThreads) norm_long_kernel(const __grid_co
     float s[1] = {0.f};
 #pragma unroll 4
     for (uint32_t c = threadIdx.x; c < a.width; c += kMostThreads) s[0] += Elem<DT>::get(x[c]);
-    group_sum<kMostThreads>(s, s_sum, turn++);
+    group_sum<(int)kMostThreads>(s, s_sum, turn++);
     const float mean = s[0] / (float)a.width;
     s[0] = 0.f;
 #pragma unroll 4
@@ -169,7 +296,7 @@ __global__ void __launch_bounds__(kMostThreads) norm_long_kernel(const __grid_co
       const float e = Elem<DT>::get(x[c]) - mean;
       s[0] = fmaf(e, e, s[0]);
     }
-    group_sum<kMostThreads>(s, s_sum, turn++);
+    group_sum<(int)kMostThreads>(s, s_sum, turn++);
     const float rstd = __frsqrt_rn(s[0] / (float)a.width + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[r] = mean;
@@ -187,17 +314,28 @@ __global__ void __launch_bounds__(kMostThreads) norm_long_kernel(const __grid_co
 // A group's rows give dx; each thread keeps the sums of its columns, which meet in shared memory (groups of a warp) and go to the
 // workspace, a row of sums per CTA, to be joined in order by the next launch.
 template <int DT, int V, int G>
-__global__ void __launch_bounds__(kGroupThreads<G>) norm_back_kernel(const __grid_constant__ NormBackArgs a) {
+__global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 : 1) norm_back_kernel(const __grid_constant__ NormBackArgs a) {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
-  constexpr int kPieces = kEach / V, kThreads = kGroupThreads<G>, kGroups = kThreads / G;
-  __shared__ float s_sum[G > 32 ? 2 * G / 32 : 1][2];
+  using Rows = RowsAhead<DT, V, G, 3>;
+  constexpr int kPieces = kEach / V, kGroups = kGroupThreads<G> / G;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ float s_sum[kSumPlaces<G>][2];
   __shared__ float s_part[kGroups > 1 ? kGroups - 1 : 1][kGroups > 1 ? G * kEach : 1];
   const uint32_t tid = threadIdx.x % G;
-  const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *add = static_cast<const T*>(a.add);
   T* dx = static_cast<T*>(a.dx);
   pdl_wait();
   pdl_trigger();
+  Rows in;
+  in.from[0] = static_cast<const T*>(a.x), in.ld[0] = a.ldx;
+  in.from[1] = static_cast<const T*>(a.dy), in.ld[1] = a.ld_dy;
+  in.from[2] = static_cast<const T*>(a.add), in.ld[2] = a.ld_add;
+  in.tid = tid, in.rows = a.rows, in.width = a.width, in.smem = smem_u32(smem);
+  const uint32_t step = gridDim.x * kGroups;
+  uint32_t r = blockIdx.x * kGroups + threadIdx.x / G, turn = 0, slot = 0;
+#pragma unroll
+  for (uint32_t n = 0; n < Rows::kDepth; ++n) in.ask(r + n * step, n);
+  float next_mean = r < a.rows ? a.mean[r] : 0.f, next_rstd = r < a.rows ? a.rstd[r] : 0.f;
   float w[kEach], dw[kEach], db[kEach];
 #pragma unroll
   for (int j = 0; j < kPieces; ++j) {
@@ -208,43 +346,26 @@ __global__ void __launch_bounds__(kGroupThreads<G>) norm_back_kernel(const __gri
       dw[j * V + i] = db[j * V + i] = 0.f;
     }
   }
-  const uint32_t step = gridDim.x * kGroups;
-  uint32_t r = blockIdx.x * kGroups + threadIdx.x / G, turn = 0;
-  typename P::Raw next_x[kPieces], next_g[kPieces];
-  float next_mean = 0.f, next_rstd = 0.f;
-  const auto ask = [&](uint32_t row) {
-    const bool in = row < a.rows;
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const uint32_t c = (tid + j * G) * V;
-      next_x[j] = in && c < a.width ? P::load(x + row * a.ldx + c) : P::none();
-      next_g[j] = in && c < a.width ? P::load(dy + row * a.ld_dy + c) : P::none();
-    }
-    next_mean = in ? a.mean[row] : 0.f;
-    next_rstd = in ? a.rstd[row] : 0.f;
-  };
-  ask(r);
   const float share = 1.f / (float)a.width;
   for (; r < a.rows; r += step) {
-    float n[kEach], g[kEach];
-    typename P::Raw more[kPieces];
+    float n[kEach], g[kEach], more[kEach];
     const float mean = next_mean, rstd = next_rstd;
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const uint32_t c = (tid + j * G) * V;
-      P::widen(next_x[j], n + j * V);
-      P::widen(next_g[j], g + j * V);
-      if (add && a.dx && c < a.width) more[j] = P::load(add + r * a.ld_add + c);
+    if constexpr (Rows::kCopies) copies_wait<Rows::kDepth - 1>();
+    in.take(slot, 0, n);
+    in.take(slot, 1, g);
+    if constexpr (!Rows::kCopies) {
+      in.take(slot, 2, more);
+      in.ask(r + step, slot);
     }
-    ask(r + step);
+    if (r + step < a.rows) next_mean = a.mean[r + step], next_rstd = a.rstd[r + step];
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
-      const bool in = (tid + j * G) * V < a.width;
+      const bool there = (tid + j * G) * V < a.width;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int e = j * V + i;
-        n[e] = in ? (n[e] - mean) * rstd : 0.f;
+        n[e] = there ? (n[e] - mean) * rstd : 0.f;
         dw[e] = fmaf(g[e], n[e], dw[e]);
         db[e] += g[e];
         g[e] *= w[e];
@@ -252,24 +373,27 @@ __global__ void __launch_bounds__(kGroupThreads<G>) norm_back_kernel(const __gri
         s[1] = fmaf(g[e], n[e], s[1]);
       }
     }
-    if (!a.dx) continue;
-    group_sum<G>(s, s_sum, turn++);
-    const float m0 = s[0] * share, m1 = s[1] * share;
+    if (a.dx) {
+      group_sum<G>(s, s_sum, turn++);
+      const float m0 = s[0] * share, m1 = s[1] * share;
+      if constexpr (Rows::kCopies) in.take(slot, 2, more);
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const uint32_t c = (tid + j * G) * V;
-      if (c < a.width) {
-        float o[V], q[V];
-        if (add) P::widen(more[j], q);
+      for (int j = 0; j < kPieces; ++j) {
+        const uint32_t c = (tid + j * G) * V;
+        if (c < a.width) {
+          float o[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          o[i] = (g[j * V + i] - m0 - n[j * V + i] * m1) * rstd;
-          if (add) o[i] += q[i];
+          for (int i = 0; i < V; ++i) o[i] = fmaf(g[j * V + i] - m0 - n[j * V + i] * m1, rstd, more[j * V + i]);
+          P::store(dx + r * a.ld_dx + c, P::narrow(o));
         }
-        P::store(dx + r * a.ld_dx + c, P::narrow(o));
       }
     }
+    if constexpr (Rows::kCopies) {
+      in.ask(r + Rows::kDepth * step, slot);
+      if (++slot == Rows::kDepth) slot = 0;
+    }
   }
+  if constexpr (Rows::kCopies) copies_wait<0>();
   if (!a.part) return;
   if constexpr (kGroups > 1) {
     const uint32_t group = threadIdx.x / G;
@@ -322,7 +446,7 @@ __global__ void __launch_bounds__(kMostThreads) norm_back_long_kernel(const __gr
       s[0] += g;
       s[1] = fmaf(g, (Elem<DT>::get(x[c]) - mean) * rstd, s[1]);
     }
-    group_sum<kMostThreads>(s, s_sum, turn++);
+    group_sum<(int)kMostThreads>(s, s_sum, turn++);
     const float m0 = s[0] / (float)a.width, m1 = s[1] / (float)a.width;
     for (uint32_t c = threadIdx.x; c < a.width; c += kMostThreads) {
       const float g = Elem<DT>::get(dy[c]) * (a.weight ? param<DT>(a.weight, c, a.wide_params) : 1.f);
@@ -377,40 +501,65 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const float*
 }
 
 // ---------------------------------------------------------------- host side
-// CTAs that fill the GPU, for a kernel of `threads` threads that takes `groups` rows at a time.
-uint32_t row_ctas(uint32_t rows, uint32_t groups, uint32_t threads, uint32_t most) {
-  const uint32_t want = (rows + groups - 1) / groups;
-  return std::min(want, std::min(most, (uint32_t)sm_count() * std::max(1u, 1024u / threads)));
+// A launch of as many CTAs as the GPU holds at a time, or as there are rows for; *ctas: how many (at most `most`).
+template <typename Args>
+cudaError_t launch_rows(void (*kernel)(Args), PerDeviceInt& held, const Args& a, uint32_t groups, uint32_t threads, uint32_t smem, uint32_t most_smem, uint32_t most,
+                        uint32_t* ctas, cudaStream_t stream) {
+  int dev, per_sm = held.get(&dev);
+  if (!per_sm) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most_smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, (int)threads, most_smem);
+    if (e != cudaSuccess) return e;
+    per_sm = std::max(per_sm, 1);
+    held.set(dev, per_sm);
+  }
+  *ctas = std::min((a.rows + groups - 1) / groups, std::min(most, (uint32_t)(sm_count() * per_sm)));
+  return launch_dependent(kernel, dim3(*ctas), dim3(threads), smem, stream, a);
 }
-template <int DT, int V, int G>
+template <int DT, int V, int E, int G>
 cudaError_t launch_forward(const NormArgs& a, cudaStream_t stream) {
-  constexpr uint32_t threads = kGroupThreads<G>;
-  return launch_dependent(norm_kernel<DT, V, G>, dim3(row_ctas(a.rows, threads / G, threads, 0x7FFFFFFFu)), dim3(threads), 0, stream, a);
+  using S = RowShape<DT, V, E, G>;
+  constexpr uint32_t kMost = S::kSmem + 2 * E * G * 4;         // with the parameters of the widest row
+  const uint32_t smem = S::kSmem + 2 * (a.width + 3u & ~3u) * 4;
+  static PerDeviceInt held;                                     // (how many CTAs of that size an SM has room for)
+  uint32_t ctas;
+  return launch_rows<NormArgs>(norm_kernel<DT, V, E, G>, held, a, S::kThreads / G, S::kThreads, smem, kMost, 0x7FFFFFFFu, &ctas, stream);
 }
 template <int DT, int V, int G>
 cudaError_t launch_backward(const NormBackArgs& a, uint32_t* ctas, cudaStream_t stream) {
   constexpr uint32_t threads = kGroupThreads<G>;
-  *ctas = row_ctas(a.rows, threads / G, threads, kColumnCtas);
-  return launch_dependent(norm_back_kernel<DT, V, G>, dim3(*ctas), dim3(threads), 0, stream, a);
+  static PerDeviceInt held;
+  return launch_rows<NormBackArgs>(norm_back_kernel<DT, V, G>, held, a, threads / G, threads, RowsAhead<DT, V, G, 3>::kSmem, RowsAhead<DT, V, G, 3>::kSmem, kColumnCtas, ctas, stream);
 }
-// threads per row: kEach elements each
-#define GD_BY_WIDTH(CALL, ...)                                                         \
-  (width <= 32 * kEach     ? CALL<DT, V, 32>(__VA_ARGS__)                              \
-   : width <= 64 * kEach   ? CALL<DT, V, 64>(__VA_ARGS__)                              \
-   : width <= 128 * kEach  ? CALL<DT, V, 128>(__VA_ARGS__)                             \
-   : width <= 256 * kEach  ? CALL<DT, V, 256>(__VA_ARGS__)                             \
-                           : CALL<DT, V, 512>(__VA_ARGS__))
+// Up to 64 elements to a thread, so that what a row costs beside its elements is shared by many, and eight threads at least, so that they read whole
+// lines.  Single elements of 16 bits take a register each: half as many (20000 x 1001: 26 against 35 us).
 template <int DT, int V>
 cudaError_t forward_v(const NormArgs& a, cudaStream_t stream) {
   const uint32_t width = a.width;
-  return GD_BY_WIDTH(launch_forward, a, stream);
+  if (width <= 8 * 8) return launch_forward<DT, V, 8, 8>(a, stream);
+  if (width <= 8 * 32) return launch_forward<DT, V, 32, 8>(a, stream);
+  if constexpr (V == 1) {
+    if (width <= 32 * 32) return launch_forward<DT, V, 32, 32>(a, stream);
+    if (width <= 64 * 32) return launch_forward<DT, V, 32, 64>(a, stream);
+    return launch_forward<DT, V, 32, 256>(a, stream);
+  } else {
+    if (width <= 8 * 64) return launch_forward<DT, V, 64, 8>(a, stream);
+    if (width <= 16 * 64) return launch_forward<DT, V, 64, 16>(a, stream);
+    if (width <= 32 * 64) return launch_forward<DT, V, 64, 32>(a, stream);
+    if (width <= 64 * 64) return launch_forward<DT, V, 64, 64>(a, stream);
+    return launch_forward<DT, V, 64, 128>(a, stream);
+  }
 }
+// backward: threads per row, kEach elements each
 template <int DT, int V>
 cudaError_t backward_v(const NormBackArgs& a, uint32_t* ctas, cudaStream_t stream) {
   const uint32_t width = a.width;
-  return GD_BY_WIDTH(launch_backward, a, ctas, stream);
+  if (width <= 32 * kEach) return launch_backward<DT, V, 32>(a, ctas, stream);
+  if (width <= 64 * kEach) return launch_backward<DT, V, 64>(a, ctas, stream);
+  if (width <= 128 * kEach) return launch_backward<DT, V, 128>(a, ctas, stream);
+  if (width <= 256 * kEach) return launch_backward<DT, V, 256>(a, ctas, stream);
+  return launch_backward<DT, V, 512>(a, ctas, stream);
 }
-#undef GD_BY_WIDTH
 
 template <int DT>
 cudaError_t forward_t(const NormArgs& a, cudaStream_t stream) {
