@@ -6,7 +6,7 @@
 // sum over the registers, not a difference of large numbers.  (32768 x 4096 in bf16: 98 us = 5.5 TB/s; 300000 x 64 22 us, 65 with a
 // warp to each row; 8000 x 8192 58 us, 74 with 16 elements to a thread: instructions, 19 an element there, and not bytes were the time.)
 //
-// Backward: each thread keeps the sums of its columns, 16 of each gradient, which is why a row is spread over 32 .. 512 threads there.
+// Backward: each thread keeps the sums of its columns, 16 of each gradient, which is why a row is spread over 4 .. 512 threads there.
 #include <algorithm>
 #include <cstring>
 
@@ -54,7 +54,6 @@ __device__ __forceinline__ float param(const void* p, uint32_t i, uint32_t wide)
 
 template <int G>
 constexpr int kGroupThreads = G > 256 ? G : 256;       // of a CTA: one group, or several side by side
-constexpr uint32_t kAhead = 4;                          // rows of a group under way
 
 // Sum over a group's N values each; every thread of it gets the same.  `turn` alternates between calls: one barrier each suffices.
 template <int G, int N>
@@ -86,53 +85,99 @@ __device__ __forceinline__ void group_sum(float (&s)[N], float (*place)[N], uint
 template <int G>
 constexpr int kSumPlaces = G > 32 ? 2 * kGroupThreads<G> / 32 : 1;
 
-// A thread's pieces of `INPUTS` matrices' rows, kAhead rows under way in shared memory: it asks for and reads its own, so nobody else waits.
-// (Pieces of two bytes, which cannot be copied so, are held in registers, a row ahead.)
+template <int G>
+__device__ __forceinline__ void group_barrier() {
+  if constexpr (G <= 32) __syncwarp();
+  else if constexpr (G > 256) __syncthreads();
+  else asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.x / G + 1u), "n"(G) : "memory");
+}
+
+// The rows of `INPUTS` matrices, a few under way in shared memory.  A thread asks for and reads its own pieces, so nobody else waits.  Rows that
+// start at odd multiples of two bytes (V = 1, 16 bits) are copied as the words that lie whole within them, each thread some, in places that keep
+// their alignment; the elements that are left at the ends come through registers, a row ahead, and the group meets before it reads.
 template <int DT, int V, int G, int INPUTS>
 struct RowsAhead {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
   static constexpr int kPieces = kEach / V, kBytes = V * (int)sizeof(T), kThreads = kGroupThreads<G>;
-  static constexpr bool kCopies = kBytes >= 4;
-  // (backward: as many as let two CTAs of 256 threads, or one of 512, have their place on an SM)
-  static constexpr uint32_t kDepth = !kCopies ? 1 : INPUTS == 1 ? kAhead : sizeof(T) == 4 ? 2 : kThreads == 256 ? 3 : 4;
-  static constexpr uint32_t kSmem = kCopies ? kDepth * INPUTS * kPieces * kThreads * kBytes : 0;
+  static constexpr bool kWords = kBytes == 2;
+  // as many as let two CTAs of 256 threads, or one of 512, have their place on an SM
+  static constexpr uint32_t kDepth = sizeof(T) == 4 ? 2 : kThreads == 256 ? 3 : 4, kRowBytes = G * kEach * 2 + 16;
+  static constexpr uint32_t kSmem = kDepth * INPUTS * (kWords ? kThreads / G * kRowBytes : kPieces * kThreads * kBytes);
   const T* from[INPUTS];
   uint64_t ld[INPUTS];
-  uint32_t tid, rows, width, smem;
-  typename P::Raw held[kCopies ? 1 : INPUTS][kCopies ? 1 : kPieces];
-  __device__ __forceinline__ uint32_t place(uint32_t slot, int input, int j) const {
-    return smem + (((slot * INPUTS + input) * kPieces + j) * kThreads + threadIdx.x) * kBytes;
+  uint32_t tid, rows, width;
+  unsigned char* smem;
+  T edge[INPUTS];
+  __device__ __forceinline__ unsigned char* place(uint32_t slot, int input, int j) const {
+    if constexpr (kWords) return smem + ((slot * INPUTS + input) * (kThreads / G) + threadIdx.x / G) * kRowBytes;
+    else return smem + (((slot * INPUTS + input) * kPieces + j) * kThreads + threadIdx.x) * kBytes;
   }
+  // 1 where a row starts between two words
+  __device__ __forceinline__ uint32_t odd(int input, uint32_t row) const { return ((uint32_t)((uintptr_t)from[input] >> 1) ^ (row & (uint32_t)ld[input])) & 1u; }
   __device__ __forceinline__ void ask(uint32_t row, uint32_t slot) {
 #pragma unroll
     for (int input = 0; input < INPUTS; ++input) {
+      if (row >= rows || !from[input]) continue;
+      const T* p = from[input] + row * ld[input];
+      if constexpr (kWords) {
+        const uint32_t o = odd(input, row), words = (width - o) / 2;
+        const uint32_t to = smem_u32(place(slot, input, 0)) + 4u * o;
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) {
-        const uint32_t c = (tid + j * G) * V;
-        const bool there = row < rows && c < width && from[input];
-        const T* p = from[input] + row * ld[input] + c;
-        if constexpr (kCopies) {
-          if (there) copy_ahead<kBytes>(place(slot, input, j), p);
-        } else {
-          held[input][j] = there ? P::load(p) : P::none();
+        for (int j = 0; j < kEach / 2; ++j) {
+          const uint32_t k = tid + j * G;
+          if (k < words) copy_ahead<4>(to + 4u * k, p + o + 2 * k);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+          const uint32_t c = (tid + j * G) * V;
+          if (c < width) copy_ahead<kBytes>(smem_u32(place(slot, input, j)), p + c);
         }
       }
     }
-    if constexpr (kCopies) copies_commit();
+    copies_commit();
   }
-  // x[input]: the row's elements (0 where there are none); `slot` may be asked for anew afterwards
-  __device__ __forceinline__ void take(uint32_t slot, int input, float* x) const {
+  // the ends of the row that is taken next: the first element by thread 0, the last by thread 1
+  __device__ __forceinline__ void ask_edges(uint32_t row) {
+    if constexpr (kWords) {
+#pragma unroll
+      for (int input = 0; input < INPUTS; ++input) {
+        if (row >= rows || !from[input]) continue;
+        const T* p = from[input] + row * ld[input];
+        const uint32_t o = odd(input, row);
+        if (tid == 0 && o) edge[input] = p[0];
+        if (tid == 1 && ((width - o) & 1u)) edge[input] = p[width - 1];
+      }
+    }
+  }
+  // the row in `slot` may be taken afterwards
+  __device__ __forceinline__ void settle(uint32_t row, uint32_t slot) {
+    copies_wait<(int)kDepth - 1>();
+    if constexpr (kWords) {
+#pragma unroll
+      for (int input = 0; input < INPUTS; ++input) {
+        if (row >= rows || !from[input]) continue;
+        const uint32_t o = odd(input, row);
+        T* to = reinterpret_cast<T*>(place(slot, input, 0)) + o;
+        if (tid == 0 && o) to[0] = edge[input];
+        if (tid == 1 && ((width - o) & 1u)) to[width - 1] = edge[input];
+      }
+      group_barrier<G>();
+    }
+  }
+  // x: the row's elements (0 where there are none)
+  __device__ __forceinline__ void take(uint32_t row, uint32_t slot, int input, float* x) const {
+    const bool there = row < rows && from[input];
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
       const uint32_t c = (tid + j * G) * V;
-      if constexpr (kCopies) {
-        typename P::Raw r = P::none();
-        if (c < width && from[input]) r = *reinterpret_cast<const typename P::Raw*>(__cvta_shared_to_generic(place(slot, input, j)));
-        P::widen(r, x + j * V);
-      } else {
-        P::widen(held[input][j], x + j * V);
+      typename P::Raw r = P::none();
+      if (there && c < width) {
+        if constexpr (kWords) r = reinterpret_cast<const typename P::Raw*>(place(slot, input, 0))[odd(input, row) + c];
+        else r = *reinterpret_cast<const typename P::Raw*>(place(slot, input, j));
       }
+      P::widen(r, x + j * V);
     }
   }
 };
@@ -311,7 +356,7 @@ __global__ void __launch_bounds__(kMostThreads) norm_long_kernel(const __grid_co
 }
 
 // ---------------------------------------------------------------- backward
-// A group's rows give dx; each thread keeps the sums of its columns, which meet in shared memory (groups of a warp) and go to the
+// A group's rows give dx; each thread keeps the sums of its columns, which meet in shared memory where a CTA has several groups and go to the
 // workspace, a row of sums per CTA, to be joined in order by the next launch.
 template <int DT, int V, int G>
 __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 : 1) norm_back_kernel(const __grid_constant__ NormBackArgs a) {
@@ -321,7 +366,7 @@ __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 
   constexpr int kPieces = kEach / V, kGroups = kGroupThreads<G> / G;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ float s_sum[kSumPlaces<G>][2];
-  __shared__ float s_part[kGroups > 1 ? kGroups - 1 : 1][kGroups > 1 ? G * kEach : 1];
+  __shared__ float s_part[kGroups][kGroups > 1 ? G * kEach : 1];
   const uint32_t tid = threadIdx.x % G;
   T* dx = static_cast<T*>(a.dx);
   pdl_wait();
@@ -330,11 +375,12 @@ __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 
   in.from[0] = static_cast<const T*>(a.x), in.ld[0] = a.ldx;
   in.from[1] = static_cast<const T*>(a.dy), in.ld[1] = a.ld_dy;
   in.from[2] = static_cast<const T*>(a.add), in.ld[2] = a.ld_add;
-  in.tid = tid, in.rows = a.rows, in.width = a.width, in.smem = smem_u32(smem);
+  in.tid = tid, in.rows = a.rows, in.width = a.width, in.smem = smem;
   const uint32_t step = gridDim.x * kGroups;
   uint32_t r = blockIdx.x * kGroups + threadIdx.x / G, turn = 0, slot = 0;
 #pragma unroll
   for (uint32_t n = 0; n < Rows::kDepth; ++n) in.ask(r + n * step, n);
+  in.ask_edges(r);
   float next_mean = r < a.rows ? a.mean[r] : 0.f, next_rstd = r < a.rows ? a.rstd[r] : 0.f;
   float w[kEach], dw[kEach], db[kEach];
 #pragma unroll
@@ -347,16 +393,15 @@ __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 
     }
   }
   const float share = 1.f / (float)a.width;
-  for (; r < a.rows; r += step) {
+  // (the groups of a warp stay together: those behind the last row go through the motions)
+  for (uint32_t first = blockIdx.x * kGroups + (G < 32 ? threadIdx.x / 32 * (32 / G) : threadIdx.x / G); first < a.rows; first += step, r += step) {
     float n[kEach], g[kEach], more[kEach];
     const float mean = next_mean, rstd = next_rstd;
-    if constexpr (Rows::kCopies) copies_wait<Rows::kDepth - 1>();
-    in.take(slot, 0, n);
-    in.take(slot, 1, g);
-    if constexpr (!Rows::kCopies) {
-      in.take(slot, 2, more);
-      in.ask(r + step, slot);
-    }
+    in.settle(r, slot);
+    in.take(r, slot, 0, n);
+    in.take(r, slot, 1, g);
+    if constexpr (Rows::kWords) in.take(r, slot, 2, more);         // (others copy into its place: read before the group meets)
+    in.ask_edges(r + step);
     if (r + step < a.rows) next_mean = a.mean[r + step], next_rstd = a.rstd[r + step];
     float s[2] = {0.f, 0.f};
 #pragma unroll
@@ -376,11 +421,11 @@ __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 
     if (a.dx) {
       group_sum<G>(s, s_sum, turn++);
       const float m0 = s[0] * share, m1 = s[1] * share;
-      if constexpr (Rows::kCopies) in.take(slot, 2, more);
+      if constexpr (!Rows::kWords) in.take(r, slot, 2, more);
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) {
         const uint32_t c = (tid + j * G) * V;
-        if (c < a.width) {
+        if (c < a.width && r < a.rows) {
           float o[V];
 #pragma unroll
           for (int i = 0; i < V; ++i) o[i] = fmaf(g[j * V + i] - m0 - n[j * V + i] * m1, rstd, more[j * V + i]);
@@ -388,40 +433,40 @@ __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 
         }
       }
     }
-    if constexpr (Rows::kCopies) {
-      in.ask(r + Rows::kDepth * step, slot);
-      if (++slot == Rows::kDepth) slot = 0;
-    }
+    if (Rows::kWords && (G <= 32 || !a.dx)) group_barrier<G>();    // (all have read; else the sum's barrier says so)
+    in.ask(r + Rows::kDepth * step, slot);
+    if (++slot == Rows::kDepth) slot = 0;
   }
-  if constexpr (Rows::kCopies) copies_wait<0>();
+  copies_wait<0>();
   if (!a.part) return;
+  float* part = a.part + (uint64_t)blockIdx.x * 2 * a.width;
   if constexpr (kGroups > 1) {
-    const uint32_t group = threadIdx.x / G;
+    // the groups' sums, in order
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
-      float* t = pass ? db : dw;
+      const float* t = pass ? db : dw;
       __syncthreads();
-      if (group) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) s_part[group - 1][e * G + tid] = t[e];
+      for (int j = 0; j < kPieces; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s_part[threadIdx.x / G][(tid + j * G) * V + i] = t[j * V + i];
       }
       __syncthreads();
-      if (!group) {
-        for (int q = 0; q < kGroups - 1; ++q) {
-#pragma unroll
-          for (int e = 0; e < kEach; ++e) t[e] += s_part[q][e * G + tid];
-        }
+      for (uint32_t c = threadIdx.x; c < a.width; c += kGroupThreads<G>) {
+        float q = 0.f;
+#pragma unroll 8
+        for (int group = 0; group < kGroups; ++group) q += s_part[group][c];
+        part[pass * a.width + c] = q;
       }
     }
-    if (group) return;
-  }
-  float* part = a.part + (uint64_t)blockIdx.x * 2 * a.width;
+  } else {
 #pragma unroll
-  for (int j = 0; j < kPieces; ++j) {
+    for (int j = 0; j < kPieces; ++j) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const uint32_t c = (tid + j * G) * V + i;
-      if (c < a.width) part[c] = dw[j * V + i], part[a.width + c] = db[j * V + i];
+      for (int i = 0; i < V; ++i) {
+        const uint32_t c = (tid + j * G) * V + i;
+        if (c < a.width) part[c] = dw[j * V + i], part[a.width + c] = db[j * V + i];
+      }
     }
   }
 }
@@ -554,6 +599,8 @@ cudaError_t forward_v(const NormArgs& a, cudaStream_t stream) {
 template <int DT, int V>
 cudaError_t backward_v(const NormBackArgs& a, uint32_t* ctas, cudaStream_t stream) {
   const uint32_t width = a.width;
+  if (width <= 4 * kEach) return launch_backward<DT, V, 4>(a, ctas, stream);
+  if (width <= 16 * kEach) return launch_backward<DT, V, 16>(a, ctas, stream);
   if (width <= 32 * kEach) return launch_backward<DT, V, 32>(a, ctas, stream);
   if (width <= 64 * kEach) return launch_backward<DT, V, 64>(a, ctas, stream);
   if (width <= 128 * kEach) return launch_backward<DT, V, 128>(a, ctas, stream);
