@@ -216,13 +216,14 @@ class LayerNormSession:
             raise ValueError(f"at most {self.max_rows} rows of a matrix, got {list(t.shape)}")
         return rows
 
-    def _params(self, *params):
-        """The type code of the parameters given, and their addresses."""
-        given = [p for p in params if p is not None]
-        dtype = given[0].dtype if given else torch.float32
-        if dtype not in (torch.float32, self.dtype):
-            raise ValueError(f"weight and bias are float32 or {self.dtype}, got {dtype}")
-        return _DTYPES[dtype], [_opt_vector(p, "weight or bias", self.width, (dtype,), self._index) for p in params]
+    def _param(self, p: Optional[torch.Tensor], name: str, other: Optional[torch.Tensor]) -> int:
+        """The address of a parameter, float32 or of the rows' type and of the other one's."""
+        if p is None:
+            return 0
+        if p.dtype is not torch.float32 and p.dtype is not self.dtype or other is not None and other.dtype is not p.dtype:
+            raise ValueError(f"weight and bias are both float32 or both {self.dtype}, got {p.dtype}" + ("" if other is None else f" and {other.dtype}"))
+        _vector(p, name, self.width, (p.dtype,), self._index)
+        return p.data_ptr()
 
     def forward(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                 mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -231,8 +232,9 @@ class LayerNormSession:
         ldx = _matrix(x, "x", rows, width, dt, index)
         if out is None:
             out = _new(rows, width, dt, stream, index)
-        code, (weight_at, bias_at) = self._params(weight, bias)
-        args = _NORM.pack(rows, width, self._code, code, self.eps, 0, x.data_ptr(), ldx, weight_at, bias_at, out.data_ptr(),
+        given = bias if weight is None else weight
+        args = _NORM.pack(rows, width, self._code, 0 if given is None else _DTYPES.get(given.dtype, -1), self.eps, 0, x.data_ptr(), ldx,
+                          self._param(weight, "weight", bias), self._param(bias, "bias", weight), out.data_ptr(),
                           _matrix(out, "out", rows, width, dt, index), _opt_vector(mean, "mean", rows, _F32, index), _opt_vector(rstd, "rstd", rows, _F32, index))
         _call(self._lib.gd_layer_norm_forward, "gd_layer_norm_forward", args, stream, index)
         return out
@@ -243,12 +245,11 @@ class LayerNormSession:
         """The gradients whose buffers are given.  add is the gradient that reaches x past the norm and is added to dx; dx may be dy or add itself.
         dweight and dbias are float32; accumulate adds to what they hold."""
         rows, width, dt, index = self._rows(dy), self.width, self.dtype, self._index
-        code, (weight_at,) = self._params(weight)
         sums = [_opt_vector(t, name, width, _F32, index) for t, name in ((dweight, "dweight"), (dbias, "dbias"))]
         _vector(mean, "mean", rows, _F32, index)
         _vector(rstd, "rstd", rows, _F32, index)
-        args = _NORM_BACK.pack(rows, width, self._code, code, GD_LAYER_NORM_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
-                               _matrix(dy, "dy", rows, width, dt, index), x.data_ptr(), _matrix(x, "x", rows, width, dt, index), weight_at, mean.data_ptr(),
+        args = _NORM_BACK.pack(rows, width, self._code, 0 if weight is None else _DTYPES.get(weight.dtype, -1), GD_LAYER_NORM_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(),
+                               _matrix(dy, "dy", rows, width, dt, index), x.data_ptr(), _matrix(x, "x", rows, width, dt, index), self._param(weight, "weight", None), mean.data_ptr(),
                                rstd.data_ptr(), *_opt_matrix(add, "add", rows, width, dt, index), *_opt_matrix(dx, "dx", rows, width, dt, index), *sums,
                                self.workspace.data_ptr(), self.workspace.numel())
         _call(self._lib.gd_layer_norm_backward, "gd_layer_norm_backward", args, stream, index)
