@@ -11,6 +11,7 @@
 #include <cstring>
 
 #include "gd_layers.cuh"
+#include "gd_mma.cuh"
 
 namespace gd {
 namespace {
@@ -41,6 +42,9 @@ struct NormBackArgs {
   const float* rstd;
   void* dx;
   float* part;                                // [ctas][2][width], or NULL: no sums of columns are wanted
+  float* dweight;                             // where they end: written here where the launch is one cluster
+  float* dbias;
+  uint32_t cluster, accumulate;
   uint64_t ld_dy, ldx, ld_add, ld_dx;
   uint32_t rows, width;
   uint32_t wide_params;
@@ -439,9 +443,10 @@ __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 
   }
   copies_wait<0>();
   if (!a.part) return;
-  float* part = a.part + (uint64_t)blockIdx.x * 2 * a.width;
+  // the CTA's sums of columns, in the rows' place
+  float* sums = reinterpret_cast<float*>(smem);
+  static_assert(Rows::kSmem >= 2 * G * kEach * 4, "two sums for every column");
   if constexpr (kGroups > 1) {
-    // the groups' sums, in order
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
       const float* t = pass ? db : dw;
@@ -456,18 +461,49 @@ __global__ void __launch_bounds__(kGroupThreads<G>, kGroupThreads<G> == 256 ? 2 
         float q = 0.f;
 #pragma unroll 8
         for (int group = 0; group < kGroups; ++group) q += s_part[group][c];
-        part[pass * a.width + c] = q;
+        sums[pass * a.width + c] = q;
       }
     }
   } else {
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const uint32_t c = (tid + j * G) * V + i;
-        if (c < a.width) part[c] = dw[j * V + i], part[a.width + c] = db[j * V + i];
+        if (c < a.width) sums[c] = dw[j * V + i], sums[a.width + c] = db[j * V + i];
       }
     }
+  }
+  // the cluster's, in rank order, each CTA a share of the columns
+  const bool clustered = a.cluster > 1, last = gridDim.x == a.cluster;
+  const uint32_t rank = clustered ? cluster_rank() : 0u;
+  if (clustered) {
+    cluster_arrive();
+    cluster_wait();
+  } else {
+    __syncthreads();
+  }
+  float* part = a.part + (uint64_t)blockIdx.x * 2 * a.width;         // (a cluster is the whole launch)
+  for (uint32_t c = rank * kGroupThreads<G> + threadIdx.x; c < 2 * a.width; c += a.cluster * kGroupThreads<G>) {
+    float q = 0.f;
+    if (clustered) {
+      const uint32_t at = smem_u32(sums + c);
+      for (uint32_t n = 0; n < a.cluster; ++n) q += peer_load1(peer_address(at, n));
+    } else {
+      q = sums[c];
+    }
+    if (!last) {
+      part[c] = q;
+    } else {
+      float* to = c < a.width ? a.dweight : a.dbias;
+      const uint32_t at = c < a.width ? c : c - a.width;
+      if (to) to[at] = a.accumulate ? to[at] + q : q;
+    }
+  }
+  if (clustered) {
+    cluster_arrive();                                  // (the others may still be reading this CTA's sums)
+    cluster_wait();
   }
 }
 
@@ -546,35 +582,65 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const float*
 }
 
 // ---------------------------------------------------------------- host side
-// A launch of as many CTAs as the GPU holds at a time, or as there are rows for; *ctas: how many (at most `most`).
-template <typename Args>
-cudaError_t launch_rows(void (*kernel)(Args), PerDeviceInt& held, const Args& a, uint32_t groups, uint32_t threads, uint32_t smem, uint32_t most_smem, uint32_t most,
-                        uint32_t* ctas, cudaStream_t stream) {
-  int dev, per_sm = held.get(&dev);
-  if (!per_sm) {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most_smem);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, (int)threads, most_smem);
+// How many CTAs of a kernel an SM holds, asked once.
+template <typename Kernel>
+cudaError_t resident_ctas(Kernel kernel, PerDeviceInt& held, uint32_t threads, uint32_t smem, uint32_t* per_sm) {
+  int dev, n = held.get(&dev);
+  if (!n) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, (int)threads, smem);
     if (e != cudaSuccess) return e;
-    per_sm = std::max(per_sm, 1);
-    held.set(dev, per_sm);
+    n = std::max(n, 1);
+    held.set(dev, n);
   }
-  *ctas = std::min((a.rows + groups - 1) / groups, std::min(most, (uint32_t)(sm_count() * per_sm)));
-  return launch_dependent(kernel, dim3(*ctas), dim3(threads), smem, stream, a);
+  *per_sm = (uint32_t)n;
+  return cudaSuccess;
 }
 template <int DT, int V, int E, int G>
 cudaError_t launch_forward(const NormArgs& a, cudaStream_t stream) {
   using S = RowShape<DT, V, E, G>;
-  constexpr uint32_t kMost = S::kSmem + 2 * E * G * 4;         // with the parameters of the widest row
+  constexpr uint32_t kMost = S::kSmem + 2 * E * G * 4, kGroups = S::kThreads / G;      // with the parameters of the widest row
   const uint32_t smem = S::kSmem + 2 * (a.width + 3u & ~3u) * 4;
-  static PerDeviceInt held;                                     // (how many CTAs of that size an SM has room for)
-  uint32_t ctas;
-  return launch_rows<NormArgs>(norm_kernel<DT, V, E, G>, held, a, S::kThreads / G, S::kThreads, smem, kMost, 0x7FFFFFFFu, &ctas, stream);
-}
-template <int DT, int V, int G>
-cudaError_t launch_backward(const NormBackArgs& a, uint32_t* ctas, cudaStream_t stream) {
-  constexpr uint32_t threads = kGroupThreads<G>;
+  auto kernel = norm_kernel<DT, V, E, G>;
   static PerDeviceInt held;
-  return launch_rows<NormBackArgs>(norm_back_kernel<DT, V, G>, held, a, threads / G, threads, RowsAhead<DT, V, G, 3>::kSmem, RowsAhead<DT, V, G, 3>::kSmem, kColumnCtas, ctas, stream);
+  uint32_t per_sm;
+  const cudaError_t e = resident_ctas(kernel, held, S::kThreads, kMost, &per_sm);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3(std::min((a.rows + kGroups - 1) / kGroups, (uint32_t)sm_count() * per_sm)), dim3(S::kThreads), smem, stream, a);
+}
+// A launch that fits one cluster ends the sums itself (*ctas = 0: nothing is left to join); others leave a row of sums per CTA.  (In clusters of four,
+// which left a quarter of the rows to join, 16384 x 4096 took 125 us in place of 87.)
+constexpr uint32_t kOneCluster = 8, kOneRows = 3;      // kOneRows: rows a group takes rather than have a launch join the sums
+template <int DT, int V, int G>
+cudaError_t launch_backward(NormBackArgs a, uint32_t* ctas, cudaStream_t stream) {
+  constexpr uint32_t threads = kGroupThreads<G>, groups = threads / G, smem = RowsAhead<DT, V, G, 3>::kSmem;
+  auto kernel = norm_back_kernel<DT, V, G>;
+  static PerDeviceInt held;
+  uint32_t per_sm;
+  cudaError_t e = resident_ctas(kernel, held, threads, smem, &per_sm);
+  if (e != cudaSuccess) return e;
+  const uint32_t want = (a.rows + groups - 1) / groups;
+  uint32_t grid = std::min(want, std::min(kColumnCtas, (uint32_t)sm_count() * per_sm));
+  a.cluster = 1;
+  if (a.part && want <= kOneCluster * kOneRows) {
+    while (a.cluster < kOneCluster && a.cluster < want) a.cluster *= 2;
+    grid = a.cluster;
+  }
+  *ctas = grid == a.cluster ? 0 : grid;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 // Up to 64 elements to a thread, so that what a row costs beside its elements is shared by many, and eight threads at least, so that they read whole
 // lines.  Single elements of 16 bits take a register each: half as many (20000 x 1001: 26 against 35 us).
@@ -701,6 +767,8 @@ int backward(const gd_layer_norm_backward_args* g, cudaStream_t stream) {
     gd_layer_norm_workspace_bytes(rows, width, &need);
     if (!g->workspace || !aligned_to(g->workspace, 256) || g->workspace_bytes < need) return GD_ERR_WORKSPACE;
     a.part = static_cast<float*>(g->workspace);
+    a.dweight = g->dweight, a.dbias = g->dbias;
+    a.accumulate = accumulate;
   }
   if (rows) {
     a.dy = g->dy, a.ld_dy = g->ld_dy;
@@ -718,7 +786,7 @@ int backward(const gd_layer_norm_backward_args* g, cudaStream_t stream) {
     if (e != cudaSuccess) return GD_ERR_CUDA;
     note_launches(1);
   }
-  if (sums) {
+  if (sums && (ctas || !rows)) {
     ProfileScope ps(stream, PT_NORM_JOIN);
     const cudaError_t e = launch_dependent(norm_join_kernel, dim3((uint32_t)((width + 31) / 32), 2), dim3(32 * kJoinWarps), 0, stream, (const float*)a.part, ctas,
                                            (uint32_t)width, g->dweight, g->dbias, (uint32_t)accumulate);

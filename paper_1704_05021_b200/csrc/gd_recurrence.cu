@@ -11,7 +11,7 @@
 // A (what came in) + C.  The states h[t-1] that dgate needs are made again from the marks, the states before every kMarkRows-th row of a sequence
 // which the forward call keeps in fp32: y is rounded and would not do where h[t-1] and value nearly agree.
 //
-// Sequences of few rows (kShortRows on average, the single step among them): a thread takes a sequence's columns through all its rows.
+// Many sequences of few rows, the single step among them: a thread takes a sequence's columns through all its rows.
 #include <algorithm>
 #include <cstring>
 
@@ -22,7 +22,7 @@ namespace gd {
 namespace {
 
 constexpr uint32_t kWarps = 8, kRows = 8, kMarkRows = kWarps * kRows;      // kMarkRows is part of the marks' layout
-constexpr uint32_t kShortRows = 24;
+constexpr uint32_t kShortRows = 48, kStepRows = 8;
 constexpr uint32_t kMostCluster = 8;
 
 struct Spans {
@@ -247,13 +247,39 @@ struct TileShape {
   static constexpr uint32_t kBytes = kDepth * kStage + (CL > 1 ? (uint32_t)sizeof(Exchange<V, CL, L>) : 0u) + 128u;
 };
 constexpr uint32_t kMarkGroups = kMarkRows / kRows;      // groups from one mark to the next
+// How a tile's rows come: as a box of a tensor map (rows at multiples of 16 bytes), by copies that each thread asks for its own places (of 4
+// bytes: pairs of 16-bit columns, or fp32), or, single columns of 16 bits, through registers, a tile ahead.
+enum Mode : int { kBoxes = 0, kOwnCopies = 1, kRegisters = 2 };
+
+// The first `most` (up to kRows) of a thread's rows from p on, its V columns, into its own places of a tile: only it reads them.
+template <typename T, int V, int L>
+__device__ __forceinline__ void own_rows(unsigned char* tile, const T* p, uint64_t ld, uint32_t most) {
+  const uint32_t to = smem_u32(tile) + ((threadIdx.x / L) * kRows * L + threadIdx.x % L) * V * (uint32_t)sizeof(T);
+#pragma unroll
+  for (uint32_t k = 0; k < kRows; ++k) {
+    if (k < most) copy_ahead<V * (int)sizeof(T)>(to + k * (L * V * (uint32_t)sizeof(T)), p);
+    p += ld;
+  }
+}
+
+// The same into registers.
+template <typename P, typename T>
+__device__ __forceinline__ void held_rows(typename P::Raw (&held)[kRows], const T* p, uint64_t ld, uint32_t most) {
+#pragma unroll
+  for (uint32_t k = 0; k < kRows; ++k) {
+    held[k] = k < most ? P::load(p) : P::none();
+    p += ld;
+  }
+}
+template <typename P, typename T>
+__device__ __forceinline__ void held_rows(typename P::Raw (&)[1], const T*, uint64_t, uint32_t) {}
 
 // ---------------------------------------------------------------- forward
 // Rows that tiled copies can read: 16-byte aligned.
 struct ScanMaps {
   CUtensorMap gate, value;
 };
-template <int DT, int V, int L, int CL>
+template <int DT, int V, int L, int CL, int MODE>
 __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel(const __grid_constant__ ScanArgs a, const __grid_constant__ ScanMaps maps) {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
@@ -270,7 +296,7 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    prefetch_map(&maps.gate), prefetch_map(&maps.value);
+    if (MODE == kBoxes) prefetch_map(&maps.gate), prefetch_map(&maps.value);
   }
   if constexpr (CL > 1) exchange_begin(s_x);
   else __syncthreads();
@@ -286,16 +312,43 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
     T* y = static_cast<T*>(a.y) + (uint64_t)first * a.ld_y + c;
     const uint64_t mark0 = first_mark(seq, first);
     const uint32_t tiles = (count + kTileRows - 1) / kTileRows, sets = (tiles + CL - 1) / CL;
-    const auto ask = [&](uint32_t set) {             // one thread: the copies of this CTA's tile of a set
+    typename P::Raw held[MODE == kRegisters ? 2 : 1][MODE == kRegisters ? R : 1];
+    // All threads: the copies of this CTA's tile of a set.
+    const T* gate = static_cast<const T*>(a.gate) + (uint64_t)first * a.ld_gate + c;
+    const T* value = static_cast<const T*>(a.value) + (uint64_t)first * a.ld_value + c;
+    const auto ask = [&](uint32_t set) {
       const uint32_t tile = set * CL + rank, s = asked % kDepth;
-      if (tile >= tiles) return;
-      mbar_arrive_expect_tx(&s_full[s], S::kStage);
-      tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
-      tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
-      ++asked;
+      if constexpr (MODE == kBoxes) {
+        if (threadIdx.x != 0 || tile >= tiles) return;
+        mbar_arrive_expect_tx(&s_full[s], S::kStage);
+        tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
+        tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
+        ++asked;
+      } else {
+        const uint32_t r0 = tile * kTileRows + group * R, most = in && tile < tiles && r0 < count ? count - r0 : 0u;
+        const T *from_g = gate + (uint64_t)r0 * a.ld_gate, *from_v = value + (uint64_t)r0 * a.ld_value;
+        if constexpr (MODE == kOwnCopies) {
+          own_rows<T, V, L>(smem + s * S::kStage, from_g, a.ld_gate, most);
+          own_rows<T, V, L>(smem + s * S::kStage + S::kInput, from_v, a.ld_value, most);
+          copies_commit();
+        } else {
+          held_rows<P>(held[0], from_g, a.ld_gate, most);
+          held_rows<P>(held[1], from_v, a.ld_value, most);
+        }
+        if (tile < tiles) ++asked;
+      }
     };
-    if (threadIdx.x == 0)
-      for (uint32_t n = 0; n < kDepth; ++n) ask(n);
+    // (registers:) what has been asked for into its stage
+    const auto settle = [&](uint32_t s) {
+#pragma unroll
+      for (uint32_t input = 0; input < 2; ++input) {
+        typename P::Raw* to = reinterpret_cast<typename P::Raw*>(smem + s * S::kStage + input * S::kInput) + group * R * L + lane;
+#pragma unroll
+        for (int k = 0; k < R; ++k) to[k * L] = held[input][k];
+      }
+    };
+    constexpr uint32_t kAhead = MODE == kRegisters ? 1 : kDepth;
+    for (uint32_t n = 0; n < kAhead; ++n) ask(n);
     float h[V];                                      // the state that enters the tile, or the cluster's tiles
 #pragma unroll
     for (int i = 0; i < V; ++i) h[i] = in && a.h0 ? a.h0[(uint64_t)seq * a.width + c + i] : 0.f;
@@ -307,9 +360,11 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
     const auto evaluate = [&](uint32_t tile, float (&f)[N], float (&sv)[N]) __attribute__((always_inline)) {
       const uint32_t rows = rows_of(tile), s = taken % kDepth;
       bool good = true;
+      if constexpr (MODE == kOwnCopies) copies_wait<(int)kDepth - 1>();
       if (tile < tiles) {
         const int never = 0;
-        good = mbar_wait(&s_full[s], (taken / kDepth) & 1u, &never);
+        if constexpr (MODE == kBoxes) good = mbar_wait(&s_full[s], (taken / kDepth) & 1u, &never);
+        if constexpr (MODE == kRegisters) settle(s);
         ++taken;
       }
       if (rows) {
@@ -370,7 +425,7 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
       const auto begin = [&](uint32_t set, float (&fn)[N], float (&svn)[N], Map<V>& before_n) __attribute__((always_inline)) {
         const Map<V> own = evaluate(set * CL + rank, fn, svn);
         __syncthreads();
-        if (threadIdx.x == 0) ask(set + kDepth);
+        ask(set + kAhead);
         before_n = identity<V>();
 #pragma unroll
         for (uint32_t w = 0; w < kGroups - 1; ++w) {
@@ -406,7 +461,7 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
         float f[N], sv[N];
         const Map<V> own = evaluate(tile, f, sv);
         __syncthreads();
-        if (threadIdx.x == 0) ask(tile + kDepth);
+        ask(tile + kAhead);
         if (tile) {
 #pragma unroll
           for (int i = 0; i < V; ++i) h[i] = s_state[turn & 1u][lane][i];
@@ -443,95 +498,8 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
   }
 }
 
-// Any other rows: read by each thread, the next tile's before this one's are worked on.
-template <int DT, int V>
-__global__ void __launch_bounds__(kWarps * 32) scan_kernel(const __grid_constant__ ScanArgs a) {
-  using P = Piece<DT, V>;
-  using T = typename Elem<DT>::type;
-  __shared__ float2 s_map[2][kWarps][32 * V];
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  pdl_wait();
-  pdl_trigger();
-  uint32_t turn = 0;
-  for (uint64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
-    const uint32_t seq = (uint32_t)(item / a.slabs), c = ((uint32_t)(item % a.slabs) * 32u + lane) * V;
-    uint32_t first, count;
-    a.spans.of(seq, &first, &count);
-    const bool in = c < a.width;
-    const T* gate = static_cast<const T*>(a.gate) + (uint64_t)first * a.ld_gate + c;
-    const T* value = static_cast<const T*>(a.value) + (uint64_t)first * a.ld_value + c;
-    T* y = static_cast<T*>(a.y) + (uint64_t)first * a.ld_y + c;
-    const uint64_t mark0 = first_mark(seq, first);
-    float h[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) h[i] = in && a.h0 ? a.h0[(uint64_t)seq * a.width + c + i] : 0.f;
-    const uint32_t tiles = (count + kMarkRows - 1) / kMarkRows;
-    typename P::Raw next_g[kRows], next_v[kRows];
-    const auto ask = [&](uint32_t tile) {
-      const uint32_t r0 = tile * kMarkRows + warp * kRows;
-#pragma unroll
-      for (uint32_t k = 0; k < kRows; ++k) {
-        const bool there = in && tile < tiles && r0 + k < count;
-        next_g[k] = there ? P::load(gate + (uint64_t)(r0 + k) * a.ld_gate) : P::none();
-        next_v[k] = there ? P::load(value + (uint64_t)(r0 + k) * a.ld_value) : P::none();
-      }
-    };
-    ask(0);
-    for (uint32_t tile = 0; tile < tiles; ++tile) {
-      const uint32_t r0 = tile * kMarkRows + warp * kRows, rows = r0 < count ? min(kRows, count - r0) : 0u;
-      float f[kRows][V], sv[kRows][V], A[V], B[V], mine[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) A[i] = 1.f, B[i] = 0.f;
-#pragma unroll
-      for (uint32_t k = 0; k < kRows; ++k) {
-        float g[V], v[V];
-        P::widen(next_g[k], g);
-        P::widen(next_v[k], v);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float s;
-          gate_of<DT>(g[i], &f[k][i], &s);
-          sv[k][i] = s * v[i];
-          if (k >= rows) f[k][i] = 1.f, sv[k][i] = 0.f;
-          A[i] *= f[k][i];
-          B[i] = fmaf(f[k][i], B[i], sv[k][i]);
-        }
-      }
-      ask(tile + 1);
-      float2(*map)[32 * V] = s_map[turn++ & 1u];
-#pragma unroll
-      for (int i = 0; i < V; ++i) map[warp][lane * V + i] = make_float2(A[i], B[i]);
-      __syncthreads();
-      if (a.marks && in && warp == 0) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) a.marks[(mark0 + tile) * a.width + c + i] = h[i];
-      }
-#pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          if (w == warp) mine[i] = h[i];
-          const float2 m = map[w][lane * V + i];
-          h[i] = fmaf(m.x, h[i], m.y);
-        }
-      }
-#pragma unroll
-      for (uint32_t k = 0; k < kRows; ++k) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) mine[i] = fmaf(f[k][i], mine[i], sv[k][i]);
-        if (in && k < rows) P::store(y + (uint64_t)(r0 + k) * a.ld_y, P::narrow(mine));
-      }
-    }
-    __syncthreads();                                 // (h_last may be h0: written when all have read it)
-    if (a.h_last && in && warp == 0) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) a.h_last[(uint64_t)seq * a.width + c + i] = h[i];
-    }
-  }
-}
-
 // One thread per sequence and V columns.
-constexpr uint32_t kShortThreads = 128, kShortAhead = 4;
+constexpr uint32_t kShortThreads = 128, kShortAhead = 8, kShortBackAhead = 4, kShortBlock = 16;
 template <int DT, int V>
 __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const __grid_constant__ ScanArgs a) {
   using P = Piece<DT, V>;
@@ -589,7 +557,7 @@ struct ScanBackMaps {
   CUtensorMap gate, value, dy;
 };
 // With a cluster a tile's rows are evaluated twice, from shared memory: for the maps that the others wait for, and a set later for the results.
-template <int DT, int V, int L, int CL>
+template <int DT, int V, int L, int CL, int MODE>
 __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const __grid_constant__ ScanBackArgs a, const __grid_constant__ ScanBackMaps maps) {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
@@ -606,7 +574,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    prefetch_map(&maps.gate), prefetch_map(&maps.value), prefetch_map(&maps.dy);
+    if (MODE == kBoxes) prefetch_map(&maps.gate), prefetch_map(&maps.value), prefetch_map(&maps.dy);
   }
   if constexpr (CL > 1) exchange_begin(s_x);
   else __syncthreads();
@@ -624,21 +592,50 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
     const float* marks = a.marks + first_mark(seq, first) * a.width + c;
     const uint32_t tiles = (count + kTileRows - 1) / kTileRows, sets = (tiles + CL - 1) / CL;
     // sets are counted from the last one: set n holds the tiles (sets - 1 - n) CL + 0 .. CL - 1
-    const auto ask = [&](uint32_t n) {               // one thread
+    const T* gate = static_cast<const T*>(a.gate) + (uint64_t)first * a.ld_gate + c;
+    const T* value = static_cast<const T*>(a.value) + (uint64_t)first * a.ld_value + c;
+    const T* dy = static_cast<const T*>(a.dy) + (uint64_t)first * a.ld_dy + c;
+    typename P::Raw held[MODE == kRegisters ? 3 : 1][MODE == kRegisters ? R : 1];
+    const auto ask = [&](uint32_t n) {               // all threads
       const uint32_t tile = (sets - 1u - n) * CL + rank, s = asked % kDepth;
-      if (n >= sets || tile >= tiles) return;
-      const int32_t row = (int32_t)(first + tile * kTileRows);
-      mbar_arrive_expect_tx(&s_full[s], S::kStage);
-      tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, row, &s_full[s]);
-      tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, row, &s_full[s]);
-      tile_load(smem + s * S::kStage + 2 * S::kInput, &maps.dy, (int32_t)col0, row, &s_full[s]);
-      ++asked;
+      const bool there = n < sets && tile < tiles;
+      if constexpr (MODE == kBoxes) {
+        if (threadIdx.x != 0 || !there) return;
+        const int32_t row = (int32_t)(first + tile * kTileRows);
+        mbar_arrive_expect_tx(&s_full[s], S::kStage);
+        tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, row, &s_full[s]);
+        tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, row, &s_full[s]);
+        tile_load(smem + s * S::kStage + 2 * S::kInput, &maps.dy, (int32_t)col0, row, &s_full[s]);
+        ++asked;
+      } else {
+        const uint32_t r0 = tile * kTileRows + group * R, most = in && there && r0 < count ? count - r0 : 0u;
+        const T *from_g = gate + (uint64_t)r0 * a.ld_gate, *from_v = value + (uint64_t)r0 * a.ld_value, *from_d = dy + (uint64_t)r0 * a.ld_dy;
+        if constexpr (MODE == kOwnCopies) {
+          own_rows<T, V, L>(smem + s * S::kStage, from_g, a.ld_gate, most);
+          own_rows<T, V, L>(smem + s * S::kStage + S::kInput, from_v, a.ld_value, most);
+          own_rows<T, V, L>(smem + s * S::kStage + 2 * S::kInput, from_d, a.ld_dy, most);
+          copies_commit();
+        } else {
+          held_rows<P>(held[0], from_g, a.ld_gate, most);
+          held_rows<P>(held[1], from_v, a.ld_value, most);
+          held_rows<P>(held[2], from_d, a.ld_dy, most);
+        }
+        if (there) ++asked;
+      }
+    };
+    // (registers:) what has been asked for into its stage
+    const auto settle = [&](uint32_t s) {
+#pragma unroll
+      for (uint32_t input = 0; input < 3; ++input) {
+        typename P::Raw* to = reinterpret_cast<typename P::Raw*>(smem + s * S::kStage + input * S::kInput) + group * R * L + lane;
+#pragma unroll
+        for (int k = 0; k < R; ++k) to[k * L] = held[input][k];
+      }
     };
     // With a cluster a set's tile is read again one set later: while the maps of set n are made, n and n - 1 hold a stage each and n + 1 may be
     // on its way.
-    constexpr uint32_t kAhead = CL > 1 ? kDepth - 2 : kDepth;
-    if (threadIdx.x == 0)
-      for (uint32_t n = 0; n < kAhead; ++n) ask(n);
+    constexpr uint32_t kAhead = MODE == kRegisters ? 1 : CL > 1 ? kDepth - 2 : kDepth;
+    for (uint32_t n = 0; n < kAhead; ++n) ask(n);
     float carry[V];                                  // f[t+1] dh[t+1] of the row behind the tile, or the cluster's tiles
 #pragma unroll
     for (int i = 0; i < V; ++i) carry[i] = in && a.dh_last ? a.dh_last[(uint64_t)seq * a.width + c + i] : 0.f;
@@ -698,7 +695,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
     };
     const auto wait = [&](uint32_t tile, uint32_t* stage) {
       *stage = taken % kDepth;
+      if constexpr (MODE == kOwnCopies) copies_wait<(int)kAhead - 1>();
       if (tile >= tiles) return true;
+      if constexpr (MODE != kBoxes) {
+        if constexpr (MODE == kRegisters) settle(*stage);
+        ++taken;
+        return true;
+      }
       const int never = 0;
       const bool good = mbar_wait(&s_full[*stage], (taken / kDepth) & 1u, &never);
       ++taken;
@@ -756,7 +759,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
         }
         __syncthreads();
         // (all are past finish of set n - 2: its stage is free)
-        if (threadIdx.x == 0) ask(n + kAhead);
+        ask(n + kAhead);
         next_behind = identity<V>();
 #pragma unroll
         for (uint32_t w = kGroups - 1; w > 0; --w) {
@@ -802,7 +805,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
         read(stage, rows_of(tile), x);
         const Map<V> own = leave(x, good);
         __syncthreads();
-        if (threadIdx.x == 0) ask(n + kAhead);
+        ask(n + kAhead);
         if (n) {
 #pragma unroll
           for (int i = 0; i < V; ++i) carry[i] = s_carry[turn & 1u][lane][i];
@@ -840,137 +843,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
   }
 }
 
-// Any other rows, read by each thread.
-template <int DT, int V>
-__global__ void __launch_bounds__(kWarps * 32, 2) scan_back_kernel(const __grid_constant__ ScanBackArgs a) {
-  using P = Piece<DT, V>;
-  using T = typename Elem<DT>::type;
-  __shared__ float2 s_map[2][kWarps][32 * V];       // (A, B): of the states
-  __shared__ float s_back[2][kWarps][32 * V];       // C: of the gradient
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  pdl_wait();
-  pdl_trigger();
-  uint32_t turn = 0;
-  for (uint64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
-    const uint32_t seq = (uint32_t)(item / a.slabs), c = ((uint32_t)(item % a.slabs) * 32u + lane) * V;
-    uint32_t first, count;
-    a.spans.of(seq, &first, &count);
-    const bool in = c < a.width;
-    const T* gate = static_cast<const T*>(a.gate) + (uint64_t)first * a.ld_gate + c;
-    const T* value = static_cast<const T*>(a.value) + (uint64_t)first * a.ld_value + c;
-    const T* dy = static_cast<const T*>(a.dy) + (uint64_t)first * a.ld_dy + c;
-    T* dgate = static_cast<T*>(a.dgate) + (uint64_t)first * a.ld_dgate + c;
-    T* dvalue = static_cast<T*>(a.dvalue) + (uint64_t)first * a.ld_dvalue + c;
-    const float* marks = a.marks + first_mark(seq, first) * a.width + c;
-    float carry[V];                                  // f[t+1] dh[t+1] of the row behind the tile
-#pragma unroll
-    for (int i = 0; i < V; ++i) carry[i] = in && a.dh_last ? a.dh_last[(uint64_t)seq * a.width + c + i] : 0.f;
-    const uint32_t tiles = (count + kMarkRows - 1) / kMarkRows;
-    typename P::Raw next_g[kRows], next_v[kRows], next_d[kRows];
-    float next_h[V];
-    const auto ask = [&](uint32_t behind) {          // of the tile before that one
-      const uint32_t tile = behind - 1, r0 = tile * kMarkRows + warp * kRows;
-#pragma unroll
-      for (uint32_t k = 0; k < kRows; ++k) {
-        const bool there = in && behind && r0 + k < count;
-        next_g[k] = there ? P::load(gate + (uint64_t)(r0 + k) * a.ld_gate) : P::none();
-        next_v[k] = there ? P::load(value + (uint64_t)(r0 + k) * a.ld_value) : P::none();
-        next_d[k] = there ? P::load(dy + (uint64_t)(r0 + k) * a.ld_dy) : P::none();
-      }
-#pragma unroll
-      for (int i = 0; i < V; ++i) next_h[i] = in && behind ? marks[(uint64_t)tile * a.width + i] : 0.f;
-    };
-    ask(tiles);
-    for (uint32_t behind = tiles; behind > 0; --behind) {
-      const uint32_t r0 = (behind - 1) * kMarkRows + warp * kRows, rows = r0 < count ? min(kRows, count - r0) : 0u;
-      float f[kRows][V], s[kRows][V], v[kRows][V], A[V], B[V], C[V], h[V];
-      typename P::Raw d_raw[kRows];
-#pragma unroll
-      for (int i = 0; i < V; ++i) A[i] = 1.f, B[i] = 0.f, C[i] = 0.f, h[i] = next_h[i];
-#pragma unroll
-      for (uint32_t k = 0; k < kRows; ++k) {
-        float g[V];
-        P::widen(next_g[k], g);
-        P::widen(next_v[k], v[k]);
-        d_raw[k] = next_d[k];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          gate_of<DT>(g[i], &f[k][i], &s[k][i]);
-          if (k >= rows) f[k][i] = 1.f, s[k][i] = 0.f;
-          A[i] *= f[k][i];
-          B[i] = fmaf(f[k][i], B[i], s[k][i] * v[k][i]);
-        }
-      }
-#pragma unroll
-      for (uint32_t k = kRows; k-- > 0;) {
-        float d[V];
-        P::widen(d_raw[k], d);
-#pragma unroll
-        for (int i = 0; i < V; ++i) C[i] = f[k][i] * (d[i] + C[i]);
-      }
-      ask(behind - 1);
-      float2(*map)[32 * V] = s_map[turn & 1u];
-      float(*back)[32 * V] = s_back[turn & 1u];
-      ++turn;
-#pragma unroll
-      for (int i = 0; i < V; ++i) map[warp][lane * V + i] = make_float2(A[i], B[i]), back[warp][lane * V + i] = C[i];
-      __syncthreads();
-      float g[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float e = carry[i];
-        g[i] = e;
-#pragma unroll
-        for (uint32_t w = kWarps; w-- > 0;) {
-          if (w == warp) g[i] = e;
-          e = fmaf(map[w][lane * V + i].x, e, back[w][lane * V + i]);
-        }
-        carry[i] = e;
-#pragma unroll
-        for (uint32_t w = 0; w < kWarps; ++w) {
-          const float2 m = map[w][lane * V + i];
-          h[i] = w < warp ? fmaf(m.x, h[i], m.y) : h[i];
-        }
-      }
-#pragma unroll
-      for (uint32_t k = 0; k < kRows; ++k) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float before = h[i];
-          h[i] = fmaf(f[k][i], h[i], s[k][i] * v[k][i]);
-          v[k][i] = before - v[k][i];
-        }
-      }
-#pragma unroll
-      for (uint32_t k = kRows; k-- > 0;) {
-        float d[V], dg[V], dv[V];
-        P::widen(d_raw[k], d);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float dh = d[i] + g[i];
-          dv[i] = s[k][i] * dh;
-          g[i] = f[k][i] * dh;
-          dg[i] = dv[i] * v[k][i] * f[k][i];
-        }
-        if (in && k < rows) {
-          P::store(dgate + (uint64_t)(r0 + k) * a.ld_dgate, P::narrow(dg));
-          P::store(dvalue + (uint64_t)(r0 + k) * a.ld_dvalue, P::narrow(dv));
-        }
-      }
-    }
-    __syncthreads();                                 // (dh0 may be dh_last: written when all have read it)
-    if (a.dh0 && in && warp == 0) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) a.dh0[(uint64_t)seq * a.width + c + i] = carry[i];
-    }
-  }
-}
-
-// One thread per sequence and V columns: kShortAhead rows at a time from the last, their states made from the nearest mark.
+// One thread per sequence and V columns: kShortBlock rows at a time from the last, first forward from the nearest mark through their states, which are
+// kept in shared memory, each thread its own, then back through the gradient.
 template <int DT, int V>
 __global__ void __launch_bounds__(kShortThreads) scan_back_short_kernel(const __grid_constant__ ScanBackArgs a) {
   using P = Piece<DT, V>;
   using T = typename Elem<DT>::type;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  float* states = reinterpret_cast<float*>(smem_raw) + threadIdx.x * V;      // of row k at k kShortThreads V
   pdl_wait();
   pdl_trigger();
   const uint64_t stride = (uint64_t)gridDim.x * kShortThreads;
@@ -988,52 +868,66 @@ __global__ void __launch_bounds__(kShortThreads) scan_back_short_kernel(const __
 #pragma unroll
     for (int i = 0; i < V; ++i) g[i] = a.dh_last ? a.dh_last[(uint64_t)seq * a.width + c + i] : 0.f;
     for (uint32_t end = count; end > 0;) {
-      const uint32_t r0 = (end - 1) / kShortAhead * kShortAhead, rows = end - r0;
-      float h[V], f[kShortAhead][V], s[kShortAhead][V], v[kShortAhead][V];
+      const uint32_t r0 = (end - 1) / kShortBlock * kShortBlock, mark = r0 / kMarkRows * kMarkRows;
+      float h[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[i] = marks[(uint64_t)(r0 / kMarkRows) * a.width + i];
-      // the state before r0 (a sequence this long among short ones goes through its rows several times)
-      for (uint32_t r = r0 / kMarkRows * kMarkRows; r < r0; ++r) {
-        float x[V], w[V];
-        P::widen(P::load_kept(gate + (uint64_t)r * a.ld_gate), x);
-        P::widen(P::load_kept(value + (uint64_t)r * a.ld_value), w);
+      for (int i = 0; i < V; ++i) h[i] = marks[(uint64_t)(mark / kMarkRows) * a.width + i];
+      for (uint32_t r = mark; r < end; r += kShortBackAhead) {
+        typename P::Raw x_raw[kShortBackAhead], v_raw[kShortBackAhead];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float p, q;
-          gate_of<DT>(x[i], &p, &q);
-          h[i] = fmaf(p, h[i], q * w[i]);
+        for (uint32_t k = 0; k < kShortBackAhead; ++k) {
+          if (r + k >= end) continue;
+          x_raw[k] = P::load_kept(gate + (uint64_t)(r + k) * a.ld_gate);
+          v_raw[k] = P::load_kept(value + (uint64_t)(r + k) * a.ld_value);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kShortBackAhead; ++k) {
+          if (r + k >= end) continue;
+          float x[V], v[V];
+          P::widen(x_raw[k], x);
+          P::widen(v_raw[k], v);
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            float f, s;
+            gate_of<DT>(x[i], &f, &s);
+            if (r >= r0) states[(r + k - r0) * kShortThreads * V + i] = h[i];
+            h[i] = fmaf(f, h[i], s * v[i]);
+          }
         }
       }
-      typename P::Raw d_raw[kShortAhead];
+      const uint32_t rows = end - r0;
+      for (uint32_t left = rows; left > 0;) {
+        const uint32_t n = min(left, kShortBackAhead);
+        typename P::Raw x_raw[kShortBackAhead], v_raw[kShortBackAhead], d_raw[kShortBackAhead];
 #pragma unroll
-      for (uint32_t k = 0; k < kShortAhead; ++k) {
-        float x[V];
-        if (k >= rows) continue;
-        d_raw[k] = P::load(dy + (uint64_t)(r0 + k) * a.ld_dy);
-        P::widen(P::load(gate + (uint64_t)(r0 + k) * a.ld_gate), x);
-        P::widen(P::load(value + (uint64_t)(r0 + k) * a.ld_value), v[k]);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          gate_of<DT>(x[i], &f[k][i], &s[k][i]);
-          const float before = h[i];
-          h[i] = fmaf(f[k][i], h[i], s[k][i] * v[k][i]);
-          v[k][i] = before - v[k][i];
+        for (uint32_t k = 0; k < kShortBackAhead; ++k) {
+          if (k >= n) continue;
+          const uint64_t r = r0 + left - 1 - k;
+          x_raw[k] = P::load(gate + r * a.ld_gate);
+          v_raw[k] = P::load(value + r * a.ld_value);
+          d_raw[k] = P::load(dy + r * a.ld_dy);
         }
-      }
 #pragma unroll
-      for (uint32_t k = kShortAhead; k-- > 0;) {
-        if (k >= rows) continue;
-        float d[V], dg[V], dv[V];
-        P::widen(d_raw[k], d);
+        for (uint32_t k = 0; k < kShortBackAhead; ++k) {
+          if (k >= n) continue;
+          const uint32_t at = left - 1 - k;
+          float x[V], v[V], d[V], dg[V], dv[V];
+          P::widen(x_raw[k], x);
+          P::widen(v_raw[k], v);
+          P::widen(d_raw[k], d);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float dh = d[i] + g[i];
-          dv[i] = s[k][i] * dh;
-          g[i] = f[k][i] * dh;
-          dg[i] = dv[i] * v[k][i] * f[k][i];
+          for (int i = 0; i < V; ++i) {
+            float f, s;
+            gate_of<DT>(x[i], &f, &s);
+            const float dh = d[i] + g[i];
+            dv[i] = s * dh;
+            g[i] = f * dh;
+            dg[i] = dv[i] * (states[at * kShortThreads * V + i] - v[i]) * f;
+          }
+          P::store(dgate + (uint64_t)(r0 + at) * a.ld_dgate, P::narrow(dg));
+          P::store(dvalue + (uint64_t)(r0 + at) * a.ld_dvalue, P::narrow(dv));
         }
-        P::store(dgate + (uint64_t)(r0 + k) * a.ld_dgate, P::narrow(dg));
-        P::store(dvalue + (uint64_t)(r0 + k) * a.ld_dvalue, P::narrow(dv));
+        left -= n;
       }
       end = r0;
     }
@@ -1070,6 +964,13 @@ cudaError_t launch_tiled(void (*kernel)(Args, Maps), PerDeviceInt& ready, const 
   return cudaLaunchKernelEx(&cfg, kernel, a, maps);
 }
 uint32_t capped(uint64_t ctas) { return (uint32_t)std::min<uint64_t>(ctas, 1u << 24); }
+// Sequences that a thread takes by itself: short ones, where there are threads enough (65536 rows of 512 in 2048 sequences: 46 against 95 us, backward
+// 123 against 160; 2000 rows in 50 sequences backward 28 against 13), and those of a few rows.
+template <typename Args>
+bool short_ones(const Args& a, uint32_t columns) {
+  const uint32_t mean = a.spans.rows / a.spans.sequences;
+  return mean < kStepRows || (mean < kShortRows && (uint64_t)a.spans.sequences * a.width >= 512ull * sm_count() * columns);
+}
 template <typename Args>
 void cut(Args& a, uint32_t columns) {
   a.slabs = (a.width + columns - 1) / columns;
@@ -1095,70 +996,84 @@ bool encode_rows(CUtensorMap* map, const void* p, uint64_t ld, const Spans& s, u
 }
 bool tiles_take(const void* p, uint64_t ld, uint64_t rows, size_t item) { return aligned_to(p, 16) && (rows <= 1 || ld * item % 16 == 0); }
 template <int DT, int V, int L, int CL>
-cudaError_t forward_in(const ScanArgs& a, const ScanMaps& m, cudaStream_t stream) {
-  static PerDeviceInt ready;
-  return launch_tiled<ScanArgs, ScanMaps>(scan_tiled_kernel<DT, V, L, CL>, ready, a, m, TileShape<DT, V, L, 2, CL>::kBytes, CL, stream);
+cudaError_t forward_in(const ScanArgs& a, const ScanMaps& m, bool boxes, cudaStream_t stream) {
+  static PerDeviceInt ready[2];
+  constexpr uint32_t bytes = TileShape<DT, V, L, 2, CL>::kBytes;
+  if constexpr (V * sizeof(typename Elem<DT>::type) < 4) {
+    return launch_tiled<ScanArgs, ScanMaps>(scan_tiled_kernel<DT, V, L, CL, kRegisters>, ready[0], a, m, bytes, CL, stream);
+  } else {
+    return launch_tiled<ScanArgs, ScanMaps>(boxes ? scan_tiled_kernel<DT, V, L, CL, kBoxes> : scan_tiled_kernel<DT, V, L, CL, kOwnCopies>, ready[boxes], a, m, bytes, CL, stream);
+  }
 }
 template <int DT, int V, int L>
-cudaError_t forward_tiled(ScanArgs a, cudaStream_t stream) {
+cudaError_t forward_tiled(ScanArgs a, bool boxes, cudaStream_t stream) {
   using S = TileShape<DT, V, L, 2, 1>;
   cut(a, S::kColumns);
   ScanMaps m;
-  if (!encode_rows<DT, S>(&m.gate, a.gate, a.ld_gate, a.spans, a.width) || !encode_rows<DT, S>(&m.value, a.value, a.ld_value, a.spans, a.width)) return cudaErrorInvalidValue;
+  std::memset(&m, 0, sizeof(m));
+  if (boxes && (!encode_rows<DT, S>(&m.gate, a.gate, a.ld_gate, a.spans, a.width) || !encode_rows<DT, S>(&m.value, a.value, a.ld_value, a.spans, a.width))) return cudaErrorInvalidValue;
   switch (choose_cluster(a.items, a.spans, S::kTileRows)) {
-    case 1: return forward_in<DT, V, L, 1>(a, m, stream);
-    case 2: return forward_in<DT, V, L, 2>(a, m, stream);
-    case 4: return forward_in<DT, V, L, 4>(a, m, stream);
-    default: return forward_in<DT, V, L, 8>(a, m, stream);
+    case 1: return forward_in<DT, V, L, 1>(a, m, boxes, stream);
+    case 2: return forward_in<DT, V, L, 2>(a, m, boxes, stream);
+    case 4: return forward_in<DT, V, L, 4>(a, m, boxes, stream);
+    default: return forward_in<DT, V, L, 8>(a, m, boxes, stream);
   }
 }
 template <int DT>
 cudaError_t launch_forward(ScanArgs a, bool two, cudaStream_t stream) {
   constexpr size_t item = sizeof(typename Elem<DT>::type);
   constexpr int W = item == 2 ? 2 : 1;
-  if (a.spans.rows / a.spans.sequences < kShortRows) {
+  if (short_ones(a, two ? W : 1)) {
     cut(a, two ? W : 1);
     const dim3 grid(capped((a.items + kShortThreads - 1) / kShortThreads)), block(kShortThreads);
     return two ? launch_dependent(scan_short_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_short_kernel<DT, 1>, grid, block, 0, stream, a);
   }
-  if ((two || item == 4) && tiles_take(a.gate, a.ld_gate, a.spans.rows, item) && tiles_take(a.value, a.ld_value, a.spans.rows, item))
-    return narrow_tiles(a, 32 * W) ? forward_tiled<DT, W, 16>(a, stream) : forward_tiled<DT, W, 32>(a, stream);
-  cut(a, 32 * (two ? W : 1));
-  const dim3 grid(capped(a.items)), block(kWarps * 32);
-  return two ? launch_dependent(scan_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_kernel<DT, 1>, grid, block, 0, stream, a);
+  if (two || item == 4) {
+    const bool boxes = tiles_take(a.gate, a.ld_gate, a.spans.rows, item) && tiles_take(a.value, a.ld_value, a.spans.rows, item);
+    return narrow_tiles(a, 32 * W) ? forward_tiled<DT, W, 16>(a, boxes, stream) : forward_tiled<DT, W, 32>(a, boxes, stream);
+  }
+  return forward_tiled<DT, 1, 32>(a, false, stream);      // single columns of 16 bits: rows that start anywhere
 }
 template <int DT, int V, int L, int CL>
-cudaError_t backward_in(const ScanBackArgs& a, const ScanBackMaps& m, cudaStream_t stream) {
-  static PerDeviceInt ready;
-  return launch_tiled<ScanBackArgs, ScanBackMaps>(scan_back_tiled_kernel<DT, V, L, CL>, ready, a, m, TileShape<DT, V, L, 3, CL>::kBytes, CL, stream);
+cudaError_t backward_in(const ScanBackArgs& a, const ScanBackMaps& m, bool boxes, cudaStream_t stream) {
+  static PerDeviceInt ready[2];
+  constexpr uint32_t bytes = TileShape<DT, V, L, 3, CL>::kBytes;
+  if constexpr (V * sizeof(typename Elem<DT>::type) < 4) {
+    return launch_tiled<ScanBackArgs, ScanBackMaps>(scan_back_tiled_kernel<DT, V, L, CL, kRegisters>, ready[0], a, m, bytes, CL, stream);
+  } else {
+    return launch_tiled<ScanBackArgs, ScanBackMaps>(boxes ? scan_back_tiled_kernel<DT, V, L, CL, kBoxes> : scan_back_tiled_kernel<DT, V, L, CL, kOwnCopies>, ready[boxes], a, m, bytes, CL, stream);
+  }
 }
 template <int DT, int V, int L>
-cudaError_t backward_tiled(ScanBackArgs a, cudaStream_t stream) {
+cudaError_t backward_tiled(ScanBackArgs a, bool boxes, cudaStream_t stream) {
   using S = TileShape<DT, V, L, 3, 1>;
   cut(a, S::kColumns);
   ScanBackMaps m;
-  if (!encode_rows<DT, S>(&m.gate, a.gate, a.ld_gate, a.spans, a.width) || !encode_rows<DT, S>(&m.value, a.value, a.ld_value, a.spans, a.width) || !encode_rows<DT, S>(&m.dy, a.dy, a.ld_dy, a.spans, a.width)) return cudaErrorInvalidValue;
+  std::memset(&m, 0, sizeof(m));
+  if (boxes && (!encode_rows<DT, S>(&m.gate, a.gate, a.ld_gate, a.spans, a.width) || !encode_rows<DT, S>(&m.value, a.value, a.ld_value, a.spans, a.width) || !encode_rows<DT, S>(&m.dy, a.dy, a.ld_dy, a.spans, a.width))) return cudaErrorInvalidValue;
   switch (choose_cluster(a.items, a.spans, S::kTileRows)) {
-    case 1: return backward_in<DT, V, L, 1>(a, m, stream);
-    case 2: return backward_in<DT, V, L, 2>(a, m, stream);
-    case 4: return backward_in<DT, V, L, 4>(a, m, stream);
-    default: return backward_in<DT, V, L, 8>(a, m, stream);
+    case 1: return backward_in<DT, V, L, 1>(a, m, boxes, stream);
+    case 2: return backward_in<DT, V, L, 2>(a, m, boxes, stream);
+    case 4: return backward_in<DT, V, L, 4>(a, m, boxes, stream);
+    default: return backward_in<DT, V, L, 8>(a, m, boxes, stream);
   }
 }
 template <int DT>
 cudaError_t launch_backward(ScanBackArgs a, bool two, cudaStream_t stream) {
   constexpr size_t item = sizeof(typename Elem<DT>::type);
   constexpr int W = item == 2 ? 2 : 1;
-  if (a.spans.rows / a.spans.sequences < kShortRows) {
+  if (short_ones(a, two ? W : 1)) {
     cut(a, two ? W : 1);
     const dim3 grid(capped((a.items + kShortThreads - 1) / kShortThreads)), block(kShortThreads);
-    return two ? launch_dependent(scan_back_short_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_back_short_kernel<DT, 1>, grid, block, 0, stream, a);
+    constexpr uint32_t bytes = kShortBlock * kShortThreads * 4;     // of one column
+    return two ? launch_dependent(scan_back_short_kernel<DT, W>, grid, block, W * bytes, stream, a)
+               : launch_dependent(scan_back_short_kernel<DT, 1>, grid, block, bytes, stream, a);
   }
-  if ((two || item == 4) && tiles_take(a.gate, a.ld_gate, a.spans.rows, item) && tiles_take(a.value, a.ld_value, a.spans.rows, item) && tiles_take(a.dy, a.ld_dy, a.spans.rows, item))
-    return narrow_tiles(a, 32 * W) ? backward_tiled<DT, W, 16>(a, stream) : backward_tiled<DT, W, 32>(a, stream);
-  cut(a, 32 * (two ? W : 1));
-  const dim3 grid(capped(a.items)), block(kWarps * 32);
-  return two ? launch_dependent(scan_back_kernel<DT, W>, grid, block, 0, stream, a) : launch_dependent(scan_back_kernel<DT, 1>, grid, block, 0, stream, a);
+  if (two || item == 4) {
+    const bool boxes = tiles_take(a.gate, a.ld_gate, a.spans.rows, item) && tiles_take(a.value, a.ld_value, a.spans.rows, item) && tiles_take(a.dy, a.ld_dy, a.spans.rows, item);
+    return narrow_tiles(a, 32 * W) ? backward_tiled<DT, W, 16>(a, boxes, stream) : backward_tiled<DT, W, 32>(a, boxes, stream);
+  }
+  return backward_tiled<DT, 1, 32>(a, false, stream);      // single columns of 16 bits: rows that start anywhere
 }
 
 int check_shape(uint64_t rows, uint64_t sequences, uint64_t width, int dtype, const void* offsets, int offset_bits) {
