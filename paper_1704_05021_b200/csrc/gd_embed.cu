@@ -6,6 +6,8 @@
 // rows of equal ids in ascending order of their positions, so that nothing is added by atomics and every row of the gradient is
 // written by one sum.  Most of the gradient is the zeros of ids that do not occur (85000 x 500 in fp32: 170 MB, 26 us, for 4000 positions), and
 // the sort is all latency: the launches that sort have CTAs that sort and CTAs that write a share of the zeros meanwhile.
+// Measured: that case 37 us (22 without zeros); 131072 positions over 32000 x 1024 125 us, of which the sums take 66 = 5.7 TB/s, the sort 40 (with
+// 131 MB of zeros under it) and the join of long runs 15; lookup of 131072 rows of 1024 59 us.
 //
 // Sums: the sorted list in chunks of kChunk positions, a CTA per chunk and block of columns.  A run of equal ids that ends in the
 // chunk after the one it begins in belongs to the latter whole; a longer one leaves the sum of its part of each chunk in the workspace, and the
@@ -24,6 +26,10 @@ constexpr uint32_t kTilePer = 4, kTileThreads = 512, kSortTile = kTileThreads * 
 constexpr uint32_t kMostTiles = 128;                   // (every one reads the counts of all)
 constexpr uint32_t kChunk = 32, kShortChunk = 8;       // positions of a chunk; of lists that one CTA sorts (more CTAs, each with less to wait for)
 constexpr uint32_t kFillCtasPerSm = 2;
+// Zeros of many bytes under the sort of one CTA: the launch that sorts writes those of the first rows, the one that sums the
+// rest, of rows that no id has (85000 x 500 in fp32, 4000 positions: 40 us where the sorting launch wrote them all).
+constexpr uint64_t kManyZeros = 32ull << 20, kMostTouched = 1ull << 20;
+constexpr double kFirstZeros = 0.6;
 
 // ---------------------------------------------------------------- lookup
 // A group of `lanes` neighbouring threads (a power of two, up to a warp) takes a row, pieces of up to 16 bytes, kLookAhead of them in hand; the next
@@ -115,6 +121,26 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, uint64_t cta, uint64_t
     }
   }
 }
+// The zeros of the rows [first, end) whose bit of `touched` is not set, a row to a warp.
+struct FillRest {
+  const uint32_t* touched;
+  uint32_t first, end;
+};
+__device__ __forceinline__ void fill_untouched(const Fill& f, const FillRest& rest, uint32_t cta, uint32_t ctas) {
+  const uint32_t lane = threadIdx.x & 31u, warps = blockDim.x / 32u;
+  for (uint64_t r = (uint64_t)rest.first + cta * warps + threadIdx.x / 32u; r < rest.end; r += (uint64_t)ctas * warps) {
+    if (rest.touched[r >> 5] >> (r & 31u) & 1u) continue;
+    const uint32_t bytes = f.width * f.item;
+    unsigned char* row = static_cast<unsigned char*>(f.p) + r * f.ld * f.item;
+    if ((((uintptr_t)row | bytes) & 15u) == 0) {
+      for (uint32_t b = lane * 16u; b < bytes; b += 512u) __stcs(reinterpret_cast<uint4*>(row + b), make_uint4(0u, 0u, 0u, 0u));
+    } else if ((((uintptr_t)row | bytes) & 3u) == 0) {
+      for (uint32_t b = lane * 4u; b < bytes; b += 128u) *reinterpret_cast<uint32_t*>(row + b) = 0u;
+    } else {
+      for (uint32_t b = lane * 2u; b < bytes; b += 64u) *reinterpret_cast<uint16_t*>(row + b) = 0;
+    }
+  }
+}
 __global__ void __launch_bounds__(512) fill_kernel(const __grid_constant__ Fill f) {
   pdl_wait();
   pdl_trigger();
@@ -138,6 +164,7 @@ struct SortArgs {
   uint32_t tiles, per_tile;    // CTAs that sort, positions each takes (a multiple of kSortTile)
   Fill fill;                   // fill.p NULL: nothing
   uint32_t fill_part, fill_parts;      // which share of the zeros this launch writes
+  uint32_t* touched;           // of the sort of one CTA: a bit for every row that is summed into, or NULL
 };
 // what a position is sorted by: its id, or `vocab`, behind all others
 __device__ __forceinline__ uint32_t key_of(const SortArgs& a, uint32_t i) {
@@ -170,15 +197,25 @@ __device__ __forceinline__ uint32_t digit_scan(uint32_t x, uint32_t* s_warp) {
 // in the warps' positions up to it; counts[w][d] afterwards is the number of positions of digit d in the warps before w.
 // Returns, in threads d < kDigits, the number of positions of digit d.  `live`: this thread's positions that exist, as bits.
 template <uint32_t THREADS, uint32_t kPer>
-__device__ __forceinline__ uint32_t rank_digits(const uint32_t (&key)[kPer], uint32_t live, uint32_t shift, uint32_t mask, uint32_t (*counts)[kDigits], uint32_t (&rank)[kPer]) {
+__device__ __forceinline__ uint32_t rank_digits(const uint32_t (&key)[kPer], uint32_t live, uint32_t shift, uint32_t bits, uint32_t (*counts)[kDigits], uint32_t (&rank)[kPer],
+                                                uint32_t rounds = kPer) {
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   for (uint32_t i = threadIdx.x; i < THREADS / 32 * kDigits; i += THREADS) (&counts[0][0])[i] = 0;
   __syncthreads();
 #pragma unroll
   for (uint32_t u = 0; u < kPer; ++u) {
+    if (u >= rounds) break;
     const bool in = live >> u & 1u;
-    const uint32_t d = in ? key[u] >> shift & mask : kDigits;
-    const uint32_t peers = __match_any_sync(0xFFFFFFFFu, d);
+    const uint32_t d = key[u] >> shift & ((1u << bits) - 1u);
+    // the lanes with the same digit, bit by bit (a match over the warp was slower: 25 against 22 us for 4000 positions)
+    uint32_t peers = __ballot_sync(0xFFFFFFFFu, in);
+#pragma unroll
+    for (uint32_t b = 0; b < kDigitBits; ++b) {
+      if (b >= bits) break;
+      const bool set = d >> b & 1u;
+      const uint32_t votes = __ballot_sync(0xFFFFFFFFu, set);
+      peers &= set ? votes : ~votes;
+    }
     const uint32_t before = in ? counts[warp][d] : 0u;
     __syncwarp();
     rank[u] = before + __popc(peers & lanemask_lt());
@@ -214,37 +251,45 @@ __global__ void __launch_bounds__(kOneThreads) sort_one_kernel(const __grid_cons
     fill_share(a, 1u);
     return;
   }
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, first = warp * 32u * kPer + lane;
+  // a warp's positions are neighbours: as many rounds of 32 as there are positions for all warps
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, rounds = (a.n + kOneThreads - 1) / kOneThreads, first = warp * 32u * rounds + lane;
   if (threadIdx.x == 0) a.splits[0] = 0;
   uint32_t key[kPer], at[kPer], rank[kPer], live = 0;
 #pragma unroll
   for (uint32_t u = 0; u < kPer; ++u) {
     const uint32_t i = first + 32u * u;
-    live |= (i < a.n ? 1u : 0u) << u;
-    key[u] = i < a.n ? key_of(a, i) : 0u;
+    const bool in = u < rounds && i < a.n;
+    live |= (in ? 1u : 0u) << u;
+    key[u] = in ? key_of(a, i) : 0u;
     at[u] = i;
   }
+  if (a.touched)
+    for (uint32_t i = threadIdx.x; i < (a.vocab + 31u) / 32u; i += kOneThreads) a.touched[i] = 0;
   const uint32_t mask = (1u << a.bits) - 1u;
   for (uint32_t p = 0; p < a.passes; ++p) {
-    const uint32_t total = rank_digits<kOneThreads, kPer>(key, live, p * a.bits, mask, s.counts, rank);
+    const uint32_t total = rank_digits<kOneThreads, kPer>(key, live, p * a.bits, a.bits, s.counts, rank, rounds);
     const uint32_t base = digit_scan(total, s_warp);
     if (threadIdx.x < kDigits) s_base[threadIdx.x] = base;
     __syncthreads();
-    const bool last = p + 1 == a.passes;
 #pragma unroll
     for (uint32_t u = 0; u < kPer; ++u) {
       if (!(live >> u & 1u)) continue;
       const uint32_t d = key[u] >> (p * a.bits) & mask, to = s_base[d] + s.counts[warp][d] + rank[u];
-      if (last) a.keys_out[to] = key[u], a.at_out[to] = at[u];
-      else s.keys[to] = key[u], s.at[to] = at[u];
+      s.keys[to] = key[u], s.at[to] = at[u];
     }
-    if (last) break;
     __syncthreads();
+    if (p + 1 == a.passes) break;
 #pragma unroll
     for (uint32_t u = 0; u < kPer; ++u) {
       const uint32_t i = first + 32u * u;
-      if (i < a.n) key[u] = s.keys[i], at[u] = s.at[i];
+      if (live >> u & 1u) key[u] = s.keys[i], at[u] = s.at[i];
     }
+  }
+  for (uint32_t i = threadIdx.x; i < a.n; i += kOneThreads) {
+    const uint32_t k = s.keys[i];
+    a.keys_out[i] = k;
+    a.at_out[i] = s.at[i];
+    if (a.touched && k < a.vocab && (i == 0 || s.keys[i - 1] != k)) atomicOr(&a.touched[k >> 5], 1u << (k & 31u));
   }
 }
 
@@ -275,7 +320,7 @@ struct TileSmem {
   uint32_t counts[kTileThreads / 32][kDigits];
 };
 template <bool FIRST>
-__global__ void __launch_bounds__(kTileThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
+__global__ void __launch_bounds__(kTileThreads, 2) sort_place_kernel(const __grid_constant__ SortArgs a) {
   static_assert(kTileThreads == kDigits, "a thread per digit");
   constexpr uint32_t kPer = kTilePer;
   __shared__ TileSmem s;
@@ -302,31 +347,29 @@ __global__ void __launch_bounds__(kTileThreads) sort_place_kernel(const __grid_c
   };
   take(i0);
   uint32_t before = 0, total = 0;      // positions of digit `tid` in the shares before this one, and in all
-#pragma unroll 32
-  for (uint32_t t = 0; t < a.tiles; ++t) {
-    const uint32_t c = a.hist[t * kDigits + tid];
-    before += t < blockIdx.x ? c : 0u;
-    total += c;
+  constexpr uint32_t kBatch = 32;      // loads in hand: the loop is all latency
+  for (uint32_t t0 = 0; t0 < a.tiles; t0 += kBatch) {
+    uint32_t c[kBatch];
+#pragma unroll
+    for (uint32_t t = 0; t < kBatch; ++t) c[t] = t0 + t < a.tiles ? __ldcg(&a.hist[(t0 + t) * kDigits + tid]) : 0u;
+#pragma unroll
+    for (uint32_t t = 0; t < kBatch; ++t) {
+      before += t0 + t < blockIdx.x ? c[t] : 0u;
+      total += c[t];
+    }
   }
   s_base[tid] = digit_scan(total, s_warp) + before;
   for (uint64_t from = i0; from < i1; from += kSortTile) {
     if (from != i0) take(from);
-    const uint32_t here = rank_digits<kTileThreads, kPer>(key, live, a.shift, mask, s.counts, rank);
+    const uint32_t here = rank_digits<kTileThreads, kPer>(key, live, a.shift, a.bits, s.counts, rank);
     __syncthreads();
 #pragma unroll
     for (uint32_t u = 0; u < kPer; ++u) {
-      const bool in = live >> u & 1u;
-      uint32_t count_at = 0xFFFFFFFFu;
-      if (in) {
-        const uint32_t d = key[u] >> a.shift & mask, to = s_base[d] + s.counts[warp][d] + rank[u];
-        a.keys_out[to] = key[u];
-        a.at_out[to] = at[u];
-        count_at = to / a.per_tile * kDigits + (key[u] >> (a.shift + a.bits) & mask);
-      }
-      if (a.next_hist) {                               // (frequent ids have their upper digit in common: one addition for all that a warp has)
-        const uint32_t peers = __match_any_sync(0xFFFFFFFFu, count_at);
-        if (in && lane == (uint32_t)__ffs(peers) - 1u) atomicAdd(&a.next_hist[count_at], (uint32_t)__popc(peers));
-      }
+      if (!(live >> u & 1u)) continue;
+      const uint32_t d = key[u] >> a.shift & mask, to = s_base[d] + s.counts[warp][d] + rank[u];
+      a.keys_out[to] = key[u];
+      a.at_out[to] = at[u];
+      if (a.next_hist) atomicAdd(&a.next_hist[to / a.per_tile * kDigits + (key[u] >> (a.shift + a.bits) & mask)], 1u);
     }
     __syncthreads();
     s_base[tid] += here;
@@ -345,7 +388,17 @@ struct SumArgs {
   uint32_t n, vocab, width, part_ld;
   float scale;
   uint32_t accumulate;
+  Fill fill;                   // zeros that are left to the launch that sums: CTAs behind the first `summing` (in x) write those of `rest`
+  FillRest rest;
+  uint32_t summing;
 };
+// True in a CTA that writes zeros, which are then written.
+__device__ __forceinline__ bool fills(const SumArgs& a) {
+  if (blockIdx.x < a.summing) return false;
+  const uint32_t here = blockIdx.y * (gridDim.x - a.summing) + blockIdx.x - a.summing;
+  fill_untouched(a.fill, a.rest, here, (gridDim.x - a.summing) * gridDim.y);
+  return true;
+}
 template <int GT, int V>
 __device__ __forceinline__ void put_row(const SumArgs& a, uint32_t key, uint32_t c, float (&sum)[V]) {
   using Q = Piece<GT, V>;
@@ -367,6 +420,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
   __shared__ uint32_t s_key[3 * kChunk + 2], s_at[2 * kChunk];      // s_key[j]: of sorted position i0 - kChunk - 1 + j
   pdl_wait();
   pdl_trigger();
+  if (fills(a)) return;
   const uint32_t i0 = blockIdx.x * kChunk, i1 = min(i0 + kChunk, a.n), tid = threadIdx.x;
   constexpr uint32_t kNone = 0xFFFFFFFFu;                            // (a key is at most vocab < 2^31)
   for (uint32_t j = tid; j < 3 * kChunk + 2; j += blockDim.x) {
@@ -461,12 +515,19 @@ __global__ void __launch_bounds__(32 * kJoinWarps) sum_join_kernel(const __grid_
         F::widen(F::load_kept(a.part + ((uint64_t)chunk * 2 + 1) * a.part_ld + c), sum);
       }
       const uint32_t m0 = (uint64_t)more * warp / kJoinWarps, m1 = (uint64_t)more * (warp + 1) / kJoinWarps;
-#pragma unroll 8
-      for (uint32_t m = m0; m < m1; ++m) {
-        float x[V];
-        F::widen(F::load_kept(a.part + ((uint64_t)chunk + 1 + m) * 2 * a.part_ld + c), x);
+      constexpr uint32_t kInHand = 8;
+      for (uint32_t m = m0; m < m1; m += kInHand) {
+        typename F::Raw raw[kInHand];
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] += x[i];
+        for (uint32_t u = 0; u < kInHand; ++u)
+          raw[u] = m + u < m1 ? F::load_kept(a.part + ((uint64_t)chunk + 1 + m + u) * 2 * a.part_ld + c) : F::none();
+#pragma unroll
+        for (uint32_t u = 0; u < kInHand; ++u) {
+          float x[V];
+          F::widen(raw[u], x);
+#pragma unroll
+          for (int i = 0; i < V; ++i) sum[i] += x[i];
+        }
       }
     }
 #pragma unroll
@@ -494,8 +555,8 @@ uint32_t bits_of(uint64_t x) {      // of the largest key
 uint32_t chunk_of(uint64_t n) { return n <= kOneMost ? kShortChunk : kChunk; }
 // Where everything is in the workspace.
 struct Layout {
-  uint64_t keys[2], at[2], hist, splits, part, part_ld, end;
-  Layout(uint64_t n, uint64_t width) {
+  uint64_t keys[2], at[2], hist, splits, touched, part, part_ld, end;
+  Layout(uint64_t n, uint64_t vocab, uint64_t width) {
     uint64_t o = 0;
     const auto take = [&](uint64_t bytes) {
       const uint64_t p = o;
@@ -508,6 +569,7 @@ struct Layout {
     const uint32_t chunk = chunk_of(n);
     const uint64_t chunks = (n + chunk - 1) / chunk;
     splits = take(4 * (chunks + 1));
+    touched = take(one && vocab <= kMostTouched ? (vocab + 31) / 32 * 4 : 0);
     part_ld = up(width, 4);
     part = take(n > 2 * chunk ? chunks * 2 * part_ld * 4 : 0);
     end = std::max<uint64_t>(o, 256);
@@ -612,10 +674,14 @@ cudaError_t launch_sort(SortArgs& a, const Layout& l, unsigned char* ws, const u
 }
 
 template <int DT, int GT, int V>
-cudaError_t launch_sums(const SumArgs& a, cudaStream_t stream) {
+cudaError_t launch_sums(SumArgs a, cudaStream_t stream) {
   const uint32_t pieces = (a.width + V - 1) / V, chunk = chunk_of(a.n), chunks = (a.n + chunk - 1) / chunk;
   const uint32_t threads = std::min(256u, (pieces + 31) / 32 * 32), across = (pieces + threads - 1) / threads;
-  cudaError_t e = launch_dependent(chunk == kShortChunk ? sum_kernel<DT, GT, V, kShortChunk> : sum_kernel<DT, GT, V, kChunk>, dim3(chunks, across), dim3(threads), 0, stream, a);
+  const uint32_t left = a.rest.end - a.rest.first;   // rows whose zeros are left to this launch
+  const uint32_t fillers = left ? std::min((left + 31) / 32, 1024u * (uint32_t)sm_count() / threads / across + 1) : 0u;
+  a.summing = chunks;
+  cudaError_t e = launch_dependent(chunk == kShortChunk ? sum_kernel<DT, GT, V, kShortChunk> : sum_kernel<DT, GT, V, kChunk>, dim3(chunks + fillers, across),
+                                   dim3(threads), 0, stream, a);
   if (e != cudaSuccess) return e;
   note_launches(1);
   if (a.n <= 2 * chunk) return e;                    // (no run can be longer)
@@ -651,7 +717,7 @@ int backward(const gd_embedding_backward_args* g, cudaStream_t stream) {
     return GD_OK;
   }
   if (!g->ids || !aligned_to(g->ids, (size_t)g->id_bits / 8) || !good_matrix(g->dy, g->ld_dy, g->tokens, g->width, dtype_bytes(g->dtype))) return GD_ERR_INVALID_ARG;
-  const Layout l(g->tokens, g->width);
+  const Layout l(g->tokens, g->vocab, g->width);
   if (!g->workspace || !aligned_to(g->workspace, 256) || g->workspace_bytes < l.end) return GD_ERR_WORKSPACE;
   unsigned char* ws = static_cast<unsigned char*>(g->workspace);
   SortArgs s;
@@ -663,6 +729,12 @@ int backward(const gd_embedding_backward_args* g, cudaStream_t stream) {
   s.fill = fill;
   SumArgs a;
   std::memset(&a, 0, sizeof(a));
+  if (fill.p && s.n <= kOneMost && g->vocab <= kMostTouched && g->vocab * g->width * item >= kManyZeros) {
+    s.touched = reinterpret_cast<uint32_t*>(ws + l.touched);
+    s.fill.rows = (uint64_t)(kFirstZeros * (double)g->vocab);
+    a.fill = fill;
+    a.rest = FillRest{s.touched, (uint32_t)s.fill.rows, (uint32_t)g->vocab};
+  }
   if (launch_sort(s, l, ws, &a.keys, &a.at, stream) != cudaSuccess) return GD_ERR_CUDA;
   a.dy = g->dy, a.ld_dy = g->ld_dy;
   a.dtable = g->dtable, a.ld_dtable = g->vocab > 1 ? g->ld_dtable : up(g->width, 4);
@@ -687,7 +759,7 @@ extern "C" {
 int gd_embedding_workspace_bytes(uint64_t tokens, uint64_t vocab, uint64_t width, size_t* bytes_out) {
   if (!bytes_out) return GD_ERR_INVALID_ARG;
   if (tokens >> 31 || vocab >> 31 || width >> 20) return GD_ERR_TOO_LARGE;
-  *bytes_out = (size_t)gd::Layout(tokens, width).end;
+  *bytes_out = (size_t)gd::Layout(tokens, vocab, width).end;
   return GD_OK;
 }
 int gd_embedding_forward(const gd_embedding_forward_args* a, void* stream) { return gd::forward(a, (cudaStream_t)stream); }
