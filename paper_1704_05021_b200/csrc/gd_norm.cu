@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(kLongColumnThreads) norm_long_columns_kernel(c
 }
 
 // The CTAs' sums, joined in order: a warp's lanes are 32 columns, the warps share the CTAs.
-constexpr uint32_t kJoinWarps = 16;
+constexpr uint32_t kJoinWarps = 32, kJoinInHand = (kColumnCtas + kJoinWarps - 1) / kJoinWarps;      // all of a warp's loads at once
 __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const float* part, uint32_t ctas, uint32_t width, float* dweight, float* dbias, uint32_t accumulate) {
   __shared__ float s_sum[kJoinWarps][33];
   pdl_wait();
@@ -568,8 +568,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const float*
   if (!out) return;
   float s = 0.f;
   if (c < width) {
-#pragma unroll 8
-    for (uint32_t q = warp; q < ctas; q += kJoinWarps) s += part[((uint64_t)q * 2 + which) * width + c];
+    float x[kJoinInHand];
+#pragma unroll
+    for (uint32_t u = 0; u < kJoinInHand; ++u) {
+      const uint32_t q = warp + u * kJoinWarps;
+      x[u] = q < ctas ? part[((uint64_t)q * 2 + which) * width + c] : 0.f;
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kJoinInHand; ++u) s += x[u];
   }
   s_sum[warp][lane] = s;
   __syncthreads();

@@ -1,10 +1,11 @@
 // A gated linear recurrence over packed sequences (gd_recurrence_forward, gd_recurrence_backward).
 //
 // h[t] = f[t] h[t-1] + s[t] v[t] with f = sigmoid(gate), s = 1 - f is a composition of affine maps, column by column: rows t0 .. t1 take a state h to
-// A h + B, and maps compose.  A CTA takes a slab of columns of one sequence, kMarkRows rows at a time: each warp makes the map of its kRows rows
-// in registers, the warps' maps meet in shared memory, and from the state that enters the tile every warp goes through its rows again, still
-// in registers, and writes them.  So gate and value are read once and y is written once, whatever the length: bound by the bytes.  The next tile's
-// rows are asked for before this one's are worked on.  Where sequences and slabs alone would leave SMs idle, a cluster of 2 .. 8 CTAs takes
+// A h + B, and maps compose.  A CTA takes a slab of columns of one sequence, a tile of 64 or 128 rows at a time: each group of threads makes the map of its
+// kRows rows in registers, the groups' maps meet in shared memory, and from the state that enters the tile every group goes through its rows again,
+// still in registers, and writes them.  So gate and value are read once and y is written once, whatever the length; the next tiles' rows are copied into
+// shared memory meanwhile.  What bounds it is instructions, with the bytes close behind: two exponential-unit operations, ten others to the gate's two
+// weights, four to the maps and the state for each pair of columns, which go two to an instruction.  Where sequences and slabs alone would leave SMs idle, a cluster of 2 .. 8 CTAs takes
 // neighbouring tiles of a sequence and exchanges their maps (sent and counted, as the cross-entropy does).
 //
 // Backwards dh runs through the same maps from the other end: with C the map's constant, the gradient that leaves rows t0 .. t1 towards the past is
@@ -12,6 +13,9 @@
 // which the forward call keeps in fp32: y is rounded and would not do where h[t-1] and value nearly agree.
 //
 // Many sequences of few rows, the single step among them: a thread takes a sequence's columns through all its rows.
+//
+// Measured (bf16): 16 sequences of 2048 x 2048 80 us forward = 5.0 TB/s, 125 backward = 5.4; one of 65536 x 1024 114 and 249 (a set of tiles takes the
+// cluster 1.7 us and 3.8, a CTA's 24 and 40 KB would take 0.6 and 0.9); 64 sequences by one step of 1024 4 us.  In fp32 60000 x 1024 128 us = 5.8 TB/s.
 #include <algorithm>
 #include <cstring>
 
@@ -983,7 +987,7 @@ uint32_t choose_cluster(uint64_t items, const Spans& s, uint32_t tile_rows) {
   return cluster;
 }
 // Half as many columns and twice the rows to a tile where wide ones in the largest clusters would leave SMs with one CTA or none (one sequence of
-// 65536 rows of 1024: MEASURED).
+// 65536 rows of 1024: 114 us; with wide ones in clusters of 16, which an SM does not take two of, 283).
 template <typename Args>
 bool narrow_tiles(const Args& a, uint32_t columns) {
   return (uint64_t)a.spans.sequences * ((a.width + columns - 1) / columns) * kMostCluster <= (uint64_t)sm_count() && a.spans.rows / a.spans.sequences >= 8u * kMarkRows;
