@@ -215,8 +215,8 @@ __device__ __forceinline__ void exchange_send(Exchange<V, CL, L>& x, uint32_t ra
     }
   }
 }
-// Waits for everybody's maps of `round` and makes the place ready for round + kPlaces (nobody sends for that before all threads here are past
-// a barrier behind this call).  From the state that enters the cluster's tiles, `carry`: what enters this CTA's, and `carry` behind the last.
+// By one warp: waits for everybody's maps of `round` and makes the place ready for round + kPlaces (nobody sends for that before this CTA has sent
+// for a later round, which it does behind a barrier behind this call).  From the state that enters the cluster's tiles, `carry`: what enters this CTA's, and `carry` behind the last.
 template <int V, int CL, bool BACKWARD, int L>
 __device__ __forceinline__ void exchange_fold(Exchange<V, CL, L>& x, uint32_t rank, uint32_t round, float (&mine)[V], float (&carry)[V]) {
   const uint32_t lane = threadIdx.x % L, at = round % kPlaces;
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
   extern __shared__ __align__(128) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
   __shared__ Map<V> s_map[2][kGroups][L];
-  __shared__ float s_state[2][L][V];                // the state behind a tile, of the last group (without a cluster)
+  __shared__ float s_state[2][L][V];                // the state behind a tile, of the last group; in a cluster the one before the CTA's tile
   Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
   __shared__ uint64_t s_full[kDepth];
   const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
@@ -426,8 +426,17 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
       // the map of the next tile is under way to the others while this one's rows are written
       float f[2][N], sv[2][N];
       Map<V> before[2];                              // of the tile's rows before this group's
+      // one warp joins the cluster's maps of a set and leaves the state that enters this CTA's tile for all (read behind the next barrier)
+      const auto join = [&](uint32_t set) __attribute__((always_inline)) {
+        if (threadIdx.x >= 32u) return;
+        float state[V];
+        exchange_fold<V, CL, false>(s_x, rank, round + set, state, h);
+#pragma unroll
+        for (int i = 0; i < V; ++i) s_state[set & 1u][lane][i] = state[i];
+      };
       const auto begin = [&](uint32_t set, float (&fn)[N], float (&svn)[N], Map<V>& before_n) __attribute__((always_inline)) {
         const Map<V> own = evaluate(set * CL + rank, fn, svn);
+        if (set) join(set - 1);
         __syncthreads();
         ask(set + kAhead);
         before_n = identity<V>();
@@ -445,8 +454,11 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
       };
       const auto end = [&](uint32_t set, const float (&fn)[N], const float (&svn)[N], const Map<V>& before_n) __attribute__((always_inline)) {
         float state[V];
-        exchange_fold<V, CL, false>(s_x, rank, round + set, state, h);
-        fma_v<V>(before_n.a, state, before_n.b, state);
+        if (set + 1 == sets) {
+          join(set);
+          __syncthreads();
+        }
+        fma_v<V>(before_n.a, s_state[set & 1u][lane], before_n.b, state);
         apply(set * CL + rank, fn, svn, state);
       };
       if (sets) begin(0, f[0], sv[0], before[0]);
@@ -571,7 +583,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
   extern __shared__ __align__(128) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
   __shared__ Map<V> s_map[2][kGroups][L], s_back[2][kGroups][L];       // of the states, and of the gradient
-  __shared__ float s_carry[2][L][V];                // what leaves a tile towards the past, of the first group (without a cluster)
+  __shared__ float s_carry[2][L][V];                // what leaves a tile towards the past, of the first group; in a cluster what reaches the CTA's tile
   Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
   __shared__ uint64_t s_full[kDepth];
   const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
@@ -751,6 +763,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
       float h[V], next_h[V];
       Map<V> behind, next_behind;                    // of the tile's rows behind this group's
       uint32_t stage = 0, next_stage = 0;
+      // one warp joins the cluster's maps of a set and leaves what reaches this CTA's tile for all (read behind the next barrier)
+      const auto join = [&](uint32_t n) __attribute__((always_inline)) {
+        if (threadIdx.x >= 32u) return;
+        float g[V];
+        exchange_fold<V, CL, true>(s_x, rank, round + n, g, carry);
+#pragma unroll
+        for (int i = 0; i < V; ++i) s_carry[n & 1u][lane][i] = g[i];
+      };
       const auto start = [&](uint32_t n) __attribute__((always_inline)) {
         const uint32_t tile = (sets - 1u - n) * CL + rank;
         mark_of(tile, next_h);
@@ -761,6 +781,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
           read(next_stage, rows_of(tile), x);
           own = leave(x, good);
         }
+        if (n) join(n - 1);
         __syncthreads();
         // (all are past finish of set n - 2: its stage is free)
         ask(n + kAhead);
@@ -783,12 +804,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
 #pragma unroll
         for (int i = 0; i < V; ++i) h[i] = next_h[i];
         behind = next_behind, stage = next_stage;
-        if (n < sets) start(n);
+        if (n < sets) {
+          start(n);
+        } else {
+          join(n - 1);
+          __syncthreads();
+        }
         if (n == 0) continue;
         const uint32_t tile = (sets - n) * CL + rank;
         float g[V];
-        exchange_fold<V, CL, true>(s_x, rank, round + n - 1, g, carry);
-        fma_v<V>(behind.a, g, behind.b, g);
+        fma_v<V>(behind.a, s_carry[(n - 1) & 1u][lane], behind.b, g);
         if (rows_of(tile)) {
           Rows x;
           read(stage, rows_of(tile), x);

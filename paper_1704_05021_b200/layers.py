@@ -141,6 +141,7 @@ def _opt_state(t: Optional[torch.Tensor], name: str, rows: int, cols: int, index
 
 
 _F32 = (torch.float32,)
+_MARK_ROWS = 64             # rows from one of the recurrence's marks to the next
 _INTS = (torch.int64, torch.int32)
 
 
@@ -283,11 +284,10 @@ def recurrence_marks(rows: int, sequences: int, width: int, device="cuda") -> to
 def _marks(marks: Optional[torch.Tensor], rows: int, sequences: int, width: int, index: int) -> int:
     if marks is None:
         return 0
-    count = C.c_uint64(0)
-    B._check(load_library().gd_recurrence_marks_rows(rows, sequences, C.byref(count)), "gd_recurrence_marks_rows")
-    if marks.dtype is not torch.float32 or marks.dim() != 2 or marks.shape[1] != width or marks.shape[0] < count.value or marks.get_device() != index or \
+    count = rows // _MARK_ROWS + sequences             # (what gd_recurrence_marks_rows says, without the call)
+    if marks.dtype is not torch.float32 or marks.dim() != 2 or marks.shape[1] != width or marks.shape[0] < count or marks.get_device() != index or \
             not marks.is_contiguous():
-        raise ValueError(f"marks: expected contiguous torch.float32 [{count.value}, {width}] on cuda:{index}, got {marks.dtype} {list(marks.shape)} on {marks.device}")
+        raise ValueError(f"marks: expected contiguous torch.float32 [{count}, {width}] on cuda:{index}, got {marks.dtype} {list(marks.shape)} on {marks.device}")
     return marks.data_ptr()
 
 

@@ -188,6 +188,8 @@ def test_workspaces_and_marks(lib):
     assert lib.gd_gated_workspace_bytes(1, 1 << 30, 1, 0, C.byref(size)) == LARGE and lib.gd_gated_workspace_bytes(1, 1, 1, 0, None) == INVALID
     count = C.c_uint64(0)
     assert lib.gd_recurrence_marks_rows(640, 3, C.byref(count)) == B.GD_OK and count.value == 13
+    for rows, sequences in ((0, 1), (63, 2), (64, 2), (1000, 7)):
+        assert lib.gd_recurrence_marks_rows(rows, sequences, C.byref(count)) == B.GD_OK and count.value == rows // L._MARK_ROWS + sequences
     assert lib.gd_recurrence_marks_rows(1, 1 << 31, C.byref(count)) == LARGE and lib.gd_recurrence_marks_rows(1, 1, None) == INVALID
 
 
