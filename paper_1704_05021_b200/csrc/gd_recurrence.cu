@@ -14,8 +14,8 @@
 //
 // Many sequences of few rows, the single step among them: a thread takes a sequence's columns through all its rows.
 //
-// Measured (bf16): 16 sequences of 2048 x 2048 80 us forward = 5.0 TB/s, 125 backward = 5.4; one of 65536 x 1024 114 and 249 (a set of tiles takes the
-// cluster 1.7 us and 3.8, a CTA's 24 and 40 KB would take 0.6 and 0.9); 64 sequences by one step of 1024 4 us.  In fp32 60000 x 1024 128 us = 5.8 TB/s.
+// Measured (bf16): 16 sequences of 2048 x 2048 80 us forward = 5.0 TB/s, 125 backward = 5.4; one of 65536 x 1024 106 and 245 (a set of tiles takes the
+// cluster 1.6 us and 3.8, a CTA's 24 and 40 KB would take 0.6 and 0.9); 64 sequences by one step of 1024 4 us.  In fp32 60000 x 1024 128 us = 5.8 TB/s.
 #include <algorithm>
 #include <cstring>
 
@@ -58,6 +58,7 @@ struct ScanArgs {
   float* marks;
   uint32_t width, slabs;
   uint64_t items;              // (sequence, slab)
+  bool by_length;              // long sequences first
 };
 struct ScanBackArgs {
   Spans spans;
@@ -72,6 +73,7 @@ struct ScanBackArgs {
   float* dh0;
   uint32_t width, slabs;
   uint64_t items;
+  bool by_length;
 };
 // the row of marks that holds the state before row 0 of a sequence
 __device__ __forceinline__ uint64_t first_mark(uint32_t sequence, uint32_t first_row) { return (uint64_t)first_row / kMarkRows + sequence; }
@@ -278,6 +280,37 @@ __device__ __forceinline__ void held_rows(typename P::Raw (&held)[kRows], const 
 template <typename P, typename T>
 __device__ __forceinline__ void held_rows(typename P::Raw (&)[1], const T*, uint64_t, uint32_t) {}
 
+// All threads of a CTA: the sequence that `place` others come before in the order by length, the longest first.  One of several times the mean length
+// that begins last runs by itself for most of the others' time: 20000 rows of 2048 in 30 ragged sequences 56 us in that order and 66 by index, backward
+// 78 and 97; 16000 of 1000 in 80 46 and 55 backward.  Every CTA counts what is longer than each sequence: work that grows with the sequences, where its own
+// grows with their length.  Of more sequences than a mean one has rows it costs more than it gives (30000 rows of 1024 in 250: 96 us and 49 by index), and
+// where each SM takes many items there is little to give.
+constexpr uint32_t kMostOrdered = kWarps * 32, kOrderedItems = 10;      // sequences; items to an SM
+struct Chosen {
+  uint32_t sequence, first, count;
+};
+__device__ __forceinline__ void longest_first(const Spans& spans, uint32_t place, uint32_t* keys, Chosen* chosen) {
+  const uint32_t me = threadIdx.x;
+  uint32_t first = 0, count = 0, key = 0;
+  if (me < spans.sequences) {
+    spans.of(me, &first, &count);
+    key = min(count, (1u << 23) - 1u) << 8 | (kMostOrdered - 1u - me) | 1u << 31;
+  }
+  __syncthreads();                                   // (what `keys` held has been read)
+  keys[me] = key;
+  __syncthreads();
+  if (key) {
+    uint32_t before = 0;
+#pragma unroll 4
+    for (uint32_t i = 0; i < spans.sequences; i += 4) {
+      const uint4 k = *reinterpret_cast<const uint4*>(keys + i);
+      before += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+    }
+    if (before == place) *chosen = Chosen{me, first, count};
+  }
+  __syncthreads();
+}
+
 // ---------------------------------------------------------------- forward
 // Rows that tiled copies can read: 16-byte aligned.
 struct ScanMaps {
@@ -292,10 +325,11 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
   constexpr int R = kRows, N = R * V;                // row k's columns at k V
   extern __shared__ __align__(128) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
-  __shared__ Map<V> s_map[2][kGroups][L];
+  __shared__ __align__(16) Map<V> s_map[2][kGroups][L];
   __shared__ float s_state[2][L][V];                // the state behind a tile, of the last group; in a cluster the one before the CTA's tile
   Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
   __shared__ uint64_t s_full[kDepth];
+  __shared__ Chosen s_chosen;
   const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
@@ -309,9 +343,14 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
   uint32_t round = 0, asked = 0, taken = 0, turn = 0;
   const uint64_t stride = gridDim.x / CL;
   for (uint64_t item = blockIdx.x / CL; item < a.items; item += stride) {
-    const uint32_t seq = (uint32_t)(item / a.slabs), col0 = (uint32_t)(item % a.slabs) * kColumns, c = col0 + lane * V;
-    uint32_t first, count;
-    a.spans.of(seq, &first, &count);
+    uint32_t seq = (uint32_t)(item / a.slabs), first, count;
+    const uint32_t col0 = (uint32_t)(item % a.slabs) * kColumns, c = col0 + lane * V;
+    if (CL == 1 && a.by_length) {
+      longest_first(a.spans, seq, reinterpret_cast<uint32_t*>(s_map), &s_chosen);
+      seq = s_chosen.sequence, first = s_chosen.first, count = s_chosen.count;
+    } else {
+      a.spans.of(seq, &first, &count);
+    }
     const bool in = c < a.width;
     T* y = static_cast<T*>(a.y) + (uint64_t)first * a.ld_y + c;
     const uint64_t mark0 = first_mark(seq, first);
@@ -582,10 +621,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
   constexpr int R = kRows, N = R * V;                // row k's columns at k V
   extern __shared__ __align__(128) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
-  __shared__ Map<V> s_map[2][kGroups][L], s_back[2][kGroups][L];       // of the states, and of the gradient
+  __shared__ __align__(16) Map<V> s_map[2][kGroups][L], s_back[2][kGroups][L];       // of the states, and of the gradient
   __shared__ float s_carry[2][L][V];                // what leaves a tile towards the past, of the first group; in a cluster what reaches the CTA's tile
   Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
   __shared__ uint64_t s_full[kDepth];
+  __shared__ Chosen s_chosen;
   const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
@@ -599,9 +639,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
   uint32_t round = 0, asked = 0, taken = 0, turn = 0;
   const uint64_t stride = gridDim.x / CL;
   for (uint64_t item = blockIdx.x / CL; item < a.items; item += stride) {
-    const uint32_t seq = (uint32_t)(item / a.slabs), col0 = (uint32_t)(item % a.slabs) * kColumns, c = col0 + lane * V;
-    uint32_t first, count;
-    a.spans.of(seq, &first, &count);
+    uint32_t seq = (uint32_t)(item / a.slabs), first, count;
+    const uint32_t col0 = (uint32_t)(item % a.slabs) * kColumns, c = col0 + lane * V;
+    if (CL == 1 && a.by_length) {
+      longest_first(a.spans, seq, reinterpret_cast<uint32_t*>(s_map), &s_chosen);
+      seq = s_chosen.sequence, first = s_chosen.first, count = s_chosen.count;
+    } else {
+      a.spans.of(seq, &first, &count);
+    }
     const bool in = c < a.width;
     T* dgate = static_cast<T*>(a.dgate) + (uint64_t)first * a.ld_dgate + c;
     T* dvalue = static_cast<T*>(a.dvalue) + (uint64_t)first * a.ld_dvalue + c;
@@ -1004,6 +1049,8 @@ template <typename Args>
 void cut(Args& a, uint32_t columns) {
   a.slabs = (a.width + columns - 1) / columns;
   a.items = (uint64_t)a.spans.sequences * a.slabs;
+  a.by_length = a.spans.offsets && a.spans.sequences > 1 && a.spans.sequences <= std::min(kMostOrdered, a.spans.rows / a.spans.sequences) &&
+                a.items > 2ull * sm_count() && a.items <= (uint64_t)kOrderedItems * sm_count();
 }
 // CTAs per sequence and slab: more while two of them would still fit every SM and each has two tiles or more.
 uint32_t choose_cluster(uint64_t items, const Spans& s, uint32_t tile_rows) {
@@ -1012,7 +1059,7 @@ uint32_t choose_cluster(uint64_t items, const Spans& s, uint32_t tile_rows) {
   return cluster;
 }
 // Half as many columns and twice the rows to a tile where wide ones in the largest clusters would leave SMs with one CTA or none (one sequence of
-// 65536 rows of 1024: 114 us; with wide ones in clusters of 16, which an SM does not take two of, 283).
+// 65536 rows of 1024: 106 us; with wide ones in clusters of 16, which an SM does not take two of, 283).
 template <typename Args>
 bool narrow_tiles(const Args& a, uint32_t columns) {
   return (uint64_t)a.spans.sequences * ((a.width + columns - 1) / columns) * kMostCluster <= (uint64_t)sm_count() && a.spans.rows / a.spans.sequences >= 8u * kMarkRows;

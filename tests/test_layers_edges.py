@@ -122,6 +122,14 @@ def test_recurrence_in_clusters_of_every_size(cuda_device, sequences, rows, widt
     _check_recurrence(cuda_device, lengths, width, dtype, False, seed=rows)
 
 
+@pytest.mark.parametrize("sequences, width, dtype, bits", [(3, 6400, BF16, 64), (40, 520, BF16, 64), (41, 1000, torch.float16, 32), (40, 300, torch.float32, 64),
+                                                           (70, 321, BF16, 32)])
+def test_recurrence_in_the_order_of_lengths(cuda_device, sequences, width, dtype, bits):
+    """More items than run at once: empty sequences, many of one length, the longest last."""
+    lengths = [(0, 40, 40, 97, 1)[i % 5] for i in range(sequences - 1)]
+    _check_recurrence(cuda_device, lengths + [sequences * sequences - sum(lengths) + 300], width, dtype, width % 2 == 0, 2, 1, bits=bits)
+
+
 def test_matrices_past_32_bits(cuda_device):
     """More than 2^31 elements: the last rows are those of a call on them alone."""
     rows, width = (1 << 20) + 37, 2056
