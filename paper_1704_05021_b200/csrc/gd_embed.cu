@@ -6,8 +6,8 @@
 // rows of equal ids in ascending order of their positions, so that nothing is added by atomics and every row of the gradient is
 // written by one sum.  Most of the gradient is the zeros of ids that do not occur (85000 x 500 in fp32: 170 MB, 26 us, for 4000 positions), and
 // the sort is all latency: the launches that sort have CTAs that sort and CTAs that write a share of the zeros meanwhile.
-// Measured: that case 37 us (22 without zeros); 131072 positions over 32000 x 1024 125 us, of which the sums take 66 = 5.7 TB/s, the sort 40 (with
-// 131 MB of zeros under it) and the join of long runs 15; lookup of 131072 rows of 1024 59 us.
+// Measured: that case 37 us (22 without zeros); 131072 positions over 32000 x 1024 113 us, of which the sums take 66 = 5.7 TB/s, the sort 27
+// and the join of long runs 15; lookup of 131072 rows of 1024 59 us.
 //
 // Sums: the sorted list in chunks of kChunk positions, a CTA per chunk and block of columns.  A run of equal ids that ends in the
 // chunk after the one it begins in belongs to the latter whole; a longer one leaves the sum of its part of each chunk in the workspace, and the
@@ -30,6 +30,10 @@ constexpr uint32_t kFillCtasPerSm = 2;
 // rest, of rows that no id has (85000 x 500 in fp32, 4000 positions: 40 us where the sorting launch wrote them all).
 constexpr uint64_t kManyZeros = 32ull << 20, kMostTouched = 1ull << 20;
 constexpr double kFirstZeros = 0.6;
+// Under the sort of many the zeros cost it their bytes at 8 TB/s.  Where there are positions enough for most rows, the launch that sums writes those of
+// the others alone, before all else (131072 positions over 32000 x 1024: 113 us and 124 with all zeros under the sort, ids evenly spread 97 and 116; 40000
+// over 85000 x 500 71 and 65).
+constexpr uint64_t kDense = 2;         // positions to a row of the table
 
 // ---------------------------------------------------------------- lookup
 // A group of `lanes` neighbouring threads (a power of two, up to a warp) takes a row, pieces of up to 16 bytes, kLookAhead of them in hand; the next
@@ -121,23 +125,37 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, uint64_t cta, uint64_t
     }
   }
 }
-// The zeros of the rows [first, end) whose bit of `touched` is not set, a row to a warp.
+// The zeros of the rows [first, end) that no id has: those whose bit of `touched` is not set, a row to a warp, or, without such bits, that are not among
+// the n sorted keys, which a warp looks for 32 at a time.
 struct FillRest {
   const uint32_t* touched;
   uint32_t first, end;
 };
-__device__ __forceinline__ void fill_untouched(const Fill& f, const FillRest& rest, uint32_t cta, uint32_t ctas) {
-  const uint32_t lane = threadIdx.x & 31u, warps = blockDim.x / 32u;
-  for (uint64_t r = (uint64_t)rest.first + cta * warps + threadIdx.x / 32u; r < rest.end; r += (uint64_t)ctas * warps) {
-    if (rest.touched[r >> 5] >> (r & 31u) & 1u) continue;
-    const uint32_t bytes = f.width * f.item;
-    unsigned char* row = static_cast<unsigned char*>(f.p) + r * f.ld * f.item;
-    if ((((uintptr_t)row | bytes) & 15u) == 0) {
-      for (uint32_t b = lane * 16u; b < bytes; b += 512u) __stcs(reinterpret_cast<uint4*>(row + b), make_uint4(0u, 0u, 0u, 0u));
-    } else if ((((uintptr_t)row | bytes) & 3u) == 0) {
-      for (uint32_t b = lane * 4u; b < bytes; b += 128u) *reinterpret_cast<uint32_t*>(row + b) = 0u;
-    } else {
-      for (uint32_t b = lane * 2u; b < bytes; b += 64u) *reinterpret_cast<uint16_t*>(row + b) = 0;
+__device__ __forceinline__ void fill_untouched(const Fill& f, const FillRest& rest, const uint32_t* keys, uint32_t n, uint32_t cta, uint32_t ctas) {
+  const uint32_t lane = threadIdx.x & 31u, warps = blockDim.x / 32u, bytes = f.width * f.item, each = rest.touched ? 1u : 32u;
+  for (uint64_t r0 = rest.first + (uint64_t)(cta * warps + threadIdx.x / 32u) * each; r0 < rest.end; r0 += (uint64_t)ctas * warps * each) {
+    const uint64_t mine = r0 + lane;
+    bool none = lane < each && mine < rest.end;
+    if (none && rest.touched) {
+      none = !(rest.touched[mine >> 5] >> (mine & 31u) & 1u);
+    } else if (none) {
+      uint32_t from = 0, to = n;                     // the first key that is not below it
+      while (from < to) {
+        const uint32_t half = from + (to - from) / 2u;
+        if (keys[half] < mine) from = half + 1u;
+        else to = half;
+      }
+      none = from == n || keys[from] != mine;
+    }
+    for (uint32_t left = __ballot_sync(0xFFFFFFFFu, none); left; left &= left - 1u) {
+      unsigned char* row = static_cast<unsigned char*>(f.p) + (r0 + __ffs(left) - 1u) * f.ld * f.item;
+      if ((((uintptr_t)row | bytes) & 15u) == 0) {
+        for (uint32_t b = lane * 16u; b < bytes; b += 512u) __stcs(reinterpret_cast<uint4*>(row + b), make_uint4(0u, 0u, 0u, 0u));
+      } else if ((((uintptr_t)row | bytes) & 3u) == 0) {
+        for (uint32_t b = lane * 4u; b < bytes; b += 128u) *reinterpret_cast<uint32_t*>(row + b) = 0u;
+      } else {
+        for (uint32_t b = lane * 2u; b < bytes; b += 64u) *reinterpret_cast<uint16_t*>(row + b) = 0;
+      }
     }
   }
 }
@@ -388,17 +406,10 @@ struct SumArgs {
   uint32_t n, vocab, width, part_ld;
   float scale;
   uint32_t accumulate;
-  Fill fill;                   // zeros that are left to the launch that sums: CTAs behind the first `summing` (in x) write those of `rest`
+  Fill fill;                   // zeros that are left to the launch that sums: its first `fillers` CTAs (in x) write those of `rest`
   FillRest rest;
-  uint32_t summing;
+  uint32_t fillers;
 };
-// True in a CTA that writes zeros, which are then written.
-__device__ __forceinline__ bool fills(const SumArgs& a) {
-  if (blockIdx.x < a.summing) return false;
-  const uint32_t here = blockIdx.y * (gridDim.x - a.summing) + blockIdx.x - a.summing;
-  fill_untouched(a.fill, a.rest, here, (gridDim.x - a.summing) * gridDim.y);
-  return true;
-}
 template <int GT, int V>
 __device__ __forceinline__ void put_row(const SumArgs& a, uint32_t key, uint32_t c, float (&sum)[V]) {
   using Q = Piece<GT, V>;
@@ -420,8 +431,11 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
   __shared__ uint32_t s_key[3 * kChunk + 2], s_at[2 * kChunk];      // s_key[j]: of sorted position i0 - kChunk - 1 + j
   pdl_wait();
   pdl_trigger();
-  if (fills(a)) return;
-  const uint32_t i0 = blockIdx.x * kChunk, i1 = min(i0 + kChunk, a.n), tid = threadIdx.x;
+  if (blockIdx.x < a.fillers) {
+    fill_untouched(a.fill, a.rest, a.keys, a.n, blockIdx.y * a.fillers + blockIdx.x, a.fillers * gridDim.y);
+    return;
+  }
+  const uint32_t chunk = blockIdx.x - a.fillers, i0 = chunk * kChunk, i1 = min(i0 + kChunk, a.n), tid = threadIdx.x;
   constexpr uint32_t kNone = 0xFFFFFFFFu;                            // (a key is at most vocab < 2^31)
   for (uint32_t j = tid; j < 3 * kChunk + 2; j += blockDim.x) {
     const int64_t i = (int64_t)i0 - kChunk - 1 + j;
@@ -445,12 +459,12 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
     goes = key[2 * kChunk] == last;
     if (!goes)
       while (key[end] == last) ++end;                                // (ends before 2 kChunk: key[2 kChunk] is another)
-    if (goes && last < a.vocab && tid == 0 && blockIdx.y == 0) a.splits[1u + atomicAdd(&a.splits[0], 1u)] = blockIdx.x;
+    if (goes && last < a.vocab && tid == 0 && blockIdx.y == 0) a.splits[1u + atomicAdd(&a.splits[0], 1u)] = chunk;
   }
   while (end > j && key[end - 1] >= a.vocab) --end;                  // positions without a row of the table
   if (c >= a.width || j >= end) return;
   const auto* dy = static_cast<const typename Elem<DT>::type*>(a.dy) + c;
-  float* part = a.part + (uint64_t)blockIdx.x * 2 * a.part_ld + c;
+  float* part = a.part + (uint64_t)chunk * 2 * a.part_ld + c;
   float sum[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) sum[i] = 0.f;
@@ -679,7 +693,7 @@ cudaError_t launch_sums(SumArgs a, cudaStream_t stream) {
   const uint32_t threads = std::min(256u, (pieces + 31) / 32 * 32), across = (pieces + threads - 1) / threads;
   const uint32_t left = a.rest.end - a.rest.first;   // rows whose zeros are left to this launch
   const uint32_t fillers = left ? std::min((left + 31) / 32, 1024u * (uint32_t)sm_count() / threads / across + 1) : 0u;
-  a.summing = chunks;
+  a.fillers = fillers;
   cudaError_t e = launch_dependent(chunk == kShortChunk ? sum_kernel<DT, GT, V, kShortChunk> : sum_kernel<DT, GT, V, kChunk>, dim3(chunks + fillers, across),
                                    dim3(threads), 0, stream, a);
   if (e != cudaSuccess) return e;
@@ -734,6 +748,11 @@ int backward(const gd_embedding_backward_args* g, cudaStream_t stream) {
     s.fill.rows = (uint64_t)(kFirstZeros * (double)g->vocab);
     a.fill = fill;
     a.rest = FillRest{s.touched, (uint32_t)s.fill.rows, (uint32_t)g->vocab};
+  }
+  if (fill.p && s.n > kOneMost && s.n >= kDense * g->vocab) {
+    s.fill.p = nullptr;
+    a.fill = fill;
+    a.rest = FillRest{nullptr, 0u, (uint32_t)g->vocab};
   }
   if (launch_sort(s, l, ws, &a.keys, &a.at, stream) != cudaSuccess) return GD_ERR_CUDA;
   a.dy = g->dy, a.ld_dy = g->ld_dy;

@@ -130,6 +130,22 @@ def test_recurrence_in_the_order_of_lengths(cuda_device, sequences, width, dtype
     _check_recurrence(cuda_device, lengths + [sequences * sequences - sum(lengths) + 300], width, dtype, width % 2 == 0, 2, 1, bits=bits)
 
 
+@pytest.mark.parametrize("tokens, vocab, width, ld", [(9000, 4500, 1204, 1204), (9001, 4499, 1203, 1210), (8200, 33, 2100, 2100), (20000, 9999, 4, 5)])
+def test_embedding_gradient_of_many_positions(cuda_device, tokens, vocab, width, ld):
+    """Positions enough for most rows: every row that no id has is zero, wherever it lies, and nothing between the rows is touched."""
+    gen = _gen(cuda_device, tokens)
+    ids = torch.randint(vocab // 3, vocab - vocab // 4, (tokens,), generator=gen, device=cuda_device)      # none of the first and of the last rows
+    ids[::7] = -100
+    dy = _rand(gen, tokens, width, dtype=BF16)
+    room = torch.full((vocab, ld), float("nan"), device=cuda_device)
+    room[:, width:] = 5.0
+    L.EmbeddingSession(vocab, width, tokens, device=cuda_device).backward(dy, ids, room[:, :width])
+    live = ids >= 0
+    ref = torch.zeros(vocab, width, dtype=torch.float64, device=cuda_device).index_add_(0, ids[live], dy[live].double())
+    size = torch.zeros_like(ref).index_add_(0, ids[live], dy[live].double().abs())
+    assert ((room[:, :width].double() - ref).abs() <= (tokens + 2) * 2.0 ** -24 * size).all() and bool((room[:, width:] == 5.0).all())
+
+
 def test_matrices_past_32_bits(cuda_device):
     """More than 2^31 elements: the last rows are those of a call on them alone."""
     rows, width = (1 << 20) + 37, 2056
