@@ -68,6 +68,7 @@ typedef struct gd_embedding_backward_args {
 } gd_embedding_backward_args;
 
 int gd_embedding_backward(const gd_embedding_backward_args* args, void* stream);
+/* Workspace of the call above for up to that many tokens. */
 int gd_embedding_workspace_bytes(uint64_t tokens, uint64_t vocab, uint64_t width, size_t* bytes_out);
 
 /*

@@ -590,6 +590,10 @@ struct Layout {
     end = std::max<uint64_t>(o, 256);
   }
 };
+// Of any number of positions up to n: short lists are cut into shorter chunks, so the longest of them may want more than n do.
+uint64_t workspace_up_to(uint64_t n, uint64_t vocab, uint64_t width) {
+  return std::max(Layout(n, vocab, width).end, Layout(std::min<uint64_t>(n, kOneMost), vocab, width).end);
+}
 
 template <int DT, int OT, int V>
 cudaError_t launch_pieces(EmbedArgs a, uint32_t width, cudaStream_t stream) {
@@ -779,7 +783,7 @@ extern "C" {
 int gd_embedding_workspace_bytes(uint64_t tokens, uint64_t vocab, uint64_t width, size_t* bytes_out) {
   if (!bytes_out) return GD_ERR_INVALID_ARG;
   if (tokens >> 31 || vocab >> 31 || width >> 20) return GD_ERR_TOO_LARGE;
-  *bytes_out = (size_t)gd::Layout(tokens, vocab, width).end;
+  *bytes_out = (size_t)gd::workspace_up_to(tokens, vocab, width);
   return GD_OK;
 }
 int gd_embedding_forward(const gd_embedding_forward_args* a, void* stream) { return gd::forward(a, (cudaStream_t)stream); }
