@@ -646,7 +646,9 @@ cudaError_t launch_backward(NormBackArgs a, uint32_t* ctas, cudaStream_t stream)
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
+  e = cudaLaunchKernelEx(&cfg, kernel, a);
+  if (e == cudaSuccess) note_launches(1);
+  return e;
 }
 // Up to 64 elements to a thread, so that what a row costs beside its elements is shared by many, and eight threads at least, so that they read whole
 // lines.  Single elements of 16 bits take a register each: half as many (20000 x 1001: 26 against 35 us).
@@ -703,7 +705,10 @@ cudaError_t backward_t(const NormBackArgs& a, uint32_t* ctas, cudaStream_t strea
       if (e != cudaSuccess) return e;
       note_launches(1);
     }
-    return a.dx ? launch_dependent(norm_back_long_kernel<DT>, dim3(std::min(a.rows, 2u * (uint32_t)sm_count())), dim3(kMostThreads), 0, stream, a) : cudaSuccess;
+    if (!a.dx) return cudaSuccess;
+    const cudaError_t e = launch_dependent(norm_back_long_kernel<DT>, dim3(std::min(a.rows, 2u * (uint32_t)sm_count())), dim3(kMostThreads), 0, stream, a);
+    if (e == cudaSuccess) note_launches(1);
+    return e;
   }
   const auto takes = [&](uint32_t v) {
     return in_pieces(a.x, a.ldx, a.rows, a.width, item, v) && in_pieces(a.dy, a.ld_dy, a.rows, a.width, item, v) &&
@@ -790,7 +795,6 @@ int backward(const gd_layer_norm_backward_args* g, cudaStream_t stream) {
                           : g->dtype == GD_DTYPE_BF16 ? backward_t<GD_DTYPE_BF16>(a, &ctas, stream)
                                                       : backward_t<GD_DTYPE_FP16>(a, &ctas, stream);
     if (e != cudaSuccess) return GD_ERR_CUDA;
-    note_launches(1);
   }
   if (sums && (ctas || !rows)) {
     ProfileScope ps(stream, PT_NORM_JOIN);
