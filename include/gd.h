@@ -346,7 +346,9 @@ int gd_compress_static(const gd_compress_args* args, void* stream, const void** 
  * 13 setup and prediction in one launch, 14 dense histogram pass, 15 walk of the dense histogram,
  * 16 add, selection and compaction of a short vector in one launch; the operators of gd_train.h: 17 layout of a
  * ragged operand, 18 activation slope and bias gradient, 19 product of few tiles, 20 cross-entropy, 21 AdamW, 22 and 23 product of many tiles,
- * 256 x 256 and 256 x 128), then forgets them.
+ * 256 x 256 and 256 x 128; those of gd_layers.h: 24 layer norm, 25 its gradient, 26 the join of its sums of columns,
+ * 27 embedding lookup, 28 a launch of the sort of ids, 29 sums of rows, 34 the join of long runs, 35 zeros of a whole table, 30 and 31
+ * recurrence and its gradient, 32 gated projections, 33 their slope and bias gradient), then forgets them.
  * At most 4096 pairs are held between two collects; later launches are not recorded.  Not thread-safe.
  */
 int gd_profile_enable(int mode);

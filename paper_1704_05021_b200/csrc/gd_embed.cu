@@ -664,6 +664,7 @@ cudaError_t launch_sort(SortArgs& a, const Layout& l, unsigned char* ws, const u
     a.keys_out = keys_at(0), a.at_out = at_at(0);
     a.fill_part = 0, a.fill_parts = 1;
     *keys = a.keys_out, *at = a.at_out;
+    ProfileScope ps(stream, PT_EMBED_SORT);
     note_launches(1);
     return launch_dependent(sort_one_kernel, dim3(1 + std::min(fillers(1, 1), (uint32_t)std::max(1, sm_count() - 1))), dim3(kOneThreads), sizeof(OneSmem), stream, a);
   }
@@ -674,9 +675,14 @@ cudaError_t launch_sort(SortArgs& a, const Layout& l, unsigned char* ws, const u
   a.hist = hist;
   a.fill_parts = 1 + a.passes;
   const dim3 grid(a.tiles + fillers(a.fill_parts, kFillCtasPerSm)), block(kTileThreads);
-  cudaError_t e = launch_dependent(sort_count_kernel, grid, block, 0, stream, a);
+  const auto launch = [&](void (*kernel)(SortArgs)) {
+    ProfileScope ps(stream, PT_EMBED_SORT);
+    const cudaError_t e = launch_dependent(kernel, grid, block, 0, stream, a);
+    if (e == cudaSuccess) note_launches(1);
+    return e;
+  };
+  cudaError_t e = launch(sort_count_kernel);
   if (e != cudaSuccess) return e;
-  note_launches(1);
   for (uint32_t p = 0; p < a.passes; ++p) {
     a.shift = p * a.bits;
     a.hist = hist + (uint64_t)p * kMostTiles * kDigits;
@@ -684,9 +690,8 @@ cudaError_t launch_sort(SortArgs& a, const Layout& l, unsigned char* ws, const u
     if (p) a.keys_in = keys_at((p - 1) & 1u), a.at_in = at_at((p - 1) & 1u);
     a.keys_out = keys_at(p & 1u), a.at_out = at_at(p & 1u);
     a.fill_part = p + 1;
-    e = launch_dependent(p ? sort_place_kernel<false> : sort_place_kernel<true>, grid, block, 0, stream, a);
+    e = launch(p ? sort_place_kernel<false> : sort_place_kernel<true>);
     if (e != cudaSuccess) return e;
-    note_launches(1);
   }
   *keys = a.keys_out, *at = a.at_out;
   return cudaSuccess;
@@ -699,13 +704,18 @@ cudaError_t launch_sums(SumArgs a, cudaStream_t stream) {
   const uint32_t left = a.rest.end - a.rest.first;   // rows whose zeros are left to this launch
   const uint32_t fillers = left ? std::min((left + 31) / 32, 1024u * (uint32_t)sm_count() / threads / across + 1) : 0u;
   a.fillers = fillers;
-  cudaError_t e = launch_dependent(chunk == kShortChunk ? sum_kernel<DT, GT, V, kShortChunk> : sum_kernel<DT, GT, V, kChunk>, dim3(chunks + fillers, across),
-                                   dim3(threads), 0, stream, a);
-  if (e != cudaSuccess) return e;
-  note_launches(1);
-  if (a.n <= 2 * chunk) return e;                    // (no run can be longer)
+  {
+    ProfileScope ps(stream, PT_EMBED_SUM);
+    const cudaError_t e = launch_dependent(chunk == kShortChunk ? sum_kernel<DT, GT, V, kShortChunk> : sum_kernel<DT, GT, V, kChunk>, dim3(chunks + fillers, across),
+                                           dim3(threads), 0, stream, a);
+    if (e != cudaSuccess) return e;
+    note_launches(1);
+  }
+  if (a.n <= 2 * chunk) return cudaSuccess;          // (no run can be longer)
   const uint32_t blocks = (a.width + 32 * V - 1) / (32 * V);
-  e = launch_dependent(sum_join_kernel<GT, V>, dim3(std::min(chunks, std::max(1u, 8u * (uint32_t)sm_count() / blocks)), blocks), dim3(32 * kJoinWarps), 0, stream, a, chunk);
+  ProfileScope ps(stream, PT_EMBED_JOIN);
+  const cudaError_t e = launch_dependent(sum_join_kernel<GT, V>, dim3(std::min(chunks, std::max(1u, 8u * (uint32_t)sm_count() / blocks)), blocks), dim3(32 * kJoinWarps),
+                                         0, stream, a, chunk);
   if (e == cudaSuccess) note_launches(1);
   return e;
 }
@@ -729,8 +739,8 @@ int backward(const gd_embedding_backward_args* g, cudaStream_t stream) {
   Fill fill;
   std::memset(&fill, 0, sizeof(fill));
   fill.p = accumulate ? nullptr : g->dtable, fill.ld = g->ld_dtable, fill.rows = g->vocab, fill.width = (uint32_t)g->width, fill.item = (uint32_t)item;
-  ProfileScope ps(stream, PT_EMBED_SORT);
   if (g->tokens == 0) {
+    ProfileScope ps(stream, PT_EMBED_FILL);
     if (launch_dependent(fill_kernel, dim3(4 * sm_count()), dim3(512), 0, stream, fill) != cudaSuccess) return GD_ERR_CUDA;
     note_launches(1);
     return GD_OK;

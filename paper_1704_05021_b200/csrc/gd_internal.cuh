@@ -370,7 +370,8 @@ enum ProfileTag : uint32_t { PT_SETUP = 0, PT_PACK_SAMPLED = 9, PT_MEANS = 10, P
                              PT_LINEAR_PACK = 17, PT_LINEAR_SLOPE = 18, PT_LINEAR = 19, PT_XENT = 20, PT_ADAMW = 21,
                              PT_LINEAR_PAIR = 22, PT_LINEAR_PAIR_NARROW = 23,
                              PT_NORM = 24, PT_NORM_BACK = 25, PT_NORM_JOIN = 26, PT_EMBED = 27, PT_EMBED_SORT = 28, PT_EMBED_SUM = 29,
-                             PT_RECURRENCE = 30, PT_RECURRENCE_BACK = 31, PT_GATED = 32, PT_GATED_SLOPE = 33 };
+                             PT_RECURRENCE = 30, PT_RECURRENCE_BACK = 31, PT_GATED = 32, PT_GATED_SLOPE = 33,
+                             PT_EMBED_JOIN = 34, PT_EMBED_FILL = 35 };
 void profile_mark(cudaStream_t stream, bool begin, uint32_t tag);
 struct ProfileScope {   // records an event pair around the launches made during its lifetime
   cudaStream_t stream;

@@ -646,6 +646,7 @@ cudaError_t launch_backward(NormBackArgs a, uint32_t* ctas, cudaStream_t stream)
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.cluster > 1 ? 2 : 1;
+  ProfileScope ps(stream, PT_NORM_BACK);
   e = cudaLaunchKernelEx(&cfg, kernel, a);
   if (e == cudaSuccess) note_launches(1);
   return e;
@@ -701,11 +702,13 @@ cudaError_t backward_t(const NormBackArgs& a, uint32_t* ctas, cudaStream_t strea
     if (a.part) {      // (first: dx may take dy's place)
       const uint32_t across = (a.width + kLongColumnThreads - 1) / kLongColumnThreads;
       *ctas = std::min(a.rows, std::min(kColumnCtas, std::max(1u, 4u * (uint32_t)sm_count() / across)));
+      ProfileScope ps(stream, PT_NORM_BACK);
       const cudaError_t e = launch_dependent(norm_long_columns_kernel<DT>, dim3(across, *ctas), dim3(kLongColumnThreads), 0, stream, a);
       if (e != cudaSuccess) return e;
       note_launches(1);
     }
     if (!a.dx) return cudaSuccess;
+    ProfileScope ps(stream, PT_NORM_BACK);
     const cudaError_t e = launch_dependent(norm_back_long_kernel<DT>, dim3(std::min(a.rows, 2u * (uint32_t)sm_count())), dim3(kMostThreads), 0, stream, a);
     if (e == cudaSuccess) note_launches(1);
     return e;
@@ -790,7 +793,6 @@ int backward(const gd_layer_norm_backward_args* g, cudaStream_t stream) {
     a.mean = g->mean, a.rstd = g->rstd;
     a.rows = (uint32_t)rows, a.width = (uint32_t)width;
     a.wide_params = g->param_dtype == GD_DTYPE_FP32;
-    ProfileScope ps(stream, PT_NORM_BACK);
     const cudaError_t e = g->dtype == GD_DTYPE_FP32   ? backward_t<GD_DTYPE_FP32>(a, &ctas, stream)
                           : g->dtype == GD_DTYPE_BF16 ? backward_t<GD_DTYPE_BF16>(a, &ctas, stream)
                                                       : backward_t<GD_DTYPE_FP16>(a, &ctas, stream);
