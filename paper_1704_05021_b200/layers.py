@@ -147,7 +147,7 @@ _INTS = (torch.int64, torch.int32)
 
 class EmbeddingSession:
     """The shape of an embedding table - vocab rows of width elements - and the workspace that its gradient for up to max_tokens positions takes
-    (gradient=False: none, for a program that only looks up).
+    (gradient=False: none, for a program that only looks up).  A lookup takes any number of them.
 
     ids are vectors of int32 or int64.  A position whose id is ignore_index is padding: its row is zeros and its gradient counts nowhere.  An
     id that is not in the table gives a row of NaN and has no part in the gradient.
@@ -163,9 +163,7 @@ class EmbeddingSession:
         self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device) if gradient else None
 
     def _ids(self, ids: torch.Tensor) -> int:
-        n = ids.shape[0] if ids.dim() == 1 else -1
-        if not 0 <= n <= self.max_tokens:
-            raise ValueError(f"at most {self.max_tokens} positions in a vector of ids, got {list(ids.shape)}")
+        n = ids.numel()
         _vector(ids, "ids", n, _INTS, self._index)
         return n
 
@@ -188,6 +186,8 @@ class EmbeddingSession:
         n, index, width = self._ids(ids), self._index, self.width
         if self.workspace is None:
             raise ValueError("a session made with gradient=False has no workspace for backward")
+        if n > self.max_tokens:
+            raise ValueError(f"the workspace is for at most {self.max_tokens} positions, got {n}")
         args = _EMBED_BACK.pack(n, self.vocab, width, _dtype_of(dy.dtype), _dtype_of(dtable.dtype), 64 if ids.dtype is torch.int64 else 32, scale, ignore_index,
                                 GD_EMBEDDING_ACCUMULATE if accumulate else 0, 0, dy.data_ptr(), _matrix(dy, "dy", n, width, dy.dtype, index),
                                 ids.data_ptr(), dtable.data_ptr(), _matrix(dtable, "dtable", self.vocab, width, dtable.dtype, index),

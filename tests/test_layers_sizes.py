@@ -36,3 +36,14 @@ def test_embedding_gradient_of_fewer_positions_than_the_session_is_for(cuda_devi
             s.backward(dy[:n], ids[:n], got)
             L.EmbeddingSession(vocab, width, n, device=cuda_device).backward(dy[:n], ids[:n], want)
             assert torch.equal(got, want), (most, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gradient", [False, True])
+def test_lookup_of_any_number_of_ids(cuda_device, gradient):
+    """max_tokens is the workspace's, which a lookup does not take; the gradient of more positions is refused."""
+    s = L.EmbeddingSession(10, 8, 4, device=cuda_device, gradient=gradient)
+    table, ids = torch.randn(10, 8, device=cuda_device), torch.arange(5000, device=cuda_device) % 10
+    assert torch.equal(s.forward(table, ids), table[ids])
+    with pytest.raises(ValueError):
+        s.backward(table[ids], ids, torch.empty_like(table))
