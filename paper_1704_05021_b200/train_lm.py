@@ -76,9 +76,11 @@ class Lm:
     def _block(self, views: List[torch.Tensor], b: int) -> List[torch.Tensor]:
         return views[1 + 12 * b:13 + 12 * b]
 
-    def forward(self, tokens: torch.Tensor, offsets: Optional[torch.Tensor], sentences: int, state: Optional[List[torch.Tensor]] = None) -> torch.Tensor:
+    def forward(self, tokens: torch.Tensor, offsets: Optional[torch.Tensor], sentences: int, state: Optional[List[torch.Tensor]] = None,
+                marks: bool = False) -> torch.Tensor:
         """The logits of every position.  tokens: the sentences one behind the other, which begin at offsets (None: equal parts); state: one
-        [sentences, width] per block, the recurrences' states before the first position, replaced by those behind the last."""
+        [sentences, width] per block, the recurrences' states before the first position, replaced by those behind the last; marks: keep what the
+        recurrences' backward pass takes, of up to the model's number of sentences."""
         r, d = len(tokens), self.width
         w, p = self.views(self.copies), self.views(self.params)
         x = [t[:r] for t in self.x]
@@ -89,7 +91,7 @@ class Lm:
             self.norm.forward(x[2 * b], g1, b1, out=k["a"], mean=k["m1"], rstd=k["r1"])
             self.project.forward(k["a"], wz, bz, out=k["z"])
             h = None if state is None else state[b]
-            recurrence_forward(k["z"][:, :d], k["z"][:, d:], out=k["h"], offsets=offsets, sequences=sentences, h0=h, h_last=h, marks=k["marks"])
+            recurrence_forward(k["z"][:, :d], k["z"][:, d:], out=k["h"], offsets=offsets, sequences=sentences, h0=h, h_last=h, marks=k["marks"] if marks else None)
             self.join.forward(k["h"], wo, bo, residual=x[2 * b], out=x[2 * b + 1])
             self.norm.forward(x[2 * b + 1], g2, b2, out=k["c"], mean=k["m2"], rstd=k["r2"])
             self.gated.forward(k["c"], wu, bu, out=k["u"], pre=k["pre"])
@@ -98,7 +100,7 @@ class Lm:
         return self.words.forward(self.f[:r], w[-2], p[-1], out=self.logits[:r])
 
     def answer(self, tokens: torch.Tensor, state: List[torch.Tensor]) -> torch.Tensor:
-        """The logits behind one more token of each sentence; `state` (new_state()) moves on."""
+        """The logits behind one more token of each of up to `rows` sentences; `state` (new_state()) moves on."""
         return self.forward(tokens, None, len(tokens), state)
 
     def new_state(self, sentences: int) -> List[torch.Tensor]:
@@ -109,7 +111,7 @@ class Lm:
         parameters); returns the positions' losses.  Positions with the target -100 count for nothing."""
         tokens, offsets = batch
         r, d, sentences = len(tokens), self.width, len(offsets) - 1
-        logits = self.forward(tokens, offsets, sentences)
+        logits = self.forward(tokens, offsets, sentences, marks=True)
         cross_entropy(logits, targets, loss=self.loss[:r], grad=logits, grad_scale=1.0 / r)
         w, p, g = self.views(self.copies), self.views(self.params), self.views(flat_grad)
         x = [t[:r] for t in self.x]

@@ -47,3 +47,19 @@ def test_lookup_of_any_number_of_ids(cuda_device, gradient):
     assert torch.equal(s.forward(table, ids), table[ids])
     with pytest.raises(ValueError):
         s.backward(table[ids], ids, torch.empty_like(table))
+
+
+@pytest.mark.gpu
+def test_answers_to_more_sentences_than_a_batch_has(cuda_device):
+    """One more token of 20 sentences, by a model made for batches of nine sentences in 300 positions: each as if it were alone, but for sums in
+    another order."""
+    from paper_1704_05021_b200 import train_lm as M
+    model = M.Lm(vocab=64, width=64, hidden=64, blocks=2, rows=300, sentences=9, device=cuda_device)
+    tokens = torch.randint(64, (20,), generator=torch.Generator(device=cuda_device).manual_seed(1), device=cuda_device)
+    state = model.new_state(20)
+    got = [model.answer(tokens, state).clone() for _ in range(2)]
+    assert all(bool(torch.isfinite(t).all()) for t in got)
+    few = model.new_state(9)
+    for n in range(2):
+        want = model.answer(tokens[:9], few)
+        assert float((got[n][:9].float() - want.float()).abs().max()) <= 10 * 2.0 ** -8 * float(want.float().abs().max())
