@@ -67,12 +67,12 @@ class Mlp:
 
 
 class Trainer:
-    """`workers` workers and one server with `shards` shards on one GPU."""
+    """`workers` workers and one server with `shards` shards on one GPU, that of `model` where one is given."""
 
     def __init__(self, batch: int = 80, workers: int = 2, drop_ppm: int = 990_000, state_bits: int = 32, shards: int = 4, hidden: int = 4096,
                  device="cuda:0", seed: int = 0, lr: float = 1e-3, model=None):
         self.model = m = Mlp(batch, device, hidden, seed) if model is None else model     # (another model: see train_lm.py)
-        n = m.layer_off[-1]
+        n, device = m.layer_off[-1], m.device
         chunk = -(-n // shards)
         shard_off = [min(j * chunk, n) for j in range(shards + 1)]
         self.lr, self.seed, self.taken = lr, seed, 0
