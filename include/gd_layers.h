@@ -136,8 +136,10 @@ int gd_layer_norm_workspace_bytes(uint64_t rows, uint64_t width, size_t* bytes_o
  * The state is fp32 throughout.  A gate of -inf forgets all that came before (a state that is not finite stays), one of +inf keeps the state.
  *
  * Sequences lie one behind the other in the rows of gate, value and y: sequence s is rows offsets[s] .. offsets[s + 1] - 1, offsets
- * ascending and at most `rows` (what is not is cut to that); rows before the first and behind the last sequence are neither read nor
- * written.  offsets = NULL: all sequences are rows / sequences long (rows a multiple of that).  A sequence of length 0 has h_last = h0.
+ * ascending and at most `rows`; rows before the first and behind the last sequence have no part in it and are not written.  A beginning or
+ * end outside 0 .. rows is cut to that, and an end before its beginning to the beginning.  Where offsets descend, sequences may come to share
+ * rows or marks: the results of all of them are undefined then and need not be the same twice, but nothing outside them is touched.
+ * offsets = NULL: all sequences are rows / sequences long (rows a multiple of that).  A sequence of length 0 has h_last = h0.
  * A call with one row per sequence is the step of a model that answers token by token; h_last may then, as always, be h0 itself.
  *
  * marks, if given, receive the states that gd_recurrence_backward starts from: gd_recurrence_marks_rows() rows of `width` fp32.  The backward

@@ -32,7 +32,7 @@ constexpr uint32_t kMostCluster = 8;
 struct Spans {
   const void* offsets;
   uint32_t bits, rows, sequences;
-  // first row of a sequence and how many it has; offsets that make no sense are cut to what does
+  // first row of a sequence and how many it has, within the rows whatever the offsets (each pair is cut by itself: where they descend, sequences may overlap)
   __device__ __forceinline__ void of(uint32_t s, uint32_t* first, uint32_t* count) const {
     if (!offsets) {
       const uint32_t per = rows / sequences;

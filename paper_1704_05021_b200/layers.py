@@ -296,7 +296,7 @@ def recurrence_forward(gate: torch.Tensor, value: torch.Tensor, out: Optional[to
                        marks: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """h[t] = f h[t-1] + (1 - f) value[t] with f = sigmoid(gate[t]), per column, over sequences that lie one behind the other in the rows.
 
-    offsets (int32 or int64, sequences + 1): where each begins and the last one ends; None: equal parts.  h0 and h_last: [sequences, width]
+    offsets (int32 or int64, sequences + 1, ascending): where each begins and the last one ends; None: equal parts.  h0 and h_last: [sequences, width]
     float32, the states before and after; they may be one tensor, as in a model that answers token by token (one row per sequence).
     `out` (of value's type; made here if None) receives the states; rows that belong to no sequence are left as they are.  marks (from
     recurrence_marks) are what recurrence_backward takes.
