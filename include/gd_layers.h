@@ -133,6 +133,7 @@ int gd_layer_norm_workspace_bytes(uint64_t rows, uint64_t width, size_t* bytes_o
 /*
  * gd_recurrence_forward - for every sequence and column, from the state h[-1] = h0:
  *     f = 1 / (1 + exp(-gate[t]))      h[t] = f * h[t-1] + (1 - f) * value[t]      y[t] = h[t], rounded to dtype
+ * A device-side wait that runs out leaves NaN in the results (these calls have no status).
  * The state is fp32 throughout.  A gate of -inf forgets all that came before (a state that is not finite stays), one of +inf keeps the state.
  *
  * Sequences lie one behind the other in the rows of gate, value and y: sequence s is rows offsets[s] .. offsets[s + 1] - 1, offsets
@@ -191,6 +192,14 @@ typedef struct gd_recurrence_backward_args {
 } gd_recurrence_backward_args;
 
 int gd_recurrence_backward(const gd_recurrence_backward_args* args, void* stream);
+
+/*
+ * Self-test of the recurrence's bounded waits, as gd_selftest_linear_wait is in gd_train.h: zeroes the workspace (256-byte aligned, at least 663552
+ * bytes) and runs a call over 8192 rows of 8 columns in bf16 whose waits, for at most budget_ns, are for more than is sent.  which: 0 forward, a
+ * tile's copies; 1 forward, the maps of a cluster; 2 and 3 the same of the backward call.  Afterwards y, or dgate, which begins at byte 401408, is NaN
+ * throughout, and so is dvalue, 131072 bytes further on, and the context stays usable.
+ */
+int gd_selftest_recurrence_wait(void* workspace, size_t workspace_bytes, int which, uint64_t budget_ns, void* stream);
 
 /*
  * gd_gated_forward - the gated feed-forward block up to its hidden layer.  x [m, k], W given as w [k, 2 n] or [2 n, k] (w_layout): the first n

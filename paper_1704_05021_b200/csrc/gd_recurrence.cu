@@ -47,6 +47,14 @@ struct Spans {
     *first = (uint32_t)b, *count = (uint32_t)(e - b);
   }
 };
+// How long a wait for a tile's copies or a cluster's maps lasts, and bytes awaited there that nobody sends (0; the self-test's 8).  A thread whose wait
+// ran out marks its count of tiles and waits no more; the CTA's flag ends the others' waits that do not succeed at once.  Rows and states that did not
+// come are NaN to it, and so is all that follows from them.  Thread 0 asks for no more copies then - a stage's may still be under way - and waits once
+// more for those it has asked for before it ends.
+struct Waits {
+  uint64_t budget_ns;
+  uint32_t missing_copies, missing_maps;
+};
 struct ScanArgs {
   Spans spans;
   const void* gate;
@@ -59,6 +67,7 @@ struct ScanArgs {
   uint32_t width, slabs;
   uint64_t items;              // (sequence, slab)
   bool by_length;              // long sequences first
+  Waits waits;
 };
 struct ScanBackArgs {
   Spans spans;
@@ -74,6 +83,7 @@ struct ScanBackArgs {
   uint32_t width, slabs;
   uint64_t items;
   bool by_length;
+  Waits waits;
 };
 // the row of marks that holds the state before row 0 of a sequence
 __device__ __forceinline__ uint64_t first_mark(uint32_t sequence, uint32_t first_row) { return (uint64_t)first_row / kMarkRows + sequence; }
@@ -190,11 +200,11 @@ struct Exchange {
   uint64_t full[kPlaces];
 };
 template <int V, int CL, int L>
-__device__ __forceinline__ void exchange_begin(Exchange<V, CL, L>& x) {
+__device__ __forceinline__ void exchange_begin(Exchange<V, CL, L>& x, uint32_t missing) {
   if (threadIdx.x == 0) {
     for (uint32_t b = 0; b < kPlaces; ++b) {
       mbar_init(&x.full[b], 1u);
-      mbar_arrive_expect_tx(&x.full[b], CL * L * (uint32_t)sizeof(Map<V>));
+      mbar_arrive_expect_tx(&x.full[b], CL * L * (uint32_t)sizeof(Map<V>) + missing);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -217,13 +227,23 @@ __device__ __forceinline__ void exchange_send(Exchange<V, CL, L>& x, uint32_t ra
     }
   }
 }
+constexpr uint32_t kGone = 1u << 31;      // of a thread's count of tiles: a wait of its ran out
+// False where it did; afterwards every second phase of a barrier that nobody begins any more looks like one that has ended, but states are NaN by then
+// and stay it.
+__device__ __forceinline__ bool wait_for(uint64_t* b, uint32_t parity, volatile int* gone, uint64_t budget_ns, uint32_t& taken) {
+  if (mbar_try_wait(b, parity)) return true;
+  if (!(taken & kGone) && mbar_wait(b, parity, gone, budget_ns)) return true;
+  *gone = 1;
+  taken |= kGone;
+  return false;
+}
 // By one warp: waits for everybody's maps of `round` and makes the place ready for round + kPlaces (nobody sends for that before this CTA has sent
 // for a later round, which it does behind a barrier behind this call).  From the state that enters the cluster's tiles, `carry`: what enters this CTA's, and `carry` behind the last.
 template <int V, int CL, bool BACKWARD, int L>
-__device__ __forceinline__ void exchange_fold(Exchange<V, CL, L>& x, uint32_t rank, uint32_t round, float (&mine)[V], float (&carry)[V]) {
+__device__ __forceinline__ void exchange_fold(Exchange<V, CL, L>& x, uint32_t rank, uint32_t round, volatile int* gone, uint64_t budget_ns, uint32_t& taken,
+                                              float (&mine)[V], float (&carry)[V]) {
   const uint32_t lane = threadIdx.x % L, at = round % kPlaces;
-  const int never = 0;
-  const bool good = mbar_wait(&x.full[at], (round / kPlaces) & 1u, &never);
+  const bool good = wait_for(&x.full[at], (round / kPlaces) & 1u, gone, budget_ns, taken);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     if (!good) carry[i] = NAN;                       // (a map that never came: the results say so)
@@ -239,7 +259,10 @@ __device__ __forceinline__ void exchange_fold(Exchange<V, CL, L>& x, uint32_t ra
     const Map<V> m = x.map[at][q][lane];
     fma_v<V>(m.a, carry, m.b, carry);
   }
-  if (threadIdx.x == 0) mbar_arrive_expect_tx(&x.full[at], CL * L * (uint32_t)sizeof(Map<V>));
+  if (threadIdx.x == 0) {
+    if (!(taken & kGone)) mbar_arrive_expect_tx(&x.full[at], CL * L * (uint32_t)sizeof(Map<V>));
+    else mbar_expect_tx(&x.full[at], CL * L * (uint32_t)sizeof(Map<V>));        // (the others send on: the count stays in its range)
+  }
 }
 
 // ---------------------------------------------------------------- tiles in shared memory
@@ -311,6 +334,21 @@ __device__ __forceinline__ void longest_first(const Spans& spans, uint32_t place
   __syncthreads();
 }
 
+// By thread 0 at the end, where a wait of its ran out.
+template <uint32_t DEPTH>
+__device__ __forceinline__ void settle_copies(uint64_t* full, uint32_t asked, uint64_t budget_ns) {
+  const int none = 0;
+  for (uint32_t n = asked > DEPTH ? asked - DEPTH : 0u; n < asked; ++n) (void)mbar_wait(&full[n % DEPTH], (n / DEPTH) & 1u, &none, budget_ns);
+}
+
+// A thread's rows of a tile that did not come, in an input of 4 bytes a place: NaN, whatever the type (or what arrives late).
+template <int L>
+__device__ __forceinline__ void spoil_rows(unsigned char* tile) {
+  uint32_t* to = reinterpret_cast<uint32_t*>(tile) + (threadIdx.x / L) * kRows * L + threadIdx.x % L;
+#pragma unroll 1
+  for (uint32_t k = 0; k < kRows; ++k) to[k * L] = 0xFFFFFFFFu;
+}
+
 // ---------------------------------------------------------------- forward
 // Rows that tiled copies can read: 16-byte aligned.
 struct ScanMaps {
@@ -330,13 +368,16 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
   Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
   __shared__ uint64_t s_full[kDepth];
   __shared__ Chosen s_chosen;
+  __shared__ int s_gone;
+  volatile int* gone = &s_gone;
   const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
   if (threadIdx.x == 0) {
+    s_gone = 0;
     for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (MODE == kBoxes) prefetch_map(&maps.gate), prefetch_map(&maps.value);
   }
-  if constexpr (CL > 1) exchange_begin(s_x);
+  if constexpr (CL > 1) exchange_begin(s_x, a.waits.missing_maps);
   else __syncthreads();
   pdl_wait();
   pdl_trigger();
@@ -362,8 +403,8 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
     const auto ask = [&](uint32_t set) {
       const uint32_t tile = set * CL + rank, s = asked % kDepth;
       if constexpr (MODE == kBoxes) {
-        if (threadIdx.x != 0 || tile >= tiles) return;
-        mbar_arrive_expect_tx(&s_full[s], S::kStage);
+        if (threadIdx.x != 0 || tile >= tiles || (taken & kGone)) return;
+        mbar_arrive_expect_tx(&s_full[s], S::kStage + a.waits.missing_copies);
         tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
         tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, (int32_t)(first + tile * kTileRows), &s_full[s]);
         ++asked;
@@ -394,7 +435,7 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
     for (uint32_t n = 0; n < kAhead; ++n) ask(n);
     float h[V];                                      // the state that enters the tile, or the cluster's tiles
 #pragma unroll
-    for (int i = 0; i < V; ++i) h[i] = in && a.h0 ? a.h0[(uint64_t)seq * a.width + c + i] : 0.f;
+    for (int i = 0; i < V; ++i) h[i] = taken & kGone ? NAN : in && a.h0 ? a.h0[(uint64_t)seq * a.width + c + i] : 0.f;
     const auto rows_of = [&](uint32_t tile) {
       const uint32_t r0 = tile * kTileRows + group * R;
       return tile < tiles && r0 < count ? min((uint32_t)R, count - r0) : 0u;
@@ -402,11 +443,11 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
     // f and s v of this group's rows of a tile, and their map, which is left for the other groups
     const auto evaluate = [&](uint32_t tile, float (&f)[N], float (&sv)[N]) __attribute__((always_inline)) {
       const uint32_t rows = rows_of(tile), s = taken % kDepth;
-      bool good = true;
       if constexpr (MODE == kOwnCopies) copies_wait<(int)kDepth - 1>();
       if (tile < tiles) {
-        const int never = 0;
-        if constexpr (MODE == kBoxes) good = mbar_wait(&s_full[s], (taken / kDepth) & 1u, &never);
+        if constexpr (MODE == kBoxes) {
+          if (!wait_for(&s_full[s], (taken / kDepth) & 1u, gone, a.waits.budget_ns, taken)) spoil_rows<L>(smem + s * S::kStage + S::kInput);
+        }
         if constexpr (MODE == kRegisters) settle(s);
         ++taken;
       }
@@ -429,7 +470,7 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
       }
       Map<V> m;
 #pragma unroll
-      for (int i = 0; i < V; ++i) m.a[i] = f[i], m.b[i] = good ? sv[i] : NAN;
+      for (int i = 0; i < V; ++i) m.a[i] = f[i], m.b[i] = sv[i];
 #pragma unroll
       for (int k = 1; k < R; ++k) {
         fma_v<V>(f + k * V, m.b, sv + k * V, m.b);
@@ -469,7 +510,7 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
       const auto join = [&](uint32_t set) __attribute__((always_inline)) {
         if (threadIdx.x >= 32u) return;
         float state[V];
-        exchange_fold<V, CL, false>(s_x, rank, round + set, state, h);
+        exchange_fold<V, CL, false>(s_x, rank, round + set, gone, a.waits.budget_ns, taken, state, h);
 #pragma unroll
         for (int i = 0; i < V; ++i) s_state[set & 1u][lane][i] = state[i];
       };
@@ -546,6 +587,9 @@ __global__ void __launch_bounds__(kWarps * 32, CL > 1 ? 2 : 3) scan_tiled_kernel
 #pragma unroll
       for (int i = 0; i < V; ++i) a.h_last[(uint64_t)seq * a.width + c + i] = h[i];
     }
+  }
+  if constexpr (MODE == kBoxes) {
+    if (threadIdx.x == 0 && (taken & kGone)) settle_copies<kDepth>(s_full, asked, a.waits.budget_ns);
   }
   if constexpr (CL > 1) {
     cluster_arrive();
@@ -626,13 +670,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
   Exchange<V, CL, L>& s_x = *reinterpret_cast<Exchange<V, CL, L>*>(smem + S::kDepth * S::kStage);
   __shared__ uint64_t s_full[kDepth];
   __shared__ Chosen s_chosen;
+  __shared__ int s_gone;
+  volatile int* gone = &s_gone;
   const uint32_t lane = threadIdx.x % L, group = threadIdx.x / L, rank = CL > 1 ? cluster_rank() : 0u;
   if (threadIdx.x == 0) {
+    s_gone = 0;
     for (uint32_t s = 0; s < kDepth; ++s) mbar_init(&s_full[s], 1u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (MODE == kBoxes) prefetch_map(&maps.gate), prefetch_map(&maps.value), prefetch_map(&maps.dy);
   }
-  if constexpr (CL > 1) exchange_begin(s_x);
+  if constexpr (CL > 1) exchange_begin(s_x, a.waits.missing_maps);
   else __syncthreads();
   pdl_wait();
   pdl_trigger();
@@ -661,9 +708,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
       const uint32_t tile = (sets - 1u - n) * CL + rank, s = asked % kDepth;
       const bool there = n < sets && tile < tiles;
       if constexpr (MODE == kBoxes) {
-        if (threadIdx.x != 0 || !there) return;
+        if (threadIdx.x != 0 || !there || (taken & kGone)) return;
         const int32_t row = (int32_t)(first + tile * kTileRows);
-        mbar_arrive_expect_tx(&s_full[s], S::kStage);
+        mbar_arrive_expect_tx(&s_full[s], S::kStage + a.waits.missing_copies);
         tile_load(smem + s * S::kStage, &maps.gate, (int32_t)col0, row, &s_full[s]);
         tile_load(smem + s * S::kStage + S::kInput, &maps.value, (int32_t)col0, row, &s_full[s]);
         tile_load(smem + s * S::kStage + 2 * S::kInput, &maps.dy, (int32_t)col0, row, &s_full[s]);
@@ -699,7 +746,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
     for (uint32_t n = 0; n < kAhead; ++n) ask(n);
     float carry[V];                                  // f[t+1] dh[t+1] of the row behind the tile, or the cluster's tiles
 #pragma unroll
-    for (int i = 0; i < V; ++i) carry[i] = in && a.dh_last ? a.dh_last[(uint64_t)seq * a.width + c + i] : 0.f;
+    for (int i = 0; i < V; ++i) carry[i] = taken & kGone ? NAN : in && a.dh_last ? a.dh_last[(uint64_t)seq * a.width + c + i] : 0.f;
     struct Rows {
       float f[N], s[N], v[N], d[N];
     };
@@ -728,12 +775,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
     };
     // Leaves the maps of this group's rows for the others: h -> A h + B of the states, and of the gradient C = sum of d[k] f[0] .. f[k], which is
     // A times what reaches the last row, plus C, at the first.  Returns the latter.
-    const auto leave = [&](const Rows& x, bool good) __attribute__((always_inline)) {
+    const auto leave = [&](const Rows& x) __attribute__((always_inline)) {
       Map<V> m, b;
       float sv[N];
       times(x.s, x.v, sv);
 #pragma unroll
-      for (int i = 0; i < V; ++i) m.a[i] = x.f[i], m.b[i] = good ? sv[i] : NAN, b.b[i] = good ? 0.f : NAN;
+      for (int i = 0; i < V; ++i) m.a[i] = x.f[i], m.b[i] = sv[i], b.b[i] = 0.f;
       fma_v<V>(m.a, x.d, b.b, b.b);
 #pragma unroll
       for (int k = 1; k < R; ++k) {
@@ -757,16 +804,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
     const auto wait = [&](uint32_t tile, uint32_t* stage) {
       *stage = taken % kDepth;
       if constexpr (MODE == kOwnCopies) copies_wait<(int)kAhead - 1>();
-      if (tile >= tiles) return true;
-      if constexpr (MODE != kBoxes) {
-        if constexpr (MODE == kRegisters) settle(*stage);
-        ++taken;
-        return true;
+      if (tile >= tiles) return;
+      if constexpr (MODE == kBoxes) {
+        if (!wait_for(&s_full[*stage], (taken / kDepth) & 1u, gone, a.waits.budget_ns, taken)) {
+          spoil_rows<L>(smem + *stage * S::kStage + S::kInput);
+          spoil_rows<L>(smem + *stage * S::kStage + 2 * S::kInput);
+        }
       }
-      const int never = 0;
-      const bool good = mbar_wait(&s_full[*stage], (taken / kDepth) & 1u, &never);
+      if constexpr (MODE == kRegisters) settle(*stage);
       ++taken;
-      return good;
     };
     // from there to the state before this group's rows
     const auto state_of = [&](float (&h)[V]) __attribute__((always_inline)) {
@@ -812,19 +858,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
       const auto join = [&](uint32_t n) __attribute__((always_inline)) {
         if (threadIdx.x >= 32u) return;
         float g[V];
-        exchange_fold<V, CL, true>(s_x, rank, round + n, g, carry);
+        exchange_fold<V, CL, true>(s_x, rank, round + n, gone, a.waits.budget_ns, taken, g, carry);
 #pragma unroll
         for (int i = 0; i < V; ++i) s_carry[n & 1u][lane][i] = g[i];
       };
       const auto start = [&](uint32_t n) __attribute__((always_inline)) {
         const uint32_t tile = (sets - 1u - n) * CL + rank;
         mark_of(tile, next_h);
-        const bool good = wait(tile, &next_stage);
+        wait(tile, &next_stage);
         Map<V> own;
         {
           Rows x;
           read(next_stage, rows_of(tile), x);
-          own = leave(x, good);
+          own = leave(x);
         }
         if (n) join(n - 1);
         __syncthreads();
@@ -875,9 +921,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
         float h[V];
         uint32_t stage;
         mark_of(tile, h);
-        const bool good = wait(tile, &stage);
+        wait(tile, &stage);
         read(stage, rows_of(tile), x);
-        const Map<V> own = leave(x, good);
+        const Map<V> own = leave(x);
         __syncthreads();
         ask(n + kAhead);
         if (n) {
@@ -910,6 +956,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) scan_back_tiled_kernel(const _
 #pragma unroll
       for (int i = 0; i < V; ++i) a.dh0[(uint64_t)seq * a.width + c + i] = carry[i];
     }
+  }
+  if constexpr (MODE == kBoxes) {
+    if (threadIdx.x == 0 && (taken & kGone)) settle_copies<kDepth>(s_full, asked, a.waits.budget_ns);
   }
   if constexpr (CL > 1) {
     cluster_arrive();
@@ -1160,7 +1209,8 @@ int check_shape(uint64_t rows, uint64_t sequences, uint64_t width, int dtype, co
   return GD_OK;
 }
 
-int forward(const gd_recurrence_forward_args* g, cudaStream_t stream) {
+constexpr Waits kWaits{kWaitBudgetNs, 0, 0};
+int forward(const gd_recurrence_forward_args* g, const Waits& waits, cudaStream_t stream) {
   if (!g) return GD_ERR_INVALID_ARG;
   const int rc = check_shape(g->rows, g->sequences, g->width, g->dtype, g->offsets, g->offset_bits);
   if (rc != GD_OK) return rc;
@@ -1177,6 +1227,7 @@ int forward(const gd_recurrence_forward_args* g, cudaStream_t stream) {
   a.value = g->value, a.ld_value = g->ld_value;
   a.y = g->y, a.ld_y = g->ld_y;
   a.h0 = g->h0, a.h_last = g->h_last, a.marks = g->marks;
+  a.waits = waits;
   a.width = (uint32_t)g->width;
   // two 16-bit columns a thread where rows take 4-byte accesses
   const auto pairs = [&](const void* p, uint64_t ld) { return in_pieces(p, ld, g->rows, g->width, item, 2); };
@@ -1190,7 +1241,7 @@ int forward(const gd_recurrence_forward_args* g, cudaStream_t stream) {
   return GD_OK;
 }
 
-int backward(const gd_recurrence_backward_args* g, cudaStream_t stream) {
+int backward(const gd_recurrence_backward_args* g, const Waits& waits, cudaStream_t stream) {
   if (!g) return GD_ERR_INVALID_ARG;
   const int rc = check_shape(g->rows, g->sequences, g->width, g->dtype, g->offsets, g->offset_bits);
   if (rc != GD_OK) return rc;
@@ -1215,6 +1266,7 @@ int backward(const gd_recurrence_backward_args* g, cudaStream_t stream) {
   a.dgate = g->dgate, a.ld_dgate = g->ld_dgate;
   a.dvalue = g->dvalue, a.ld_dvalue = g->ld_dvalue;
   a.dh_last = g->dh_last, a.dh0 = g->dh0;
+  a.waits = waits;
   a.width = (uint32_t)width;
   const auto pairs = [&](const void* p, uint64_t ld) { return in_pieces(p, ld, rows, width, item, 2); };
   const bool two = g->width % 2 == 0 && pairs(g->dy, g->ld_dy) && pairs(g->gate, g->ld_gate) && pairs(g->value, g->ld_value) && pairs(g->dgate, g->ld_dgate) && pairs(g->dvalue, g->ld_dvalue);
@@ -1238,7 +1290,42 @@ int gd_recurrence_marks_rows(uint64_t rows, uint64_t sequences, uint64_t* rows_o
   *rows_out = rows / gd::kMarkRows + sequences;
   return GD_OK;
 }
-int gd_recurrence_forward(const gd_recurrence_forward_args* a, void* stream) { return gd::forward(a, (cudaStream_t)stream); }
-int gd_recurrence_backward(const gd_recurrence_backward_args* a, void* stream) { return gd::backward(a, (cudaStream_t)stream); }
+int gd_recurrence_forward(const gd_recurrence_forward_args* a, void* stream) { return gd::forward(a, gd::kWaits, (cudaStream_t)stream); }
+int gd_recurrence_backward(const gd_recurrence_backward_args* a, void* stream) { return gd::backward(a, gd::kWaits, (cudaStream_t)stream); }
+
+int gd_selftest_recurrence_wait(void* workspace, size_t workspace_bytes, int which, uint64_t budget_ns, void* stream) {
+  using namespace gd;
+  // 8192 rows: one sequence in a cluster, or, by one CTA, the first of many by their number, of which the others are empty
+  constexpr uint64_t rows = 8192, width = 8, many = 64, matrix = rows * width * 2, offsets = 0, marks = 1024, gate = 8192, value = gate + matrix, dy = value + matrix,
+                     first = dy + matrix, second = first + matrix, end = second + matrix;
+  static_assert(marks + (rows / kMarkRows + many) * width * 4 <= gate && offsets + (many + 1) * 4 <= marks, "the parts of the workspace");
+  if (which < 0 || which > 3) return GD_ERR_INVALID_ARG;
+  if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < end) return GD_ERR_WORKSPACE;
+  unsigned char* base = (unsigned char*)workspace;
+  if (cudaMemsetAsync(base, 0, end, (cudaStream_t)stream) != cudaSuccess) return GD_ERR_CUDA;
+  if (cudaMemsetAsync(base + offsets + 4, 0x7F, many * 4, (cudaStream_t)stream) != cudaSuccess) return GD_ERR_CUDA;      // (behind the rows: cut to them)
+  const bool maps = (which & 1) != 0;
+  const Waits waits{budget_ns, maps ? 0u : 8u, maps ? 8u : 0u};
+  const auto common = [&](auto& a) {
+    a.rows = rows, a.width = width, a.sequences = maps ? 1 : many;
+    a.dtype = GD_DTYPE_BF16, a.offset_bits = 32, a.offsets = maps ? nullptr : base + offsets;
+    a.gate = base + gate, a.value = base + value;
+    a.ld_gate = a.ld_value = width;
+    a.marks = (float*)(base + marks);
+  };
+  if (which < 2) {
+    gd_recurrence_forward_args a;
+    std::memset(&a, 0, sizeof(a));
+    common(a);
+    a.y = base + first, a.ld_y = width;
+    return gd::forward(&a, waits, (cudaStream_t)stream);
+  }
+  gd_recurrence_backward_args a;
+  std::memset(&a, 0, sizeof(a));
+  common(a);
+  a.dy = base + dy, a.dgate = base + first, a.dvalue = base + second;
+  a.ld_dy = a.ld_dgate = a.ld_dvalue = width;
+  return gd::backward(&a, waits, (cudaStream_t)stream);
+}
 
 }  // extern "C"
