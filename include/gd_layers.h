@@ -260,6 +260,13 @@ typedef struct gd_gated_backward_args {
 
 int gd_gated_backward(const gd_gated_backward_args* args, void* stream);
 
+/*
+ * Self-test of a bounded wait, as gd_selftest_linear_wait is in gd_train.h: zeroes the workspace (256-byte aligned, at least 25088 bytes) and sums the
+ * bias gradient of 128 rows by two CTAs, one waiting (for at most budget_ns) for more than the other sends.  Afterwards gd_linear_status() is
+ * GD_ERR_DEVICE_TIMEOUT and the 64 floats behind the status word's 256 bytes are NaN; the context stays usable.
+ */
+int gd_selftest_gated_wait(void* workspace, size_t workspace_bytes, uint64_t budget_ns, void* stream);
+
 /* Workspace of the two calls above for up to m rows; any_layout and the status word as in gd_linear_workspace_bytes(), read by gd_linear_status(). */
 int gd_gated_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, int any_layout, size_t* bytes_out);
 

@@ -26,6 +26,8 @@ struct SlopeArgs {
   int32_t activation;
   uint32_t accumulate, vectors;
   int* status;
+  uint64_t budget_ns;  // of the wait for the other CTAs' sums
+  uint32_t missing;    // bytes awaited that nobody sends (0; the self-test's 8)
   Packs packs;
 };
 // (a, u, g) -> the two halves of dz, in a's and u's place
@@ -65,7 +67,7 @@ __global__ void __launch_bounds__(kSlopeThreads, 3) gated_slope_kernel(const __g
       s_never = 0;
       mbar_init(&s_in, 1u);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      if (rank == 0) mbar_arrive_expect_tx(&s_in, a.split * a.width * 8u);
+      if (rank == 0) mbar_arrive_expect_tx(&s_in, a.split * a.width * 8u + a.missing);
     }
     __syncthreads();
     cluster_arrive_relaxed();
@@ -171,7 +173,7 @@ __global__ void __launch_bounds__(kSlopeThreads, 3) gated_slope_kernel(const __g
       send_peer2(peer_address(smem_u32(&s_all[rank][p]), 0), t, peer_address(smem_u32(&s_in), 0));
     }
     if (rank == 0 && h < 2) {
-      const bool there = mbar_wait(&s_in, 0u, &s_never);
+      const bool there = mbar_wait(&s_in, 0u, &s_never, a.budget_ns);
       if (!there) atomicExch(a.status, GD_ERR_DEVICE_TIMEOUT);
       float t = there ? 0.f : NAN;
       for (uint32_t q = 0; q < a.split; ++q) t += s_all[q][tid];
@@ -287,6 +289,7 @@ int backward(const gd_gated_backward_args* a, cudaStream_t stream) {
   if (has_dw && m && (rc = operand(a->x, a->ldx, m, k, ws, &s.packs, &q.x)) != GD_OK) return rc;
   if (products || has_db) {
     s.status = (int*)a->workspace;
+    s.budget_ns = kWaitBudgetNs;
     s.dy = a->dy, s.ld_dy = row_step(a->ld_dy, m, n);
     s.pre = a->pre, s.ld_pre = row_step(a->ld_pre, m, 2 * n);
     s.db = has_db ? a->db : nullptr;
@@ -327,5 +330,26 @@ int gd_gated_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, int any_layout,
 }
 int gd_gated_forward(const gd_gated_forward_args* a, void* stream) { return gd::forward(a, (cudaStream_t)stream); }
 int gd_gated_backward(const gd_gated_backward_args* a, void* stream) { return gd::backward(a, (cudaStream_t)stream); }
+
+int gd_selftest_gated_wait(void* workspace, size_t workspace_bytes, uint64_t budget_ns, void* stream) {
+  using namespace gd;
+  constexpr uint32_t rows = 128, cols = 32;              // two CTAs in a cluster
+  constexpr size_t sums = kStatusBytes, dy = sums + 2 * cols * 4, pre = dy + rows * cols * 2, end = pre + rows * 2 * cols * 2;
+  if (check_workspace(workspace, workspace_bytes) != GD_OK || workspace_bytes < end) return GD_ERR_WORKSPACE;
+  unsigned char* base = (unsigned char*)workspace;
+  if (cudaMemsetAsync(base, 0, end, (cudaStream_t)stream) != cudaSuccess) return GD_ERR_CUDA;
+  SlopeArgs s;
+  std::memset(&s, 0, sizeof(s));
+  s.dy = base + dy, s.ld_dy = cols;
+  s.pre = base + pre, s.ld_pre = 2 * cols;
+  s.db = (float*)(base + sums);
+  s.rows = rows, s.cols = cols;
+  s.activation = GD_ACT_SILU;
+  s.vectors = 1;
+  s.status = (int*)workspace;
+  s.budget_ns = budget_ns;
+  s.missing = 8;
+  return launch_slope(s, GD_DTYPE_BF16, (cudaStream_t)stream) == cudaSuccess ? GD_OK : GD_ERR_CUDA;
+}
 
 }  // extern "C"

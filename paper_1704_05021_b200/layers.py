@@ -25,7 +25,7 @@ GD_LAYER_NORM_ACCUMULATE = 1
 
 EXPORTS = ["gd_embedding_forward", "gd_embedding_backward", "gd_embedding_workspace_bytes", "gd_layer_norm_forward", "gd_layer_norm_backward",
            "gd_layer_norm_workspace_bytes", "gd_recurrence_forward", "gd_recurrence_backward", "gd_recurrence_marks_rows",
-           "gd_selftest_recurrence_wait", "gd_gated_forward", "gd_gated_backward", "gd_gated_workspace_bytes"]
+           "gd_selftest_recurrence_wait", "gd_gated_forward", "gd_gated_backward", "gd_gated_workspace_bytes", "gd_selftest_gated_wait"]
 
 
 class _EmbeddingForwardArgs(C.Structure):
@@ -104,6 +104,7 @@ def load_library():
         lib.gd_embedding_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.POINTER(C.c_size_t)]
         lib.gd_layer_norm_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.POINTER(C.c_size_t)]
         lib.gd_gated_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.c_int, C.POINTER(C.c_size_t)]
+        lib.gd_selftest_gated_wait.argtypes = [C.c_void_p, C.c_size_t, C.c_uint64, C.c_void_p]
         lib.gd_selftest_recurrence_wait.argtypes = [C.c_void_p, C.c_size_t, C.c_int, C.c_uint64, C.c_void_p]
         lib.gd_recurrence_marks_rows.argtypes = [C.c_uint64, C.c_uint64, C.POINTER(C.c_uint64)]
         _lib = lib

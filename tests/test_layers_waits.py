@@ -43,3 +43,21 @@ def test_a_wait_of_the_recurrence_that_runs_out_leaves_nan(cuda_device, which):
     dgate, dvalue = torch.empty_like(gate), torch.empty_like(gate)
     L.recurrence_backward(value, gate, value, marks, dgate, dvalue)
     assert bool((dvalue[:-20] == 1).all()) and bool((dvalue[-1] == 0.5).all()) and bool(torch.isfinite(dgate).all())
+
+
+@pytest.mark.gpu
+def test_a_wait_of_the_gated_blocks_bias_gradient_that_runs_out_reaches_the_status(cuda_device):
+    """The status says so, the sums are NaN, and the next call works once the word is zeroed."""
+    s = L.GatedLinearSession(32, 32, 512, device=cuda_device)
+    ws, lib = s.workspace, L.load_library()
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.gd_selftest_gated_wait(ws.data_ptr(), 25087, 1_000_000, stream) == B.GD_ERR_WORKSPACE
+    assert lib.gd_selftest_gated_wait(ws.data_ptr(), ws.numel(), 1_000_000, stream) == B.GD_OK
+    assert s.status() == B.GD_ERR_DEVICE_TIMEOUT
+    assert bool(torch.isnan(ws[256:512].view(torch.float32)).all())
+    ws[:256].zero_()
+    dy, pre, db = torch.ones(512, 32, dtype=BF16, device=cuda_device), torch.ones(512, 64, dtype=BF16, device=cuda_device), torch.empty(64, device=cuda_device)
+    s.backward(dy, None, None, pre, db=db)
+    silu = 1 / (1 + 2.718281828459045 ** -1)             # of 1, and its slope there s (1 + 1 - s)
+    # (sums of 512 equal terms up to 0.93: 20 additions in a row of 2^-24 and a sigmoid good to 2^-20 are below 1e-3 of them)
+    assert bool(((db[32:] - 512 * silu).abs() < 1e-3).all()) and bool(((db[:32] - 512 * silu * (2 - silu)).abs() < 1e-3).all()) and s.status() == B.GD_OK
