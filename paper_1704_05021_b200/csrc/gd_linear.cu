@@ -101,6 +101,26 @@ struct SlopeArgs {
   uint32_t missing;    // bytes awaited that nobody sends (0; the self-test's 8)
   Packs packs;
 };
+// Eight 16-bit elements from column c of a row that starts anywhere: the two aligned vectors around them, moved into place. Both lie within
+// the row where `inner` holds; a row's ends are read element by element.
+__device__ __forceinline__ bool inner(uint32_t c, uint32_t cols) { return c >= 8 && c + 16 <= cols; }
+struct Around {
+  uint4 lo, hi;
+};
+__device__ __forceinline__ Around load_around(const uint16_t* s) {
+  const uint4* at = reinterpret_cast<const uint4*>((uintptr_t)s & ~(uintptr_t)15);
+  return Around{at[0], at[1]};
+}
+__device__ __forceinline__ uint4 into_place(const Around& a, const uint16_t* s) {
+  const uint32_t off = (uint32_t)(uintptr_t)s & 15u;
+  uint32_t w[8] = {a.lo.x, a.lo.y, a.lo.z, a.lo.w, a.hi.x, a.hi.y, a.hi.z, a.hi.w};
+#pragma unroll
+  for (int j = 0; j < 6; ++j) w[j] = off & 8u ? w[j + 2] : w[j];
+#pragma unroll
+  for (int j = 0; j < 5; ++j) w[j] = off & 4u ? w[j + 1] : w[j];
+  const uint32_t bits = (off & 2u) * 8u;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
 // RAGGED: rows of kWideRow columns and more that start anywhere, read by `load_around`; shorter ones are read element by element, two rows at a
 // time.  Backward of 6563 x 1120 <- 3347 155 against 197 us, column sums of 2000 x 85001 138 against 182; slopes of 6214 x 38 14.6
 // against 12.6, of 11506 x 433 26.9 against 25.2 (few loads in hand and many ends).

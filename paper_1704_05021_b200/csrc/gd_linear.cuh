@@ -56,27 +56,6 @@ inline uint32_t pack_ctas(const Packs& all, uint32_t threads) {
 }
 cudaError_t launch_pack(const Packs& all, cudaStream_t stream);
 
-// Eight 16-bit elements from column c of a row that starts anywhere: the two aligned vectors around them, moved into place. Both lie within
-// the row where `inner` holds; a row's ends are read element by element.
-__device__ __forceinline__ bool inner(uint32_t c, uint32_t cols) { return c >= 8 && c + 16 <= cols; }
-struct Around {
-  uint4 lo, hi;
-};
-__device__ __forceinline__ Around load_around(const uint16_t* s) {
-  const uint4* at = reinterpret_cast<const uint4*>((uintptr_t)s & ~(uintptr_t)15);
-  return Around{at[0], at[1]};
-}
-__device__ __forceinline__ uint4 into_place(const Around& a, const uint16_t* s) {
-  const uint32_t off = (uint32_t)(uintptr_t)s & 15u;
-  uint32_t w[8] = {a.lo.x, a.lo.y, a.lo.z, a.lo.w, a.hi.x, a.hi.y, a.hi.z, a.hi.w};
-#pragma unroll
-  for (int j = 0; j < 6; ++j) w[j] = off & 8u ? w[j + 2] : w[j];
-#pragma unroll
-  for (int j = 0; j < 5; ++j) w[j] = off & 4u ? w[j + 1] : w[j];
-  const uint32_t bits = (off & 2u) * 8u;
-  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
-}
-
 // ---------------------------------------------------------------- host side
 inline uint64_t up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 inline bool tiles_as_it_is(const void* p, uint64_t ld) { return aligned_to(p, 16) && ld % 8 == 0; }
