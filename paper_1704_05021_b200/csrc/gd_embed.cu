@@ -6,7 +6,7 @@
 // rows of equal ids in ascending order of their positions, so that nothing is added by atomics and every row of the gradient is
 // written by one sum.  Most of the gradient is the zeros of ids that do not occur (85000 x 500 in fp32: 170 MB, 26 us, for 4000 positions), and
 // the sort is all latency: the launches that sort have CTAs that sort and CTAs that write a share of the zeros meanwhile.
-// Measured: that case 37 us (22 without zeros); 131072 positions over 32000 x 1024 113 us, of which the sums take 66 = 5.7 TB/s, the sort 27
+// Measured: that case 37 us (22 without zeros); 131072 positions over 32000 x 1024 113 us, of which the sums take 70 = 5.7 TB/s, the sort 27
 // and the join of long runs 15; lookup of 131072 rows of 1024 59 us.
 //
 // Sums: the sorted list in chunks of kChunk positions, a CTA per chunk and block of columns.  A run of equal ids that ends in the

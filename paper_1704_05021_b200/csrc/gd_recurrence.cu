@@ -14,8 +14,8 @@
 //
 // Many sequences of few rows, the single step among them: a thread takes a sequence's columns through all its rows.
 //
-// Measured (bf16): 16 sequences of 2048 x 2048 80 us forward = 5.0 TB/s, 125 backward = 5.4; one of 65536 x 1024 106 and 245 (a set of tiles takes the
-// cluster 1.6 us and 3.8, a CTA's 24 and 40 KB would take 0.6 and 0.9); 64 sequences by one step of 1024 4 us.  In fp32 60000 x 1024 128 us = 5.8 TB/s.
+// Measured (bf16): 16 sequences of 2048 x 2048 78 us forward = 5.2 TB/s, 127 backward = 5.3; one of 65536 x 1024 103 and 236 (a set of tiles takes the
+// cluster 1.6 us and 3.7, a CTA's 24 and 40 KB would take 0.6 and 0.9); 64 sequences by one step of 1024 4 us.  In fp32 one of 60000 x 1024 129 us = 5.7 TB/s.
 #include <algorithm>
 #include <cstring>
 
@@ -1108,7 +1108,7 @@ uint32_t choose_cluster(uint64_t items, const Spans& s, uint32_t tile_rows) {
   return cluster;
 }
 // Half as many columns and twice the rows to a tile where wide ones in the largest clusters would leave SMs with one CTA or none (one sequence of
-// 65536 rows of 1024: 106 us; with wide ones in clusters of 16, which an SM does not take two of, 283).
+// 65536 rows of 1024: 103 us; with wide ones in clusters of 16, which an SM does not take two of, 283).
 template <typename Args>
 bool narrow_tiles(const Args& a, uint32_t columns) {
   return (uint64_t)a.spans.sequences * ((a.width + columns - 1) / columns) * kMostCluster <= (uint64_t)sm_count() && a.spans.rows / a.spans.sequences >= 8u * kMarkRows;
